@@ -349,9 +349,11 @@ def exact(case, seed):
     if c["op"] == "quantize":
         return _exact_f8(s["x"].double()) if rows * d <= 1 << 30 else None
     if c["op"] == "norm":
+        # the norm reads the sum as it is stored, and the 8 bits are those of the row as it is stored
         total = s["x"].double() + s["residual"].double()
-        y = total / torch.sqrt((total * total).sum(dim=1, keepdim=True) / d + EPS) * s["weight"].double()
-        return dict(_exact_f8(y), sum=total, y=y)
+        stored = total.to(_dtype(c)).double()
+        y = stored / torch.sqrt((stored * stored).sum(dim=1, keepdim=True) / d + EPS) * s["weight"].double()
+        return dict(_exact_f8(y.to(_dtype(c)).double()), sum=total, y=y)
     if c["op"] == "logits":
         h = _exact_rows(s["h"], d) if c["dtype"] == "f8" else s["h"].double()
         q, scales = s["U"]
