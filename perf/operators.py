@@ -245,13 +245,13 @@ def _own(s):
         q = sv.quantize_rows(s["x"])
         return {"q": q.q, "scales": q.scales}
     if c["op"] == "norm":
-        y, total, q = sv.rms_norm(s["x"], s["weight"], EPS, residual=s["residual"], want_f8=True)
+        y, total, q = sv.rms_norm(s["x"], s["weight"], EPS, residual=s["residual"], want_quantized=True)
         return {"sum": total, "y": y, "q": q.q, "scales": q.scales}
     if c["op"] == "logits":
-        h, U = sv.F8Rows(*s["h"]) if c["dtype"] == "f8" else s["h"], sv.F8Rows(*s["U"])
+        h, U = sv.QuantizedRows(*s["h"]) if c["dtype"] == "f8" else s["h"], sv.QuantizedRows(*s["U"])
         if s["idx"] is None:
-            return sv.dense_logits_f8(h, U)
-        return sv.subset_logits_f8(h, U, s["idx"], padded=c["padded"])
+            return sv.quantized_dense_logits(h, U)
+        return sv.quantized_subset_logits(h, U, s["idx"], padded=c["padded"])
     tok, prob = sv.sample(s["logits"], s["u"], temperature=s["temperature"], top_k=s["top_k"], top_p=s["top_p"],
                           min_p=s["min_p"], idx=s["idx"])
     return {"tok": tok, "prob": prob}
