@@ -68,7 +68,8 @@ typedef enum {
     SV_ERR_HIP = 8          /* a HIP runtime call (kernel launch, device query) failed */
 } sv_status;
 
-typedef enum { SV_F32 = 0, SV_BF16 = 1 } sv_dtype;
+/* SV_E4M3 names rows in 8 bits (see specvocab_quantize_rows); only specvocab_workspace_bytes takes it. */
+typedef enum { SV_F32 = 0, SV_BF16 = 1, SV_E4M3 = 2 } sv_dtype;
 
 /* SV_IDX_PER_ROW: idx is [rows x k], row r of h uses idx[r, :].
  * SV_IDX_PER_STEP: idx is [k], one set shared by every row of the step. */
@@ -104,7 +105,11 @@ typedef enum {
     SV_OP_DENSE_LOGITS = 3,
     SV_OP_DRAFT_STEP = 4,
     SV_OP_INDEXED_HEAD_NAIVE = 5,
-    SV_OP_AUX_LOG_SOFTMAX = 6
+    SV_OP_AUX_LOG_SOFTMAX = 6,
+    SV_OP_QUANTIZED_DENSE_LOGITS = 7,  /* dt: what h is, SV_BF16 or SV_E4M3 */
+    SV_OP_QUANTIZED_SUBSET_LOGITS = 8, /* the same */
+    SV_OP_QUANTIZED_SAMPLE_STEP = 9,   /* the same; k: 0 for the whole vocabulary */
+    SV_OP_SAMPLE = 10                  /* k: logits of a row (n) */
 } sv_op;
 
 /* Largest kd the draft top-kd accepts. */
@@ -286,6 +291,76 @@ int specvocab_dense_logits(const void* h, int64_t rows, int64_t d, int64_t ldh,
                            const void* U, int64_t V, int64_t ldu, int dt,
                            float* logits_out,
                            void* ws, size_t ws_bytes, void* stream);
+
+/* ---- From a layer's output to a token, with the output embedding in 8 bits ------------------------------------------------
+ *
+ * Rows in 8 bits: a row of d values (d a multiple of 16) is d e4m3 codes and, in another array, one byte per block of 128 values,
+ * the exponent of the block's scale: 2^(byte - 127), 255 for NaN (e8m0).  Value i of the row is scale[i / 128] * code[i].  A row has
+ * 4 * ceil(d / 512) scale bytes (whole words; bytes past the last block are 127).  Row strides: of codes at least d and a multiple of
+ * 16, of scales at least that number and a multiple of 4, bases aligned likewise; else SV_ERR_ALIGN.
+ *
+ * specvocab_quantize_rows: the rows of x [rows x d] (SV_F32 or SV_BF16, d a multiple of 16) in 8 bits -- the output embedding
+ * once, hidden rows per step.  A block's scale is the smallest 2^e, e >= -126, with max|x| <= 448 * 2^e (1 for a block of zeros); a
+ * code is x / 2^e, which is exact, rounded to nearest even.  A block with an infinity or a NaN in it has scale 255 and
+ * NaN codes.  rows is limited by int32 only. */
+int specvocab_quantize_rows(const void* x, int64_t rows, int64_t d, int64_t ldx, int dt,
+                            uint8_t* q_out, int64_t ldq, uint8_t* scales_out, int64_t lds, void* stream);
+
+/* The root-mean-square norm in front of a head, with the residual's addition:
+ *     t[r] = x[r] + residual[r]                       (x[r] where residual is NULL), rounded to `dt`
+ *     y[r] = t[r] / sqrt(mean_i t[r, i]^2 + eps) * (weight + weight_offset), rounded to `dt`
+ * sum_out (needs residual), y_out, and q_out with scales_out (y in 8 bits) receive t, y and the 8 bits of y as it is stored: the same
+ * bits as an addition, a norm and specvocab_quantize_rows called one after the other.  Each may be NULL, but not both y_out and
+ * q_out.  The selector reads y (specvocab_select), the 8-bit head q.  weight: [d] in `dt`; weight_offset: 0, or 1 for models that store
+ * the weight's distance from 1.  Sums are float32.  sum_out and y_out may be x or residual themselves (same base and stride), not
+ * otherwise overlap them or each other.  d a multiple of 16; eps >= 0 and finite.  No workspace.  A row with an infinity or a NaN
+ * in t gets NaN. */
+int specvocab_rms_norm(const void* x, int64_t rows, int64_t d, int64_t ldx, const void* residual, int64_t ldr,
+                       const void* weight, float weight_offset, float eps, int dt,
+                       void* sum_out, int64_t ld_sum, void* y_out, int64_t ldy,
+                       uint8_t* q_out, int64_t ldq, uint8_t* scales_out, int64_t lds, void* stream);
+
+/* specvocab_dense_logits and specvocab_subset_logits with the embedding in 8 bits:
+ *     logits_out[r, j] = < U[row(j), :], h[r, :] >     over the values that codes and scales stand for, accumulated in float32
+ * h: rows in 8 bits (h_scales not NULL; ldh in codes, ldhs in scale bytes), or bfloat16 rows (h_scales NULL; ldh in elements,
+ * ldhs ignored).  d a multiple of 16.  idx, k, idx_mode as in specvocab_subset_logits (SV_IDX_SORTED makes no difference).  A
+ * NaN code or scale makes the logits that use it NaN.  The values are widened to bfloat16, which is exact, and multiplied as such (h_scales so
+ * small that a value lies below 2^-126 lose it). */
+int specvocab_quantized_dense_logits(const void* h, const uint8_t* h_scales, int64_t rows, int64_t d, int64_t ldh, int64_t ldhs,
+                                     const uint8_t* U, const uint8_t* U_scales, int64_t V, int64_t ldu, int64_t ldus,
+                                     float* logits_out, void* ws, size_t ws_bytes, void* stream);
+int specvocab_quantized_subset_logits(const void* h, const uint8_t* h_scales, int64_t rows, int64_t d, int64_t ldh, int64_t ldhs,
+                                      const uint8_t* U, const uint8_t* U_scales, int64_t V, int64_t ldu, int64_t ldus,
+                                      const int32_t* idx, int64_t k, int idx_mode,
+                                      float* logits_out, void* ws, size_t ws_bytes, void* stream);
+
+/* One token per row, drawn with a given random number u[r] in [0, 1) (smaller ones count as 0, larger ones and 1 as the
+ * largest float below 1).  logits: device [rows x n] float32, row stride ld (any alignment).  With T = temperature[r] and the row's places ordered by
+ * descending logit, equal logits by place (for ascending lists: by token id), w = exp((logit - largest) / T):
+ *   1. top_k[r] > 0:  the first top_k[r] places stay;
+ *   2. top_p[r] < 1:  of those, the ones stay that have less than top_p[r] of their mass in front of them (always the first);
+ *   3. min_p[r] > 0:  of those, the ones with w >= min_p[r] stay (above 1 counts as 1);
+ *   4. the first place of those at which the running sum of w exceeds u[r] times the sum over all of them is drawn.
+ * T <= 0 or NaN: the first place, with probability 1.  NaN in top_p or min_p: no such step.  temperature, top_k, top_p,
+ * min_p: device [rows], or NULL for 1, 0, 1, 0.  Places with a logit of -inf or NaN are masked: they are in none of the steps.
+ * Places with w below 2^-64 have no mass and count as masked too.  A +inf logit takes all of a row's mass.
+ * tok_out: device [rows] int32, the place, or idx(r, place) where idx (as in specvocab_subset_logits, padding slots having a logit of
+ * -inf) is not NULL; -1 for a row that is masked throughout.  prob_out: device [rows] float32, w over the sum in 4 (0 for such
+ * a row), or NULL.
+ * Sums are kept as exactly as 64-bit floating point keeps them, whatever n is, and do not depend on the run.  One to three launches.  Thousands of
+ * equal logits among the kept ones, or top_k and borders among logits that crowd into few values, cost some tens of passes over the row. */
+int specvocab_sample(const float* logits, int64_t ld, int64_t rows, int64_t n, const int32_t* idx, int idx_mode,
+                     const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
+                     int32_t* tok_out, float* prob_out, void* ws, size_t ws_bytes, void* stream);
+
+/* The step from hidden rows to tokens: specvocab_quantized_subset_logits (idx NULL: specvocab_quantized_dense_logits, k ignored)
+ * followed by specvocab_sample on its logits, enqueued back to back.  logits_out: device [rows x k] (or V) float32, required. */
+int specvocab_quantized_sample_step(const void* h, const uint8_t* h_scales, int64_t rows, int64_t d, int64_t ldh, int64_t ldhs,
+                                    const uint8_t* U, const uint8_t* U_scales, int64_t V, int64_t ldu, int64_t ldus,
+                                    const int32_t* idx, int64_t k, int idx_mode,
+                                    const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                                    const float* u, float* logits_out, int32_t* tok_out, float* prob_out,
+                                    void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple, Union
 
 import torch
 
@@ -22,6 +22,8 @@ SV_IDX_PER_ROW, SV_IDX_PER_STEP = 0, 1
 SV_OP_SELECT, SV_OP_SUBSET_LOGITS, SV_OP_DRAFT_TOPK, SV_OP_DENSE_LOGITS, SV_OP_DRAFT_STEP = 0, 1, 2, 3, 4
 SV_OP_INDEXED_HEAD_NAIVE = 5
 SV_OP_AUX_LOG_SOFTMAX = 6
+SV_OP_QUANTIZED_DENSE_LOGITS, SV_OP_QUANTIZED_SUBSET_LOGITS, SV_OP_QUANTIZED_SAMPLE_STEP, SV_OP_SAMPLE = 7, 8, 9, 10
+SV_E4M3 = 2              # rows in 8 bits, where a workspace size is asked for
 SV_IDX_PADDED = 4        # OR into idx_mode: the list may hold padding slots (-1)
 SV_IDX_SORTED = 8        # OR into idx_mode: every list is sorted by ascending id (what select emits)
 MAX_KD = 64
@@ -44,6 +46,12 @@ EXPORTS = (
     "specvocab_aux_log_softmax",
     "specvocab_stream_read_probe",
     "specvocab_dense_logits",
+    "specvocab_quantize_rows",
+    "specvocab_rms_norm",
+    "specvocab_quantized_dense_logits",
+    "specvocab_quantized_subset_logits",
+    "specvocab_sample",
+    "specvocab_quantized_sample_step",
 )
 
 
@@ -103,6 +111,20 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.specvocab_stream_read_probe.argtypes = [vp, ctypes.c_size_t, vp, ctypes.c_size_t, vp]
     lib.specvocab_dense_logits.restype = ci
     lib.specvocab_dense_logits.argtypes = [vp, i64, i64, i64, vp, i64, i64, ci, vp, vp, ctypes.c_size_t, vp]
+    sz, cf = ctypes.c_size_t, ctypes.c_float
+    lib.specvocab_quantize_rows.restype = ci
+    lib.specvocab_quantize_rows.argtypes = [vp, i64, i64, i64, ci, vp, i64, vp, i64, vp]
+    lib.specvocab_rms_norm.restype = ci
+    lib.specvocab_rms_norm.argtypes = [vp, i64, i64, i64, vp, i64, vp, cf, cf, ci, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    head = [vp, vp, i64, i64, i64, i64, vp, vp, i64, i64, i64]
+    lib.specvocab_quantized_dense_logits.restype = ci
+    lib.specvocab_quantized_dense_logits.argtypes = head + [vp, vp, sz, vp]
+    lib.specvocab_quantized_subset_logits.restype = ci
+    lib.specvocab_quantized_subset_logits.argtypes = head + [vp, i64, ci, vp, vp, sz, vp]
+    lib.specvocab_sample.restype = ci
+    lib.specvocab_sample.argtypes = [vp, i64, i64, i64, vp, ci, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.specvocab_quantized_sample_step.restype = ci
+    lib.specvocab_quantized_sample_step.argtypes = head + [vp, i64, ci, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     if path is None:
         _lib = lib
     return lib
@@ -448,3 +470,228 @@ def dense_logits(h: torch.Tensor, U: torch.Tensor, out: Optional[torch.Tensor] =
                                                  _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)),
            "specvocab_dense_logits")
     return out
+
+
+# ---- from a layer's output to a token, with the output embedding in 8 bits
+
+class QuantizedRows(NamedTuple):
+    """Rows in 8 bits: q [rows x d] float8_e4m3fn and scales [rows x scale_columns(d)] float8_e8m0fnu, one per block of 128."""
+    q: torch.Tensor
+    scales: torch.Tensor
+
+
+def _on_current(*tensors: Optional[torch.Tensor]) -> None:
+    """The library works on the current device: its stream, and memory of its own."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != here):
+            raise ValueError(f"every tensor must live on the current GPU (cuda:{here}), got one on {t.device}")
+
+
+def scale_columns(d: int) -> int:
+    """Scale bytes of a row of d values: one per block of 128, in whole words."""
+    return 4 * ((d + 511) // 512)
+
+
+def _quantized(t: QuantizedRows, name: str) -> Tuple[int, int, int, int]:
+    """(rows, d, row stride of the codes, row stride of the scales)."""
+    rows, d, ld = _mat(t.q, name)
+    if t.q.dtype != torch.float8_e4m3fn or t.scales.dtype != torch.float8_e8m0fnu:
+        raise TypeError(f"{name} must be float8_e4m3fn codes with float8_e8m0fnu scales")
+    srows, cols, lds = _mat(t.scales, f"{name}.scales")
+    if srows != rows or cols != scale_columns(d):
+        raise ValueError(f"{name}.scales must be [{rows} x {scale_columns(d)}]")
+    if t.scales.device != t.q.device:
+        raise ValueError(f"{name}'s codes and scales must live on the same GPU")
+    return rows, d, ld, lds
+
+
+def _new_quantized(rows: int, d: int, device, out: Optional[QuantizedRows]) -> QuantizedRows:
+    if out is None:
+        return QuantizedRows(torch.empty((rows, d), dtype=torch.float8_e4m3fn, device=device),
+                             torch.empty((rows, scale_columns(d)), dtype=torch.float8_e8m0fnu, device=device))
+    r, c, _, _ = _quantized(out, "out")
+    if (r, c) != (rows, d):
+        raise ValueError(f"out must be [{rows} x {d}]")
+    return out
+
+
+def quantize_rows(x: torch.Tensor, out: Optional[QuantizedRows] = None,
+                  stream: Optional[torch.cuda.Stream] = None) -> QuantizedRows:
+    """specvocab_quantize_rows: the rows of x in 8 bits, a power-of-two scale per block of 128."""
+    rows, d, ldx = _mat(x, "x")
+    dt = _dt(x)
+    out = _new_quantized(rows, d, x.device, out)
+    _, _, ldq, lds = _quantized(out, "out")
+    _on_current(x, *out)
+    _check(load_library().specvocab_quantize_rows(_ptr(x), rows, d, ldx, dt, _ptr(out.q), ldq, _ptr(out.scales), lds,
+                                                  _stream(stream)), "specvocab_quantize_rows")
+    return out
+
+
+def _like(t: Optional[torch.Tensor], x: torch.Tensor, name: str) -> int:
+    """Row stride of a matrix of x's shape and type."""
+    if t is None:
+        return 0
+    rows, d, ld = _mat(t, name)
+    if t.shape != x.shape or t.dtype != x.dtype:
+        raise ValueError(f"{name} must have x's shape and dtype")
+    return ld
+
+
+def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Optional[torch.Tensor] = None,
+             weight_offset: float = 0.0, want_y: bool = True, want_quantized: bool = False,
+             sum_out: Optional[torch.Tensor] = None, y_out: Optional[torch.Tensor] = None,
+             quantized_out: Optional[QuantizedRows] = None, stream: Optional[torch.cuda.Stream] = None):
+    """specvocab_rms_norm: root-mean-square norm of x + residual.
+    Returns (y or None, the sum (x itself without a residual), QuantizedRows of y or None)."""
+    rows, d, ldx = _mat(x, "x")
+    dt = _dt(x)
+    if weight.shape != (d,) or weight.dtype != x.dtype or not weight.is_contiguous() or not weight.is_cuda:
+        raise ValueError("weight must be a contiguous [d] GPU tensor of x's dtype")
+    if sum_out is not None and residual is None:
+        raise ValueError("sum_out needs a residual")
+    ldr = _like(residual, x, "residual")
+    if residual is not None and sum_out is None:
+        sum_out = torch.empty((rows, d), dtype=x.dtype, device=x.device)
+    if y_out is None and want_y:
+        y_out = torch.empty((rows, d), dtype=x.dtype, device=x.device)
+    if quantized_out is not None or want_quantized:
+        quantized_out = _new_quantized(rows, d, x.device, quantized_out)
+    ld_sum, ldy = _like(sum_out, x, "sum_out"), _like(y_out, x, "y_out")
+    q, scales, ldq, lds = None, None, 0, 0
+    if quantized_out is not None:
+        q, scales = quantized_out
+        _, _, ldq, lds = _quantized(quantized_out, "quantized_out")
+    _on_current(x, weight, residual, sum_out, y_out, q, scales)
+    _check(load_library().specvocab_rms_norm(_ptr(x), rows, d, ldx, _ptr(residual), ldr, _ptr(weight), weight_offset, eps, dt,
+                                             _ptr(sum_out), ld_sum, _ptr(y_out), ldy, _ptr(q), ldq, _ptr(scales), lds,
+                                             _stream(stream)), "specvocab_rms_norm")
+    return y_out, sum_out if sum_out is not None else x, quantized_out
+
+
+def _head_operands(h: Union[torch.Tensor, QuantizedRows], U: QuantizedRows):
+    """(leading arguments of the products with an 8-bit embedding, rows, d, V, dtype of h, device)."""
+    V, d2, ldu, ldus = _quantized(U, "U")
+    if isinstance(h, QuantizedRows):
+        rows, d, ldh, ldhs = _quantized(h, "h")
+        hp, hs, dt, device = h.q.data_ptr(), h.scales.data_ptr(), SV_E4M3, h.q.device
+    else:
+        rows, d, ldh = _mat(h, "h")
+        if h.dtype != torch.bfloat16:
+            raise TypeError(f"h must be bfloat16 or QuantizedRows, got {h.dtype}")
+        hp, hs, ldhs, dt, device = h.data_ptr(), None, 0, SV_BF16, h.device
+    if d2 != d:
+        raise ValueError("U and h disagree on d")
+    _on_current(*U, *(h if isinstance(h, QuantizedRows) else (h,)))
+    return (hp, hs, rows, d, ldh, ldhs, U.q.data_ptr(), U.scales.data_ptr(), V, ldu, ldus), rows, d, V, dt, device
+
+
+def _out_logits(out: Optional[torch.Tensor], rows: int, n: int, device) -> torch.Tensor:
+    if out is None:
+        return torch.empty((rows, n), dtype=torch.float32, device=device)
+    if out.shape != (rows, n) or out.dtype != torch.float32 or not out.is_contiguous() or not out.is_cuda:
+        raise ValueError(f"logits must go to a contiguous [{rows} x {n}] float32 GPU tensor")
+    return out
+
+
+def quantized_dense_logits(h: Union[torch.Tensor, QuantizedRows], U: QuantizedRows, out: Optional[torch.Tensor] = None,
+                           ws: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """specvocab_quantized_dense_logits: out[r, v] = <U[v], h_r> with U in 8 bits, h in 8 bits or bfloat16."""
+    args, rows, d, V, dt, device = _head_operands(h, U)
+    out = _out_logits(out, rows, V, device)
+    ws = _workspace(workspace_bytes(SV_OP_QUANTIZED_DENSE_LOGITS, rows, d, V, 0, 0, 0, dt), device, ws)
+    _on_current(out, ws)
+    _check(load_library().specvocab_quantized_dense_logits(*args, _ptr(out), _ptr(ws), 0 if ws is None else ws.numel(),
+                                                           _stream(stream)), "specvocab_quantized_dense_logits")
+    return out
+
+
+def quantized_subset_logits(h: Union[torch.Tensor, QuantizedRows], U: QuantizedRows, idx: torch.Tensor,
+                            out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                            stream: Optional[torch.cuda.Stream] = None, padded: bool = False) -> torch.Tensor:
+    """specvocab_quantized_subset_logits: out[r, j] = <U[idx(r, j)], h_r>.  padded: idx may hold padding slots (-1)."""
+    args, rows, d, V, dt, device = _head_operands(h, U)
+    mode, k = _idx(idx, rows)
+    if padded:
+        mode |= SV_IDX_PADDED
+    out = _out_logits(out, rows, k, device)
+    ws = _workspace(workspace_bytes(SV_OP_QUANTIZED_SUBSET_LOGITS, rows, d, V, k, 0, 0, dt, mode), device, ws)
+    _on_current(idx, out, ws)
+    _check(load_library().specvocab_quantized_subset_logits(*args, _ptr(idx), k, mode, _ptr(out), _ptr(ws),
+                                                            0 if ws is None else ws.numel(), _stream(stream)),
+           "specvocab_quantized_subset_logits")
+    return out
+
+
+def _per_row(t: Optional[torch.Tensor], rows: int, dtype: torch.dtype, name: str) -> Optional[int]:
+    if t is None:
+        return None
+    if t.shape != (rows,) or t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{name} must be a contiguous [{rows}] {dtype} GPU tensor")
+    return t.data_ptr()
+
+
+def _sampling(rows: int, u, temperature, top_k, top_p, min_p):
+    f32 = torch.float32
+    if u is None:
+        raise ValueError("u must be given")
+    return (_per_row(temperature, rows, f32, "temperature"), _per_row(top_k, rows, torch.int32, "top_k"),
+            _per_row(top_p, rows, f32, "top_p"), _per_row(min_p, rows, f32, "min_p"), _per_row(u, rows, f32, "u"))
+
+
+def _drawn(rows: int, device, tok_out: Optional[torch.Tensor], prob_out: Optional[torch.Tensor]):
+    if tok_out is None:
+        tok_out = torch.empty(rows, dtype=torch.int32, device=device)
+    if prob_out is None:
+        prob_out = torch.empty(rows, dtype=torch.float32, device=device)
+    _per_row(tok_out, rows, torch.int32, "tok_out")
+    _per_row(prob_out, rows, torch.float32, "prob_out")
+    return tok_out, prob_out
+
+
+def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None,
+           top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
+           idx: Optional[torch.Tensor] = None, tok_out: Optional[torch.Tensor] = None, prob_out: Optional[torch.Tensor] = None,
+           ws: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """specvocab_sample: one token per row from the random numbers u [rows]; temperature, top_p, min_p float32 [rows], top_k int32
+    [rows], each or None.  idx: the token ids of the places, [n] or [rows x n].
+    Returns (tok [rows] int32, prob [rows] float32)."""
+    rows, n, ld = _mat(logits, "logits")
+    if logits.dtype != torch.float32:
+        raise TypeError(f"logits must be float32, got {logits.dtype}")
+    settings = _sampling(rows, u, temperature, top_k, top_p, min_p)
+    mode = SV_IDX_PER_ROW
+    if idx is not None:
+        mode, k = _idx(idx, rows)
+        if k != n:
+            raise ValueError("idx and logits disagree on n")
+    tok_out, prob_out = _drawn(rows, logits.device, tok_out, prob_out)
+    ws = _workspace(workspace_bytes(SV_OP_SAMPLE, rows, 0, 0, n, 0, 0, SV_F32), logits.device, ws)
+    _on_current(logits, u, temperature, top_k, top_p, min_p, idx, tok_out, prob_out, ws)
+    _check(load_library().specvocab_sample(_ptr(logits), ld, rows, n, _ptr(idx), mode, *settings, _ptr(tok_out), _ptr(prob_out),
+                                           _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)), "specvocab_sample")
+    return tok_out, prob_out
+
+
+def quantized_sample_step(h: Union[torch.Tensor, QuantizedRows], U: QuantizedRows, u: torch.Tensor,
+                          idx: Optional[torch.Tensor] = None, temperature: Optional[torch.Tensor] = None,
+                          top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+                          min_p: Optional[torch.Tensor] = None, logits_out: Optional[torch.Tensor] = None,
+                          tok_out: Optional[torch.Tensor] = None, prob_out: Optional[torch.Tensor] = None,
+                          ws: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None, padded: bool = False):
+    """specvocab_quantized_sample_step: logits over idx (None: the whole vocabulary) with U in 8 bits, then a token per row.
+    Returns (logits, tok, prob)."""
+    args, rows, d, V, dt, device = _head_operands(h, U)
+    mode, k = (SV_IDX_PER_ROW, 0) if idx is None else _idx(idx, rows)
+    if padded:
+        mode |= SV_IDX_PADDED
+    settings = _sampling(rows, u, temperature, top_k, top_p, min_p)
+    logits_out = _out_logits(logits_out, rows, V if idx is None else k, device)
+    tok_out, prob_out = _drawn(rows, device, tok_out, prob_out)
+    ws = _workspace(workspace_bytes(SV_OP_QUANTIZED_SAMPLE_STEP, rows, d, V, k, 0, 0, dt, mode), device, ws)
+    _on_current(idx, u, temperature, top_k, top_p, min_p, logits_out, tok_out, prob_out, ws)
+    _check(load_library().specvocab_quantized_sample_step(*args, _ptr(idx), k, mode, *settings, _ptr(logits_out), _ptr(tok_out),
+                                                          _ptr(prob_out), _ptr(ws), 0 if ws is None else ws.numel(),
+                                                          _stream(stream)), "specvocab_quantized_sample_step")
+    return logits_out, tok_out, prob_out

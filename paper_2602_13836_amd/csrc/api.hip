@@ -59,6 +59,8 @@ hipError_t device_state(const DeviceState** out) {
             if (e != hipSuccess) return e;
             e = configure_panel_lds();
             if (e != hipSuccess) return e;
+            e = configure_sample_lds();
+            if (e != hipSuccess) return e;
             void* p = nullptr;
             e = hipGetSymbolAddress(&p, HIP_SYMBOL(scratch));
             if (e != hipSuccess) return e;
@@ -338,6 +340,174 @@ AuxWs aux_ws(int64_t rows, int64_t V, int64_t d_prime, int dt) {
     return w;
 }
 
+// ---- rows in 8 bits
+constexpr int64_t kMaxLength = 1 << 24;        // of a row
+
+// a row of `d` codes and its scale bytes
+int check_quantized(const void* q, int64_t d, int64_t ldq, const void* scales, int64_t lds) {
+    if (d < 1 || ldq < d || lds < sv::scale_bytes_of_row(d)) return SV_ERR_SHAPE;
+    if (d % 16 != 0 || d > kMaxLength) return SV_ERR_UNSUPPORTED;
+    if (ldq % 16 != 0 || lds % 4 != 0 || !aligned16(q) || (reinterpret_cast<uintptr_t>(scales) & 3u)) return SV_ERR_ALIGN;
+    return SV_OK;
+}
+
+// rows of the storage type that go into them
+int check_stored(const void* x, int64_t d, int64_t ld, int dt) {
+    if (d < 1 || ld < d) return SV_ERR_SHAPE;
+    if (d % 16 != 0 || d > kMaxLength) return SV_ERR_UNSUPPORTED;
+    if (ld % (16 / esize_of(dt)) != 0 || !aligned16(x)) return SV_ERR_ALIGN;
+    return SV_OK;
+}
+
+// Which way a product with an 8-bit embedding goes: a hidden row at a time, all rows over one list, or over the union of the rows'
+// lists (where reading U once pays for the launches that make the union: the rule of the bfloat16 products).
+enum QuantizedWay { Q_ROWS, Q_SHARED, Q_UNION };
+QuantizedWay quantized_way(int64_t rows, int64_t d, int64_t k, bool list, int idx_mode) {
+    if (rows == 1) return Q_ROWS;
+    if (!list || base_mode(idx_mode) == SV_IDX_PER_STEP) return Q_SHARED;
+    const bool many = rows * k >= 16384 && (rows >= 16 || rows * k * d >= ((int64_t)512 << 20));
+    return many ? Q_UNION : Q_ROWS;
+}
+
+struct QuantizedWs {
+    size_t hidden, list, work, total;     // hidden rows as bfloat16; the clean copy of a padded list; the union and its product
+};
+QuantizedWs quantized_ws(int64_t rows, int64_t d, int64_t V, int64_t k, bool quantized_h, bool list, int idx_mode) {
+    QuantizedWs w{};
+    const QuantizedWay way = quantized_way(rows, d, k, list, idx_mode);
+    if (way != Q_ROWS) {
+        if (quantized_h) w.hidden = round256((size_t)rows * (size_t)d * 2);
+        if (list && is_padded(idx_mode)) w.list = round256((size_t)(base_mode(idx_mode) == SV_IDX_PER_ROW ? rows : 1) * (size_t)k * sizeof(int32_t));
+    }
+    if (way == Q_UNION) w.work = sv::union_ws_bytes(rows, V, k);
+    w.total = w.hidden + w.list + w.work;
+    return w;
+}
+
+struct QuantizedCall {
+    const void* h;
+    const uint8_t* h_scales;
+    int64_t rows, d, ldh, ldhs;
+    const uint8_t *U, *U_scales;
+    int64_t V, ldu, ldus;
+    const int32_t* idx;      // nullptr: all of U
+    int64_t k;
+    int idx_mode;
+    float* out;
+    void* ws;
+    size_t ws_bytes;
+};
+
+// everything a call can be refused for
+int check_quantized_call(const QuantizedCall& c) {
+    if (!c.h || !c.U || !c.U_scales || !c.out) return SV_ERR_NULL;
+    if (c.idx && !mode_ok(c.idx_mode)) return SV_ERR_DTYPE;
+    if (c.rows < 1 || c.rows > kMaxRows || c.V < 1 || c.V > kMaxVocab || c.k < 1 || c.k > kMaxVocab) return SV_ERR_SHAPE;
+    int st = c.h_scales ? check_quantized(c.h, c.d, c.ldh, c.h_scales, c.ldhs) : check_stored(c.h, c.d, c.ldh, SV_BF16);
+    if (st != SV_OK) return st;
+    st = check_quantized(c.U, c.d, c.ldu, c.U_scales, c.ldus);
+    if (st != SV_OK) return st;
+    const size_t need = quantized_ws(c.rows, c.d, c.V, c.k, c.h_scales != nullptr, c.idx != nullptr, c.idx_mode).total;
+    if (need) {
+        if (!c.ws || c.ws_bytes < need) return SV_ERR_WORKSPACE;
+        if (!aligned16(c.ws)) return SV_ERR_ALIGN;
+    }
+    return SV_OK;
+}
+
+int launch_quantized(const QuantizedCall& c, hipStream_t s) {
+    const bool per_row = c.idx && base_mode(c.idx_mode) == SV_IDX_PER_ROW, padded = c.idx && is_padded(c.idx_mode);
+    const int64_t sets = per_row ? c.rows : 1;
+    if (c.idx) {
+        const int st = validate_indices(c.idx, sets * c.k, c.V, s, padded, is_sorted(c.idx_mode) ? c.k : 0);
+        if (st != SV_OK) return st;
+    }
+    sv::QuantizedArgs a{};
+    a.h = static_cast<const char*>(c.h);
+    a.ldh = c.h_scales ? c.ldh : c.ldh * 2;
+    a.h_scales = c.h_scales;
+    a.ldhs = c.ldhs;
+    a.U = c.U;
+    a.ldu = c.ldu;
+    a.u_scales = c.U_scales;
+    a.ldus = c.ldus;
+    a.idx = c.idx;
+    a.idx_row_stride = per_row ? c.k : 0;
+    a.n_items = c.k;
+    a.units = (int)(c.d / 16);
+    a.rows = (int)c.rows;
+    a.out = c.out;
+    a.out_row_stride = c.k;
+    a.u_rows = c.V;
+    const QuantizedWay way = quantized_way(c.rows, c.d, c.k, c.idx != nullptr, c.idx_mode);
+    if (way == Q_ROWS) return sv::launch_quantized_gemv(a, s) == hipSuccess ? SV_OK : SV_ERR_HIP;
+    const QuantizedWs w = quantized_ws(c.rows, c.d, c.V, c.k, c.h_scales != nullptr, c.idx != nullptr, c.idx_mode);
+    char* ws = static_cast<char*>(c.ws);
+    if (c.h_scales) {
+        if (sv::launch_widen_rows(static_cast<const uint8_t*>(c.h), c.ldh, c.h_scales, c.ldhs, c.rows, (int)c.d, ws, s) != hipSuccess) return SV_ERR_HIP;
+        a.h = ws;
+        a.ldh = c.d * 2;
+        a.h_scales = nullptr;
+    }
+    const int32_t* use = c.idx;
+    if (padded) {
+        int32_t* clean = reinterpret_cast<int32_t*>(ws + w.hidden);
+        if (sv::launch_pad_clean(c.idx, sets * c.k, clean, s) != hipSuccess) return SV_ERR_HIP;
+        use = clean;
+    }
+    if (way == Q_SHARED) {
+        a.idx = use;
+        if (sv::launch_quantized_product(a, s) != hipSuccess) return SV_ERR_HIP;
+    } else {
+        sv::UnionList u;
+        if (sv::launch_union_list(use, a.rows, c.k, c.V, ws + w.hidden + w.list, s, &u) != hipSuccess) return SV_ERR_HIP;
+        a.idx = u.tokens;
+        a.idx_row_stride = 0;
+        a.n_items = u.stride;
+        a.n_items_dev = u.count;
+        a.plain_order = u.ordered ? 0 : 1;
+        a.out = u.product;
+        a.out_row_stride = u.stride;
+        if (sv::launch_quantized_product(a, s) != hipSuccess) return SV_ERR_HIP;
+        if (sv::launch_union_pick(u, use, a.rows, c.k, c.out, s) != hipSuccess) return SV_ERR_HIP;
+    }
+    if (padded && sv::launch_pad_mask(c.idx, per_row ? c.k : 0, (int)c.rows, c.k, c.out, s) != hipSuccess) return SV_ERR_HIP;
+    return SV_OK;
+}
+
+// ---- sampling
+int check_sample(const float* logits, int64_t ld, int64_t rows, int64_t n, const int32_t* idx, int idx_mode, const float* u, const int32_t* tok_out,
+                 const void* ws, size_t ws_bytes) {
+    if (!logits || !u || !tok_out) return SV_ERR_NULL;
+    if (idx && !mode_ok(idx_mode)) return SV_ERR_DTYPE;
+    if (rows < 1 || rows > kMaxRows || n < 1 || n > kMaxVocab || ld < n) return SV_ERR_SHAPE;
+    const size_t need = sv::sample_scratch_bytes(rows, n);
+    if (need) {
+        if (!ws || ws_bytes < need) return SV_ERR_WORKSPACE;
+        if (!aligned16(ws)) return SV_ERR_ALIGN;
+    }
+    return SV_OK;
+}
+sv::SampleArgs sample_args(const float* logits, int64_t ld, int64_t rows, int64_t n, const int32_t* idx, int idx_mode, const float* temperature,
+                           const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* tok_out, float* prob_out, void* ws) {
+    sv::SampleArgs a{};
+    a.logits = logits;
+    a.ld = ld;
+    a.n = n;
+    a.rows = (int)rows;
+    a.idx = idx;
+    a.idx_row_stride = idx && base_mode(idx_mode) == SV_IDX_PER_ROW ? n : 0;
+    a.temperature = temperature;
+    a.top_k = top_k;
+    a.top_p = top_p;
+    a.min_p = min_p;
+    a.u = u;
+    a.tok_out = tok_out;
+    a.prob_out = prob_out;
+    a.scratch = static_cast<char*>(ws);
+    return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -391,6 +561,22 @@ int specvocab_workspace_bytes(int op, int64_t rows, int64_t d, int64_t V, int64_
             *bytes_out = aux_ws(rows, V, d_prime, dt).total;
             return SV_OK;
         }
+        case SV_OP_QUANTIZED_DENSE_LOGITS:
+        case SV_OP_QUANTIZED_SUBSET_LOGITS:
+        case SV_OP_QUANTIZED_SAMPLE_STEP: {
+            const bool list = op == SV_OP_QUANTIZED_SUBSET_LOGITS || (op == SV_OP_QUANTIZED_SAMPLE_STEP && k > 0);
+            if ((dt != SV_BF16 && dt != SV_E4M3) || (list && !mode_ok(idx_mode))) return SV_ERR_DTYPE;
+            const int64_t n = list ? k : V;
+            if (rows < 1 || rows > kMaxRows || V < 1 || V > kMaxVocab || n < 1 || n > kMaxVocab || d < 1) return SV_ERR_SHAPE;
+            if (d % 16 != 0 || d > kMaxLength) return SV_ERR_UNSUPPORTED;
+            *bytes_out = quantized_ws(rows, d, V, n, dt == SV_E4M3, list, idx_mode).total;
+            if (op == SV_OP_QUANTIZED_SAMPLE_STEP && sv::sample_scratch_bytes(rows, n) > *bytes_out) *bytes_out = sv::sample_scratch_bytes(rows, n);
+            return SV_OK;
+        }
+        case SV_OP_SAMPLE:
+            if (rows < 1 || rows > kMaxRows || k < 1 || k > kMaxVocab) return SV_ERR_SHAPE;
+            *bytes_out = sv::sample_scratch_bytes(rows, k);
+            return SV_OK;
         case SV_OP_DRAFT_TOPK:
         case SV_OP_DENSE_LOGITS:
             return SV_OK;
@@ -742,6 +928,109 @@ int specvocab_draft_step(const void* h, int64_t rows, int64_t d, int64_t ldh, co
     }
     if (sv::launch_softmax_topk(t, s) != hipSuccess) return SV_ERR_HIP;
     return SV_OK;
+}
+
+int specvocab_quantize_rows(const void* x, int64_t rows, int64_t d, int64_t ldx, int dt, uint8_t* q_out, int64_t ldq, uint8_t* scales_out,
+                            int64_t lds, void* stream) {
+    if (!x || !q_out || !scales_out) return SV_ERR_NULL;
+    if (!dtype_ok(dt)) return SV_ERR_DTYPE;
+    if (rows < 1 || rows > kMaxVocab) return SV_ERR_SHAPE;
+    int st = check_stored(x, d, ldx, dt);
+    if (st != SV_OK) return st;
+    st = check_quantized(q_out, d, ldq, scales_out, lds);
+    if (st != SV_OK) return st;
+    if (ensure_device() != SV_OK) return SV_ERR_HIP;
+    return sv::launch_quantize_rows(dt, static_cast<const char*>(x), ldx * esize_of(dt), rows, (int)d, q_out, ldq, scales_out, lds,
+                                    static_cast<hipStream_t>(stream)) == hipSuccess
+               ? SV_OK
+               : SV_ERR_HIP;
+}
+
+int specvocab_rms_norm(const void* x, int64_t rows, int64_t d, int64_t ldx, const void* residual, int64_t ldr, const void* weight,
+                       float weight_offset, float eps, int dt, void* sum_out, int64_t ld_sum, void* y_out, int64_t ldy, uint8_t* q_out,
+                       int64_t ldq, uint8_t* scales_out, int64_t lds, void* stream) {
+    if (!x || !weight || (!y_out && !q_out) || (sum_out && !residual) || (q_out && !scales_out)) return SV_ERR_NULL;
+    if (!dtype_ok(dt)) return SV_ERR_DTYPE;
+    if (rows < 1 || rows > kMaxVocab || !(eps >= 0.0f) || eps == INFINITY || weight_offset != weight_offset) return SV_ERR_SHAPE;
+    int st = check_stored(x, d, ldx, dt);
+    if (st == SV_OK) st = check_stored(weight, d, d, dt);
+    if (st == SV_OK && residual) st = check_stored(residual, d, ldr, dt);
+    if (st == SV_OK && sum_out) st = check_stored(sum_out, d, ld_sum, dt);
+    if (st == SV_OK && y_out) st = check_stored(y_out, d, ldy, dt);
+    if (st == SV_OK && q_out) st = check_quantized(q_out, d, ldq, scales_out, lds);
+    if (st != SV_OK) return st;
+    if (ensure_device() != SV_OK) return SV_ERR_HIP;
+    const int es = esize_of(dt);
+    sv::NormArgs a{};
+    a.x = static_cast<const char*>(x);
+    a.x_row_bytes = ldx * es;
+    a.residual = static_cast<const char*>(residual);
+    a.res_row_bytes = ldr * es;
+    a.weight = static_cast<const char*>(weight);
+    a.offset = weight_offset;
+    a.eps = eps;
+    a.rows = rows;
+    a.d = (int)d;
+    a.sum = static_cast<char*>(sum_out);
+    a.sum_row_bytes = ld_sum * es;
+    a.y = static_cast<char*>(y_out);
+    a.y_row_bytes = ldy * es;
+    a.q = q_out;
+    a.ldq = ldq;
+    a.scales = scales_out;
+    a.lds = lds;
+    return sv::launch_rms_norm(dt, a, static_cast<hipStream_t>(stream)) == hipSuccess ? SV_OK : SV_ERR_HIP;
+}
+
+int specvocab_quantized_dense_logits(const void* h, const uint8_t* h_scales, int64_t rows, int64_t d, int64_t ldh, int64_t ldhs,
+                                     const uint8_t* U, const uint8_t* U_scales, int64_t V, int64_t ldu, int64_t ldus, float* logits_out,
+                                     void* ws, size_t ws_bytes, void* stream) {
+    const QuantizedCall c{h, h_scales, rows, d, ldh, ldhs, U, U_scales, V, ldu, ldus, nullptr, V, 0, logits_out, ws, ws_bytes};
+    const int st = check_quantized_call(c);
+    if (st != SV_OK) return st;
+    if (ensure_device() != SV_OK) return SV_ERR_HIP;
+    return launch_quantized(c, static_cast<hipStream_t>(stream));
+}
+
+int specvocab_quantized_subset_logits(const void* h, const uint8_t* h_scales, int64_t rows, int64_t d, int64_t ldh, int64_t ldhs,
+                                      const uint8_t* U, const uint8_t* U_scales, int64_t V, int64_t ldu, int64_t ldus, const int32_t* idx,
+                                      int64_t k, int idx_mode, float* logits_out, void* ws, size_t ws_bytes, void* stream) {
+    if (!idx) return SV_ERR_NULL;
+    const QuantizedCall c{h, h_scales, rows, d, ldh, ldhs, U, U_scales, V, ldu, ldus, idx, k, idx_mode, logits_out, ws, ws_bytes};
+    const int st = check_quantized_call(c);
+    if (st != SV_OK) return st;
+    if (ensure_device() != SV_OK) return SV_ERR_HIP;
+    return launch_quantized(c, static_cast<hipStream_t>(stream));
+}
+
+int specvocab_sample(const float* logits, int64_t ld, int64_t rows, int64_t n, const int32_t* idx, int idx_mode, const float* temperature,
+                     const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* tok_out, float* prob_out,
+                     void* ws, size_t ws_bytes, void* stream) {
+    const int st = check_sample(logits, ld, rows, n, idx, idx_mode, u, tok_out, ws, ws_bytes);
+    if (st != SV_OK) return st;
+    if (ensure_device() != SV_OK) return SV_ERR_HIP;
+    const sv::SampleArgs a = sample_args(logits, ld, rows, n, idx, idx_mode, temperature, top_k, top_p, min_p, u, tok_out, prob_out, ws);
+    return sv::launch_sample(a, static_cast<hipStream_t>(stream)) == hipSuccess ? SV_OK : SV_ERR_HIP;
+}
+
+int specvocab_quantized_sample_step(const void* h, const uint8_t* h_scales, int64_t rows, int64_t d, int64_t ldh, int64_t ldhs,
+                                    const uint8_t* U, const uint8_t* U_scales, int64_t V, int64_t ldu, int64_t ldus, const int32_t* idx,
+                                    int64_t k, int idx_mode, const float* temperature, const int32_t* top_k, const float* top_p,
+                                    const float* min_p, const float* u, float* logits_out, int32_t* tok_out, float* prob_out, void* ws,
+                                    size_t ws_bytes, void* stream) {
+    const int64_t n = idx ? k : V;
+    const QuantizedCall c{h, h_scales, rows, d, ldh, ldhs, U, U_scales, V, ldu, ldus, idx, n, idx_mode, logits_out, ws, ws_bytes};
+    int st = check_quantized_call(c);
+    if (st != SV_OK) return st;
+    st = check_sample(logits_out, n, rows, n, idx, idx_mode, u, tok_out, ws, ws_bytes);
+    if (st != SV_OK) return st;
+    if (ensure_device() != SV_OK) return SV_ERR_HIP;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    st = launch_quantized(c, s);
+    if (st != SV_OK) return st;
+    // (in the same workspace: the logits are done with it)
+    const sv::SampleArgs a = sample_args(logits_out, n, rows, n, idx, idx_mode, temperature, top_k, top_p, min_p, u, tok_out, prob_out, ws);
+    return sv::launch_sample(a, s) == hipSuccess ? SV_OK : SV_ERR_HIP;
 }
 
 int specvocab_stream_read_probe(const void* buf, size_t bytes, void* ws, size_t ws_bytes, void* stream) {

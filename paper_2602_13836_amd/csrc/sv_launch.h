@@ -210,6 +210,17 @@ struct DeferredPick {
     const float* zu;
     int64_t zu_stride;
 };
+// the path's steps by themselves, for a product of another kind
+struct UnionList {
+    int32_t* tokens;         // the union's tokens
+    uint32_t* count;         // how many, on the device
+    uint32_t* pos;           // [V] a token's place in the list
+    float* product;          // [rows x stride] room for the product over the list
+    int64_t stride;          // the most tokens that the list can have
+    bool ordered;            // the list is the same in every run
+};
+hipError_t launch_union_list(const int32_t* idx, int rows, int64_t k, int64_t V, void* ws, hipStream_t stream, UnionList* out);
+hipError_t launch_union_pick(const UnionList& u, const int32_t* idx, int rows, int64_t k, float* out, hipStream_t stream);
 // defer != nullptr: everything but the pick is launched, *defer says what is left to do (a.out_f32 stays unwritten)
 hipError_t launch_union_logits(const GemvArgs& a, int64_t V, void* ws, hipStream_t stream, DeferredPick* defer = nullptr);
 
@@ -325,5 +336,79 @@ struct TopkArgs {
 hipError_t launch_softmax_topk(const TopkArgs& a, hipStream_t stream);
 // true if launch_softmax_topk can do the pick itself for these arguments (pick_* not looked at)
 bool softmax_topk_can_pick(const TopkArgs& a);
+
+// ---- rows in 8 bits (quantized_rows.h), the norm that leaves them, products with an embedding held so
+// scale bytes of a row of d values: one per block of 128, in whole words
+inline int64_t scale_bytes_of_row(int64_t d) { return (d + 511) / 512 * 4; }
+struct NormArgs {
+    const char* x;
+    int64_t x_row_bytes;
+    const char* residual;    // or nullptr
+    int64_t res_row_bytes;
+    const char* weight;
+    float offset, eps;
+    int64_t rows;
+    int d;                   // a multiple of 16
+    char* sum;               // each of the outputs, or nullptr
+    int64_t sum_row_bytes;
+    char* y;
+    int64_t y_row_bytes;
+    uint8_t* q;
+    int64_t ldq;
+    uint8_t* scales;
+    int64_t lds;
+};
+hipError_t launch_rms_norm(int dt, const NormArgs& a, hipStream_t stream);
+hipError_t launch_quantize_rows(int dt, const char* x, int64_t row_bytes, int64_t rows, int d, uint8_t* q, int64_t ldq, uint8_t* scales,
+                                int64_t lds, hipStream_t stream);
+// hidden rows in 8 bits as bfloat16, row stride d
+hipError_t launch_widen_rows(const uint8_t* q, int64_t ldq, const uint8_t* scales, int64_t lds, int64_t rows, int d, char* out,
+                             hipStream_t stream);
+// out[r, j] = < U[row(r, j), :], h[r, :] >, row(r, j) as in GemvArgs
+struct QuantizedArgs {
+    const char* h;           // bfloat16 rows, or (h_scales != nullptr, the kernel for one row at a time only) rows in 8 bits
+    int64_t ldh;             // bytes
+    const uint8_t* h_scales;
+    int64_t ldhs;
+    const uint8_t* U;
+    int64_t ldu;
+    const uint8_t* u_scales;
+    int64_t ldus;
+    const int32_t* idx;
+    int64_t idx_row_stride;
+    int64_t n_items;
+    const uint32_t* n_items_dev;   // as in GemvArgs
+    int units;               // 16-value units of a row
+    int rows;
+    float* out;
+    int64_t out_row_stride;
+    int64_t u_rows;          // rows of U that idx may name
+    int plain_order;         // as in GemvArgs
+};
+// any lists, a hidden row at a time; entries of -1 read row 0 and get -inf
+hipError_t launch_quantized_gemv(const QuantizedArgs& a, hipStream_t stream);
+// one set of rows of U for all hidden rows (bfloat16), on the matrix cores
+hipError_t launch_quantized_product(const QuantizedArgs& a, hipStream_t stream);
+
+// ---- one token per row from given random numbers (sample_kernels.hip)
+struct SampleArgs {
+    const float* logits;     // rows of n, ld apart
+    int64_t ld;
+    int64_t n;
+    int rows;
+    const int32_t* idx;      // token ids of a row's places, or nullptr
+    int64_t idx_row_stride;  // n (per row) or 0 (one list)
+    const float* temperature;      // [rows] each, or nullptr
+    const int32_t* top_k;
+    const float* top_p;
+    const float* min_p;
+    const float* u;
+    int32_t* tok_out;
+    float* prob_out;         // or nullptr
+    char* scratch;           // sample_scratch_bytes
+};
+size_t sample_scratch_bytes(int64_t rows, int64_t n);
+hipError_t configure_sample_lds();
+hipError_t launch_sample(const SampleArgs& a, hipStream_t stream);
 
 }  // namespace sv

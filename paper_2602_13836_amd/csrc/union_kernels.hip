@@ -366,13 +366,13 @@ size_t union_ws_bytes(int64_t rows, int64_t V, int64_t k) {
     return (4 + flag_words(V) + 2 * vpad + (size_t)rows * (size_t)union_cap(rows, V, k)) * sizeof(uint32_t);
 }
 
-hipError_t launch_union_logits(const GemvArgs& a, int64_t V, void* ws, hipStream_t stream, DeferredPick* defer) {
+// The union of the rows' lists: its tokens, how many, and each token's place, in the workspace.
+hipError_t launch_union_list(const int32_t* idx, int rows, int64_t k, int64_t V, void* ws, hipStream_t stream, UnionList* out) {
     DeviceInfo di;
     hipError_t e = device_info(&di);
     if (e != hipSuccess) return e;
-    const int64_t k = a.n_items;
-    const int64_t pairs = (int64_t)a.rows * k;
-    const UnionWs w = carve(ws, a.rows, V, k);
+    const int64_t pairs = (int64_t)rows * k;
+    const UnionWs w = carve(ws, rows, V, k);
 
     const size_t nclear = 4 + flag_words(V);              // counter + flag bytes (contiguous)
     unsigned cb = (unsigned)((nclear + 1023) / 1024);
@@ -380,7 +380,7 @@ hipError_t launch_union_logits(const GemvArgs& a, int64_t V, void* ws, hipStream
     hipLaunchKernelGGL(clear_kernel, dim3(cb), dim3(256), 0, stream, w.counter, nclear);
     unsigned mb = (unsigned)((pairs + 1023) / 1024);
     if (mb > (unsigned)di.cus * 8) mb = (unsigned)di.cus * 8;
-    hipLaunchKernelGGL(mark_kernel, dim3(mb), dim3(256), 0, stream, a.idx, pairs, w.flag);
+    hipLaunchKernelGGL(mark_kernel, dim3(mb), dim3(256), 0, stream, idx, pairs, w.flag);
     const int64_t vb = (V + kUThreads * kUEpt - 1) / (kUThreads * kUEpt);
     const bool ordered = vb <= kOrderedMaxBlocks;
     if (ordered)
@@ -389,30 +389,50 @@ hipError_t launch_union_logits(const GemvArgs& a, int64_t V, void* ws, hipStream
     else
         hipLaunchKernelGGL(compact_kernel<false>, dim3((unsigned)vb), dim3(kUThreads), 0, stream, w.flag, w.pos, V, w.ulist,
                            w.counter);
+    out->tokens = w.ulist;
+    out->count = w.counter;
+    out->pos = w.pos;
+    out->product = w.zu;
+    out->stride = w.zu_stride;
+    out->ordered = ordered;
+    return hipSuccess;
+}
+
+// out[r, j] = product[r, place of idx[r, j]]
+hipError_t launch_union_pick(const UnionList& u, const int32_t* idx, int rows, int64_t k, float* out, hipStream_t stream) {
+    DeviceInfo di;
+    const hipError_t e = device_info(&di);
+    if (e != hipSuccess) return e;
+    unsigned pb = (unsigned)((k + 1023) / 1024);              // four entries per thread
+    if ((int64_t)pb * rows > (int64_t)di.cus * 16) pb = (unsigned)(((int64_t)di.cus * 16 + rows - 1) / rows);
+    hipLaunchKernelGGL(pick_kernel, dim3(pb, (unsigned)rows), dim3(256), 0, stream, idx, k, u.pos, u.product, u.stride, out);
+    return hipGetLastError();
+}
+
+hipError_t launch_union_logits(const GemvArgs& a, int64_t V, void* ws, hipStream_t stream, DeferredPick* defer) {
+    const int64_t k = a.n_items;
+    UnionList w;
+    hipError_t e = launch_union_list(a.idx, a.rows, k, V, ws, stream, &w);
+    if (e != hipSuccess) return e;
 
     GemvArgs u = a;                                       // product over the union list, all hidden rows
-    u.idx = w.ulist;
+    u.idx = w.tokens;
     u.idx_row_stride = 0;
-    u.n_items = w.zu_stride;                              // upper bound: sizes the grid
-    u.n_items_dev = w.counter;
+    u.n_items = w.stride;                                 // upper bound: sizes the grid
+    u.n_items_dev = w.count;
     u.n_items_min = k;                                    // every row's k items are in the union
-    u.plain_order = ordered ? 0 : 1;                      // a list in run-dependent order: no rotated reduction
-    u.out_f32 = w.zu;
-    u.out_row_stride = w.zu_stride;
+    u.plain_order = w.ordered ? 0 : 1;                    // a list in run-dependent order: no rotated reduction
+    u.out_f32 = w.product;
+    u.out_row_stride = w.stride;
     e = launch_skinny_mfma(u, stream);
     if (e != hipSuccess) return e;
     if (defer) {
         defer->pos = w.pos;
-        defer->zu = w.zu;
-        defer->zu_stride = w.zu_stride;
+        defer->zu = w.product;
+        defer->zu_stride = w.stride;
         return hipSuccess;
     }
-
-    unsigned pb = (unsigned)((k + 1023) / 1024);              // four entries per thread
-    if ((int64_t)pb * a.rows > (int64_t)di.cus * 16) pb = (unsigned)(((int64_t)di.cus * 16 + a.rows - 1) / a.rows);
-    hipLaunchKernelGGL(pick_kernel, dim3(pb, (unsigned)a.rows), dim3(256), 0, stream, a.idx, k, w.pos, w.zu, w.zu_stride,
-                       a.out_f32);
-    return hipGetLastError();
+    return launch_union_pick(w, a.idx, a.rows, k, a.out_f32, stream);
 }
 
 }  // namespace sv
