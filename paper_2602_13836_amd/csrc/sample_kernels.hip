@@ -6,7 +6,7 @@
 //
 // Nothing is sorted.  A histogram over the distance from the row's maximum gives mass (and count) of every bin of the order; the
 // bins in which the three borders and the drawn place lie are known from its running sums, and only the places of those few bins
-// (a few hundred of a vocabulary) are brought together, ranked and summed one by one.
+// (a few hundred of a vocabulary) are brought together, and a bin's are ranked and summed one by one.
 //
 // Precision.  A drawn place changes when a running sum crosses u, so sums are made to be the same as 64-bit ones: w is a double;
 // a bin's mass is a sum of 64-bit integers -- w relative to the bin's upper edge, 1 / 64 of an octave away at most, in units of 2^-S
@@ -25,7 +25,7 @@ namespace sv {
 
 namespace {
 
-constexpr int kCap = 1536;                    // places that are ranked one by one
+constexpr int kList = 1536, kBinPlaces = 1024;        // places that are brought together, and those of a bin that are ranked
 constexpr int kWideBins = 4096, kNarrowBins = 1024;
 constexpr double kOctaves = 64.0;
 typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));      // rows start anywhere
@@ -34,26 +34,55 @@ typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));      // 
 struct RowSettings {
     double c;           // octaves of weight per unit of logit: log2(e) / T
     double width, inv;  // of a bin
-    double limit;       // distance at which the weight is 2^-64
-    float top;          // the row's largest logit
+    double top64;       // the row's largest logit
+    float top;
+    float floor;        // the smallest logit that has mass: 64 octaves below it
 };
 
-__device__ __forceinline__ bool has_mass(float z) { return z > -__builtin_inff(); }      // not -inf, not NaN
+__device__ __forceinline__ bool is_logit(float z) { return z > -__builtin_inff(); }      // not -inf, not NaN
+
+// The smallest key in lo .. hi that ok holds for (ok(hi) does, and it does from there on), 64 candidates at a time: every wavefront by
+// itself, all lanes active.
+template <class F>
+__device__ __forceinline__ uint32_t first_key(uint32_t lo, uint32_t hi, F ok) {
+    while (lo < hi) {
+        const uint32_t step = (hi - lo) / 64u + 1u, lane = threadIdx.x & 63u;
+        const uint32_t at = min(hi - lo, lane * step) + lo;
+        const uint64_t yes = __builtin_amdgcn_ballot_w64(ok(ord_to_f32(at)));
+        const uint32_t n = yes ? (uint32_t)__ffsll((unsigned long long)yes) - 1u : 64u;      // candidates below n are not it
+        const uint32_t up = n < 64u ? min(hi - lo, n * step) + lo : hi;
+        lo = n == 0u ? lo : min(hi - lo, (n - 1u) * step) + lo + 1u;
+        hi = up;
+        if (n == 0u) break;
+    }
+    return hi;
+}
+constexpr uint32_t kLowestKey = 0x00800000u;              // of the lowest finite float
+
+__device__ __forceinline__ double distance_of(const RowSettings& s, float z) { return z == s.top ? 0.0 : s.top64 - (double)z; }
+__device__ __forceinline__ int bin_at(const RowSettings& s, double dist, int bins) { return min((int)(dist * s.inv), bins - 1); }
+// (of a logit that has mass)
+__device__ __forceinline__ int bin_of(const RowSettings& s, float z, int bins) { return bin_at(s, distance_of(s, z), bins); }
+__device__ __forceinline__ double weight_of(const RowSettings& s, float z) { return exp2(-distance_of(s, z) * s.c); }
 
 __device__ __forceinline__ RowSettings settings_of(float t, float top, float low, int bins) {
     RowSettings s;
     s.c = fmax(1.4426950408889634074 / (double)t, 1e-300);
-    s.limit = kOctaves / s.c;
-    // 64 octaves, or the row's range where that is less
-    const double range = top < __builtin_inff() ? (double)top - (double)low : __builtin_inf();
-    s.width = fmax(fmin(s.limit, range * (1.0 + 0x1p-30)) / bins, 1e-290);
-    s.inv = 1.0 / s.width;
     s.top = top;
+    s.top64 = (double)top;
+    const double limit = kOctaves / s.c;
+    // 64 octaves, or the row's range where that is less
+    const double range = top < __builtin_inff() ? s.top64 - (double)low : __builtin_inf();
+    s.width = fmax(fmin(limit, range * (1.0 + 0x1p-30)) / bins, 1e-290);
+    s.inv = 1.0 / s.width;
+    s.floor = ord_to_f32(first_key(kLowestKey, f32_to_ord(top), [&](float z) { return distance_of(s, z) <= limit; }));
     return s;
 }
-__device__ __forceinline__ double distance_of(const RowSettings& s, float z) { return z == s.top ? 0.0 : (double)s.top - (double)z; }
-__device__ __forceinline__ int bin_of(const RowSettings& s, double dist, int bins) { return (int)fmin(dist * s.inv, (double)(bins - 1)); }
-__device__ __forceinline__ double weight_of(const RowSettings& s, float z) { return exp2(-distance_of(s, z) * s.c); }
+
+// the smallest logit whose weight is at least min_p
+__device__ __forceinline__ uint32_t least_key(const RowSettings& s, double min_p) {
+    return first_key(kLowestKey, f32_to_ord(s.top), [&](float z) { return weight_of(s, z) >= min_p; });
+}
 
 // exp(-y), 0 <= y <= ln 2 / (BINS / 64)  (and a rounding more): the series up to where its next term is below 2^-48
 template <int BINS>
@@ -80,19 +109,30 @@ __host__ __device__ inline int mass_bits(int64_t n) {
 }
 
 // a place into the histogram
+struct CountSettings {
+    double cn, wn;       // weight's logarithm per unit of logit, and over a bin
+    double unit;         // 2^S
+};
+__device__ __forceinline__ CountSettings count_settings(const RowSettings& s, int64_t n) {
+    CountSettings c;
+    c.cn = s.c * 0.69314718055994530942;
+    c.wn = s.width * c.cn;
+    c.unit = ldexp(1.0, mass_bits(n));
+    return c;
+}
 template <int BINS>
-__device__ __forceinline__ void count_place(const RowSettings& s, float z, double unit, bool counts, unsigned long long* mass, uint32_t* cnt) {
+__device__ __forceinline__ void count_place(const RowSettings& s, const CountSettings& c, float z, bool counts, unsigned long long* mass, uint32_t* cnt) {
+    if (!(z >= s.floor)) return;
     const double dist = distance_of(s, z);
-    if (!(has_mass(z) && dist <= s.limit)) return;
-    const int b = bin_of(s, dist, BINS);
-    const double y = fmax(dist - b * s.width, 0.0) * (s.c * 0.69314718055994530942);
-    const double w = exp_in_bin<BINS>(y) * unit;
-    // (logits that are all the same: one addition instead of 64 to one address)
-    const uint64_t all = __builtin_amdgcn_ballot_w64(true);
-    const uint32_t first = (uint32_t)__builtin_amdgcn_readfirstlane(__float_as_int(z));
-    unsigned long long m = (unsigned long long)(w + 0.5);
+    const int b = bin_at(s, dist, BINS);
+    const double y = fma(-(double)b, c.wn, dist * c.cn);                // (below zero by a rounding at most)
+    // the mass as an integer: what the addition of 2^52 leaves in the low bits
+    unsigned long long m = (unsigned long long)__double_as_longlong(fma(exp_in_bin<BINS>(y), c.unit, 0x1p52)) & 0xFFFFFFFFFFFFFull;
     uint32_t one = 1u;
-    if (__builtin_amdgcn_ballot_w64(__float_as_uint(z) == first) == all) {
+    // (logits that are all the same: one addition instead of 64 to one address)
+    const uint32_t first = (uint32_t)__builtin_amdgcn_readfirstlane(__float_as_int(z));
+    if (__builtin_amdgcn_ballot_w64(__float_as_uint(z) != first) == 0ull) {
+        const uint64_t all = __builtin_amdgcn_ballot_w64(true);
         one = (uint32_t)__popcll(all);
         m *= one;
         if ((threadIdx.x & 63) != (unsigned)__ffsll((unsigned long long)all) - 1u) return;
@@ -175,7 +215,8 @@ struct RowWork {
     static_assert(BINS % NT == 0, "whole bins per thread");
     unsigned long long mass[BINS];    // of a bin, then (as a double) of the bins in front of it
     uint32_t cnt[BINS];               // the same in places
-    unsigned long long list[kCap], sorted[kCap];
+    unsigned long long list[kList];   // places of a few bins, in no order
+    unsigned long long bin[kBinPlaces], sorted[kBinPlaces];   // those of one bin; then running sums (as doubles), and the places in order
     double red[32];
     int found[4];
     uint32_t fill;
@@ -193,26 +234,32 @@ struct RowSampler {
     uint32_t all;            // places that have any (only if counted)
     int lo[2], hi[2];        // bins whose places are in the list
     uint32_t len;            // of the list
-    bool full;               // the list did not hold a bin's places
+    int ordered;             // the bin that is ranked
+    uint32_t members;        // its places
+    bool full;               // the list, or the room for a bin, did not hold what it had to
 
     __device__ double before(int b) const { return b >= BINS ? total : __longlong_as_double((long long)w.mass[b]); }
     __device__ uint32_t places_before(int b) const { return b >= BINS ? all : w.cnt[b]; }
 
     // running sums over the bins
-    __device__ void scan(double unit, bool counts) {
+    __device__ __forceinline__ void scan(double unit, bool counts) {
         double m[Work::kPer], sum = 0.0;
         uint32_t c[Work::kPer], csum = 0u;
         __syncthreads();
+        const double inv_unit = 1.0 / unit, octaves = s.width * s.c;
 #pragma unroll
         for (int i = 0; i < Work::kPer; ++i) {
             const int b = (int)threadIdx.x * Work::kPer + i;
-            m[i] = (double)w.mass[b] / unit * exp2(-(double)b * s.width * s.c);
+            const unsigned long long raw = w.mass[b];
+            m[i] = raw ? (double)raw * inv_unit * exp2(-(double)b * octaves) : 0.0;
             c[i] = counts ? w.cnt[b] : 0u;
             sum += m[i];
             csum += c[i];
         }
         double at = block_scan_exclusive<Work::kWaves>(sum, w.red, &total);
-        uint32_t cat = block_scan_exclusive<Work::kWaves>(csum, reinterpret_cast<uint32_t*>(w.red), &all);
+        uint32_t cat = 0u;
+        all = 0u;
+        if (counts) cat = block_scan_exclusive<Work::kWaves>(csum, reinterpret_cast<uint32_t*>(w.red), &all);
 #pragma unroll
         for (int i = 0; i < Work::kPer; ++i) {
             const int b = (int)threadIdx.x * Work::kPer + i;
@@ -224,28 +271,24 @@ struct RowSampler {
         __syncthreads();
         lo[0] = lo[1] = 0;
         hi[0] = hi[1] = -1;
-        len = 0u;
+        len = members = 0u;
+        ordered = -1;
         full = false;
     }
 
     // the last bin that `ok` holds for (bin 0, which has the largest logit, if for none)
     template <class F>
-    __device__ int last_bin(F ok) {
-        __syncthreads();
-        if (threadIdx.x == 0) w.found[0] = 0;
-        __syncthreads();
-        int mine = -1;
+    __device__ __forceinline__ int last_bin(F ok) {
+        int mine = 0;
 #pragma unroll
         for (int i = 0; i < Work::kPer; ++i) {
             const int b = (int)threadIdx.x * Work::kPer + i;
             if (ok(b)) mine = b;
         }
-        if (mine >= 0) atomicMax(&w.found[0], mine);
-        __syncthreads();
-        return w.found[0];
+        return (int)block_reduce<Work::kWaves>((uint32_t)mine, reinterpret_cast<uint32_t*>(w.red), [](uint32_t a, uint32_t b) { return umax32(a, b); });
     }
     // the last bin up to `most` that has mass and less than, or `reached`: no more than, `goal` in front of it
-    __device__ int bin_with_mass(double goal, bool reached, int most) {
+    __device__ __forceinline__ int bin_with_mass(double goal, bool reached, int most) {
         return last_bin([&](int b) {
             const double in = before(b);
             return b <= most && before(b + 1) > in && (reached ? in <= goal : in < goal);
@@ -253,41 +296,80 @@ struct RowSampler {
     }
 
     __device__ bool covered(int b) const { return (b >= lo[0] && b <= hi[0]) || (b >= lo[1] && b <= hi[1]); }
+    // the smallest logit of bins 0 .. b; the largest of bins b .. (as bounds that no logit lies between)
+    __device__ __forceinline__ float lowest(int b) const {
+        return ord_to_f32(first_key(f32_to_ord(s.floor), f32_to_ord(s.top), [&](float z) { return bin_of(s, z, BINS) <= b; }));
+    }
+    __device__ __forceinline__ float highest(int b) const { return b == 0 ? s.top : ord_to_f32(f32_to_ord(lowest(b - 1)) - 1u); }
 
-    // the places of bins lo0 .. hi0 and lo1 .. hi1, in order, with the running sums of their weights
-    __device__ void collect(int lo0, int hi0, int lo1, int hi1) {
+    // the places of bins lo0 .. hi0 and lo1 .. hi1
+    __device__ __forceinline__ void collect(int lo0, int hi0, int lo1, int hi1) {
         if (full) return;
+        const float from0 = lowest(hi0), to0 = highest(lo0);
+        const float from1 = hi1 >= lo1 ? lowest(hi1) : 1.0f, to1 = hi1 >= lo1 ? highest(lo1) : 0.0f;
         __syncthreads();
         if (threadIdx.x == 0) w.fill = 0u;
         __syncthreads();
         places([&](float z, int64_t p) {
-            const double dist = distance_of(s, z);
-            if (!(has_mass(z) && dist <= s.limit)) return;
-            const int b = bin_of(s, dist, BINS);
-            if ((b >= lo0 && b <= hi0) || (b >= lo1 && b <= hi1)) {
+            if ((z >= from0 && z <= to0) || (z >= from1 && z <= to1)) {
                 const uint32_t at = atomicAdd(&w.fill, 1u);
-                if (at < (uint32_t)kCap) w.list[at] = make_key(z, (int32_t)p);
+                if (at < (uint32_t)kList) w.list[at] = make_key(z, (int32_t)p);
             }
         });
         __syncthreads();
         len = w.fill;
-        if (len > (uint32_t)kCap) {
+        ordered = -1;
+        if (len > (uint32_t)kList) {
             full = true;
             return;
         }
+        lo[0] = lo0;
+        hi[0] = hi0;
+        lo[1] = lo1;
+        hi[1] = hi1;
+    }
+    // the places of bin b in order, with the running sums of their weights
+    __device__ __forceinline__ void order(int b) {
+        if (ordered == b || full) return;
+        __syncthreads();
+        if (threadIdx.x == 0) w.fill = 0u;
+        __syncthreads();
         for (uint32_t i = threadIdx.x; i < len; i += NT) {
             const unsigned long long k = w.list[i];
-            uint32_t rank = 0u;
-            for (uint32_t j = 0; j < len; ++j) rank += w.list[j] > k ? 1u : 0u;
+            if (bin_of(s, key_value(k), BINS) == b) {
+                const uint32_t at = atomicAdd(&w.fill, 1u);
+                if (at < (uint32_t)kBinPlaces) w.bin[at] = k;
+            }
+        }
+        __syncthreads();
+        members = w.fill;
+        if (members > (uint32_t)kBinPlaces) {
+            full = true;
+            return;
+        }
+        constexpr int kEach = (kBinPlaces + NT - 1) / NT;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const uint32_t at = threadIdx.x + i * NT;
+            if (at >= members) break;
+            const unsigned long long k = w.bin[at];
+            uint32_t rank = 0u, j = 0u;
+            for (; j + 8u <= members; j += 8u) {
+                unsigned long long o[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = w.bin[j + e];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) rank += o[e] > k ? 1u : 0u;
+            }
+            for (; j < members; ++j) rank += w.bin[j] > k ? 1u : 0u;
             w.sorted[rank] = k;
         }
         __syncthreads();
-        constexpr int kEach = (kCap + NT - 1) / NT;
         double v[kEach], sum = 0.0, unused;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const uint32_t at = threadIdx.x * kEach + i;
-            v[i] = at < len ? weight_of(s, key_value(w.sorted[at])) : 0.0;
+            v[i] = at < members ? weight_of(s, key_value(w.sorted[at])) : 0.0;
             sum += v[i];
         }
         double run = block_scan_exclusive<Work::kWaves>(sum, w.red, &unused);
@@ -295,143 +377,111 @@ struct RowSampler {
         for (int i = 0; i < kEach; ++i) {
             run += v[i];
             const uint32_t at = threadIdx.x * kEach + i;
-            if (at < len) w.list[at] = (unsigned long long)__double_as_longlong(run);
+            if (at < members) w.bin[at] = (unsigned long long)__double_as_longlong(run);
         }
         __syncthreads();
-        lo[0] = lo0;
-        hi[0] = hi0;
-        lo[1] = lo1;
-        hi[1] = hi1;
+        ordered = b;
     }
-    __device__ void need(int b) {
-        if (!covered(b)) collect(b, b, 0, -1);
+    // mass of everything up to the first `count` places of bin b (which is ordered)
+    __device__ double mass_upto(int b, uint32_t count) const {
+        return count == 0u ? before(b) : before(b) + __longlong_as_double((long long)w.bin[count - 1u]);
     }
-    __device__ double upto(uint32_t i) const { return __longlong_as_double((long long)w.list[i]); }      // of the first i + 1
-
-    // how many places of bin b fulfil ok(i, sum in front of place i, sum with it); they come first among the bin's
-    template <class F>
-    __device__ uint32_t count_in_bin(int b, uint32_t* first, F ok) {
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            w.found[1] = 0x7fffffff;
-            w.found[2] = 0;
-        }
-        __syncthreads();
-        for (uint32_t i = threadIdx.x; i < len; i += NT) {
-            if (bin_of(s, distance_of(s, key_value(w.sorted[i])), BINS) == b) atomicMin(&w.found[1], (int)i);
-        }
-        __syncthreads();
-        const uint32_t start = (uint32_t)w.found[1];
-        const double shift = start > 0u && start < len ? upto(start - 1) : 0.0;
-        for (uint32_t i = threadIdx.x; i < len; i += NT) {
-            if (i < start || bin_of(s, distance_of(s, key_value(w.sorted[i])), BINS) != b) continue;
-            const double in = before(b) + ((i > start ? upto(i - 1) : shift) - shift);
-            if (ok(i, in, before(b) + (upto(i) - shift))) atomicAdd(&w.found[2], 1);
-        }
-        __syncthreads();
-        *first = start;
-        return (uint32_t)w.found[2];
-    }
-    __device__ double mass_upto(int b, uint32_t first, uint32_t count) {     // of everything up to the first `count` places of bin b
-        if (count == 0u) return before(b);
-        return before(b) + (upto(first + count - 1) - (first > 0u ? upto(first - 1) : 0.0));
-    }
-
-    // the smallest key whose weight is at least min_p
-    __device__ uint32_t least_key(double min_p) const {
-        uint32_t hi_k = f32_to_ord(s.top), lo_k = 0x00800000u;          // (the lowest finite number's)
-        while (lo_k < hi_k) {
-            const uint32_t mid = lo_k + (hi_k - lo_k) / 2;
-            if (weight_of(s, ord_to_f32(mid)) >= min_p) hi_k = mid;
-            else lo_k = mid + 1;
-        }
-        return hi_k;
-    }
-
-    // k: 0 = all places; p >= 1, m <= 0: no such border.  False if the list was too short.
-    __device__ bool draw(uint32_t k, double p, double m, double u, Drawn* out) {
+    // k: 0 = all places; p >= 1, m <= 0: no such border.  False if there was not room enough.
+    __device__ __forceinline__ bool draw(uint32_t k, double p, double m, double u, Drawn* out) {
+        enum { TOP_K, TOP_P, MIN_P, TOKEN };
         const bool with_k = k > 0u && k < all, with_p = p < 1.0, with_m = m > 0.0;
         int border = BINS;                  // bins in front of it are kept as a whole, and the first `take` places of it
-        uint32_t take = 0u, first = 0u;
+        uint32_t take = 0u;
         double kept = total;
-        const uint32_t least = with_m ? least_key(fmin(m, 1.0)) : 0u;
-        const int bin_m = with_m ? bin_of(s, distance_of(s, ord_to_f32(least)), BINS) : BINS;
-        if (with_k) {
-            border = last_bin([&](int b) { return places_before(b) < k && places_before(b + 1) > places_before(b); });
-            const uint32_t ahead = places_before(border);
-            if (places_before(border + 1) <= (uint32_t)kCap) collect(0, border, 0, -1);
-            else collect(border, border, 0, -1);
+        const uint32_t least = with_m ? least_key(s, fmin(m, 1.0)) : 0u;
+        const int bin_m = with_m ? (int)fmin(distance_of(s, ord_to_f32(least)) * s.inv, (double)(BINS - 1)) : BINS;
+#pragma nounroll
+        for (int stage = with_k ? TOP_K : with_p ? TOP_P : with_m ? MIN_P : TOKEN; stage <= TOKEN; ++stage) {
+            if ((stage == TOP_P && !with_p) || (stage == MIN_P && (!with_m || bin_m > border))) continue;
+            const double goal = (stage == TOP_P ? p : u) * kept;
+            int b = bin_m;
+            if (stage == TOP_K) b = last_bin([&](int i) { return places_before(i) < k && places_before(i + 1) > places_before(i); });
+            else if (stage != MIN_P) b = bin_with_mass(goal, stage == TOKEN, stage == TOKEN && take == 0u ? border - 1 : border);
+            if (stage == TOP_P && b > bin_m) continue;               // (the other border comes first)
+            if (!covered(b)) {
+                int l = b, h = b;
+                if (stage == TOP_K) {
+                    if (places_before(b + 1) <= (uint32_t)kList) l = 0;                      // all there will be
+                } else if (stage != TOKEN) {                         // in one pass with the bins where the drawn place can lie then
+                    l = bin_with_mass(u * before(b), true, b);
+                    h = bin_with_mass(u * before(b + 1), true, b);
+                }
+                collect(l, h, b, b);
+            }
+            order(b);
             if (full) return false;
-            count_in_bin(border, &first, [](uint32_t, double, double) { return false; });
-            take = k - ahead;
-            kept = mass_upto(border, first, take);
-        } else if (with_p || with_m) {
-            // the border's bin, and with it, in one pass, the bins where the drawn place can lie
-            const int b = min(with_p ? bin_with_mass(p * total, false, BINS) : BINS - 1, bin_m);
-            const int from = bin_with_mass(u * before(b), true, b), to = bin_with_mass(u * before(b + 1), true, b);
-            collect(from, to, b, b);
-            if (full) return false;
-        }
-        if (with_p) {
-            const double goal = p * kept;
-            const int b = bin_with_mass(goal, false, border);
-            need(b);
-            if (full) return false;
-            uint32_t f;
-            const uint32_t c = max(count_in_bin(b, &f, [&](uint32_t, double in, double) { return in < goal; }), 1u);   // (p <= 0: the first place stays)
+            uint32_t mine = 0u;
+            for (uint32_t i = threadIdx.x; i < members; i += NT) {
+                const bool in = stage == TOP_P ? mass_upto(b, i) < goal : stage == MIN_P ? (uint32_t)(w.sorted[i] >> 32) >= least
+                                                                                       : mass_upto(b, i + 1u) <= goal;
+                mine += in ? 1u : 0u;
+            }
+            uint32_t c = block_reduce<Work::kWaves>(mine, reinterpret_cast<uint32_t*>(w.red), [](uint32_t x, uint32_t y) { return x + y; });
+            if (stage == TOKEN) {
+                c = min(c, (b == border ? min(members, take) : members) - 1u);
+                const unsigned long long key = w.sorted[c];
+                out->place = (int64_t)key_token(key);
+                out->prob = weight_of(s, key_value(key)) / kept;
+                return true;
+            }
+            if (stage == TOP_K) c = k - places_before(b);
+            if (stage == TOP_P) c = umax32(c, 1u);                   // (p <= 0: the first place stays)
             if (b < border || c < take) {
                 border = b;
                 take = c;
-                first = f;
+                kept = mass_upto(b, c);
             }
         }
-        if (with_m && bin_m <= border) {
-            need(bin_m);
-            if (full) return false;
-            uint32_t f;
-            const uint32_t c = count_in_bin(bin_m, &f, [&](uint32_t i, double, double) { return (uint32_t)(w.sorted[i] >> 32) >= least; });
-            if (bin_m < border || c < take) {
-                border = bin_m;
-                take = c;
-                first = f;
-            }
-        }
-        if (border < BINS) {
-            need(border);
-            if (full) return false;
-            count_in_bin(border, &first, [](uint32_t, double, double) { return false; });
-            kept = mass_upto(border, first, take);
-        }
-        const double goal = u * kept;
-        const int b = bin_with_mass(goal, true, take > 0u ? border : border - 1);
-        need(b);
-        if (full) return false;
-        uint32_t f;
-        uint32_t c = count_in_bin(b, &f, [&](uint32_t, double, double with) { return with <= goal; });
-        __syncthreads();
-        if (threadIdx.x == 0) w.found[3] = 0;
-        __syncthreads();
-        for (uint32_t i = threadIdx.x; i < len; i += NT)
-            if (bin_of(s, distance_of(s, key_value(w.sorted[i])), BINS) == b) atomicAdd(&w.found[3], 1);
-        __syncthreads();
-        uint32_t most = (uint32_t)w.found[3];
-        if (b == border) most = min(most, take);
-        c = min(c, most - 1u);
-        const unsigned long long key = w.sorted[f + c];
-        out->place = (int64_t)key_token(key);
-        out->prob = weight_of(s, key_value(key)) / kept;
-        return true;
+        return false;
     }
+};
 
-    // ---- the slow form: borders as (key, how many of the places with that key), found digit by digit
+struct RowInput {
+    float t, p, m;
+    double u;
+    uint32_t k;
+    bool greedy;
+};
+__device__ __forceinline__ RowInput input_of(const SampleArgs& a, int64_t r) {
+    RowInput in;
+    in.t = a.temperature ? a.temperature[r] : 1.0f;
+    in.greedy = !(in.t > 0.0f);
+    const int32_t k = a.top_k ? a.top_k[r] : 0;
+    in.k = k > 0 ? (uint32_t)k : 0u;
+    in.p = a.top_p ? a.top_p[r] : 1.0f;
+    in.m = a.min_p ? a.min_p[r] : 0.0f;
+    const float u = a.u[r];
+    in.u = u > 0.0f ? (double)fminf(u, 0x1.fffffep-1f) : 0.0;       // (the largest below 1)
+    return in;
+}
+__device__ __forceinline__ void put_token(const SampleArgs& a, int64_t r, int64_t place, double prob) {
+    if (threadIdx.x != 0) return;
+    a.tok_out[r] = place < 0 ? -1 : a.idx ? a.idx[r * a.idx_row_stride + place] : (int32_t)place;
+    if (a.prob_out) a.prob_out[r] = (float)prob;
+}
+// ---- the slow form: borders as (key, how many of the places with that key), found digit by digit, from the row in memory
+template <int NT, int BINS>
+struct SlowSampler {
+    using Work = RowWork<NT, BINS>;
+    Work& w;
+    const RowSettings s;
+    const float* z;
+    const int64_t n;
+    double total;
+    uint32_t all;
     struct Edge {
         uint32_t key, ties, places_above;
         double above;                    // mass of the places with larger keys
     };
-    __device__ double units_of(float z, double unit) const { return floor(weight_of(s, z) * unit + 0.5); }
+    __device__ double units_of(float v, double unit) const { return floor(weight_of(s, v) * unit + 0.5); }
     // by rank (the place with `rank` places in front of it) or by mass (the last key with less than, or `reached`: no more
     // than, `goal` in front of it), among the keys from `least` on
-    __device__ Edge descend(bool by_rank, uint32_t rank, double goal, bool reached, uint32_t least, double unit) {
+    __device__ __noinline__ Edge descend(bool by_rank, uint32_t rank, double goal, bool reached, uint32_t least, double unit) {
         Edge e{0u, 0u, 0u, 0.0};
         for (int shift = 24; shift >= 0; shift -= 8) {
             __syncthreads();
@@ -440,11 +490,11 @@ struct RowSampler {
                 w.cnt[i] = 0u;
             }
             __syncthreads();
-            places([&](float z, int64_t) {
-                if (!(has_mass(z) && distance_of(s, z) <= s.limit)) return;
-                const uint32_t key = f32_to_ord(z);
+            for_places<NT>(z, 0, n, [&](float v, int64_t) {
+                if (!(v >= s.floor)) return;
+                const uint32_t key = f32_to_ord(v);
                 if (key < least || (shift < 24 && key >> (shift + 8) != e.key)) return;
-                unsigned long long m = (unsigned long long)units_of(z, unit);
+                unsigned long long m = (unsigned long long)units_of(v, unit);
                 uint32_t one = 1u;
                 const uint64_t active = __builtin_amdgcn_ballot_w64(true);
                 if (__builtin_amdgcn_ballot_w64(key == (uint32_t)__builtin_amdgcn_readfirstlane((int)key)) == active) {
@@ -491,8 +541,7 @@ struct RowSampler {
         }
         return e;
     }
-    // z, from memory: for the order of places with equal logits
-    __device__ void draw_slowly(const float* z, uint32_t k, double p, double m, double u, Drawn* out) {
+    __device__ void draw(uint32_t k, double p, double m, double u, Drawn* out) {
         const double unit = ldexp(1.0, mass_bits(n));
         uint32_t edge = 0u, take = 0u;          // kept: keys above `edge`, and `take` of its own
         auto shorten = [&](uint32_t key, uint32_t t) {
@@ -514,11 +563,11 @@ struct RowSampler {
             const double t = each > 0.0 ? ceil((goal - e.above) / each) : 1.0;
             shorten(e.key, (uint32_t)fmin(fmax(t, 1.0), (double)e.ties));
         }
-        if (m > 0.0) shorten(least_key(fmin(m, 1.0)) - 1u, 0u);
+        if (m > 0.0) shorten(least_key(s, fmin(m, 1.0)) - 1u, 0u);
         // what is kept
         unsigned long long sum = 0ull;
-        places([&](float z_, int64_t) {
-            if (has_mass(z_) && distance_of(s, z_) <= s.limit && f32_to_ord(z_) > edge) sum += (unsigned long long)units_of(z_, unit);
+        for_places<NT>(z, 0, n, [&](float z_, int64_t) {
+            if (z_ >= s.floor && f32_to_ord(z_) > edge) sum += (unsigned long long)units_of(z_, unit);
         });
         sum = block_reduce<Work::kWaves>(sum, reinterpret_cast<unsigned long long*>(w.red), [](unsigned long long a, unsigned long long b) { return a + b; });
         kept = (double)sum / unit + (take ? take * (units_of(ord_to_f32(edge), unit) / unit) : 0.0);
@@ -563,36 +612,20 @@ struct RowSampler {
     }
 };
 
-// ---- a row, from its largest logit on
-struct RowInput {
-    float t, p, m;
-    double u;
-    uint32_t k;
-    bool greedy;
-};
-__device__ __forceinline__ RowInput input_of(const SampleArgs& a, int64_t r) {
-    RowInput in;
-    in.t = a.temperature ? a.temperature[r] : 1.0f;
-    in.greedy = !(in.t > 0.0f);
-    const int32_t k = a.top_k ? a.top_k[r] : 0;
-    in.k = k > 0 ? (uint32_t)k : 0u;
-    in.p = a.top_p ? a.top_p[r] : 1.0f;
-    in.m = a.min_p ? a.min_p[r] : 0.0f;
-    const float u = a.u[r];
-    in.u = u > 0.0f ? (double)fminf(u, 0x1.fffffep-1f) : 0.0;       // (the largest below 1)
-    return in;
+template <int NT, int BINS>
+__device__ __noinline__ void draw_slowly(RowWork<NT, BINS>& w, const SampleArgs& a, int64_t r, float top, double total, uint32_t all) {
+    const RowInput in = input_of(a, r);
+    SlowSampler<NT, BINS> slow{w, settings_of(in.t, top, top, BINS), a.logits + r * a.ld, a.n, total, all};
+    Drawn d;
+    slow.draw(in.k, in.p, in.m, in.u, &d);
+    put_token(a, r, d.place, d.prob);
 }
-__device__ __forceinline__ void put_token(const SampleArgs& a, int64_t r, int64_t place, double prob) {
-    if (threadIdx.x != 0) return;
-    a.tok_out[r] = place < 0 ? -1 : a.idx ? a.idx[r * a.idx_row_stride + place] : (int32_t)place;
-    if (a.prob_out) a.prob_out[r] = (float)prob;
-}
+
 // `filled`: the histogram is there already
 template <int NT, int BINS, class Places>
-__device__ void sample_row(const SampleArgs& a, int64_t r, const RowInput& in, float top, float low, RowWork<NT, BINS>& w,
+__device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t r, const RowInput& in, float top, float low, RowWork<NT, BINS>& w,
                            const Places& places, bool filled) {
-    const float* z = a.logits + r * a.ld;
-    if (!has_mass(top)) return put_token(a, r, -1, 0.0);
+    if (!is_logit(top)) return put_token(a, r, -1, 0.0);
     if (in.greedy) {
         if (threadIdx.x == 0) w.found[0] = 0x7fffffff;
         __syncthreads();
@@ -603,18 +636,18 @@ __device__ void sample_row(const SampleArgs& a, int64_t r, const RowInput& in, f
         return put_token(a, r, w.found[0], 1.0);
     }
     RowSampler<NT, BINS, Places> row{w, places, settings_of(in.t, top, low, BINS), a.n};
-    const double unit = ldexp(1.0, mass_bits(a.n));
+    const CountSettings c = count_settings(row.s, a.n);
     if (!filled) {
         for (int i = threadIdx.x; i < BINS; i += NT) {
             w.mass[i] = 0ull;
             w.cnt[i] = 0u;
         }
         __syncthreads();
-        places([&](float v, int64_t) { count_place<BINS>(row.s, v, unit, in.k > 0u, w.mass, w.cnt); });
+        places([&](float v, int64_t) { count_place<BINS>(row.s, c, v, in.k > 0u, w.mass, w.cnt); });
     }
-    row.scan(unit, in.k > 0u);
+    row.scan(c.unit, in.k > 0u);
     Drawn d;
-    if (!row.draw(in.k, in.p, in.m, in.u, &d)) row.draw_slowly(z, in.k, in.p, in.m, in.u, &d);
+    if (!row.draw(in.k, in.p, in.m, in.u, &d)) return draw_slowly<NT, BINS>(w, a, r, top, row.total, row.all);
     put_token(a, r, d.place, d.prob);
 }
 
@@ -635,7 +668,7 @@ __global__ __launch_bounds__(NT) void sample_short_kernel(const SampleArgs a) {
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        if (has_mass(v[e])) {
+        if (is_logit(v[e])) {
             top = fmaxf(top, v[e]);
             low = fminf(low, v[e]);
         }
@@ -644,7 +677,10 @@ __global__ __launch_bounds__(NT) void sample_short_kernel(const SampleArgs a) {
     low = block_reduce<NT / 64>(low, reinterpret_cast<float*>(w.red), [](float x, float y) { return fminf(x, y); });
     auto places = [&](auto f) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) f(v[e], (int64_t)(e * NT + (int)threadIdx.x));
+        for (int e = 0; e < E; ++e) {
+            f(v[e], (int64_t)(e * NT + (int)threadIdx.x));
+            if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);       // (four at a time: sixteen take more registers than there are)
+        }
     };
     sample_row<NT, BINS>(a, r, in, top, low, w, places, false);
 }
@@ -666,7 +702,7 @@ template <int NT>
 __device__ __forceinline__ float2 range_of(const float* z, int64_t from, int64_t to, float* red) {
     float top = -__builtin_inff(), low = __builtin_inff();
     for_places<NT>(z, from, to, [&](float v, int64_t) {
-        if (has_mass(v)) {
+        if (is_logit(v)) {
             top = fmaxf(top, v);
             low = fminf(low, v);
         }
@@ -705,9 +741,9 @@ __global__ __launch_bounds__(kPartThreads) void sample_count_kernel(const Sample
     const int64_t r = blockIdx.y;
     const RowInput in = input_of(a, r);
     const float2 x = range_of_parts(s, r);
-    if (in.greedy || !has_mass(x.x)) return;
+    if (in.greedy || !is_logit(x.x)) return;
     const RowSettings set = settings_of(in.t, x.x, x.y, kWideBins);
-    const double unit = ldexp(1.0, mass_bits(a.n));
+    const CountSettings c = count_settings(set, a.n);
     for (int i = threadIdx.x; i < kWideBins; i += kPartThreads) {
         mass[i] = 0ull;
         cnt[i] = 0u;
@@ -715,7 +751,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_count_kernel(const Sample
     __syncthreads();
     int64_t from, to;
     part_of(a.n, s.parts, &from, &to);
-    for_places<kPartThreads>(a.logits + r * a.ld, from, to, [&](float v, int64_t) { count_place<kWideBins>(set, v, unit, in.k > 0u, mass, cnt); });
+    for_places<kPartThreads>(a.logits + r * a.ld, from, to, [&](float v, int64_t) { count_place<kWideBins>(set, c, v, in.k > 0u, mass, cnt); });
     __syncthreads();
     for (int i = threadIdx.x; i < kWideBins; i += kPartThreads) {
         if (mass[i]) atomicAdd(&s.mass[r * kWideBins + i], mass[i]);
