@@ -141,65 +141,115 @@ __device__ __forceinline__ void count_place(const RowSettings& s, const CountSet
     if (counts) atomicAdd(&cnt[b], one);
 }
 
-// places [from, to) of a row, f(z, place); all wavefronts of the workgroup
+// Places [from, to) of a row, four at a time on all threads of the workgroup: f(their logits, the first one's place, the step to the
+// next), -inf for those past the end.  Two groups of loads are on their way.
+typedef float (&Quad)[4];
 template <int NT, class F>
-__device__ __forceinline__ void for_places(const float* z, int64_t from, int64_t to, F f) {
+__device__ __forceinline__ void for_quads(const float* z, int64_t from, int64_t to, F f) {
     constexpr int kAhead = 4;
-    const int64_t step = (int64_t)NT * 4;
-    for (int64_t base = from + (int64_t)threadIdx.x * 4; base < to; base += step * kAhead) {
-        f32x4u_t v[kAhead];
+    constexpr int64_t kStep = (int64_t)NT * 4;
+    const int64_t whole = from + ((to - from) & ~(int64_t)3);           // (a last quad that is not whole is read by itself)
+    f32x4u_t now[kAhead], next[kAhead];
+    auto load = [&](int64_t base, f32x4u_t (&v)[kAhead]) {
 #pragma unroll
         for (int a = 0; a < kAhead; ++a) {
-            const int64_t p = base + a * step;
-            v[a] = *reinterpret_cast<const f32x4u_t*>(z + (p + 4 <= to ? p : base + 4 <= to ? base : to - 4));
+            const int64_t p = base + a * kStep;
+            v[a] = p < whole ? *reinterpret_cast<const f32x4u_t*>(z + p) : f32x4u_t{-__builtin_inff(), -__builtin_inff(), -__builtin_inff(), -__builtin_inff()};
         }
+    };
+    const int64_t first = from + (int64_t)threadIdx.x * 4;
+    load(first, now);
+    for (int64_t base = first; base < whole; base += kStep * kAhead) {
+        load(base + kStep * kAhead, next);
 #pragma unroll
         for (int a = 0; a < kAhead; ++a) {
-            const int64_t p = base + a * step;
-            if (p + 4 <= to) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) f(v[a][i], p + i);
-            } else {
-                for (int64_t q = p; q < to; ++q) f(z[q], q);
-            }
+            float v[4] = {now[a][0], now[a][1], now[a][2], now[a][3]};
+            f(v, base + a * kStep, 1);
         }
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) now[a] = next[a];
+    }
+    if (threadIdx.x < 64 && whole < to) {
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = threadIdx.x == 0 && whole + i < to ? z[whole + i] : -__builtin_inff();
+        f(v, whole, 1);
     }
 }
 
-// ---- workgroup-wide reductions and scans of doubles in a fixed order, and of words.  s: 32 doubles of LDS.
-template <int WAVES, class T, class F>
-__device__ __forceinline__ T block_reduce(T x, T* s, F f) {
-    for (int o = 32; o > 0; o >>= 1) x = f(x, __shfl_xor(x, o));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
-    __syncthreads();
-    T t = s[0];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) t = f(t, s[w]);
-    return t;
+// ---- sums over a workgroup, in a fixed order.  Each takes room of its own in LDS, `slot` of two by turns, so that one barrier does.
+__device__ __forceinline__ double dpp_shifted(double x, uint64_t y) { return x + __longlong_as_double((long long)y); }
+__device__ __forceinline__ double wave_prefix_inclusive(double x) {
+    auto bits = [](double v) { return (uint64_t)__double_as_longlong(v); };
+    x = dpp_shifted(x, dpp_u64<DPP_ROW_SHR1>(bits(x)));
+    x = dpp_shifted(x, dpp_u64<DPP_ROW_SHR2>(bits(x)));
+    x = dpp_shifted(x, dpp_u64<DPP_ROW_SHR4>(bits(x)));
+    x = dpp_shifted(x, dpp_u64<DPP_ROW_SHR8>(bits(x)));
+    const double r0 = __longlong_as_double((long long)readlane_u64(bits(x), 15)), r1 = __longlong_as_double((long long)readlane_u64(bits(x), 31)),
+                 r2 = __longlong_as_double((long long)readlane_u64(bits(x), 47));
+    const int row = (threadIdx.x & 63) >> 4;
+    return x + (row >= 1 ? r0 : 0.0) + (row >= 2 ? r1 : 0.0) + (row >= 3 ? r2 : 0.0);
 }
-template <int WAVES, class T>
-__device__ __forceinline__ T block_scan_exclusive(T x, T* s, T* total) {
+__device__ __forceinline__ double lane_f64(double x, int lane) { return __longlong_as_double((long long)readlane_u64((uint64_t)__double_as_longlong(x), lane)); }
+template <int WAVES>
+struct Sums {
+    double d[2][WAVES];
+    uint32_t u[2][WAVES];
+    float f[2][WAVES][2];
+};
+// of the threads in front, and of all
+template <int WAVES>
+__device__ __forceinline__ void block_scan(Sums<WAVES>& s, int slot, double x, uint32_t c, double* before, uint32_t* c_before, double* total, uint32_t* c_total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    T incl = x;
-    for (int o = 1; o < 64; o <<= 1) {
-        const T y = __shfl_up(incl, o);
-        if (lane >= o) incl += y;
+    const double incl = wave_prefix_inclusive(x);
+    const uint32_t c_incl = wave_prefix_inclusive_u32(c);
+    if (lane == 63) {
+        s.d[slot][wave] = incl;
+        s.u[slot][wave] = c_incl;
     }
-    T excl = __shfl_up(incl, 1);
-    if (lane == 0) excl = T(0);
     __syncthreads();
-    if (lane == 63) s[wave] = incl;
-    __syncthreads();
-    T lower = T(0), all = T(0);
+    double lower = 0.0, all = 0.0;
+    uint32_t c_lower = 0u, c_all = 0u;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-        const T v = s[w];
-        if (w < wave) lower += v;
+        const double v = s.d[slot][w];
+        const uint32_t cv = s.u[slot][w];
+        lower += w < wave ? v : 0.0;
+        c_lower += w < wave ? cv : 0u;
         all += v;
+        c_all += cv;
     }
+    *before = lower + (incl - x);
+    *c_before = c_lower + (c_incl - c);
     *total = all;
-    return lower + excl;
+    *c_total = c_all;
+}
+template <int WAVES>
+__device__ __forceinline__ uint32_t block_sum(Sums<WAVES>& s, int slot, uint32_t x) {
+    const uint32_t sum = wave_sum_u32(x);
+    if ((threadIdx.x & 63) == 0) s.u[slot][threadIdx.x >> 6] = sum;
+    __syncthreads();
+    uint32_t all = 0u;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) all += s.u[slot][w];
+    return all;
+}
+// (largest, smallest)
+template <int WAVES>
+__device__ __forceinline__ float2 block_range(Sums<WAVES>& s, int slot, float top, float low) {
+    top = wave_max_f32(top);
+    low = -wave_max_f32(-low);
+    if ((threadIdx.x & 63) == 0) {
+        s.f[slot][threadIdx.x >> 6][0] = top;
+        s.f[slot][threadIdx.x >> 6][1] = low;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        top = fmaxf(top, s.f[slot][w][0]);
+        low = fminf(low, s.f[slot][w][1]);
+    }
+    return float2{top, low};
 }
 
 struct Drawn {
@@ -207,59 +257,62 @@ struct Drawn {
     double prob;
 };
 
-// Everything that happens to one row, by one workgroup.
+// What one workgroup needs for a row.
 template <int NT, int BINS>
 struct RowWork {
     static constexpr int kWaves = NT / 64;
     static constexpr int kPer = BINS / NT;                    // bins of a thread
-    static_assert(BINS % NT == 0, "whole bins per thread");
+    static_assert(BINS % NT == 0 && BINS % 64 == 0 && BINS <= 4096, "whole bins per thread; two rounds of 64 find one");
     unsigned long long mass[BINS];    // of a bin, then (as a double) of the bins in front of it
     uint32_t cnt[BINS];               // the same in places
     unsigned long long list[kList];   // places of a few bins, in no order
     unsigned long long bin[kBinPlaces], sorted[kBinPlaces];   // those of one bin; then running sums (as doubles), and the places in order
-    double red[32];
+    Sums<kWaves> sums;
+    uint32_t fill[8];                 // counters, zero from the start, each used once
     int found[4];
-    uint32_t fill;
 };
 
-// `places(f)` calls f(z, place) for every place of the row on some thread, the same places on the same threads every time.
-template <int NT, int BINS, class Places>
+// `quads(f)` calls f for every four places of the row on some thread, the same places on the same threads every time.  Whatever is
+// found is found by every wavefront for itself where 64 lanes are enough for it: bins (64 x 64), and places of lists of up to 64.
+template <int NT, int BINS, class Quads>
 struct RowSampler {
     using Work = RowWork<NT, BINS>;
     Work& w;
-    const Places& places;
+    const Quads& quads;
     const RowSettings s;
-    const int64_t n;
     double total;            // mass of the row
     uint32_t all;            // places that have any (only if counted)
     int lo[2], hi[2];        // bins whose places are in the list
     uint32_t len;            // of the list
-    int ordered;             // the bin that is ranked
-    uint32_t members;        // its places
+    uint32_t members;        // places of the bin that is ranked
+    unsigned long long key;  // up to 64: this lane's place in order, and the sum up to it
+    double run;
+    int used, slot;
     bool full;               // the list, or the room for a bin, did not hold what it had to
 
-    __device__ double before(int b) const { return b >= BINS ? total : __longlong_as_double((long long)w.mass[b]); }
-    __device__ uint32_t places_before(int b) const { return b >= BINS ? all : w.cnt[b]; }
+    __device__ __forceinline__ double before(int b) const { return b >= BINS ? total : __longlong_as_double((long long)w.mass[b]); }
+    __device__ __forceinline__ uint32_t places_before(int b) const { return b >= BINS ? all : w.cnt[b]; }
+    __device__ __forceinline__ int turn() { return slot ^= 1; }
 
     // running sums over the bins
     __device__ __forceinline__ void scan(double unit, bool counts) {
         double m[Work::kPer], sum = 0.0;
         uint32_t c[Work::kPer], csum = 0u;
+        const double octaves = s.width * s.c, ratio = exp2(-octaves);
+        double edge = exp2(-(double)((int)threadIdx.x * Work::kPer) * octaves) * (1.0 / unit);
         __syncthreads();
-        const double inv_unit = 1.0 / unit, octaves = s.width * s.c;
 #pragma unroll
         for (int i = 0; i < Work::kPer; ++i) {
             const int b = (int)threadIdx.x * Work::kPer + i;
-            const unsigned long long raw = w.mass[b];
-            m[i] = raw ? (double)raw * inv_unit * exp2(-(double)b * octaves) : 0.0;
+            m[i] = (double)w.mass[b] * edge;
+            edge *= ratio;
             c[i] = counts ? w.cnt[b] : 0u;
             sum += m[i];
             csum += c[i];
         }
-        double at = block_scan_exclusive<Work::kWaves>(sum, w.red, &total);
-        uint32_t cat = 0u;
-        all = 0u;
-        if (counts) cat = block_scan_exclusive<Work::kWaves>(csum, reinterpret_cast<uint32_t*>(w.red), &all);
+        double at;
+        uint32_t cat;
+        block_scan<Work::kWaves>(w.sums, turn(), sum, csum, &at, &cat, &total, &all);
 #pragma unroll
         for (int i = 0; i < Work::kPer; ++i) {
             const int b = (int)threadIdx.x * Work::kPer + i;
@@ -269,80 +322,95 @@ struct RowSampler {
             cat += c[i];
         }
         __syncthreads();
-        lo[0] = lo[1] = 0;
-        hi[0] = hi[1] = -1;
-        len = members = 0u;
-        ordered = -1;
-        full = false;
     }
 
-    // the last bin that `ok` holds for (bin 0, which has the largest logit, if for none)
+    // the last bin up to `most` that `ok` holds for; it holds up to some bin (bin 0, if for none)
     template <class F>
-    __device__ __forceinline__ int last_bin(F ok) {
-        int mine = 0;
-#pragma unroll
-        for (int i = 0; i < Work::kPer; ++i) {
-            const int b = (int)threadIdx.x * Work::kPer + i;
-            if (ok(b)) mine = b;
-        }
-        return (int)block_reduce<Work::kWaves>((uint32_t)mine, reinterpret_cast<uint32_t*>(w.red), [](uint32_t a, uint32_t b) { return umax32(a, b); });
+    __device__ __forceinline__ int last_bin(int most, F ok) const {
+        const int lane = threadIdx.x & 63;
+        const uint64_t coarse = __builtin_amdgcn_ballot_w64(lane * (BINS / 64) <= most && ok(lane * (BINS / 64)));
+        const int base = (coarse ? 63 - __builtin_clzll(coarse) : 0) * (BINS / 64);
+        const int b = base + lane;
+        const uint64_t fine = __builtin_amdgcn_ballot_w64(lane < BINS / 64 && b <= most && ok(b));
+        return base + (fine ? 63 - __builtin_clzll(fine) : 0);
     }
     // the last bin up to `most` that has mass and less than, or `reached`: no more than, `goal` in front of it
-    __device__ __forceinline__ int bin_with_mass(double goal, bool reached, int most) {
-        return last_bin([&](int b) {
-            const double in = before(b);
-            return b <= most && before(b + 1) > in && (reached ? in <= goal : in < goal);
-        });
+    __device__ __forceinline__ int bin_with_mass(double goal, bool reached, int most) const {
+        most = min(most, BINS - 1);
+        const double end = before(most + 1);
+        if (goal >= end) return last_bin(most, [&](int b) { return before(b) < end; });
+        return last_bin(most, [&](int b) { return reached ? before(b) <= goal : before(b) < goal; });
     }
 
-    __device__ bool covered(int b) const { return (b >= lo[0] && b <= hi[0]) || (b >= lo[1] && b <= hi[1]); }
+    __device__ __forceinline__ bool covered(int b) const { return (b >= lo[0] && b <= hi[0]) || (b >= lo[1] && b <= hi[1]); }
     // the smallest logit of bins 0 .. b; the largest of bins b .. (as bounds that no logit lies between)
     __device__ __forceinline__ float lowest(int b) const {
         return ord_to_f32(first_key(f32_to_ord(s.floor), f32_to_ord(s.top), [&](float z) { return bin_of(s, z, BINS) <= b; }));
     }
     __device__ __forceinline__ float highest(int b) const { return b == 0 ? s.top : ord_to_f32(f32_to_ord(lowest(b - 1)) - 1u); }
 
-    // the places of bins lo0 .. hi0 and lo1 .. hi1
+    // the places of bins lo0 .. hi0 and lo1 .. hi1 (hi0 <= hi1)
     __device__ __forceinline__ void collect(int lo0, int hi0, int lo1, int hi1) {
-        if (full) return;
-        const float from0 = lowest(hi0), to0 = highest(lo0);
-        const float from1 = hi1 >= lo1 ? lowest(hi1) : 1.0f, to1 = hi1 >= lo1 ? highest(lo1) : 0.0f;
-        __syncthreads();
-        if (threadIdx.x == 0) w.fill = 0u;
-        __syncthreads();
-        places([&](float z, int64_t p) {
-            if ((z >= from0 && z <= to0) || (z >= from1 && z <= to1)) {
-                const uint32_t at = atomicAdd(&w.fill, 1u);
-                if (at < (uint32_t)kList) w.list[at] = make_key(z, (int32_t)p);
+        const float from1 = lowest(hi1), to1 = highest(lo1), to0 = highest(lo0), from0 = hi0 == hi1 ? from1 : lowest(hi0);
+        if (used > 0) __syncthreads();                               // (an earlier list is read)
+        uint32_t* fill = &w.fill[used++];
+        quads([&](Quad v, int64_t p, int step) {
+            if (!(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) >= from1)) return;        // (fmaxf: NaN only of NaNs)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float z = v[i];
+                if ((z >= from0 && z <= to0) || (z >= from1 && z <= to1)) {
+                    const uint32_t at = atomicAdd(fill, 1u);
+                    if (at < (uint32_t)kList) w.list[at] = make_key(z, (int32_t)(p + i * step));
+                }
             }
         });
         __syncthreads();
-        len = w.fill;
-        ordered = -1;
-        if (len > (uint32_t)kList) {
-            full = true;
-            return;
-        }
+        len = *fill;
+        full = len > (uint32_t)kList;
         lo[0] = lo0;
         hi[0] = hi0;
         lo[1] = lo1;
         hi[1] = hi1;
     }
-    // the places of bin b in order, with the running sums of their weights
+    // The places of bin b, which the list has, in order, with the running sums of their weights: up to 64 in the lanes of every wavefront,
+    // more in LDS
     __device__ __forceinline__ void order(int b) {
-        if (ordered == b || full) return;
-        __syncthreads();
-        if (threadIdx.x == 0) w.fill = 0u;
-        __syncthreads();
+        const uint32_t lane = threadIdx.x & 63u;
+        unsigned long long mine = 0ull;
+        if (len <= 64u) {
+            if (lane < len) mine = w.list[lane];
+            if (lane >= len || bin_of(s, key_value(mine), BINS) != b) mine = 0ull;       // (no place's key)
+            members = (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(mine != 0ull));
+            uint32_t rank = 0u;
+            for (uint32_t j = 0; j < len; ++j) {
+                const unsigned long long o = readlane_u64(mine, (int)j);
+                rank += o > mine ? 1u : 0u;
+            }
+            rank_lanes(mine, rank);
+            return;
+        }
+        uint32_t* fill = &w.fill[used++];
+        __syncthreads();                                              // (what an earlier bin left there is read)
         for (uint32_t i = threadIdx.x; i < len; i += NT) {
             const unsigned long long k = w.list[i];
             if (bin_of(s, key_value(k), BINS) == b) {
-                const uint32_t at = atomicAdd(&w.fill, 1u);
+                const uint32_t at = atomicAdd(fill, 1u);
                 if (at < (uint32_t)kBinPlaces) w.bin[at] = k;
             }
         }
         __syncthreads();
-        members = w.fill;
+        members = *fill;
+        if (members <= 64u) {
+            if (lane < members) mine = w.bin[lane];
+            uint32_t rank = 0u;
+            for (uint32_t j = 0; j < members; ++j) {
+                const unsigned long long o = readlane_u64(mine, (int)j);
+                rank += o > mine ? 1u : 0u;
+            }
+            rank_lanes(mine, rank);
+            return;
+        }
         if (members > (uint32_t)kBinPlaces) {
             full = true;
             return;
@@ -365,30 +433,63 @@ struct RowSampler {
             w.sorted[rank] = k;
         }
         __syncthreads();
-        double v[kEach], sum = 0.0, unused;
+        double v[kEach], sum = 0.0, at_sum, unused;
+        uint32_t u0, u1;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const uint32_t at = threadIdx.x * kEach + i;
             v[i] = at < members ? weight_of(s, key_value(w.sorted[at])) : 0.0;
             sum += v[i];
         }
-        double run = block_scan_exclusive<Work::kWaves>(sum, w.red, &unused);
+        block_scan<Work::kWaves>(w.sums, turn(), sum, 0u, &at_sum, &u0, &unused, &u1);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            run += v[i];
+            at_sum += v[i];
             const uint32_t at = threadIdx.x * kEach + i;
-            if (at < members) w.bin[at] = (unsigned long long)__double_as_longlong(run);
+            if (at < members) w.bin[at] = (unsigned long long)__double_as_longlong(at_sum);
         }
         __syncthreads();
-        ordered = b;
     }
-    // mass of everything up to the first `count` places of bin b (which is ordered)
-    __device__ double mass_upto(int b, uint32_t count) const {
-        return count == 0u ? before(b) : before(b) + __longlong_as_double((long long)w.bin[count - 1u]);
+    // up to 64 places, one per lane, to the lanes of their ranks
+    __device__ __forceinline__ void rank_lanes(unsigned long long mine, uint32_t rank) {
+        const uint32_t lane = threadIdx.x & 63u;
+        // (lanes without a place go to the ranks behind: which, does not matter as long as they differ from the others')
+        const uint64_t none = __builtin_amdgcn_ballot_w64(mine == 0ull);
+        if (mine == 0ull) rank = members + (uint32_t)__popcll(none & ((1ull << lane) - 1ull));
+        const uint32_t l = (uint32_t)__builtin_amdgcn_ds_permute((int)(rank * 4u), (int)(uint32_t)mine);
+        const uint32_t h = (uint32_t)__builtin_amdgcn_ds_permute((int)(rank * 4u), (int)(uint32_t)(mine >> 32));
+        key = (unsigned long long)h << 32 | l;
+        run = wave_prefix_inclusive(lane < members ? weight_of(s, key_value(key)) : 0.0);
     }
+    __device__ __forceinline__ unsigned long long place_key(uint32_t i) const { return members <= 64u ? readlane_u64(key, (int)i) : w.sorted[i]; }
+    // mass of everything up to the first `count` places of bin b (which is in order)
+    __device__ __forceinline__ double mass_upto(int b, uint32_t count) const {
+        if (count == 0u) return before(b);
+        return before(b) + (members <= 64u ? lane_f64(run, (int)count - 1) : __longlong_as_double((long long)w.bin[count - 1u]));
+    }
+    // how many of the places of bin b have `less` than goal in front of them, or key >= least, or no more than goal up to and with them
+    __device__ __forceinline__ uint32_t count_places(int b, bool ahead, bool by_key, double goal, uint32_t least) {
+        if (members <= 64u) {
+            const int lane = threadIdx.x & 63;
+            const double in = __shfl_up(run, 1), mine = before(b) + (ahead ? lane == 0 ? 0.0 : in : run);
+            const bool ok = by_key ? (uint32_t)(key >> 32) >= least : ahead ? mine < goal : mine <= goal;
+            return (uint32_t)__popcll(__builtin_amdgcn_ballot_w64((uint32_t)lane < members && ok));
+        }
+        uint32_t mine = 0u;
+        for (uint32_t i = threadIdx.x; i < members; i += NT) {
+            const bool ok = by_key ? (uint32_t)(w.sorted[i] >> 32) >= least : ahead ? mass_upto(b, i) < goal : mass_upto(b, i + 1u) <= goal;
+            mine += ok ? 1u : 0u;
+        }
+        return block_sum<Work::kWaves>(w.sums, turn(), mine);
+    }
+
     // k: 0 = all places; p >= 1, m <= 0: no such border.  False if there was not room enough.
     __device__ __forceinline__ bool draw(uint32_t k, double p, double m, double u, Drawn* out) {
         enum { TOP_K, TOP_P, MIN_P, TOKEN };
+        lo[0] = lo[1] = 0;
+        hi[0] = hi[1] = -1;
+        len = members = 0u;
+        full = false;
         const bool with_k = k > 0u && k < all, with_p = p < 1.0, with_m = m > 0.0;
         int border = BINS;                  // bins in front of it are kept as a whole, and the first `take` places of it
         uint32_t take = 0u;
@@ -400,7 +501,7 @@ struct RowSampler {
             if ((stage == TOP_P && !with_p) || (stage == MIN_P && (!with_m || bin_m > border))) continue;
             const double goal = (stage == TOP_P ? p : u) * kept;
             int b = bin_m;
-            if (stage == TOP_K) b = last_bin([&](int i) { return places_before(i) < k && places_before(i + 1) > places_before(i); });
+            if (stage == TOP_K) b = last_bin(BINS - 1, [&](int i) { return places_before(i) < k; });
             else if (stage != MIN_P) b = bin_with_mass(goal, stage == TOKEN, stage == TOKEN && take == 0u ? border - 1 : border);
             if (stage == TOP_P && b > bin_m) continue;               // (the other border comes first)
             if (!covered(b)) {
@@ -412,24 +513,18 @@ struct RowSampler {
                     h = bin_with_mass(u * before(b + 1), true, b);
                 }
                 collect(l, h, b, b);
+                if (full) return false;
             }
             order(b);
             if (full) return false;
-            uint32_t mine = 0u;
-            for (uint32_t i = threadIdx.x; i < members; i += NT) {
-                const bool in = stage == TOP_P ? mass_upto(b, i) < goal : stage == MIN_P ? (uint32_t)(w.sorted[i] >> 32) >= least
-                                                                                       : mass_upto(b, i + 1u) <= goal;
-                mine += in ? 1u : 0u;
-            }
-            uint32_t c = block_reduce<Work::kWaves>(mine, reinterpret_cast<uint32_t*>(w.red), [](uint32_t x, uint32_t y) { return x + y; });
+            uint32_t c = stage == TOP_K ? k - places_before(b) : count_places(b, stage == TOP_P, stage == MIN_P, goal, least);
             if (stage == TOKEN) {
                 c = min(c, (b == border ? min(members, take) : members) - 1u);
-                const unsigned long long key = w.sorted[c];
-                out->place = (int64_t)key_token(key);
-                out->prob = weight_of(s, key_value(key)) / kept;
+                const unsigned long long drawn = place_key(c);
+                out->place = (int64_t)key_token(drawn);
+                out->prob = weight_of(s, key_value(drawn)) / kept;
                 return true;
             }
-            if (stage == TOP_K) c = k - places_before(b);
             if (stage == TOP_P) c = umax32(c, 1u);                   // (p <= 0: the first place stays)
             if (b < border || c < take) {
                 border = b;
@@ -490,29 +585,34 @@ struct SlowSampler {
                 w.cnt[i] = 0u;
             }
             __syncthreads();
-            for_places<NT>(z, 0, n, [&](float v, int64_t) {
-                if (!(v >= s.floor)) return;
+            for_quads<NT>(z, 0, n, [&](Quad q, int64_t, int) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float v = q[i];
+                if (!(v >= s.floor)) continue;
                 const uint32_t key = f32_to_ord(v);
-                if (key < least || (shift < 24 && key >> (shift + 8) != e.key)) return;
+                if (key < least || (shift < 24 && key >> (shift + 8) != e.key)) continue;
                 unsigned long long m = (unsigned long long)units_of(v, unit);
                 uint32_t one = 1u;
                 const uint64_t active = __builtin_amdgcn_ballot_w64(true);
                 if (__builtin_amdgcn_ballot_w64(key == (uint32_t)__builtin_amdgcn_readfirstlane((int)key)) == active) {
                     one = (uint32_t)__popcll(active);
                     m *= one;
-                    if ((threadIdx.x & 63) != (unsigned)__ffsll((unsigned long long)active) - 1u) return;
+                    if ((threadIdx.x & 63) != (unsigned)__ffsll((unsigned long long)active) - 1u) continue;
                 }
                 atomicAdd(&w.mass[key >> shift & 255u], m);
                 atomicAdd(&w.cnt[key >> shift & 255u], one);
+              }
             });
             __syncthreads();
             const int digit = 255 - (int)threadIdx.x;
             const uint32_t c = digit >= 0 ? w.cnt[digit] : 0u;
             const double m = digit >= 0 ? (double)w.mass[digit] / unit : 0.0;
-            double msum;
-            uint32_t csum;
-            const double in = e.above + block_scan_exclusive<Work::kWaves>(m, w.red, &msum);
-            const uint32_t cin = e.places_above + block_scan_exclusive<Work::kWaves>(c, reinterpret_cast<uint32_t*>(w.red), &csum);
+            double in, msum;
+            uint32_t cin, csum;
+            block_scan<Work::kWaves>(w.sums, (shift >> 3) & 1, m, c, &in, &cin, &msum, &csum);
+            in += e.above;
+            cin += e.places_above;
             __syncthreads();
             if (threadIdx.x == 0) w.found[0] = 0;
             __syncthreads();
@@ -529,12 +629,12 @@ struct SlowSampler {
                 at = w.found[0];
             }
             if ((int)threadIdx.x == at) {
-                w.red[30] = in;
+                w.mass[256] = (unsigned long long)__double_as_longlong(in);
                 w.found[1] = (int)cin;
                 w.found[2] = (int)c;
             }
             __syncthreads();
-            e.above = w.red[30];
+            e.above = __longlong_as_double((long long)w.mass[256]);
             e.places_above = (uint32_t)w.found[1];
             e.ties = (uint32_t)w.found[2];
             e.key = e.key << 8 | (uint32_t)(255 - at);
@@ -566,10 +666,17 @@ struct SlowSampler {
         if (m > 0.0) shorten(least_key(s, fmin(m, 1.0)) - 1u, 0u);
         // what is kept
         unsigned long long sum = 0ull;
-        for_places<NT>(z, 0, n, [&](float z_, int64_t) {
-            if (z_ >= s.floor && f32_to_ord(z_) > edge) sum += (unsigned long long)units_of(z_, unit);
+        for_quads<NT>(z, 0, n, [&](Quad q, int64_t, int) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (q[i] >= s.floor && f32_to_ord(q[i]) > edge) sum += (unsigned long long)units_of(q[i], unit);
         });
-        sum = block_reduce<Work::kWaves>(sum, reinterpret_cast<unsigned long long*>(w.red), [](unsigned long long a, unsigned long long b) { return a + b; });
+        __syncthreads();
+        if (threadIdx.x == 0) w.mass[0] = 0ull;
+        __syncthreads();
+        atomicAdd(&w.mass[0], sum);                                  // (integers: in any order)
+        __syncthreads();
+        sum = w.mass[0];
         kept = (double)sum / unit + (take ? take * (units_of(ord_to_f32(edge), unit) / unit) : 0.0);
         const double goal = u * kept;
         const Edge e = descend(false, 0u, goal, true, take ? edge : edge + 1u, unit);
@@ -621,29 +728,40 @@ __device__ __noinline__ void draw_slowly(RowWork<NT, BINS>& w, const SampleArgs&
     put_token(a, r, d.place, d.prob);
 }
 
+// counters and (bins) the histogram; a barrier has to follow
+template <int NT, int BINS>
+__device__ __forceinline__ void clear_work(RowWork<NT, BINS>& w, bool bins) {
+    if (threadIdx.x < 8) w.fill[threadIdx.x] = 0u;
+    if (threadIdx.x == 0) w.found[0] = 0x7fffffff;
+    if (!bins) return;
+    for (int i = threadIdx.x; i < BINS; i += NT) {
+        w.mass[i] = 0ull;
+        w.cnt[i] = 0u;
+    }
+}
 // `filled`: the histogram is there already
-template <int NT, int BINS, class Places>
+template <int NT, int BINS, class Quads>
 __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t r, const RowInput& in, float top, float low, RowWork<NT, BINS>& w,
-                           const Places& places, bool filled) {
+                                           const Quads& quads, bool filled) {
     if (!is_logit(top)) return put_token(a, r, -1, 0.0);
     if (in.greedy) {
-        if (threadIdx.x == 0) w.found[0] = 0x7fffffff;
-        __syncthreads();
-        places([&](float v, int64_t p) {
-            if (v == top) atomicMin(&w.found[0], (int)p);
+        quads([&](Quad v, int64_t p, int step) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (v[i] == top) atomicMin(&w.found[0], (int)p + i * step);
         });
         __syncthreads();
         return put_token(a, r, w.found[0], 1.0);
     }
-    RowSampler<NT, BINS, Places> row{w, places, settings_of(in.t, top, low, BINS), a.n};
+    RowSampler<NT, BINS, Quads> row{w, quads, settings_of(in.t, top, low, BINS)};
+    row.used = 0;
+    row.slot = 0;
     const CountSettings c = count_settings(row.s, a.n);
     if (!filled) {
-        for (int i = threadIdx.x; i < BINS; i += NT) {
-            w.mass[i] = 0ull;
-            w.cnt[i] = 0u;
-        }
-        __syncthreads();
-        places([&](float v, int64_t) { count_place<BINS>(row.s, c, v, in.k > 0u, w.mass, w.cnt); });
+        quads([&](Quad v, int64_t, int) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) count_place<BINS>(row.s, c, v[i], in.k > 0u, w.mass, w.cnt);
+        });
     }
     row.scan(c.unit, in.k > 0u);
     Drawn d;
@@ -660,12 +778,13 @@ __global__ __launch_bounds__(NT) void sample_short_kernel(const SampleArgs a) {
     const float* z = a.logits + r * a.ld;
     const RowInput in = input_of(a, r);
     float v[E];
-    float top = -__builtin_inff(), low = __builtin_inff();
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         const int p = e * NT + (int)threadIdx.x;
         v[e] = p < a.n ? z[p] : -__builtin_inff();
     }
+    clear_work(w, true);
+    float top = -__builtin_inff(), low = __builtin_inff();
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         if (is_logit(v[e])) {
@@ -673,16 +792,16 @@ __global__ __launch_bounds__(NT) void sample_short_kernel(const SampleArgs a) {
             low = fminf(low, v[e]);
         }
     }
-    top = block_reduce<NT / 64>(top, reinterpret_cast<float*>(w.red), [](float x, float y) { return fmaxf(x, y); });
-    low = block_reduce<NT / 64>(low, reinterpret_cast<float*>(w.red), [](float x, float y) { return fminf(x, y); });
-    auto places = [&](auto f) {
+    const float2 x = block_range<NT / 64>(w.sums, 0, top, low);
+    auto quads = [&](auto f) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            f(v[e], (int64_t)(e * NT + (int)threadIdx.x));
-            if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);       // (four at a time: sixteen take more registers than there are)
+        for (int e = 0; e < E; e += 4) {
+            float q[4] = {v[e], v[e + 1], v[e + 2], v[e + 3]};
+            f(q, (int64_t)(e * NT + (int)threadIdx.x), NT);
+            __builtin_amdgcn_sched_barrier(0);                       // (four at a time: sixteen take more registers than there are)
         }
     };
-    sample_row<NT, BINS>(a, r, in, top, low, w, places, false);
+    sample_row<NT, BINS>(a, r, in, x.x, x.y, w, quads, false);
 }
 
 // ---- longer rows.  A workgroup per row reads it once for its range, once for the histogram and once for each list; where rows are
@@ -699,17 +818,16 @@ __device__ __forceinline__ void part_of(int64_t n, int parts, int64_t* from, int
     *to = min(*from + len, n);
 }
 template <int NT>
-__device__ __forceinline__ float2 range_of(const float* z, int64_t from, int64_t to, float* red) {
+__device__ __forceinline__ float2 range_of(const float* z, int64_t from, int64_t to, Sums<NT / 64>& sums) {
     float top = -__builtin_inff(), low = __builtin_inff();
-    for_places<NT>(z, from, to, [&](float v, int64_t) {
-        if (is_logit(v)) {
-            top = fmaxf(top, v);
-            low = fminf(low, v);
+    for_quads<NT>(z, from, to, [&](Quad v, int64_t, int) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            top = fmaxf(top, v[i]);                                  // (NaN and -inf change nothing)
+            low = fminf(low, is_logit(v[i]) ? v[i] : __builtin_inff());
         }
     });
-    top = block_reduce<NT / 64>(top, red, [](float x, float y) { return fmaxf(x, y); });
-    low = block_reduce<NT / 64>(low, red, [](float x, float y) { return fminf(x, y); });
-    return float2{top, low};
+    return block_range<NT / 64>(sums, 0, top, low);
 }
 __device__ __forceinline__ float2 range_of_parts(const SampleScratch& s, int64_t r) {
     float top = -__builtin_inff(), low = __builtin_inff();
@@ -723,7 +841,7 @@ __device__ __forceinline__ float2 range_of_parts(const SampleScratch& s, int64_t
 
 constexpr int kPartThreads = 256;
 __global__ __launch_bounds__(kPartThreads) void sample_range_kernel(const SampleArgs a, const SampleScratch s) {
-    __shared__ float red[32];
+    __shared__ Sums<kPartThreads / 64> sums;
     const int64_t r = blockIdx.y;
     for (int i = (int)blockIdx.x * kPartThreads + (int)threadIdx.x; i < kWideBins; i += (int)gridDim.x * kPartThreads) {
         s.mass[r * kWideBins + i] = 0ull;
@@ -731,7 +849,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_range_kernel(const Sample
     }
     int64_t from, to;
     part_of(a.n, s.parts, &from, &to);
-    const float2 x = range_of<kPartThreads>(a.logits + r * a.ld, from, to, red);
+    const float2 x = range_of<kPartThreads>(a.logits + r * a.ld, from, to, sums);
     if (threadIdx.x == 0) s.range[r * s.parts + blockIdx.x] = x;
 }
 __global__ __launch_bounds__(kPartThreads) void sample_count_kernel(const SampleArgs a, const SampleScratch s) {
@@ -751,7 +869,10 @@ __global__ __launch_bounds__(kPartThreads) void sample_count_kernel(const Sample
     __syncthreads();
     int64_t from, to;
     part_of(a.n, s.parts, &from, &to);
-    for_places<kPartThreads>(a.logits + r * a.ld, from, to, [&](float v, int64_t) { count_place<kWideBins>(set, c, v, in.k > 0u, mass, cnt); });
+    for_quads<kPartThreads>(a.logits + r * a.ld, from, to, [&](Quad v, int64_t, int) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) count_place<kWideBins>(set, c, v[i], in.k > 0u, mass, cnt);
+    });
     __syncthreads();
     for (int i = threadIdx.x; i < kWideBins; i += kPartThreads) {
         if (mass[i]) atomicAdd(&s.mass[r * kWideBins + i], mass[i]);
@@ -767,6 +888,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_long_kernel(const SampleAr
     const int64_t r = blockIdx.x;
     const float* z = a.logits + r * a.ld;
     const RowInput in = input_of(a, r);
+    clear_work(w, !PARTS);
     float2 x;
     if constexpr (PARTS) {
         x = range_of_parts(s, r);
@@ -775,10 +897,11 @@ __global__ __launch_bounds__(kRowThreads) void sample_long_kernel(const SampleAr
             w.cnt[i] = s.cnt[r * kWideBins + i];
         }
     } else {
-        x = range_of<kRowThreads>(z, 0, a.n, reinterpret_cast<float*>(w.red));
+        x = range_of<kRowThreads>(z, 0, a.n, w.sums);
     }
-    auto places = [&](auto f) { for_places<kRowThreads>(z, 0, a.n, f); };
-    sample_row<kRowThreads, kWideBins>(a, r, in, x.x, x.y, w, places, PARTS);
+    auto quads = [&](auto f) { for_quads<kRowThreads>(z, 0, a.n, f); };
+    if (PARTS) __syncthreads();
+    sample_row<kRowThreads, kWideBins>(a, r, in, x.x, x.y, w, quads, PARTS);
 }
 
 constexpr int64_t kShort = 16384;
@@ -813,6 +936,8 @@ hipError_t launch_sample(const SampleArgs& a, hipStream_t stream) {
         hipLaunchKernelGGL((sample_short_kernel<256, 4, kNarrowBins>), dim3(rows), dim3(256), sizeof(RowWork<256, kNarrowBins>), stream, a);
     else if (a.n <= 4096)
         hipLaunchKernelGGL((sample_short_kernel<256, 16, kNarrowBins>), dim3(rows), dim3(256), sizeof(RowWork<256, kNarrowBins>), stream, a);
+    else if (a.n <= 8192)
+        hipLaunchKernelGGL((sample_short_kernel<512, 16, kNarrowBins>), dim3(rows), dim3(512), sizeof(RowWork<512, kNarrowBins>), stream, a);
     else if (a.n <= kShort)
         hipLaunchKernelGGL((sample_short_kernel<1024, 16, kNarrowBins>), dim3(rows), dim3(1024), sizeof(RowWork<1024, kNarrowBins>), stream, a);
     else {
