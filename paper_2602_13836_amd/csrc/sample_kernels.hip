@@ -41,22 +41,6 @@ struct RowSettings {
 
 __device__ __forceinline__ bool is_logit(float z) { return z > -__builtin_inff(); }      // not -inf, not NaN
 
-// The smallest key in lo .. hi that ok holds for (ok(hi) does, and it does from there on), 64 candidates at a time: every wavefront by
-// itself, all lanes active.
-template <class F>
-__device__ __forceinline__ uint32_t first_key(uint32_t lo, uint32_t hi, F ok) {
-    while (lo < hi) {
-        const uint32_t step = (hi - lo) / 64u + 1u, lane = threadIdx.x & 63u;
-        const uint32_t at = min(hi - lo, lane * step) + lo;
-        const uint64_t yes = __builtin_amdgcn_ballot_w64(ok(ord_to_f32(at)));
-        const uint32_t n = yes ? (uint32_t)__ffsll((unsigned long long)yes) - 1u : 64u;      // candidates below n are not it
-        const uint32_t up = n < 64u ? min(hi - lo, n * step) + lo : hi;
-        lo = n == 0u ? lo : min(hi - lo, (n - 1u) * step) + lo + 1u;
-        hi = up;
-        if (n == 0u) break;
-    }
-    return hi;
-}
 constexpr uint32_t kLowestKey = 0x00800000u;              // of the lowest finite float
 
 __device__ __forceinline__ double distance_of(const RowSettings& s, float z) { return z == s.top ? 0.0 : s.top64 - (double)z; }
@@ -75,13 +59,32 @@ __device__ __forceinline__ RowSettings settings_of(float t, float top, float low
     const double range = top < __builtin_inff() ? s.top64 - (double)low : __builtin_inf();
     s.width = fmax(fmin(limit, range * (1.0 + 0x1p-30)) / bins, 1e-290);
     s.inv = 1.0 / s.width;
-    s.floor = ord_to_f32(first_key(kLowestKey, f32_to_ord(top), [&](float z) { return distance_of(s, z) <= limit; }));
+    s.floor = fmaxf((float)(s.top64 - limit), -3.402823466e38f);
     return s;
 }
 
-// the smallest logit whose weight is at least min_p
+// The smallest key of a logit whose weight is at least min_p: among the 64 around where the logarithm puts it, or (a logarithm that is too
+// far off for that, with logits so close to zero that their keys are dense) 64 candidates at a time among all.  All lanes active.
 __device__ __forceinline__ uint32_t least_key(const RowSettings& s, double min_p) {
-    return first_key(kLowestKey, f32_to_ord(s.top), [&](float z) { return weight_of(s, z) >= min_p; });
+    const uint32_t lane = threadIdx.x & 63u, last = f32_to_ord(s.top);
+    auto enough = [&](uint32_t key) { return weight_of(s, ord_to_f32(key)) >= min_p; };
+    auto first_of = [](uint64_t yes) { return (uint32_t)__ffsll((unsigned long long)yes) - 1u; };
+    const uint32_t guess = f32_to_ord(fmaxf((float)(s.top64 + log2(min_p) / s.c), -3.402823466e38f));
+    uint32_t lo = guess > kLowestKey + 32u ? guess - 32u : kLowestKey, hi = last;
+    uint64_t yes = __builtin_amdgcn_ballot_w64(lo + lane >= last || enough(lo + lane));
+    if (yes != 0ull && ((yes & 1ull) == 0ull || lo == kLowestKey)) return min(lo + first_of(yes), last);
+    lo = kLowestKey;
+    while (lo < hi) {                                       // (`hi` fulfils it)
+        const uint32_t step = (hi - lo) / 64u + 1u;
+        auto candidate = [&](uint32_t i) { return min(hi - lo, i * step) + lo; };
+        yes = __builtin_amdgcn_ballot_w64(enough(candidate(lane)));
+        const uint32_t n = yes ? first_of(yes) : 64u;       // candidates in front of the n-th are not it
+        if (n == 0u) return lo;
+        const uint32_t up = n < 64u ? candidate(n) : hi;
+        lo = candidate(n - 1u) + 1u;
+        hi = up;
+    }
+    return hi;
 }
 
 // exp(-y), 0 <= y <= ln 2 / (BINS / 64)  (and a rounding more): the series up to where its next term is below 2^-48
@@ -144,9 +147,9 @@ __device__ __forceinline__ void count_place(const RowSettings& s, const CountSet
 // Places [from, to) of a row, four at a time on all threads of the workgroup: f(their logits, the first one's place, the step to the
 // next), -inf for those past the end.  Two groups of loads are on their way.
 typedef float (&Quad)[4];
-template <int NT, class F>
+template <int NT, int AHEAD, class F>
 __device__ __forceinline__ void for_quads(const float* z, int64_t from, int64_t to, F f) {
-    constexpr int kAhead = 4;
+    constexpr int kAhead = AHEAD;
     constexpr int64_t kStep = (int64_t)NT * 4;
     const int64_t whole = from + ((to - from) & ~(int64_t)3);           // (a last quad that is not whole is read by itself)
     f32x4u_t now[kAhead], next[kAhead];
@@ -257,6 +260,11 @@ struct Drawn {
     double prob;
 };
 
+struct SlowInput {
+    RowSettings s;
+    double total, p, m, u;
+    uint32_t all, k;
+};
 // What one workgroup needs for a row.
 template <int NT, int BINS>
 struct RowWork {
@@ -270,6 +278,8 @@ struct RowWork {
     Sums<kWaves> sums;
     uint32_t fill[8];                 // counters, zero from the start, each used once
     int found[4];
+    SlowInput slow;
+    Drawn drawn;
 };
 
 // `quads(f)` calls f for every four places of the row on some thread, the same places on the same threads every time.  Whatever is
@@ -343,26 +353,50 @@ struct RowSampler {
     }
 
     __device__ __forceinline__ bool covered(int b) const { return (b >= lo[0] && b <= hi[0]) || (b >= lo[1] && b <= hi[1]); }
-    // the smallest logit of bins 0 .. b; the largest of bins b .. (as bounds that no logit lies between)
+    // no logit of bins 0 .. b is smaller, none of bins b .. larger
     __device__ __forceinline__ float lowest(int b) const {
-        return ord_to_f32(first_key(f32_to_ord(s.floor), f32_to_ord(s.top), [&](float z) { return bin_of(s, z, BINS) <= b; }));
+        const double z = s.top64 - ((double)(b + 1) * s.width + margin());
+        return fmaxf((float)(z - fabs(z) * 0x1p-23), s.floor);                       // (the conversion rounds by half of that)
     }
-    __device__ __forceinline__ float highest(int b) const { return b == 0 ? s.top : ord_to_f32(f32_to_ord(lowest(b - 1)) - 1u); }
+    __device__ __forceinline__ float highest(int b) const {
+        const double z = s.top64 - ((double)b * s.width - margin());
+        return (float)(z + fabs(z) * 0x1p-23);
+    }
+    __device__ __forceinline__ double margin() const { return s.width * 0x1p-20 + fabs(s.top64) * 0x1p-48; }     // of the arithmetic that makes bins
 
     // the places of bins lo0 .. hi0 and lo1 .. hi1 (hi0 <= hi1)
     __device__ __forceinline__ void collect(int lo0, int hi0, int lo1, int hi1) {
-        const float from1 = lowest(hi1), to1 = highest(lo1), to0 = highest(lo0), from0 = hi0 == hi1 ? from1 : lowest(hi0);
+        const float from0 = lowest(hi0), to0 = highest(lo0), from1 = lowest(hi1), to1 = highest(lo1);
         if (used > 0) __syncthreads();                               // (an earlier list is read)
         uint32_t* fill = &w.fill[used++];
+        const int lane = threadIdx.x & 63;
         quads([&](Quad v, int64_t p, int step) {
-            if (!(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) >= from1)) return;        // (fmaxf: NaN only of NaNs)
+            bool in[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) in[i] = (v[i] >= from0 && v[i] <= to0) || (v[i] >= from1 && v[i] <= to1);
+            if (__builtin_amdgcn_ballot_w64(in[0] | in[1] | in[2] | in[3]) == 0ull) return;
+            uint64_t who[4];
+            uint32_t n = 0u;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float z = v[i];
-                if ((z >= from0 && z <= to0) || (z >= from1 && z <= to1)) {
-                    const uint32_t at = atomicAdd(fill, 1u);
-                    if (at < (uint32_t)kList) w.list[at] = make_key(z, (int32_t)(p + i * step));
+                if (in[i]) {                                         // (the bounds are a little too wide)
+                    const int b = bin_of(s, v[i], BINS);
+                    in[i] = (b >= lo0 && b <= hi0) || (b >= lo1 && b <= hi1);
                 }
+                who[i] = __builtin_amdgcn_ballot_w64(in[i]);
+                n += (uint32_t)__popcll(who[i]);
+            }
+            if (n == 0u) return;
+            uint32_t base = 0u;
+            const uint64_t active = __builtin_amdgcn_ballot_w64(true);
+            const int leader = __ffsll((unsigned long long)active) - 1;
+            if (lane == leader) base = atomicAdd(fill, n);
+            base = (uint32_t)__builtin_amdgcn_readlane((int)base, leader);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t at = base + (uint32_t)__popcll(who[i] & ((1ull << lane) - 1ull));
+                if (in[i] && at < (uint32_t)kList) w.list[at] = make_key(v[i], (int32_t)(p + i * step));
+                base += (uint32_t)__popcll(who[i]);
             }
         });
         __syncthreads();
@@ -585,7 +619,7 @@ struct SlowSampler {
                 w.cnt[i] = 0u;
             }
             __syncthreads();
-            for_quads<NT>(z, 0, n, [&](Quad q, int64_t, int) {
+            for_quads<NT, 2>(z, 0, n, [&](Quad q, int64_t, int) {
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 const float v = q[i];
@@ -666,7 +700,7 @@ struct SlowSampler {
         if (m > 0.0) shorten(least_key(s, fmin(m, 1.0)) - 1u, 0u);
         // what is kept
         unsigned long long sum = 0ull;
-        for_quads<NT>(z, 0, n, [&](Quad q, int64_t, int) {
+        for_quads<NT, 2>(z, 0, n, [&](Quad q, int64_t, int) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (q[i] >= s.floor && f32_to_ord(q[i]) > edge) sum += (unsigned long long)units_of(q[i], unit);
@@ -719,13 +753,16 @@ struct SlowSampler {
     }
 };
 
+// (apart from the rest, with what it needs in LDS: its registers are none of the fast form's)
 template <int NT, int BINS>
-__device__ __noinline__ void draw_slowly(RowWork<NT, BINS>& w, const SampleArgs& a, int64_t r, float top, double total, uint32_t all) {
-    const RowInput in = input_of(a, r);
-    SlowSampler<NT, BINS> slow{w, settings_of(in.t, top, top, BINS), a.logits + r * a.ld, a.n, total, all};
+__device__ __noinline__ void draw_slowly(RowWork<NT, BINS>& w, const float* z, int64_t n) {
+    const SlowInput in = w.slow;
+    SlowSampler<NT, BINS> slow{w, in.s, z, n, in.total, in.all};
     Drawn d;
     slow.draw(in.k, in.p, in.m, in.u, &d);
-    put_token(a, r, d.place, d.prob);
+    __syncthreads();
+    if (threadIdx.x == 0) w.drawn = d;
+    __syncthreads();
 }
 
 // counters and (bins) the histogram; a barrier has to follow
@@ -765,43 +802,64 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t r, const
     }
     row.scan(c.unit, in.k > 0u);
     Drawn d;
-    if (!row.draw(in.k, in.p, in.m, in.u, &d)) return draw_slowly<NT, BINS>(w, a, r, top, row.total, row.all);
+    if (!row.draw(in.k, in.p, in.m, in.u, &d)) {
+        if (threadIdx.x == 0) w.slow = SlowInput{row.s, row.total, in.p, in.m, in.u, row.all, in.k};
+        __syncthreads();
+        draw_slowly<NT, BINS>(w, a.logits + r * a.ld, a.n);
+        d = w.drawn;
+    }
     put_token(a, r, d.place, d.prob);
 }
 
-// ---- rows of up to NT * E places: in registers, one launch
-template <int NT, int E, int BINS>
-__global__ __launch_bounds__(NT) void sample_short_kernel(const SampleArgs a) {
+// ---- rows of up to LEN places, kept in LDS: one launch
+template <int NT, int LEN>
+struct ShortWork {
+    RowWork<NT, kNarrowBins> w;
+    float z[LEN];
+};
+template <int NT, int LEN>
+__global__ __launch_bounds__(NT, 4) void sample_short_kernel(const SampleArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    RowWork<NT, BINS>& w = *reinterpret_cast<RowWork<NT, BINS>*>(smem);
+    ShortWork<NT, LEN>& sw = *reinterpret_cast<ShortWork<NT, LEN>*>(smem);
+    RowWork<NT, kNarrowBins>& w = sw.w;
+    constexpr int kQuads = LEN / (4 * NT);
     const int64_t r = blockIdx.x;
     const float* z = a.logits + r * a.ld;
-    const RowInput in = input_of(a, r);
-    float v[E];
+    const int n = (int)a.n;
+    // (whole quads of -inf behind the row)
+    f32x4u_t v[kQuads];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const int p = e * NT + (int)threadIdx.x;
-        v[e] = p < a.n ? z[p] : -__builtin_inff();
+    for (int e = 0; e < kQuads; ++e) {
+        const int p = (e * NT + (int)threadIdx.x) * 4;
+        if (p + 4 <= n) {
+            v[e] = *reinterpret_cast<const f32x4u_t*>(z + p);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[e][i] = p + i < n ? z[p + i] : -__builtin_inff();
+        }
     }
+    const RowInput in = input_of(a, r);
     clear_work(w, true);
     float top = -__builtin_inff(), low = __builtin_inff();
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        if (is_logit(v[e])) {
-            top = fmaxf(top, v[e]);
-            low = fminf(low, v[e]);
+    for (int e = 0; e < kQuads; ++e) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            top = fmaxf(top, v[e][i]);                               // (NaN and -inf change nothing)
+            low = fminf(low, is_logit(v[e][i]) ? v[e][i] : __builtin_inff());
         }
+        *reinterpret_cast<u32x4*>(&sw.z[(e * NT + (int)threadIdx.x) * 4]) = __builtin_bit_cast(u32x4, v[e]);
     }
     const float2 x = block_range<NT / 64>(w.sums, 0, top, low);
     auto quads = [&](auto f) {
-#pragma unroll
-        for (int e = 0; e < E; e += 4) {
-            float q[4] = {v[e], v[e + 1], v[e + 2], v[e + 3]};
-            f(q, (int64_t)(e * NT + (int)threadIdx.x), NT);
-            __builtin_amdgcn_sched_barrier(0);                       // (four at a time: sixteen take more registers than there are)
+#pragma nounroll
+        for (int p = (int)threadIdx.x * 4; p < n; p += NT * 4) {
+            const u32x4 b = *reinterpret_cast<const u32x4*>(&sw.z[p]);
+            float q[4] = {__uint_as_float(b[0]), __uint_as_float(b[1]), __uint_as_float(b[2]), __uint_as_float(b[3])};
+            f(q, (int64_t)p, 1);
         }
     };
-    sample_row<NT, BINS>(a, r, in, x.x, x.y, w, quads, false);
+    sample_row<NT, kNarrowBins>(a, r, in, x.x, x.y, w, quads, false);
 }
 
 // ---- longer rows.  A workgroup per row reads it once for its range, once for the histogram and once for each list; where rows are
@@ -820,7 +878,7 @@ __device__ __forceinline__ void part_of(int64_t n, int parts, int64_t* from, int
 template <int NT>
 __device__ __forceinline__ float2 range_of(const float* z, int64_t from, int64_t to, Sums<NT / 64>& sums) {
     float top = -__builtin_inff(), low = __builtin_inff();
-    for_quads<NT>(z, from, to, [&](Quad v, int64_t, int) {
+    for_quads<NT, 4>(z, from, to, [&](Quad v, int64_t, int) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             top = fmaxf(top, v[i]);                                  // (NaN and -inf change nothing)
@@ -829,14 +887,12 @@ __device__ __forceinline__ float2 range_of(const float* z, int64_t from, int64_t
     });
     return block_range<NT / 64>(sums, 0, top, low);
 }
-__device__ __forceinline__ float2 range_of_parts(const SampleScratch& s, int64_t r) {
-    float top = -__builtin_inff(), low = __builtin_inff();
-    for (int i = 0; i < s.parts; ++i) {
-        const float2 x = s.range[r * s.parts + i];
-        top = fmaxf(top, x.x);
-        low = fminf(low, x.y);
-    }
-    return float2{top, low};
+constexpr int kMostParts = 64;
+__device__ __forceinline__ float2 range_of_parts(const SampleScratch& s, int64_t r) {        // (a lane each)
+    const int lane = threadIdx.x & 63;
+    float2 x{-__builtin_inff(), __builtin_inff()};
+    if (lane < s.parts) x = s.range[r * s.parts + lane];
+    return float2{wave_max_f32(x.x), -wave_max_f32(-x.y)};
 }
 
 constexpr int kPartThreads = 256;
@@ -869,7 +925,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_count_kernel(const Sample
     __syncthreads();
     int64_t from, to;
     part_of(a.n, s.parts, &from, &to);
-    for_quads<kPartThreads>(a.logits + r * a.ld, from, to, [&](Quad v, int64_t, int) {
+    for_quads<kPartThreads, 2>(a.logits + r * a.ld, from, to, [&](Quad v, int64_t, int) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) count_place<kWideBins>(set, c, v[i], in.k > 0u, mass, cnt);
     });
@@ -880,10 +936,13 @@ __global__ __launch_bounds__(kPartThreads) void sample_count_kernel(const Sample
     }
 }
 
-constexpr int kRowThreads = 1024;
+// (a workgroup per row: two of 512 threads share a CU and fill each other's pauses; rows in parts, which are few: one of 1024)
 template <bool PARTS>
-__global__ __launch_bounds__(kRowThreads) void sample_long_kernel(const SampleArgs a, const SampleScratch s) {
+constexpr int row_threads() { return PARTS ? 1024 : 512; }
+template <bool PARTS>
+__global__ __launch_bounds__(row_threads<PARTS>(), 4) void sample_long_kernel(const SampleArgs a, const SampleScratch s) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    constexpr int kRowThreads = row_threads<PARTS>();
     RowWork<kRowThreads, kWideBins>& w = *reinterpret_cast<RowWork<kRowThreads, kWideBins>*>(smem);
     const int64_t r = blockIdx.x;
     const float* z = a.logits + r * a.ld;
@@ -899,19 +958,19 @@ __global__ __launch_bounds__(kRowThreads) void sample_long_kernel(const SampleAr
     } else {
         x = range_of<kRowThreads>(z, 0, a.n, w.sums);
     }
-    auto quads = [&](auto f) { for_quads<kRowThreads>(z, 0, a.n, f); };
+    auto quads = [&](auto f) { for_quads<kRowThreads, 2>(z, 0, a.n, f); };
     if (PARTS) __syncthreads();
     sample_row<kRowThreads, kWideBins>(a, r, in, x.x, x.y, w, quads, PARTS);
 }
 
-constexpr int64_t kShort = 16384;
+constexpr int kShort = 16384;
 // workgroups that share a long row: enough rows to fill the chip need none (a rule of the sizes alone: the workspace depends on it)
 constexpr int64_t kChip = 256;
 int parts_of(int64_t rows, int64_t n) {
     if (n <= kShort || rows >= kChip) return 1;
     const int64_t want = (2 * kChip + rows - 1) / rows, most = n / 4096;
     const int64_t p = want < most ? want : most;
-    return (int)(p < 64 ? p : 64);
+    return (int)(p < kMostParts ? p : kMostParts);
 }
 
 }  // namespace
@@ -923,36 +982,38 @@ size_t sample_scratch_bytes(int64_t rows, int64_t n) {
 
 hipError_t configure_sample_lds() {
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&sample_long_kernel<false>),
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RowWork<kRowThreads, kWideBins>));
+                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RowWork<row_threads<false>(), kWideBins>));
+    if (e == hipSuccess)
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&sample_short_kernel<512, 8192>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                (int)sizeof(ShortWork<512, 8192>));
+    if (e == hipSuccess)
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&sample_short_kernel<1024, kShort>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                (int)sizeof(ShortWork<1024, kShort>));
     if (e == hipSuccess)
         e = hipFuncSetAttribute(reinterpret_cast<const void*>(&sample_long_kernel<true>),
-                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RowWork<kRowThreads, kWideBins>));
+                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RowWork<row_threads<true>(), kWideBins>));
     return e;
 }
 
 hipError_t launch_sample(const SampleArgs& a, hipStream_t stream) {
     const unsigned rows = (unsigned)a.rows;
-    if (a.n <= 1024)
-        hipLaunchKernelGGL((sample_short_kernel<256, 4, kNarrowBins>), dim3(rows), dim3(256), sizeof(RowWork<256, kNarrowBins>), stream, a);
-    else if (a.n <= 4096)
-        hipLaunchKernelGGL((sample_short_kernel<256, 16, kNarrowBins>), dim3(rows), dim3(256), sizeof(RowWork<256, kNarrowBins>), stream, a);
-    else if (a.n <= 8192)
-        hipLaunchKernelGGL((sample_short_kernel<512, 16, kNarrowBins>), dim3(rows), dim3(512), sizeof(RowWork<512, kNarrowBins>), stream, a);
-    else if (a.n <= kShort)
-        hipLaunchKernelGGL((sample_short_kernel<1024, 16, kNarrowBins>), dim3(rows), dim3(1024), sizeof(RowWork<1024, kNarrowBins>), stream, a);
+    auto go = [&](auto kernel, int threads, size_t lds) { hipLaunchKernelGGL(kernel, dim3(rows), dim3(threads), lds, stream, a); };
+    if (a.n <= 1024) go(&sample_short_kernel<256, 1024>, 256, sizeof(ShortWork<256, 1024>));
+    else if (a.n <= 4096) go(&sample_short_kernel<256, 4096>, 256, sizeof(ShortWork<256, 4096>));
+    else if (a.n <= 8192) go(&sample_short_kernel<512, 8192>, 512, sizeof(ShortWork<512, 8192>));
+    else if (a.n <= kShort) go(&sample_short_kernel<1024, kShort>, 1024, sizeof(ShortWork<1024, kShort>));
     else {
         SampleScratch s{};
         s.parts = parts_of(a.rows, a.n);
-        constexpr size_t lds = sizeof(RowWork<kRowThreads, kWideBins>);
         if (s.parts > 1) {
             s.mass = reinterpret_cast<unsigned long long*>(a.scratch);
             s.range = reinterpret_cast<float2*>(s.mass + (size_t)a.rows * kWideBins);
             s.cnt = reinterpret_cast<uint32_t*>(s.range + (size_t)a.rows * s.parts);
             hipLaunchKernelGGL(sample_range_kernel, dim3(s.parts, rows), dim3(kPartThreads), 0, stream, a, s);
             hipLaunchKernelGGL(sample_count_kernel, dim3(s.parts, rows), dim3(kPartThreads), (size_t)kWideBins * 12, stream, a, s);
-            hipLaunchKernelGGL(sample_long_kernel<true>, dim3(rows), dim3(kRowThreads), lds, stream, a, s);
+            hipLaunchKernelGGL(sample_long_kernel<true>, dim3(rows), dim3(row_threads<true>()), sizeof(RowWork<row_threads<true>(), kWideBins>), stream, a, s);
         } else {
-            hipLaunchKernelGGL(sample_long_kernel<false>, dim3(rows), dim3(kRowThreads), lds, stream, a, s);
+            hipLaunchKernelGGL(sample_long_kernel<false>, dim3(rows), dim3(row_threads<false>()), sizeof(RowWork<row_threads<false>(), kWideBins>), stream, a, s);
         }
     }
     return hipGetLastError();
