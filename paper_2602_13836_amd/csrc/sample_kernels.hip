@@ -21,6 +21,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 namespace sv {
 
 namespace {
@@ -282,7 +284,8 @@ struct RowWork {
     Drawn drawn;
 };
 
-// `quads(f)` calls f for every four places of the row on some thread, the same places on the same threads every time.  Whatever is
+// `quads(little, f)` calls f, which does little or not, for every four places of the row on some thread, the same places on the same
+// threads every time.  Whatever is
 // found is found by every wavefront for itself where 64 lanes are enough for it: bins (64 x 64), and places of lists of up to 64.
 template <int NT, int BINS, class Quads>
 struct RowSampler {
@@ -370,7 +373,8 @@ struct RowSampler {
         if (used > 0) __syncthreads();                               // (an earlier list is read)
         uint32_t* fill = &w.fill[used++];
         const int lane = threadIdx.x & 63;
-        quads([&](Quad v, int64_t p, int step) {
+        quads(std::true_type{}, [&](Quad v, int64_t p, int step) {
+            if (__builtin_amdgcn_ballot_w64(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) >= from1) == 0ull) return;      // (from1 <= from0)
             bool in[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) in[i] = (v[i] >= from0 && v[i] <= to0) || (v[i] >= from1 && v[i] <= to1);
@@ -782,7 +786,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t r, const
                                            const Quads& quads, bool filled) {
     if (!is_logit(top)) return put_token(a, r, -1, 0.0);
     if (in.greedy) {
-        quads([&](Quad v, int64_t p, int step) {
+        quads(std::true_type{}, [&](Quad v, int64_t p, int step) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (v[i] == top) atomicMin(&w.found[0], (int)p + i * step);
@@ -795,7 +799,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t r, const
     row.slot = 0;
     const CountSettings c = count_settings(row.s, a.n);
     if (!filled) {
-        quads([&](Quad v, int64_t, int) {
+        quads(std::false_type{}, [&](Quad v, int64_t, int) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) count_place<BINS>(row.s, c, v[i], in.k > 0u, w.mass, w.cnt);
         });
@@ -851,7 +855,7 @@ __global__ __launch_bounds__(NT, 4) void sample_short_kernel(const SampleArgs a)
         *reinterpret_cast<u32x4*>(&sw.z[(e * NT + (int)threadIdx.x) * 4]) = __builtin_bit_cast(u32x4, v[e]);
     }
     const float2 x = block_range<NT / 64>(w.sums, 0, top, low);
-    auto quads = [&](auto f) {
+    auto quads = [&](auto, auto f) {
 #pragma nounroll
         for (int p = (int)threadIdx.x * 4; p < n; p += NT * 4) {
             const u32x4 b = *reinterpret_cast<const u32x4*>(&sw.z[p]);
@@ -887,7 +891,7 @@ __device__ __forceinline__ float2 range_of(const float* z, int64_t from, int64_t
     });
     return block_range<NT / 64>(sums, 0, top, low);
 }
-constexpr int kMostParts = 64;
+constexpr int kMostParts = 16;
 __device__ __forceinline__ float2 range_of_parts(const SampleScratch& s, int64_t r) {        // (a lane each)
     const int lane = threadIdx.x & 63;
     float2 x{-__builtin_inff(), __builtin_inff()};
@@ -895,7 +899,7 @@ __device__ __forceinline__ float2 range_of_parts(const SampleScratch& s, int64_t
     return float2{wave_max_f32(x.x), -wave_max_f32(-x.y)};
 }
 
-constexpr int kPartThreads = 256;
+constexpr int kPartThreads = 1024;
 __global__ __launch_bounds__(kPartThreads) void sample_range_kernel(const SampleArgs a, const SampleScratch s) {
     __shared__ Sums<kPartThreads / 64> sums;
     const int64_t r = blockIdx.y;
@@ -958,7 +962,8 @@ __global__ __launch_bounds__(row_threads<PARTS>(), 4) void sample_long_kernel(co
     } else {
         x = range_of<kRowThreads>(z, 0, a.n, w.sums);
     }
-    auto quads = [&](auto f) { for_quads<kRowThreads, 2>(z, 0, a.n, f); };
+    // (a pass is one CU's: what it has on its way decides how long a pass that does little takes)
+    auto quads = [&](auto little, auto f) { for_quads<kRowThreads, decltype(little)::value ? 3 : 2>(z, 0, a.n, f); };
     if (PARTS) __syncthreads();
     sample_row<kRowThreads, kWideBins>(a, r, in, x.x, x.y, w, quads, PARTS);
 }
@@ -968,7 +973,7 @@ constexpr int kShort = 16384;
 constexpr int64_t kChip = 256;
 int parts_of(int64_t rows, int64_t n) {
     if (n <= kShort || rows >= kChip) return 1;
-    const int64_t want = (2 * kChip + rows - 1) / rows, most = n / 4096;
+    const int64_t want = (kChip + rows - 1) / rows, most = n / 8192;
     const int64_t p = want < most ? want : most;
     return (int)(p < kMostParts ? p : kMostParts);
 }
