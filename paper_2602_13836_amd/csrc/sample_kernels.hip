@@ -184,12 +184,16 @@ __device__ __forceinline__ void for_quads(const float* z, int64_t from, int64_t 
 
 // ---- sums over a workgroup, in a fixed order.  Each takes room of its own in LDS, `slot` of two by turns, so that one barrier does.
 __device__ __forceinline__ double dpp_shifted(double x, uint64_t y) { return x + __longlong_as_double((long long)y); }
-__device__ __forceinline__ double wave_prefix_inclusive(double x) {
+__device__ __forceinline__ double row_prefix_inclusive(double x) {          // within 16 lanes
     auto bits = [](double v) { return (uint64_t)__double_as_longlong(v); };
     x = dpp_shifted(x, dpp_u64<DPP_ROW_SHR1>(bits(x)));
     x = dpp_shifted(x, dpp_u64<DPP_ROW_SHR2>(bits(x)));
     x = dpp_shifted(x, dpp_u64<DPP_ROW_SHR4>(bits(x)));
-    x = dpp_shifted(x, dpp_u64<DPP_ROW_SHR8>(bits(x)));
+    return dpp_shifted(x, dpp_u64<DPP_ROW_SHR8>(bits(x)));
+}
+__device__ __forceinline__ double wave_prefix_inclusive(double x) {
+    auto bits = [](double v) { return (uint64_t)__double_as_longlong(v); };
+    x = row_prefix_inclusive(x);
     const double r0 = __longlong_as_double((long long)readlane_u64(bits(x), 15)), r1 = __longlong_as_double((long long)readlane_u64(bits(x), 31)),
                  r2 = __longlong_as_double((long long)readlane_u64(bits(x), 47));
     const int row = (threadIdx.x & 63) >> 4;
@@ -213,31 +217,24 @@ __device__ __forceinline__ void block_scan(Sums<WAVES>& s, int slot, double x, u
         s.u[slot][wave] = c_incl;
     }
     __syncthreads();
-    double lower = 0.0, all = 0.0;
-    uint32_t c_lower = 0u, c_all = 0u;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-        const double v = s.d[slot][w];
-        const uint32_t cv = s.u[slot][w];
-        lower += w < wave ? v : 0.0;
-        c_lower += w < wave ? cv : 0u;
-        all += v;
-        c_all += cv;
-    }
-    *before = lower + (incl - x);
-    *c_before = c_lower + (c_incl - c);
-    *total = all;
-    *c_total = c_all;
+    // (a wavefront's sum per lane, added up by every wavefront)
+    const double each = lane < WAVES ? s.d[slot][lane] : 0.0;
+    const uint32_t c_each = lane < WAVES ? s.u[slot][lane] : 0u;
+    const double upto = row_prefix_inclusive(each);
+    const uint32_t c_upto = wave_prefix_inclusive_u32(c_each);
+    const int w = __builtin_amdgcn_readfirstlane(wave);
+    *before = lane_f64(upto - each, w) + (incl - x);
+    *c_before = (uint32_t)__builtin_amdgcn_readlane((int)(c_upto - c_each), w) + (c_incl - c);
+    *total = lane_f64(upto, WAVES - 1);
+    *c_total = (uint32_t)__builtin_amdgcn_readlane((int)c_upto, WAVES - 1);
 }
 template <int WAVES>
 __device__ __forceinline__ uint32_t block_sum(Sums<WAVES>& s, int slot, uint32_t x) {
     const uint32_t sum = wave_sum_u32(x);
     if ((threadIdx.x & 63) == 0) s.u[slot][threadIdx.x >> 6] = sum;
     __syncthreads();
-    uint32_t all = 0u;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) all += s.u[slot][w];
-    return all;
+    const int lane = threadIdx.x & 63;
+    return wave_sum_u32(lane < WAVES ? s.u[slot][lane] : 0u);
 }
 // (largest, smallest)
 template <int WAVES>
@@ -249,12 +246,8 @@ __device__ __forceinline__ float2 block_range(Sums<WAVES>& s, int slot, float to
         s.f[slot][threadIdx.x >> 6][1] = low;
     }
     __syncthreads();
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-        top = fmaxf(top, s.f[slot][w][0]);
-        low = fminf(low, s.f[slot][w][1]);
-    }
-    return float2{top, low};
+    const int lane = min((int)threadIdx.x & 63, WAVES - 1);
+    return float2{wave_max_f32(s.f[slot][lane][0]), -wave_max_f32(-s.f[slot][lane][1])};
 }
 
 struct Drawn {
@@ -367,7 +360,7 @@ struct RowSampler {
     }
     __device__ __forceinline__ double margin() const { return s.width * 0x1p-20 + fabs(s.top64) * 0x1p-48; }     // of the arithmetic that makes bins
 
-    // the places of bins lo0 .. hi0 and lo1 .. hi1 (hi0 <= hi1)
+    // the places of bins lo0 .. hi0 and lo1 .. hi1 (hi0 <= hi1), and maybe some next to those
     __device__ __forceinline__ void collect(int lo0, int hi0, int lo1, int hi1) {
         const float from0 = lowest(hi0), to0 = highest(lo0), from1 = lowest(hi1), to1 = highest(lo1);
         if (used > 0) __syncthreads();                               // (an earlier list is read)
@@ -383,10 +376,6 @@ struct RowSampler {
             uint32_t n = 0u;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (in[i]) {                                         // (the bounds are a little too wide)
-                    const int b = bin_of(s, v[i], BINS);
-                    in[i] = (b >= lo0 && b <= hi0) || (b >= lo1 && b <= hi1);
-                }
                 who[i] = __builtin_amdgcn_ballot_w64(in[i]);
                 n += (uint32_t)__popcll(who[i]);
             }
@@ -940,13 +929,12 @@ __global__ __launch_bounds__(kPartThreads) void sample_count_kernel(const Sample
     }
 }
 
-// (a workgroup per row: two of 512 threads share a CU and fill each other's pauses; rows in parts, which are few: one of 1024)
+// (a workgroup per row: two of 512 threads share a CU and fill each other's pauses; rows in parts, which are few, have a CU and twice
+// the registers to themselves)
+constexpr int kRowThreads = 512;
 template <bool PARTS>
-constexpr int row_threads() { return PARTS ? 1024 : 512; }
-template <bool PARTS>
-__global__ __launch_bounds__(row_threads<PARTS>(), 4) void sample_long_kernel(const SampleArgs a, const SampleScratch s) {
+__global__ __launch_bounds__(kRowThreads, PARTS ? 2 : 4) void sample_long_kernel(const SampleArgs a, const SampleScratch s) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    constexpr int kRowThreads = row_threads<PARTS>();
     RowWork<kRowThreads, kWideBins>& w = *reinterpret_cast<RowWork<kRowThreads, kWideBins>*>(smem);
     const int64_t r = blockIdx.x;
     const float* z = a.logits + r * a.ld;
@@ -963,7 +951,7 @@ __global__ __launch_bounds__(row_threads<PARTS>(), 4) void sample_long_kernel(co
         x = range_of<kRowThreads>(z, 0, a.n, w.sums);
     }
     // (a pass is one CU's: what it has on its way decides how long a pass that does little takes)
-    auto quads = [&](auto little, auto f) { for_quads<kRowThreads, decltype(little)::value ? 3 : 2>(z, 0, a.n, f); };
+    auto quads = [&](auto little, auto f) { for_quads<kRowThreads, decltype(little)::value ? (PARTS ? 8 : 3) : 2>(z, 0, a.n, f); };
     if (PARTS) __syncthreads();
     sample_row<kRowThreads, kWideBins>(a, r, in, x.x, x.y, w, quads, PARTS);
 }
@@ -987,7 +975,7 @@ size_t sample_scratch_bytes(int64_t rows, int64_t n) {
 
 hipError_t configure_sample_lds() {
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&sample_long_kernel<false>),
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RowWork<row_threads<false>(), kWideBins>));
+                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RowWork<kRowThreads, kWideBins>));
     if (e == hipSuccess)
         e = hipFuncSetAttribute(reinterpret_cast<const void*>(&sample_short_kernel<512, 8192>), hipFuncAttributeMaxDynamicSharedMemorySize,
                                 (int)sizeof(ShortWork<512, 8192>));
@@ -996,7 +984,7 @@ hipError_t configure_sample_lds() {
                                 (int)sizeof(ShortWork<1024, kShort>));
     if (e == hipSuccess)
         e = hipFuncSetAttribute(reinterpret_cast<const void*>(&sample_long_kernel<true>),
-                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RowWork<row_threads<true>(), kWideBins>));
+                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RowWork<kRowThreads, kWideBins>));
     return e;
 }
 
@@ -1016,9 +1004,9 @@ hipError_t launch_sample(const SampleArgs& a, hipStream_t stream) {
             s.cnt = reinterpret_cast<uint32_t*>(s.range + (size_t)a.rows * s.parts);
             hipLaunchKernelGGL(sample_range_kernel, dim3(s.parts, rows), dim3(kPartThreads), 0, stream, a, s);
             hipLaunchKernelGGL(sample_count_kernel, dim3(s.parts, rows), dim3(kPartThreads), (size_t)kWideBins * 12, stream, a, s);
-            hipLaunchKernelGGL(sample_long_kernel<true>, dim3(rows), dim3(row_threads<true>()), sizeof(RowWork<row_threads<true>(), kWideBins>), stream, a, s);
+            hipLaunchKernelGGL(sample_long_kernel<true>, dim3(rows), dim3(kRowThreads), sizeof(RowWork<kRowThreads, kWideBins>), stream, a, s);
         } else {
-            hipLaunchKernelGGL(sample_long_kernel<false>, dim3(rows), dim3(row_threads<false>()), sizeof(RowWork<row_threads<false>(), kWideBins>), stream, a, s);
+            hipLaunchKernelGGL(sample_long_kernel<false>, dim3(rows), dim3(kRowThreads), sizeof(RowWork<kRowThreads, kWideBins>), stream, a, s);
         }
     }
     return hipGetLastError();
