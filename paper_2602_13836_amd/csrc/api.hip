@@ -61,6 +61,8 @@ hipError_t device_state(const DeviceState** out) {
             if (e != hipSuccess) return e;
             e = configure_sample_lds();
             if (e != hipSuccess) return e;
+            e = configure_quantized_tile_lds();
+            if (e != hipSuccess) return e;
             void* p = nullptr;
             e = hipGetSymbolAddress(&p, HIP_SYMBOL(scratch));
             if (e != hipSuccess) return e;

@@ -266,6 +266,7 @@ hipError_t launch_quantized_gemv(const QuantizedArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_quantized_product(const QuantizedArgs& a, hipStream_t stream) {
+    if (quantized_tile_supported(a)) return launch_quantized_tile(a, stream);
     const int64_t bx = (a.n_items + 63) / 64;
     if (bx > 0x7fffffffLL) return hipErrorInvalidValue;
     for (int row0 = 0; row0 < a.rows; row0 += 64) {

@@ -389,6 +389,10 @@ struct QuantizedArgs {
 hipError_t launch_quantized_gemv(const QuantizedArgs& a, hipStream_t stream);
 // one set of rows of U for all hidden rows (bfloat16), on the matrix cores
 hipError_t launch_quantized_product(const QuantizedArgs& a, hipStream_t stream);
+// ... through LDS, where it serves (launch_quantized_product hands over)
+bool quantized_tile_supported(const QuantizedArgs& a);
+hipError_t launch_quantized_tile(const QuantizedArgs& a, hipStream_t stream);
+hipError_t configure_quantized_tile_lds();
 
 // ---- one token per row from given random numbers (sample_kernels.hip)
 struct SampleArgs {
