@@ -480,60 +480,88 @@ class QuantizedRows(NamedTuple):
     scales: torch.Tensor
 
 
-def _on_current(*tensors: Optional[torch.Tensor]) -> None:
-    """The library works on the current device: its stream, and memory of its own."""
-    here = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != here):
-            raise ValueError(f"every tensor must live on the current GPU (cuda:{here}), got one on {t.device}")
-
-
 def scale_columns(d: int) -> int:
     """Scale bytes of a row of d values: one per block of 128, in whole words."""
     return 4 * ((d + 511) // 512)
 
 
-def _quantized(t: QuantizedRows, name: str) -> Tuple[int, int, int, int]:
+# These calls check that what they are given lives on the current device, whose stream they go to, and spend as little
+# as they can on it: a norm of one row is over in less time than ten Python calls take.  Tensors that they make are not checked.
+def _rows(t: torch.Tensor, name: str, here: int) -> Tuple[int, int, int]:
+    """_mat of a tensor on the current device."""
+    if t.get_device() != here:
+        raise ValueError(f"{name} must live on the current GPU (cuda:{here}), not on {t.device}")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-D tensor with contiguous rows")
+    ld, step = t.stride()
+    rows, cols = t.shape
+    if step != 1 and cols > 1:
+        raise ValueError(f"{name} must be a 2-D tensor with contiguous rows")
+    return rows, cols, ld if rows > 1 or ld > cols else cols
+
+
+def _flat(t: Optional[torch.Tensor], shape: tuple, dtype: torch.dtype, name: str, here: int) -> Optional[int]:
+    """Pointer of a contiguous tensor of this shape and type on the current device, or None."""
+    if t is None:
+        return None
+    if t.get_device() != here or t.shape != shape or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {list(shape)} {dtype} tensor on the current GPU (cuda:{here})")
+    return t.data_ptr()
+
+
+def _raw_stream(stream: Optional[torch.cuda.Stream], here: int) -> int:
+    return _current_raw_stream(here) if stream is None else stream.cuda_stream
+
+
+def _scratch(nbytes: int, like: torch.Tensor, ws: Optional[torch.Tensor], here: int) -> Tuple[Optional[torch.Tensor], Optional[int], int]:
+    """(workspace, its pointer, its size)."""
+    if ws is None:
+        if nbytes == 0:
+            return None, None, 0
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    elif ws.get_device() != here or ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.numel() < nbytes:
+        raise ValueError(f"workspace must be a contiguous uint8 tensor of >= {nbytes} bytes on the current GPU (cuda:{here})")
+    return ws, ws.data_ptr(), ws.numel()
+
+
+def _quantized(t: QuantizedRows, name: str, here: int) -> Tuple[int, int, int, int]:
     """(rows, d, row stride of the codes, row stride of the scales)."""
-    rows, d, ld = _mat(t.q, name)
-    if t.q.dtype != torch.float8_e4m3fn or t.scales.dtype != torch.float8_e8m0fnu:
+    q, scales = t
+    rows, d, ld = _rows(q, name, here)
+    if q.dtype != torch.float8_e4m3fn or scales.dtype != torch.float8_e8m0fnu:
         raise TypeError(f"{name} must be float8_e4m3fn codes with float8_e8m0fnu scales")
-    srows, cols, lds = _mat(t.scales, f"{name}.scales")
+    srows, cols, lds = _rows(scales, f"{name}.scales", here)
     if srows != rows or cols != scale_columns(d):
         raise ValueError(f"{name}.scales must be [{rows} x {scale_columns(d)}]")
-    if t.scales.device != t.q.device:
-        raise ValueError(f"{name}'s codes and scales must live on the same GPU")
     return rows, d, ld, lds
 
 
-def _new_quantized(rows: int, d: int, device, out: Optional[QuantizedRows]) -> QuantizedRows:
+def _quantized_out(rows: int, d: int, like: torch.Tensor, out: Optional[QuantizedRows], here: int) -> Tuple[QuantizedRows, int, int]:
+    """(where rows in 8 bits go, row stride of the codes, of the scales)."""
     if out is None:
-        return QuantizedRows(torch.empty((rows, d), dtype=torch.float8_e4m3fn, device=device),
-                             torch.empty((rows, scale_columns(d)), dtype=torch.float8_e8m0fnu, device=device))
-    r, c, _, _ = _quantized(out, "out")
-    if (r, c) != (rows, d):
-        raise ValueError(f"out must be [{rows} x {d}]")
-    return out
+        cols = scale_columns(d)
+        return QuantizedRows(torch.empty((rows, d), dtype=torch.float8_e4m3fn, device=like.device),
+                             torch.empty((rows, cols), dtype=torch.float8_e8m0fnu, device=like.device)), d, cols
+    r, c, ldq, lds = _quantized(out, "the quantized output", here)
+    if r != rows or c != d:
+        raise ValueError(f"the quantized output must be [{rows} x {d}]")
+    return out, ldq, lds
 
 
 def quantize_rows(x: torch.Tensor, out: Optional[QuantizedRows] = None,
                   stream: Optional[torch.cuda.Stream] = None) -> QuantizedRows:
     """specvocab_quantize_rows: the rows of x in 8 bits, a power-of-two scale per block of 128."""
-    rows, d, ldx = _mat(x, "x")
-    dt = _dt(x)
-    out = _new_quantized(rows, d, x.device, out)
-    _, _, ldq, lds = _quantized(out, "out")
-    _on_current(x, *out)
-    _check(load_library().specvocab_quantize_rows(_ptr(x), rows, d, ldx, dt, _ptr(out.q), ldq, _ptr(out.scales), lds,
-                                                  _stream(stream)), "specvocab_quantize_rows")
+    here = torch.cuda.current_device()
+    rows, d, ldx = _rows(x, "x", here)
+    out, ldq, lds = _quantized_out(rows, d, x, out, here)
+    _check(load_library().specvocab_quantize_rows(x.data_ptr(), rows, d, ldx, _dt(x), out.q.data_ptr(), ldq, out.scales.data_ptr(),
+                                                  lds, _raw_stream(stream, here)), "specvocab_quantize_rows")
     return out
 
 
-def _like(t: Optional[torch.Tensor], x: torch.Tensor, name: str) -> int:
+def _like(t: torch.Tensor, x: torch.Tensor, name: str, here: int) -> int:
     """Row stride of a matrix of x's shape and type."""
-    if t is None:
-        return 0
-    rows, d, ld = _mat(t, name)
+    ld = _rows(t, name, here)[2]
     if t.shape != x.shape or t.dtype != x.dtype:
         raise ValueError(f"{name} must have x's shape and dtype")
     return ld
@@ -545,65 +573,79 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Option
              quantized_out: Optional[QuantizedRows] = None, stream: Optional[torch.cuda.Stream] = None):
     """specvocab_rms_norm: root-mean-square norm of x + residual.
     Returns (y or None, the sum (x itself without a residual), QuantizedRows of y or None)."""
-    rows, d, ldx = _mat(x, "x")
-    dt = _dt(x)
-    if weight.shape != (d,) or weight.dtype != x.dtype or not weight.is_contiguous() or not weight.is_cuda:
-        raise ValueError("weight must be a contiguous [d] GPU tensor of x's dtype")
-    if sum_out is not None and residual is None:
+    here = torch.cuda.current_device()
+    rows, d, ldx = _rows(x, "x", here)
+    w = _flat(weight, (d,), x.dtype, "weight", here)
+    if w is None:
+        raise ValueError("weight must be given")
+    r = t = y = q = s = None
+    ldr = ld_sum = ldy = ldq = lds = 0
+    if residual is not None:
+        ldr, r = _like(residual, x, "residual", here), residual.data_ptr()
+        if sum_out is None:
+            sum_out, ld_sum = torch.empty((rows, d), dtype=x.dtype, device=x.device), d
+        else:
+            ld_sum = _like(sum_out, x, "sum_out", here)
+        t = sum_out.data_ptr()
+    elif sum_out is not None:
         raise ValueError("sum_out needs a residual")
-    ldr = _like(residual, x, "residual")
-    if residual is not None and sum_out is None:
-        sum_out = torch.empty((rows, d), dtype=x.dtype, device=x.device)
-    if y_out is None and want_y:
-        y_out = torch.empty((rows, d), dtype=x.dtype, device=x.device)
+    if y_out is not None:
+        ldy, y = _like(y_out, x, "y_out", here), y_out.data_ptr()
+    elif want_y:
+        y_out, ldy = torch.empty((rows, d), dtype=x.dtype, device=x.device), d
+        y = y_out.data_ptr()
     if quantized_out is not None or want_quantized:
-        quantized_out = _new_quantized(rows, d, x.device, quantized_out)
-    ld_sum, ldy = _like(sum_out, x, "sum_out"), _like(y_out, x, "y_out")
-    q, scales, ldq, lds = None, None, 0, 0
-    if quantized_out is not None:
-        q, scales = quantized_out
-        _, _, ldq, lds = _quantized(quantized_out, "quantized_out")
-    _on_current(x, weight, residual, sum_out, y_out, q, scales)
-    _check(load_library().specvocab_rms_norm(_ptr(x), rows, d, ldx, _ptr(residual), ldr, _ptr(weight), weight_offset, eps, dt,
-                                             _ptr(sum_out), ld_sum, _ptr(y_out), ldy, _ptr(q), ldq, _ptr(scales), lds,
-                                             _stream(stream)), "specvocab_rms_norm")
-    return y_out, sum_out if sum_out is not None else x, quantized_out
+        quantized_out, ldq, lds = _quantized_out(rows, d, x, quantized_out, here)
+        q, s = quantized_out.q.data_ptr(), quantized_out.scales.data_ptr()
+    _check(load_library().specvocab_rms_norm(x.data_ptr(), rows, d, ldx, r, ldr, w, weight_offset, eps, _dt(x), t, ld_sum, y, ldy,
+                                             q, ldq, s, lds, _raw_stream(stream, here)), "specvocab_rms_norm")
+    return y_out, x if residual is None else sum_out, quantized_out
 
 
-def _head_operands(h: Union[torch.Tensor, QuantizedRows], U: QuantizedRows):
-    """(leading arguments of the products with an 8-bit embedding, rows, d, V, dtype of h, device)."""
-    V, d2, ldu, ldus = _quantized(U, "U")
+def _head_operands(h: Union[torch.Tensor, QuantizedRows], U: QuantizedRows, here: int):
+    """(leading arguments of the products with an 8-bit embedding, rows, d, V, dtype of h)."""
+    V, d2, ldu, ldus = _quantized(U, "U", here)
     if isinstance(h, QuantizedRows):
-        rows, d, ldh, ldhs = _quantized(h, "h")
-        hp, hs, dt, device = h.q.data_ptr(), h.scales.data_ptr(), SV_E4M3, h.q.device
+        rows, d, ldh, ldhs = _quantized(h, "h", here)
+        hp, hs, dt = h.q.data_ptr(), h.scales.data_ptr(), SV_E4M3
     else:
-        rows, d, ldh = _mat(h, "h")
+        rows, d, ldh = _rows(h, "h", here)
         if h.dtype != torch.bfloat16:
             raise TypeError(f"h must be bfloat16 or QuantizedRows, got {h.dtype}")
-        hp, hs, ldhs, dt, device = h.data_ptr(), None, 0, SV_BF16, h.device
+        hp, hs, ldhs, dt = h.data_ptr(), None, 0, SV_BF16
     if d2 != d:
         raise ValueError("U and h disagree on d")
-    _on_current(*U, *(h if isinstance(h, QuantizedRows) else (h,)))
-    return (hp, hs, rows, d, ldh, ldhs, U.q.data_ptr(), U.scales.data_ptr(), V, ldu, ldus), rows, d, V, dt, device
+    return (hp, hs, rows, d, ldh, ldhs, U.q.data_ptr(), U.scales.data_ptr(), V, ldu, ldus), rows, d, V, dt
 
 
-def _out_logits(out: Optional[torch.Tensor], rows: int, n: int, device) -> torch.Tensor:
+def _logits_out(out: Optional[torch.Tensor], rows: int, n: int, U: QuantizedRows, here: int) -> Tuple[torch.Tensor, int]:
     if out is None:
-        return torch.empty((rows, n), dtype=torch.float32, device=device)
-    if out.shape != (rows, n) or out.dtype != torch.float32 or not out.is_contiguous() or not out.is_cuda:
-        raise ValueError(f"logits must go to a contiguous [{rows} x {n}] float32 GPU tensor")
-    return out
+        out = torch.empty((rows, n), dtype=torch.float32, device=U.q.device)
+        return out, out.data_ptr()
+    return out, _flat(out, (rows, n), torch.float32, "the logits' tensor", here)
+
+
+def _list(idx: torch.Tensor, rows: int, padded: bool, here: int) -> Tuple[int, int, int]:
+    """(pointer, idx_mode, length) of an index list."""
+    if idx.get_device() != here or idx.dtype != torch.int32 or not idx.is_contiguous():
+        raise ValueError(f"idx must be a contiguous int32 tensor on the current GPU (cuda:{here})")
+    flag = SV_IDX_PADDED if padded else 0
+    if idx.dim() == 1:
+        return idx.data_ptr(), SV_IDX_PER_STEP | flag, idx.shape[0]
+    if idx.dim() == 2 and idx.shape[0] == rows:
+        return idx.data_ptr(), SV_IDX_PER_ROW | flag, idx.shape[1]
+    raise ValueError("idx must be [k] (one set per step) or [rows x k]")
 
 
 def quantized_dense_logits(h: Union[torch.Tensor, QuantizedRows], U: QuantizedRows, out: Optional[torch.Tensor] = None,
                            ws: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """specvocab_quantized_dense_logits: out[r, v] = <U[v], h_r> with U in 8 bits, h in 8 bits or bfloat16."""
-    args, rows, d, V, dt, device = _head_operands(h, U)
-    out = _out_logits(out, rows, V, device)
-    ws = _workspace(workspace_bytes(SV_OP_QUANTIZED_DENSE_LOGITS, rows, d, V, 0, 0, 0, dt), device, ws)
-    _on_current(out, ws)
-    _check(load_library().specvocab_quantized_dense_logits(*args, _ptr(out), _ptr(ws), 0 if ws is None else ws.numel(),
-                                                           _stream(stream)), "specvocab_quantized_dense_logits")
+    here = torch.cuda.current_device()
+    args, rows, d, V, dt = _head_operands(h, U, here)
+    out, op = _logits_out(out, rows, V, U, here)
+    ws, wp, wn = _scratch(workspace_bytes(SV_OP_QUANTIZED_DENSE_LOGITS, rows, d, V, 0, 0, 0, dt), U.q, ws, here)
+    _check(load_library().specvocab_quantized_dense_logits(*args, op, wp, wn, _raw_stream(stream, here)),
+           "specvocab_quantized_dense_logits")
     return out
 
 
@@ -611,42 +653,33 @@ def quantized_subset_logits(h: Union[torch.Tensor, QuantizedRows], U: QuantizedR
                             out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
                             stream: Optional[torch.cuda.Stream] = None, padded: bool = False) -> torch.Tensor:
     """specvocab_quantized_subset_logits: out[r, j] = <U[idx(r, j)], h_r>.  padded: idx may hold padding slots (-1)."""
-    args, rows, d, V, dt, device = _head_operands(h, U)
-    mode, k = _idx(idx, rows)
-    if padded:
-        mode |= SV_IDX_PADDED
-    out = _out_logits(out, rows, k, device)
-    ws = _workspace(workspace_bytes(SV_OP_QUANTIZED_SUBSET_LOGITS, rows, d, V, k, 0, 0, dt, mode), device, ws)
-    _on_current(idx, out, ws)
-    _check(load_library().specvocab_quantized_subset_logits(*args, _ptr(idx), k, mode, _ptr(out), _ptr(ws),
-                                                            0 if ws is None else ws.numel(), _stream(stream)),
+    here = torch.cuda.current_device()
+    args, rows, d, V, dt = _head_operands(h, U, here)
+    ip, mode, k = _list(idx, rows, padded, here)
+    out, op = _logits_out(out, rows, k, U, here)
+    ws, wp, wn = _scratch(workspace_bytes(SV_OP_QUANTIZED_SUBSET_LOGITS, rows, d, V, k, 0, 0, dt, mode), U.q, ws, here)
+    _check(load_library().specvocab_quantized_subset_logits(*args, ip, k, mode, op, wp, wn, _raw_stream(stream, here)),
            "specvocab_quantized_subset_logits")
     return out
 
 
-def _per_row(t: Optional[torch.Tensor], rows: int, dtype: torch.dtype, name: str) -> Optional[int]:
-    if t is None:
-        return None
-    if t.shape != (rows,) or t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError(f"{name} must be a contiguous [{rows}] {dtype} GPU tensor")
-    return t.data_ptr()
-
-
-def _sampling(rows: int, u, temperature, top_k, top_p, min_p):
-    f32 = torch.float32
+def _sampling(rows: int, u, temperature, top_k, top_p, min_p, here: int):
+    f32, shape = torch.float32, (rows,)
     if u is None:
         raise ValueError("u must be given")
-    return (_per_row(temperature, rows, f32, "temperature"), _per_row(top_k, rows, torch.int32, "top_k"),
-            _per_row(top_p, rows, f32, "top_p"), _per_row(min_p, rows, f32, "min_p"), _per_row(u, rows, f32, "u"))
+    return (_flat(temperature, shape, f32, "temperature", here), _flat(top_k, shape, torch.int32, "top_k", here),
+            _flat(top_p, shape, f32, "top_p", here), _flat(min_p, shape, f32, "min_p", here), _flat(u, shape, f32, "u", here))
 
 
-def _drawn(rows: int, device, tok_out: Optional[torch.Tensor], prob_out: Optional[torch.Tensor]):
+def _drawn(rows: int, like: torch.Tensor, tok_out: Optional[torch.Tensor], prob_out: Optional[torch.Tensor], here: int):
     if tok_out is None:
-        tok_out = torch.empty(rows, dtype=torch.int32, device=device)
+        tok_out = torch.empty(rows, dtype=torch.int32, device=like.device)
+    else:
+        _flat(tok_out, (rows,), torch.int32, "tok_out", here)
     if prob_out is None:
-        prob_out = torch.empty(rows, dtype=torch.float32, device=device)
-    _per_row(tok_out, rows, torch.int32, "tok_out")
-    _per_row(prob_out, rows, torch.float32, "prob_out")
+        prob_out = torch.empty(rows, dtype=torch.float32, device=like.device)
+    else:
+        _flat(prob_out, (rows,), torch.float32, "prob_out", here)
     return tok_out, prob_out
 
 
@@ -657,20 +690,20 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Te
     """specvocab_sample: one token per row from the random numbers u [rows]; temperature, top_p, min_p float32 [rows], top_k int32
     [rows], each or None.  idx: the token ids of the places, [n] or [rows x n].
     Returns (tok [rows] int32, prob [rows] float32)."""
-    rows, n, ld = _mat(logits, "logits")
+    here = torch.cuda.current_device()
+    rows, n, ld = _rows(logits, "logits", here)
     if logits.dtype != torch.float32:
         raise TypeError(f"logits must be float32, got {logits.dtype}")
-    settings = _sampling(rows, u, temperature, top_k, top_p, min_p)
-    mode = SV_IDX_PER_ROW
+    settings = _sampling(rows, u, temperature, top_k, top_p, min_p, here)
+    ip, mode = None, SV_IDX_PER_ROW
     if idx is not None:
-        mode, k = _idx(idx, rows)
+        ip, mode, k = _list(idx, rows, False, here)
         if k != n:
             raise ValueError("idx and logits disagree on n")
-    tok_out, prob_out = _drawn(rows, logits.device, tok_out, prob_out)
-    ws = _workspace(workspace_bytes(SV_OP_SAMPLE, rows, 0, 0, n, 0, 0, SV_F32), logits.device, ws)
-    _on_current(logits, u, temperature, top_k, top_p, min_p, idx, tok_out, prob_out, ws)
-    _check(load_library().specvocab_sample(_ptr(logits), ld, rows, n, _ptr(idx), mode, *settings, _ptr(tok_out), _ptr(prob_out),
-                                           _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)), "specvocab_sample")
+    tok_out, prob_out = _drawn(rows, logits, tok_out, prob_out, here)
+    ws, wp, wn = _scratch(workspace_bytes(SV_OP_SAMPLE, rows, 0, 0, n, 0, 0, SV_F32), logits, ws, here)
+    _check(load_library().specvocab_sample(logits.data_ptr(), ld, rows, n, ip, mode, *settings, tok_out.data_ptr(),
+                                           prob_out.data_ptr(), wp, wn, _raw_stream(stream, here)), "specvocab_sample")
     return tok_out, prob_out
 
 
@@ -682,16 +715,13 @@ def quantized_sample_step(h: Union[torch.Tensor, QuantizedRows], U: QuantizedRow
                           ws: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None, padded: bool = False):
     """specvocab_quantized_sample_step: logits over idx (None: the whole vocabulary) with U in 8 bits, then a token per row.
     Returns (logits, tok, prob)."""
-    args, rows, d, V, dt, device = _head_operands(h, U)
-    mode, k = (SV_IDX_PER_ROW, 0) if idx is None else _idx(idx, rows)
-    if padded:
-        mode |= SV_IDX_PADDED
-    settings = _sampling(rows, u, temperature, top_k, top_p, min_p)
-    logits_out = _out_logits(logits_out, rows, V if idx is None else k, device)
-    tok_out, prob_out = _drawn(rows, device, tok_out, prob_out)
-    ws = _workspace(workspace_bytes(SV_OP_QUANTIZED_SAMPLE_STEP, rows, d, V, k, 0, 0, dt, mode), device, ws)
-    _on_current(idx, u, temperature, top_k, top_p, min_p, logits_out, tok_out, prob_out, ws)
-    _check(load_library().specvocab_quantized_sample_step(*args, _ptr(idx), k, mode, *settings, _ptr(logits_out), _ptr(tok_out),
-                                                          _ptr(prob_out), _ptr(ws), 0 if ws is None else ws.numel(),
-                                                          _stream(stream)), "specvocab_quantized_sample_step")
+    here = torch.cuda.current_device()
+    args, rows, d, V, dt = _head_operands(h, U, here)
+    ip, mode, k = (None, SV_IDX_PER_ROW, 0) if idx is None else _list(idx, rows, padded, here)
+    settings = _sampling(rows, u, temperature, top_k, top_p, min_p, here)
+    logits_out, op = _logits_out(logits_out, rows, V if idx is None else k, U, here)
+    tok_out, prob_out = _drawn(rows, U.q, tok_out, prob_out, here)
+    ws, wp, wn = _scratch(workspace_bytes(SV_OP_QUANTIZED_SAMPLE_STEP, rows, d, V, k, 0, 0, dt, mode), U.q, ws, here)
+    _check(load_library().specvocab_quantized_sample_step(*args, ip, k, mode, *settings, op, tok_out.data_ptr(), prob_out.data_ptr(),
+                                                          wp, wn, _raw_stream(stream, here)), "specvocab_quantized_sample_step")
     return logits_out, tok_out, prob_out
