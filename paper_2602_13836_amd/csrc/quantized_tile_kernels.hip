@@ -107,19 +107,26 @@ __device__ __forceinline__ void store_product(const QuantizedArgs& a, const Tile
     }
 }
 
-// ---- Up to 64 hidden rows: TM = 32 WM of them, and TN = 32 GN items, a wavefront for every 32.  A ring of three stages in LDS, two slices of
-// 128 values on their way, one barrier per slice: behind it everybody has slice s and nobody reads slice s - 1 any more, whose
-// stage takes slice s + 2.  Rows of 128 bytes (h's slice as two halves), the 16-byte unit u of row r at place u ^ ((r >> 1) & 7).
-constexpr int kRing = 3;
-template <int WM, int GN>
-constexpr size_t ring_bytes() { return (size_t)kRing * (32 * GN * 128 + 32 * WM * 256); }
-template <int WM, int GN, bool FAR>
-__global__ __launch_bounds__(64 * GN) void quantized_ring_kernel(const QuantizedArgs a, const int balance_cus) {
-    constexpr int TM = 32 * WM, TN = 32 * GN, kStage = TN * 128 + TM * 256, kPass = 8 * GN;
-    constexpr int LB = TN / kPass, LX = 2 * TM / kPass;               // requests per wavefront and slice, 8 rows of 128 bytes each
-    static_assert(LB == 4 && GN % 2 == 0 && LX * kPass == 2 * TM, "whole requests, a constant swizzle per lane");
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];     // [kRing][TN rows of U, TM rows of h twice], scales
+// ---- Up to 64 hidden rows: TM = 32 WM of them and TN = 32 WN GN items; KS wavefronts share each group of 32 WN items and split every
+// slice of 128 values between them (what a wavefront reads of h from LDS is for more items then: with 64 items a wavefront instead of 32, half
+// as much), their sums being added up at the end.  A ring of D stages in LDS, D - 1 slices on their way, one barrier per slice: behind
+// it everybody has slice s and nobody reads slice s - 1 any more, whose stage takes slice s + D - 1.  Rows of 128 bytes (h's slice as
+// two halves), the 16-byte unit u of row r at place u ^ ((r >> 1) & 7).
+template <int WM, int WN, int GN, int KS, int D>
+struct Ring {
+    static constexpr int kWaves = GN * KS, TM = 32 * WM, TN = 32 * WN * GN, kStage = TN * 128 + TM * 256, kPass = 8 * kWaves;
+    static constexpr int LB = (TN + kPass - 1) / kPass, LX = 2 * TM / kPass;      // requests per wavefront and slice, 8 rows of 128 bytes each
+    static constexpr size_t kBytes = (size_t)D * kStage;
+    static_assert(LX * kPass == 2 * TM && kWaves % 2 == 0 && D >= 3, "whole requests for h, a constant swizzle per lane");
+    static_assert(kBytes >= (size_t)kWaves * WM * WN * 4096, "the ring holds the wavefronts' sums");
+};
+template <int WM, int WN, int GN, int KS, int D, bool FAR>
+__global__ __launch_bounds__(64 * GN * KS) void quantized_ring_kernel(const QuantizedArgs a, const int balance_cus) {
+    using R = Ring<WM, WN, GN, KS, D>;
+    constexpr int TM = R::TM, TN = R::TN, kStage = R::kStage, kPass = R::kPass, LB = R::LB, LX = R::LX;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];     // [D][TN rows of U, TM rows of h twice], scales
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
+    const int wc = wave % GN, kh = wave / GN;                         // its group of items, and its part of every slice
     const Tile t = find_tile<TM, TN>(a, balance_cus);
     if (!t.any) return;
     const int units = a.units, nk = (units + 7) / 8;
@@ -134,7 +141,7 @@ __global__ __launch_bounds__(64 * GN) void quantized_ring_kernel(const Quantized
     LaneSource<FAR> src_x[LX], src_u[LB];
 #pragma unroll
     for (int i = 0; i < LX; ++i) {
-        const int q = wave + GN * i, row = 8 * (q % (TM / 8)) + l8, half = q / (TM / 8);
+        const int q = wave + R::kWaves * i, row = 8 * (q % (TM / 8)) + l8, half = q / (TM / 8);
         src_x[i].set(base_x, min(t.rt * TM + row, a.rows - 1) - t.rt * TM, a.ldh, (uint32_t)(half * 128 + unit * 16));
     }
 #pragma unroll
@@ -143,17 +150,25 @@ __global__ __launch_bounds__(64 * GN) void quantized_ring_kernel(const Quantized
         src_u[i].set(base_u, a.idx ? (int64_t)a.idx[item] : item - t.first, a.ldu, (uint32_t)unit * 16u);
     }
     const i32x4_t buf_x = buffer_of(base_x), buf_u = buffer_of(base_u);
-    unsigned char* const scales = smem + (size_t)kRing * kStage;
+    unsigned char* const scales = smem + R::kBytes;
     const int stride = scale_row_bytes(units);
-    f32x16_t acc[WM][1];
+    f32x16_t acc[WM][WN];
 #pragma unroll
     for (int m = 0; m < WM; ++m)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[m][0][e] = 0.f;
+        for (int n = 0; n < WN; ++n)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[m][n][e] = 0.f;
+    // The slice is four groups of 32 values, two steps each: this wavefront's are groups q0 .. q0 + NQ - 1, steps k0 .. k0 + NK - 1 of them.
+    constexpr int NQ = KS >= 4 ? 1 : 4 / KS, NK = KS >= 8 ? 1 : 2;
+    static_assert(KS == 2 || KS == 4 || KS == 8, "eight steps");
+    const int q0 = KS == 8 ? kh >> 1 : kh * NQ, k0 = KS == 8 ? kh & 1 : 0;
     const int swz = (lane >> 1) & 7;
-    const int fx0 = TN * 128 + (lane & 31) * 128 + ((2 * g) ^ swz) * 16, fu0 = (wave * 32 + (lane & 31)) * 128 + (g ^ swz) * 16;
+    const int fx0 = TN * 128 + (lane & 31) * 128 + ((((2 * g) ^ swz) * 16) ^ ((4 * (q0 & 1) + k0) * 16)) + (q0 >> 1) * TM * 128;
+    const int fu0 = (wc * 32 * WN + (lane & 31)) * 128 + (((g ^ swz) * 16) ^ (q0 * 32));
     // What lies past the tile's width is neither requested nor multiplied.
-    const bool none = wave * 32 >= t.tn;
+    const bool none = wc * 32 * WN >= t.tn;
+    const unsigned char* const my_scales = scales + (wc * 32 * WN + (lane & 31)) * stride;
     auto walk = [&](auto mine) {
         constexpr int MINE = decltype(mine)::value;
         auto request = [&](int s, int stage) {
@@ -166,47 +181,82 @@ __global__ __launch_bounds__(64 * GN) void quantized_ring_kernel(const Quantized
             if constexpr (MINE % 2 == 1) bring(src_u[MINE - 1], cut_u, buf_u, (int64_t)e * 128, at + (uint32_t)((MINE - 1) * kPass * 128));
 #pragma unroll
             for (int i = 0; i < LX; ++i) {
-                const int half = (wave + GN * i) / (TM / 8);
+                const int half = (wave + R::kWaves * i) / (TM / 8);
                 bring(src_x[i], e * 16 + half * 8 + unit >= 2 * units, buf_x, (int64_t)e * 256, at + (uint32_t)(TN * 128 + i * kPass * 128));
             }
         };
-        request(0, 0);
-        request(1, 1);
+#pragma unroll
+        for (int i = 0; i < D - 1; ++i) request(i, i);
         bring_scales(a, t, TN, scales);
         int st = 0;
         for (int s = 0; s < nk; ++s) {
             // (lgkmcnt: this wavefront's own reads of slice s - 1, and its scales, are done too)
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LX + MINE) : "memory");
-            request(s + 2, st == 0 ? 2 : st - 1);
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((D - 2) * (LX + MINE)) : "memory");
+            request(s + D - 1, st == 0 ? D - 1 : st - 1);
             if (!none) {                                             // (uniform; the same barriers)
                 const unsigned char* base = smem + (size_t)st * kStage;
-                const float scale = __uint_as_float((uint32_t)scales[(wave * 32 + (lane & 31)) * stride + eff(s)] << 23);
+                float scale[WN];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const u32x4 raw = *reinterpret_cast<const u32x4*>(base + (fu0 ^ (q * 32)));
+                for (int n = 0; n < WN; ++n) scale[n] = __uint_as_float((uint32_t)my_scales[32 * n * stride + eff(s)] << 23);
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const bf16x8_t b = widen_8(raw[2 * k], raw[2 * k + 1], scale);
+                for (int q = 0; q < NQ; ++q) {
+                    u32x4 raw[WN];
 #pragma unroll
-                        for (int m = 0; m < WM; ++m) {
-                            const bf16x8_t f = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4*>(
+                    for (int n = 0; n < WN; ++n) raw[n] = *reinterpret_cast<const u32x4*>(base + (fu0 ^ (q * 32)) + 32 * n * 128);
+#pragma unroll
+                    for (int k = 0; k < NK; ++k) {
+                        bf16x8_t f[WM];
+#pragma unroll
+                        for (int m = 0; m < WM; ++m)
+                            f[m] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4*>(
                                 base + (fx0 ^ ((4 * (q & 1) + k) * 16)) + (q >> 1) * TM * 128 + 32 * m * 128));
-                            acc[m][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, b, acc[m][0], 0, 0, 0);
+#pragma unroll
+                        for (int n = 0; n < WN; ++n) {
+                            const uint32_t lo = NK == 1 && k0 ? raw[n][2] : raw[n][2 * k], hi = NK == 1 && k0 ? raw[n][3] : raw[n][2 * k + 1];
+                            const bf16x8_t b = widen_8(lo, hi, scale[n]);
+#pragma unroll
+                            for (int m = 0; m < WM; ++m) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[m], b, acc[m][n], 0, 0, 0);
                         }
                     }
                 }
             }
-            st = st == 2 ? 0 : st + 1;
+            st = st == D - 1 ? 0 : st + 1;
         }
     };
-    const int live = (t.tn - 8 * wave + kPass - 1) / kPass;          // 0 .. 4
-    if (live >= 4) walk(std::integral_constant<int, 4>{});
-    else if (live == 3) walk(std::integral_constant<int, 3>{});
-    else if (live == 2) walk(std::integral_constant<int, 2>{});
-    else if (live == 1) walk(std::integral_constant<int, 1>{});
+    const int live = (t.tn - 8 * wave + kPass - 1) / kPass;          // requests for U: 0 .. LB
+    if (LB >= 4 && live >= 4) walk(std::integral_constant<int, (LB < 4 ? LB : 4)>{});
+    else if (LB >= 3 && live == 3) walk(std::integral_constant<int, (LB < 3 ? LB : 3)>{});
+    else if (LB >= 2 && live >= 2) walk(std::integral_constant<int, (LB < 2 ? LB : 2)>{});
+    else if (live >= 1) walk(std::integral_constant<int, 1>{});
     else walk(std::integral_constant<int, 0>{});
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                 // (slices past the end: requested, never read)
-    store_product<WM, 1>(a, t, acc, t.rt * TM, t.first + wave * 32, scales, wave * 32);
+    // Everybody has read its last slice, and nothing is on its way into the ring any more (slices past the end: requested, never
+    // read): the wavefronts' sums go there, [part][group][value][lane], and each of the KS adds up and stores its share of the group's.
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    constexpr int kValues = WM * WN * 16, kShare = kValues / KS;
+    float* const sums = reinterpret_cast<float*>(smem);
+    if (!none) {
+#pragma unroll
+        for (int m = 0; m < WM; ++m)
+#pragma unroll
+            for (int n = 0; n < WN; ++n)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sums[((kh * GN + wc) * kValues + (m * WN + n) * 16 + e) * 64 + lane] = acc[m][n][e];
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (none) return;
+#pragma unroll 4
+    for (int i = 0; i < kShare; ++i) {
+        const int v = kh * kShare + i, e = v % 16, n = v / 16 % WN, m = v / (16 * WN);
+        float sum = sums[(wc * kValues + v) * 64 + lane];
+#pragma unroll
+        for (int k = 1; k < KS; ++k) sum += sums[((k * GN + wc) * kValues + v) * 64 + lane];
+        const int in_tile = wc * 32 * WN + 32 * n + (lane & 31);
+        const int64_t item = t.first + in_tile;
+        const int r = t.rt * TM + 32 * m + 8 * (e >> 2) + (e & 3) + 4 * (lane >> 5);
+        if (item < t.end && r < a.rows)
+            a.out[(int64_t)r * a.out_row_stride + item] =
+                *reinterpret_cast<const uint32_t*>(scales + in_tile * stride + stride - 4) != 0u ? __builtin_nanf("") : sum;
+    }
 }
 
 // ---- More hidden rows: two wavefronts share a SIMD and take turns, a barrier ending every turn: while one multiplies a 16-value step (nothing
@@ -386,8 +436,27 @@ hipError_t opt_in(F* kernel) {
     return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLdsBytes);
 }
 
-template <int WM, int GN>
-bool ring_fits(const QuantizedArgs& a) { return ring_bytes<WM, GN>() + (size_t)32 * GN * scale_row_bytes(a.units) <= kLdsBytes; }
+// the rings: tiles of 32, 64, 128 and 256 items
+template <int WM, int TN>
+struct RingOf;
+template <int WM>
+struct RingOf<WM, 32> { static constexpr int WN = 1, GN = 1, KS = 8, D = WM == 1 ? 8 : 6; };
+template <int WM>
+struct RingOf<WM, 64> { static constexpr int WN = 1, GN = 2, KS = 4, D = 6; };
+template <int WM>
+struct RingOf<WM, 128> { static constexpr int WN = 2, GN = 2, KS = 4, D = WM == 1 ? 6 : 4; };
+template <int WM>
+struct RingOf<WM, 256> { static constexpr int WN = 2, GN = 4, KS = 2, D = 3; };
+template <int WM, int TN, bool FAR>
+constexpr auto ring_kernel() {
+    using P = RingOf<WM, TN>;
+    return &quantized_ring_kernel<WM, P::WN, P::GN, P::KS, P::D, FAR>;
+}
+template <int WM, int TN>
+size_t ring_lds(const QuantizedArgs& a) {
+    using P = RingOf<WM, TN>;
+    return Ring<WM, P::WN, P::GN, P::KS, P::D>::kBytes + (size_t)TN * scale_row_bytes(a.units);
+}
 template <int WM, int WN>
 bool turns_fit(const QuantizedArgs& a) { return turns_bytes<WM, WN>() + (size_t)128 * WN * scale_row_bytes(a.units) <= kLdsBytes; }
 
@@ -406,10 +475,11 @@ hipError_t launch(K kernel_near, K kernel_far, const QuantizedArgs& a, int tm, i
         hipLaunchKernelGGL(kernel, dim3((unsigned)bx), dim3(threads), lds, stream, a);
     return hipGetLastError();
 }
-template <int WM, int GN>
+template <int TN>
 hipError_t launch_ring(const QuantizedArgs& a, int balance_cus, hipStream_t stream) {
-    return launch<void (*)(QuantizedArgs, int)>(&quantized_ring_kernel<WM, GN, false>, &quantized_ring_kernel<WM, GN, true>, a, 32 * WM, 32 * GN,
-                                                balance_cus, 64 * GN, ring_bytes<WM, GN>() + (size_t)32 * GN * scale_row_bytes(a.units), stream);
+    using K = void (*)(QuantizedArgs, int);
+    return a.rows <= 32 ? launch<K>(ring_kernel<1, TN, false>(), ring_kernel<1, TN, true>(), a, 32, TN, balance_cus, 512, ring_lds<1, TN>(a), stream)
+                        : launch<K>(ring_kernel<2, TN, false>(), ring_kernel<2, TN, true>(), a, 64, TN, balance_cus, 512, ring_lds<2, TN>(a), stream);
 }
 template <int WM, int WN>
 hipError_t launch_turns(const QuantizedArgs& a, hipStream_t stream) {
@@ -425,12 +495,14 @@ hipError_t configure_quantized_tile_lds() {
         if (e == hipSuccess) e = opt_in(near_kernel);
         if (e == hipSuccess) e = opt_in(far_kernel);
     };
-    both(&quantized_ring_kernel<1, 2, false>, &quantized_ring_kernel<1, 2, true>);
-    both(&quantized_ring_kernel<1, 4, false>, &quantized_ring_kernel<1, 4, true>);
-    both(&quantized_ring_kernel<1, 8, false>, &quantized_ring_kernel<1, 8, true>);
-    both(&quantized_ring_kernel<2, 2, false>, &quantized_ring_kernel<2, 2, true>);
-    both(&quantized_ring_kernel<2, 4, false>, &quantized_ring_kernel<2, 4, true>);
-    both(&quantized_ring_kernel<2, 8, false>, &quantized_ring_kernel<2, 8, true>);
+    both(ring_kernel<1, 32, false>(), ring_kernel<1, 32, true>());
+    both(ring_kernel<1, 64, false>(), ring_kernel<1, 64, true>());
+    both(ring_kernel<1, 128, false>(), ring_kernel<1, 128, true>());
+    both(ring_kernel<1, 256, false>(), ring_kernel<1, 256, true>());
+    both(ring_kernel<2, 32, false>(), ring_kernel<2, 32, true>());
+    both(ring_kernel<2, 64, false>(), ring_kernel<2, 64, true>());
+    both(ring_kernel<2, 128, false>(), ring_kernel<2, 128, true>());
+    both(ring_kernel<2, 256, false>(), ring_kernel<2, 256, true>());
     both(&quantized_turns_kernel<2, 1, false>, &quantized_turns_kernel<2, 1, true>);
     both(&quantized_turns_kernel<2, 2, false>, &quantized_turns_kernel<2, 2, true>);
     both(&quantized_turns_kernel<4, 2, false>, &quantized_turns_kernel<4, 2, true>);
@@ -438,7 +510,10 @@ hipError_t configure_quantized_tile_lds() {
 }
 
 // True if one of these kernels can: the scales of a tile's rows have to fit into LDS beside its slices.
-bool quantized_tile_supported(const QuantizedArgs& a) { return a.rows > 64 ? turns_fit<4, 2>(a) : ring_fits<2, 8>(a); }
+bool quantized_tile_supported(const QuantizedArgs& a) {
+    return a.rows > 64 ? turns_fit<4, 2>(a) : ring_lds<2, 64>(a) <= kLdsBytes && ring_lds<2, 128>(a) <= kLdsBytes && ring_lds<2, 256>(a) <= kLdsBytes &&
+                                                  ring_lds<1, 128>(a) <= kLdsBytes;
+}
 
 hipError_t launch_quantized_tile(const QuantizedArgs& a, hipStream_t stream) {
     DeviceInfo di;
@@ -446,9 +521,10 @@ hipError_t launch_quantized_tile(const QuantizedArgs& a, hipStream_t stream) {
     if (e != hipSuccess) return e;
     if (a.rows <= 64) {
         const int64_t cus = di.cus;
-        if (a.n_items <= 64 * cus) return a.rows <= 32 ? launch_ring<1, 2>(a, 0, stream) : launch_ring<2, 2>(a, 0, stream);
-        if (a.n_items <= 128 * cus) return a.rows <= 32 ? launch_ring<1, 4>(a, 0, stream) : launch_ring<2, 4>(a, 0, stream);
-        return a.rows <= 32 ? launch_ring<1, 8>(a, di.cus, stream) : launch_ring<2, 8>(a, di.cus, stream);
+        if (a.n_items <= 32 * cus) return launch_ring<32>(a, 0, stream);
+        if (a.n_items <= 64 * cus) return launch_ring<64>(a, 0, stream);
+        if (a.n_items <= 128 * cus) return launch_ring<128>(a, 0, stream);
+        return launch_ring<256>(a, di.cus, stream);
     }
     if (a.n_items <= 128 * (int64_t)di.cus) return launch_turns<2, 1>(a, stream);
     return a.rows <= 128 ? launch_turns<2, 2>(a, stream) : launch_turns<4, 2>(a, stream);
