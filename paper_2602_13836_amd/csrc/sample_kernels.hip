@@ -30,7 +30,8 @@ namespace {
 constexpr int kList = 1536, kBinPlaces = 1024;        // places that are brought together, and those of a bin that are ranked
 constexpr int kWideBins = 4096, kNarrowBins = 1024;
 constexpr double kOctaves = 64.0;
-typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));      // rows start anywhere
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));      // in memory: rows start anywhere
 
 // settings of a row
 struct RowSettings {
@@ -146,40 +147,45 @@ __device__ __forceinline__ void count_place(const RowSettings& s, const CountSet
     if (counts) atomicAdd(&cnt[b], one);
 }
 
-// Places [from, to) of a row, four at a time on all threads of the workgroup: f(their logits, the first one's place, the step to the
-// next), -inf for those past the end.  Two groups of loads are on their way.
-typedef float (&Quad)[4];
+// Places [from, to) of a row on all threads of the workgroup, AHEAD quads at a time: f(quads, the first one's first place, places from a
+// quad to the next), -inf for those past the end.  A group is on its way while one is worked on.
 template <int NT, int AHEAD, class F>
-__device__ __forceinline__ void for_quads(const float* z, int64_t from, int64_t to, F f) {
-    constexpr int kAhead = AHEAD;
+__device__ __forceinline__ void for_groups(const float* z, int64_t from, int64_t to, F f) {
     constexpr int64_t kStep = (int64_t)NT * 4;
     const int64_t whole = from + ((to - from) & ~(int64_t)3);           // (a last quad that is not whole is read by itself)
-    f32x4u_t now[kAhead], next[kAhead];
-    auto load = [&](int64_t base, f32x4u_t (&v)[kAhead]) {
+    const float none = -__builtin_inff();
+    f32x4_t now[AHEAD], next[AHEAD];
+    auto load = [&](int64_t base, f32x4_t (&v)[AHEAD]) {
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
+        for (int a = 0; a < AHEAD; ++a) {
             const int64_t p = base + a * kStep;
-            v[a] = p < whole ? *reinterpret_cast<const f32x4u_t*>(z + p) : f32x4u_t{-__builtin_inff(), -__builtin_inff(), -__builtin_inff(), -__builtin_inff()};
+            v[a] = f32x4_t{none, none, none, none};
+            if (p < whole) v[a] = *reinterpret_cast<const f32x4u_t*>(z + p);
         }
     };
     const int64_t first = from + (int64_t)threadIdx.x * 4;
     load(first, now);
-    for (int64_t base = first; base < whole; base += kStep * kAhead) {
-        load(base + kStep * kAhead, next);
+    for (int64_t base = first; base < whole; base += kStep * AHEAD) {
+        load(base + kStep * AHEAD, next);
+        f(now, base, kStep);
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
-            float v[4] = {now[a][0], now[a][1], now[a][2], now[a][3]};
-            f(v, base + a * kStep, 1);
-        }
-#pragma unroll
-        for (int a = 0; a < kAhead; ++a) now[a] = next[a];
+        for (int a = 0; a < AHEAD; ++a) now[a] = next[a];
     }
     if (threadIdx.x < 64 && whole < to) {
-        float v[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = threadIdx.x == 0 && whole + i < to ? z[whole + i] : -__builtin_inff();
-        f(v, whole, 1);
+        for (int a = 0; a < AHEAD; ++a) now[a] = f32x4_t{none, none, none, none};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) now[0][i] = threadIdx.x == 0 && whole + i < to ? z[whole + i] : none;
+        f(now, whole, kStep);
     }
+}
+// a quad at a time: f(its logits, its first place)
+template <int NT, int AHEAD, class F>
+__device__ __forceinline__ void for_quads(const float* z, int64_t from, int64_t to, F f) {
+    for_groups<NT, AHEAD>(z, from, to, [&](f32x4_t (&v)[AHEAD], int64_t p, int64_t step) {
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) f(v[a], p + a * step);
+    });
 }
 
 // ---- sums over a workgroup, in a fixed order.  Each takes room of its own in LDS, `slot` of two by turns, so that one barrier does.
@@ -277,14 +283,14 @@ struct RowWork {
     Drawn drawn;
 };
 
-// `quads(little, f)` calls f, which does little or not, for every four places of the row on some thread, the same places on the same
-// threads every time.  Whatever is
-// found is found by every wavefront for itself where 64 lanes are enough for it: bins (64 x 64), and places of lists of up to 64.
-template <int NT, int BINS, class Quads>
+// `places` hands out the row's logits, some threads some of them: quads(f) four at a time as for_quads does, groups(f) several quads at a
+// time for what does little with each.  Whatever is found is found by every wavefront for itself where 64 lanes are enough for it: bins
+// (64 x 64), and places of lists of up to 64.
+template <int NT, int BINS, class Places>
 struct RowSampler {
     using Work = RowWork<NT, BINS>;
     Work& w;
-    const Quads& quads;
+    const Places& places;
     const RowSettings s;
     double total;            // mass of the row
     uint32_t all;            // places that have any (only if counted)
@@ -365,32 +371,31 @@ struct RowSampler {
         const float from0 = lowest(hi0), to0 = highest(lo0), from1 = lowest(hi1), to1 = highest(lo1);
         if (used > 0) __syncthreads();                               // (an earlier list is read)
         uint32_t* fill = &w.fill[used++];
-        const int lane = threadIdx.x & 63;
-        quads(std::true_type{}, [&](Quad v, int64_t p, int step) {
-            if (__builtin_amdgcn_ballot_w64(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) >= from1) == 0ull) return;      // (from1 <= from0)
-            bool in[4];
+        places.groups([&](auto& v, int64_t p, int64_t step) {
+            constexpr int kGroup = sizeof(v) / sizeof(v[0]);
+            auto in = [&](float z) { return z >= from1 && (z <= to1 || (z >= from0 && z <= to0)); };      // (from1 <= from0)
+            float most = v[0][0];                                    // (fmaxf: NaN only of NaNs)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) in[i] = (v[i] >= from0 && v[i] <= to0) || (v[i] >= from1 && v[i] <= to1);
-            if (__builtin_amdgcn_ballot_w64(in[0] | in[1] | in[2] | in[3]) == 0ull) return;
-            uint64_t who[4];
-            uint32_t n = 0u;
+            for (int a = 0; a < kGroup; ++a) most = fmaxf(most, fmaxf(fmaxf(v[a][0], v[a][1]), fmaxf(v[a][2], v[a][3])));
+            if (__builtin_amdgcn_ballot_w64(most >= from1) == 0ull) return;
+            uint32_t mine = 0u;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                who[i] = __builtin_amdgcn_ballot_w64(in[i]);
-                n += (uint32_t)__popcll(who[i]);
-            }
-            if (n == 0u) return;
-            uint32_t base = 0u;
-            const uint64_t active = __builtin_amdgcn_ballot_w64(true);
-            const int leader = __ffsll((unsigned long long)active) - 1;
-            if (lane == leader) base = atomicAdd(fill, n);
-            base = (uint32_t)__builtin_amdgcn_readlane((int)base, leader);
+            for (int a = 0; a < kGroup; ++a)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t at = base + (uint32_t)__popcll(who[i] & ((1ull << lane) - 1ull));
-                if (in[i] && at < (uint32_t)kList) w.list[at] = make_key(v[i], (int32_t)(p + i * step));
-                base += (uint32_t)__popcll(who[i]);
-            }
+                for (int i = 0; i < 4; ++i) mine += in(v[a][i]) ? 1u : 0u;
+            const uint64_t who = __builtin_amdgcn_ballot_w64(mine > 0u);
+            if (who == 0ull) return;
+            if (mine == 0u) return;
+            uint32_t at = atomicAdd(fill, mine);                     // (one instruction for the wavefront)
+#pragma unroll
+            for (int a = 0; a < kGroup; ++a)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (in(v[a][i])) {
+                        if (at < (uint32_t)kList) w.list[at] = make_key(v[a][i], (int32_t)(p + a * step + i));
+                        ++at;
+                    }
+                }
         });
         __syncthreads();
         len = *fill;
@@ -612,7 +617,7 @@ struct SlowSampler {
                 w.cnt[i] = 0u;
             }
             __syncthreads();
-            for_quads<NT, 2>(z, 0, n, [&](Quad q, int64_t, int) {
+            for_quads<NT, 2>(z, 0, n, [&](const f32x4_t& q, int64_t) {
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 const float v = q[i];
@@ -693,7 +698,7 @@ struct SlowSampler {
         if (m > 0.0) shorten(least_key(s, fmin(m, 1.0)) - 1u, 0u);
         // what is kept
         unsigned long long sum = 0ull;
-        for_quads<NT, 2>(z, 0, n, [&](Quad q, int64_t, int) {
+        for_quads<NT, 2>(z, 0, n, [&](const f32x4_t& q, int64_t) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (q[i] >= s.floor && f32_to_ord(q[i]) > edge) sum += (unsigned long long)units_of(q[i], unit);
@@ -770,25 +775,27 @@ __device__ __forceinline__ void clear_work(RowWork<NT, BINS>& w, bool bins) {
     }
 }
 // `filled`: the histogram is there already
-template <int NT, int BINS, class Quads>
+template <int NT, int BINS, class Places>
 __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t r, const RowInput& in, float top, float low, RowWork<NT, BINS>& w,
-                                           const Quads& quads, bool filled) {
+                                           const Places& places, bool filled) {
     if (!is_logit(top)) return put_token(a, r, -1, 0.0);
     if (in.greedy) {
-        quads(std::true_type{}, [&](Quad v, int64_t p, int step) {
+        places.groups([&](auto& v, int64_t p, int64_t step) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (v[i] == top) atomicMin(&w.found[0], (int)p + i * step);
+            for (int a = 0; a < (int)(sizeof(v) / sizeof(v[0])); ++a)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (v[a][i] == top) atomicMin(&w.found[0], (int)(p + a * step + i));
         });
         __syncthreads();
         return put_token(a, r, w.found[0], 1.0);
     }
-    RowSampler<NT, BINS, Quads> row{w, quads, settings_of(in.t, top, low, BINS)};
+    RowSampler<NT, BINS, Places> row{w, places, settings_of(in.t, top, low, BINS)};
     row.used = 0;
     row.slot = 0;
     const CountSettings c = count_settings(row.s, a.n);
     if (!filled) {
-        quads(std::false_type{}, [&](Quad v, int64_t, int) {
+        places.quads([&](const f32x4_t& v, int64_t) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) count_place<BINS>(row.s, c, v[i], in.k > 0u, w.mass, w.cnt);
         });
@@ -810,6 +817,23 @@ struct ShortWork {
     RowWork<NT, kNarrowBins> w;
     float z[LEN];
 };
+template <int NT>
+struct LdsPlaces {
+    const float* z;
+    int n;
+    template <class F>
+    __device__ __forceinline__ void groups(F f) const {
+#pragma nounroll
+        for (int p = (int)threadIdx.x * 4; p < n; p += NT * 4) {
+            f32x4_t v[1] = {__builtin_bit_cast(f32x4_t, *reinterpret_cast<const u32x4*>(z + p))};
+            f(v, (int64_t)p, (int64_t)(NT * 4));
+        }
+    }
+    template <class F>
+    __device__ __forceinline__ void quads(F f) const {
+        groups([&](f32x4_t (&v)[1], int64_t p, int64_t) { f(v[0], p); });
+    }
+};
 template <int NT, int LEN>
 __global__ __launch_bounds__(NT, 4) void sample_short_kernel(const SampleArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -820,7 +844,7 @@ __global__ __launch_bounds__(NT, 4) void sample_short_kernel(const SampleArgs a)
     const float* z = a.logits + r * a.ld;
     const int n = (int)a.n;
     // (whole quads of -inf behind the row)
-    f32x4u_t v[kQuads];
+    f32x4_t v[kQuads];
 #pragma unroll
     for (int e = 0; e < kQuads; ++e) {
         const int p = (e * NT + (int)threadIdx.x) * 4;
@@ -844,15 +868,8 @@ __global__ __launch_bounds__(NT, 4) void sample_short_kernel(const SampleArgs a)
         *reinterpret_cast<u32x4*>(&sw.z[(e * NT + (int)threadIdx.x) * 4]) = __builtin_bit_cast(u32x4, v[e]);
     }
     const float2 x = block_range<NT / 64>(w.sums, 0, top, low);
-    auto quads = [&](auto, auto f) {
-#pragma nounroll
-        for (int p = (int)threadIdx.x * 4; p < n; p += NT * 4) {
-            const u32x4 b = *reinterpret_cast<const u32x4*>(&sw.z[p]);
-            float q[4] = {__uint_as_float(b[0]), __uint_as_float(b[1]), __uint_as_float(b[2]), __uint_as_float(b[3])};
-            f(q, (int64_t)p, 1);
-        }
-    };
-    sample_row<NT, kNarrowBins>(a, r, in, x.x, x.y, w, quads, false);
+    const LdsPlaces<NT> places{sw.z, n};
+    sample_row<NT, kNarrowBins>(a, r, in, x.x, x.y, w, places, false);
 }
 
 // ---- longer rows.  A workgroup per row reads it once for its range, once for the histogram and once for each list; where rows are
@@ -871,7 +888,7 @@ __device__ __forceinline__ void part_of(int64_t n, int parts, int64_t* from, int
 template <int NT>
 __device__ __forceinline__ float2 range_of(const float* z, int64_t from, int64_t to, Sums<NT / 64>& sums) {
     float top = -__builtin_inff(), low = __builtin_inff();
-    for_quads<NT, 4>(z, from, to, [&](Quad v, int64_t, int) {
+    for_quads<NT, 4>(z, from, to, [&](const f32x4_t& v, int64_t) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             top = fmaxf(top, v[i]);                                  // (NaN and -inf change nothing)
@@ -918,7 +935,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_count_kernel(const Sample
     __syncthreads();
     int64_t from, to;
     part_of(a.n, s.parts, &from, &to);
-    for_quads<kPartThreads, 2>(a.logits + r * a.ld, from, to, [&](Quad v, int64_t, int) {
+    for_quads<kPartThreads, 2>(a.logits + r * a.ld, from, to, [&](const f32x4_t& v, int64_t) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) count_place<kWideBins>(set, c, v[i], in.k > 0u, mass, cnt);
     });
@@ -929,6 +946,16 @@ __global__ __launch_bounds__(kPartThreads) void sample_count_kernel(const Sample
     }
 }
 
+// (a pass over a row is one CU's: what it has on its way decides how long one that does little takes)
+template <int NT, int GROUP>
+struct RowPlaces {
+    const float* z;
+    int64_t n;
+    template <class F>
+    __device__ __forceinline__ void groups(F f) const { for_groups<NT, GROUP>(z, 0, n, f); }
+    template <class F>
+    __device__ __forceinline__ void quads(F f) const { for_quads<NT, 2>(z, 0, n, f); }
+};
 // (a workgroup per row: two of 512 threads share a CU and fill each other's pauses; rows in parts, which are few, have a CU and twice
 // the registers to themselves)
 constexpr int kRowThreads = 512;
@@ -950,10 +977,9 @@ __global__ __launch_bounds__(kRowThreads, PARTS ? 2 : 4) void sample_long_kernel
     } else {
         x = range_of<kRowThreads>(z, 0, a.n, w.sums);
     }
-    // (a pass is one CU's: what it has on its way decides how long a pass that does little takes)
-    auto quads = [&](auto little, auto f) { for_quads<kRowThreads, decltype(little)::value ? (PARTS ? 8 : 3) : 2>(z, 0, a.n, f); };
+    const RowPlaces<kRowThreads, (PARTS ? 8 : 3)> places{z, a.n};
     if (PARTS) __syncthreads();
-    sample_row<kRowThreads, kWideBins>(a, r, in, x.x, x.y, w, quads, PARTS);
+    sample_row<kRowThreads, kWideBins>(a, r, in, x.x, x.y, w, places, PARTS);
 }
 
 constexpr int kShort = 16384;
