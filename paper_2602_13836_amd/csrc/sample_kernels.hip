@@ -373,33 +373,36 @@ struct RowSampler {
         uint32_t* fill = &w.fill[used++];
         places.groups([&](auto& v, int64_t p, int64_t step) {
             constexpr int kGroup = sizeof(v) / sizeof(v[0]);
-            auto in = [&](float z) { return z >= from1 && (z <= to1 || (z >= from0 && z <= to0)); };      // (from1 <= from0)
+            static_assert(kGroup <= 8, "a bit per logit");
             float most = v[0][0];                                    // (fmaxf: NaN only of NaNs)
 #pragma unroll
             for (int a = 0; a < kGroup; ++a) most = fmaxf(most, fmaxf(fmaxf(v[a][0], v[a][1]), fmaxf(v[a][2], v[a][3])));
-            if (__builtin_amdgcn_ballot_w64(most >= from1) == 0ull) return;
-            uint32_t mine = 0u;
-#pragma unroll
-            for (int a = 0; a < kGroup; ++a)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) mine += in(v[a][i]) ? 1u : 0u;
-            const uint64_t who = __builtin_amdgcn_ballot_w64(mine > 0u);
-            if (who == 0ull) return;
-            if (mine == 0u) return;
-            uint32_t at = atomicAdd(fill, mine);                     // (one instruction for the wavefront)
+            if (__builtin_amdgcn_ballot_w64(most >= from1) == 0ull) return;      // (from1 <= from0)
+            uint32_t mine = 0u;                                      // which of them (without branches: of 2048 logits one is often in)
 #pragma unroll
             for (int a = 0; a < kGroup; ++a)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    if (in(v[a][i])) {
-                        if (at < (uint32_t)kList) w.list[at] = make_key(v[a][i], (int32_t)(p + a * step + i));
-                        ++at;
-                    }
+                    const float z = v[a][i];
+                    const bool in = ((z >= from1) & (z <= to1)) | ((z >= from0) & (z <= to0));
+                    mine |= in ? 1u << (4 * a + i) : 0u;
                 }
+            if (mine == 0u) return;
+            uint32_t at = atomicAdd(fill, (uint32_t)__popc(mine));
+            for (; mine; mine &= mine - 1u, ++at) {
+                const int e = __ffs((int)mine) - 1;
+                if (at < (uint32_t)kList) w.list[at] = (unsigned long long)(uint32_t)(p + (e >> 2) * step + (e & 3));
+            }
         });
         __syncthreads();
         len = *fill;
         full = len > (uint32_t)kList;
+        if (full) return;
+        for (uint32_t i = threadIdx.x; i < len; i += NT) {           // their logits, all at once
+            const int32_t place = (int32_t)w.list[i];
+            w.list[i] = make_key(places.z[place], place);
+        }
+        __syncthreads();
         lo[0] = lo0;
         hi[0] = hi0;
         lo[1] = lo1;
