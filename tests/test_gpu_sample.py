@@ -120,6 +120,38 @@ def test_masks(n):
     check(z, u=s["u"], p=np.full(10, 0.9), m=np.full(10, 0.01))
 
 
+@pytest.mark.parametrize("rows, n", [(260, 20000), (257, 100001)])
+def test_rows_whose_first_places_are_unlike_the_rest(rows, n):
+    """Rows that a workgroup each reads, whose first 8192 places say nothing, little or the wrong thing about the rest."""
+    rng = np.random.default_rng(n)
+    z = language_like(rng, 14, n).numpy()
+    z[0, :9000] = -np.inf                                      # nothing there
+    z[1, :9000] = np.finfo(np.float32).min                     # a mask's lowest value
+    z[2, :9000] = 0.0                                          # all the same
+    z[3, :9000] = 0.0
+    z[3, 9000:] *= 0.001
+    z[4, 12000] = 60.0                                         # one far above
+    z[5, 12000:12004] = [200.0, 199.9, 199.8, 150.0]
+    z[6, 9000:] -= 100.0                                       # the rest far below
+    z[7] = 1e-4 * rng.standard_normal(n)                       # flat, with a rest that spreads more
+    z[7, 9000:] *= 50
+    z[8] = 7.0                                                 # all equal
+    z[9, 15000] = np.inf
+    z[10, 100] = np.inf
+    z[11] *= 1e37                                              # near the largest float
+    z[12, ::3] = np.nan
+    z[13] = np.where(rng.random(n) < 0.999, -np.inf, z[13])
+    kinds = z.shape[0]
+    z = np.concatenate([z] * 19)[:rows]
+    s = dict(u=rng.random(rows, dtype=np.float32), t=rng.choice([0.3, 0.7, 1.0, 2.0, 1e30], rows), k=rng.choice([0, 0, 0, 40, 2000], rows),
+             p=rng.choice([1.0, 0.9, 0.99], rows), m=rng.choice([0.0, 0.0, 0.05], rows))
+    dev = [torch.as_tensor(s[x], dtype=torch.int32 if x == "k" else torch.float32).to(DEV) for x in ("u", "t", "k", "p", "m")]
+    tok, prob = (x.cpu().numpy() for x in sv.sample(torch.from_numpy(z).to(DEV), *dev))
+    for r in range(5 * kinds):
+        at, pr = sample_row(z[r], s["u"][r], float(np.float32(s["t"][r])), int(s["k"][r]), float(np.float32(s["p"][r])), float(np.float32(s["m"][r])))
+        assert tok[r] == at and abs(prob[r] - pr) <= pr * (2.0 ** -24 + 2.0 ** -40) + 1e-38, (r, r % kinds, tok[r], at, prob[r], pr)
+
+
 def test_lists_name_the_tokens():
     rng = np.random.default_rng(8)
     z = language_like(rng, 12, 2048)
