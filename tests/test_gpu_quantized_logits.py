@@ -53,6 +53,28 @@ def lists(seed, rows, V, k, mode, padded):
     return idx if mode == "own" else idx[0].contiguous()
 
 
+def spread(r, stride):
+    """The same rows `stride` bytes apart."""
+    rows, d = r.q.shape
+    q = torch.empty(((rows - 1) * stride + d,), dtype=torch.uint8, device=DEV).as_strided((rows, d), (stride, 1)).view(torch.float8_e4m3fn)
+    q.copy_(r.q)
+    return sv.QuantizedRows(q, r.scales)
+
+
+@pytest.mark.parametrize("rows", [1, 5, 40, 70, 140])
+def test_rows_gigabytes_apart(rows):
+    """An embedding whose rows 32 bits do not reach, by list (5 MB apart) and from a tile's first row (17 MB apart)."""
+    h, U, full = case(rows, rows, 256, 900, True)
+    far = spread(U, 5_000_000 // 16 * 16)
+    idx = lists(rows, rows, 900, 400, "shared", False)
+    assert torch.equal(sv.quantized_subset_logits(h, far, idx.to(DEV)).cpu().double(), picked(full, idx))
+    own = lists(rows, rows, 900, 500, "own", True)
+    assert torch.equal(sv.quantized_subset_logits(h, far, own.to(DEV), padded=True).cpu().double(), picked(full, own))
+    del far
+    few = sv.QuantizedRows(U.q[:300], U.scales[:300])
+    assert torch.equal(sv.quantized_dense_logits(h, spread(few, 17_000_000 // 16 * 16)).cpu().double(), full[:, :300])
+
+
 def picked(full, idx):
     at = idx.long().expand(full.shape[0], -1)
     return full.gather(1, at.clamp(min=0)).masked_fill(at < 0, -np.inf)
@@ -64,6 +86,12 @@ SHAPES = [
     (1, 20000, 64, 7), (2, 256, 300, 100), (3, 4096, 500, 129), (5, 272, 1000, 64), (15, 2048, 1200, 300), (16, 512, 3000, 1100), (17, 528, 2000, 65),
     (32, 1040, 900, 600), (33, 4096, 600, 520), (60, 2560, 3000, 700), (64, 256, 2049, 300), (65, 512, 1500, 400), (100, 4096, 700, 300),
     (128, 1024, 3000, 900), (129, 144, 4000, 200), (200, 3840, 600, 200), (256, 512, 2000, 300), (300, 272, 1111, 1111), (513, 128, 700, 64),
+    (20, 8208, 300, 40), (70, 16400, 200, 50),               # scales of a tile's rows do not fit into LDS
+    # lists of every length class of the ring (tiles of 32, 64, 128 and 256 items, the last of a width that fills rounds), ragged
+    (3, 400, 9000, 8000), (31, 144, 17001, 12345), (8, 272, 33001, 20000), (32, 128, 70001, 66000), (64, 144, 9001, 8500),
+    (40, 256, 20000, 16385), (63, 272, 40001, 30000), (50, 144, 80003, 500),
+    # tiles of the alternating loop past a round: 128 x 256 and 256 x 256
+    (97, 144, 40003, 300), (260, 272, 33333, 300), (129, 400, 35000, 33000),
 ]
 
 
@@ -174,20 +202,15 @@ def test_captured_on_another_stream_and_with_workspaces_of_their_own():
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g):
         sv.quantized_subset_logits(h, U, dev_idx, out=out, ws=ws[:n], padded=True)
-    for source, ref in ((h, full), (h2, ref2), (h, full)):
-        keep = (source.q.clone(), source.scales.clone())
-        h.q.copy_(keep[0])
-        h.scales.copy_(keep[1])
+    first = sv.QuantizedRows(h.q.clone(), h.scales.clone())
+    for source, ref in ((first, full), (h2, ref2), (first, full), (h2, ref2)):
+        h.q.copy_(source.q)
+        h.scales.copy_(source.scales)
         out.zero_()
         g.replay()
         torch.cuda.synchronize()
-        if source is h2:
-            assert torch.equal(out.cpu().double(), picked(ref2, idx))
-            h_first, _, _ = case(21, 40, 512, 2500, True)
-            h.q.copy_(h_first.q)
-            h.scales.copy_(h_first.scales)
-        else:
-            assert torch.equal(out.cpu().double(), picked(full, idx))
+        assert torch.equal(out.cpu().double(), picked(ref, idx))
+        assert torch.equal(sv.quantized_subset_logits(h, U, dev_idx, padded=True), out)
 
 
 def test_refusals_of_the_binding():
