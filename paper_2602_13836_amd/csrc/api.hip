@@ -446,7 +446,10 @@ int launch_quantized(const QuantizedCall& c, hipStream_t s) {
     const QuantizedWs w = quantized_ws(c.rows, c.d, c.V, c.k, c.h_scales != nullptr, c.idx != nullptr, c.idx_mode);
     char* ws = static_cast<char*>(c.ws);
     if (c.h_scales) {
-        if (sv::launch_widen_rows(static_cast<const uint8_t*>(c.h), c.ldh, c.h_scales, c.ldhs, c.rows, (int)c.d, ws, s) != hipSuccess) return SV_ERR_HIP;
+        size_t words = 0;
+        uint32_t* const clear = way == Q_UNION ? sv::union_clear_range(a.rows, c.k, c.V, ws + w.hidden + w.list, &words) : nullptr;
+        if (sv::launch_widen_rows(static_cast<const uint8_t*>(c.h), c.ldh, c.h_scales, c.ldhs, c.rows, (int)c.d, ws, clear, words, s) != hipSuccess)
+            return SV_ERR_HIP;
         a.h = ws;
         a.ldh = c.d * 2;
         a.h_scales = nullptr;
@@ -462,7 +465,7 @@ int launch_quantized(const QuantizedCall& c, hipStream_t s) {
         if (sv::launch_quantized_product(a, s) != hipSuccess) return SV_ERR_HIP;
     } else {
         sv::UnionList u;
-        if (sv::launch_union_list(use, a.rows, c.k, c.V, ws + w.hidden + w.list, s, &u) != hipSuccess) return SV_ERR_HIP;
+        if (sv::launch_union_list(use, a.rows, c.k, c.V, ws + w.hidden + w.list, s, &u, c.h_scales != nullptr) != hipSuccess) return SV_ERR_HIP;
         a.idx = u.tokens;
         a.idx_row_stride = 0;
         a.n_items = u.stride;

@@ -29,8 +29,10 @@ __device__ __forceinline__ uint2 widen_4(uint32_t codes, float scale) {
 
 // ---- hidden rows in 8 bits, widened: out[r, i] = 2^e q[r, i] as bfloat16 (exact).  16 values per thread.
 __global__ __launch_bounds__(256) void widen_rows_kernel(const uint8_t* q, const int64_t ldq, const uint8_t* scales, const int64_t lds,
-                                                         const int64_t rows, const int units, char* out) {
+                                                         const int64_t rows, const int units, char* out, uint32_t* zero_ptr,
+                                                         const size_t zero_words) {
     const int64_t n = rows * units;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < zero_words; i += (size_t)gridDim.x * 256) zero_ptr[i] = 0u;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / units;
         const int u = (int)(i - r * units);
@@ -254,10 +256,11 @@ hipError_t gemv(const QuantizedArgs& a, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_widen_rows(const uint8_t* q, int64_t ldq, const uint8_t* scales, int64_t lds, int64_t rows, int d, char* out,
-                             hipStream_t stream) {
-    const int64_t n = rows * (d / 16);
+                             uint32_t* zero_ptr, size_t zero_words, hipStream_t stream) {
+    const int64_t units = rows * (d / 16), n = units > (int64_t)zero_words ? units : (int64_t)zero_words;
     const unsigned blocks = (unsigned)((n + 255) / 256 < 4096 ? (n + 255) / 256 : 4096);
-    hipLaunchKernelGGL(widen_rows_kernel, dim3(blocks), dim3(256), 0, stream, q, ldq, scales, lds, rows, d / 16, out);
+    hipLaunchKernelGGL(widen_rows_kernel, dim3(blocks), dim3(256), 0, stream, q, ldq, scales, lds, rows, d / 16, out, zero_ptr,
+                       zero_words);
     return hipGetLastError();
 }
 

@@ -101,6 +101,9 @@ bool ksplit_rows_supported(int dt, const GemvArgs& a);
 hipError_t launch_ksplit_rows(const GemvArgs& a, hipStream_t stream);
 // more than 64 rows of x, and some lists from 17 rows on: LDS-tiled product (launch_skinny_mfma forwards to it)
 hipError_t launch_tile_mfma(const GemvArgs& a, hipStream_t stream);
+// which tiles (hidden rows x items) of the loop of alternating wavefronts take such a product the least time
+enum TileShape { TILE_256x256, TILE_128x256, TILE_128x128 };
+TileShape tile_shape(int rows, int64_t n_items, int cus, bool wide_only);
 
 // The tiled product with the epilogue of the bracketed selection instead of a store: nothing of the product
 // is written; per hidden row r and item j the score f = out[r, j] is compared with the row's bracket
@@ -219,7 +222,9 @@ struct UnionList {
     int64_t stride;          // the most tokens that the list can have
     bool ordered;            // the list is the same in every run
 };
-hipError_t launch_union_list(const int32_t* idx, int rows, int64_t k, int64_t V, void* ws, hipStream_t stream, UnionList* out);
+// cleared: an earlier launch has set the words of union_clear_range to zero
+uint32_t* union_clear_range(int rows, int64_t k, int64_t V, void* ws, size_t* words);
+hipError_t launch_union_list(const int32_t* idx, int rows, int64_t k, int64_t V, void* ws, hipStream_t stream, UnionList* out, bool cleared = false);
 hipError_t launch_union_pick(const UnionList& u, const int32_t* idx, int rows, int64_t k, float* out, hipStream_t stream);
 // defer != nullptr: everything but the pick is launched, *defer says what is left to do (a.out_f32 stays unwritten)
 hipError_t launch_union_logits(const GemvArgs& a, int64_t V, void* ws, hipStream_t stream, DeferredPick* defer = nullptr);
@@ -361,9 +366,9 @@ struct NormArgs {
 hipError_t launch_rms_norm(int dt, const NormArgs& a, hipStream_t stream);
 hipError_t launch_quantize_rows(int dt, const char* x, int64_t row_bytes, int64_t rows, int d, uint8_t* q, int64_t ldq, uint8_t* scales,
                                 int64_t lds, hipStream_t stream);
-// hidden rows in 8 bits as bfloat16, row stride d
+// hidden rows in 8 bits as bfloat16, row stride d; on the way clears zero_words words for a later launch
 hipError_t launch_widen_rows(const uint8_t* q, int64_t ldq, const uint8_t* scales, int64_t lds, int64_t rows, int d, char* out,
-                             hipStream_t stream);
+                             uint32_t* zero_ptr, size_t zero_words, hipStream_t stream);
 // out[r, j] = < U[row(r, j), :], h[r, :] >, row(r, j) as in GemvArgs
 struct QuantizedArgs {
     const char* h;           // bfloat16 rows, or (h_scales != nullptr, the kernel for one row at a time only) rows in 8 bits

@@ -762,8 +762,7 @@ hipError_t configure_tile_mfma_lds() {
 // 78-88 for twice the tiles); in between a square law fits within a few per cent, and d = 1536 scales all of them alike.
 // 256 rows: 4096 items 42 us on 128 x 128 against 70 on 256 x 256, 32768 82 on 128 x 256 against 88, 65536 141 on
 // 256 x 256 against 163.
-enum TileShape { TILE_256x256, TILE_128x256, TILE_128x128 };
-static TileShape tile_shape(int rows, int64_t n_items, int cus, bool wide_only) {
+TileShape tile_shape(int rows, int64_t n_items, int cus, bool wide_only) {
     const double rt128 = (rows + 127) / 128, rt256 = (rows + 255) / 256, it128 = (double)((n_items + 127) / 128), it256 = (double)((n_items + 255) / 256);
     auto cost = [&](double tiles, double alone, double full) {
         const double rounds = tiles / cus, whole = floor(rounds), part = rounds - whole;

@@ -367,17 +367,25 @@ size_t union_ws_bytes(int64_t rows, int64_t V, int64_t k) {
 }
 
 // The union of the rows' lists: its tokens, how many, and each token's place, in the workspace.
-hipError_t launch_union_list(const int32_t* idx, int rows, int64_t k, int64_t V, void* ws, hipStream_t stream, UnionList* out) {
+uint32_t* union_clear_range(int rows, int64_t k, int64_t V, void* ws, size_t* words) {
+    const UnionWs w = carve(ws, rows, V, k);
+    *words = 4 + flag_words(V);                           // counter + flag bytes (contiguous)
+    return w.counter;
+}
+hipError_t launch_union_list(const int32_t* idx, int rows, int64_t k, int64_t V, void* ws, hipStream_t stream, UnionList* out, bool cleared) {
     DeviceInfo di;
     hipError_t e = device_info(&di);
     if (e != hipSuccess) return e;
     const int64_t pairs = (int64_t)rows * k;
     const UnionWs w = carve(ws, rows, V, k);
 
-    const size_t nclear = 4 + flag_words(V);              // counter + flag bytes (contiguous)
-    unsigned cb = (unsigned)((nclear + 1023) / 1024);
-    if (cb > (unsigned)di.cus * 4) cb = (unsigned)di.cus * 4;
-    hipLaunchKernelGGL(clear_kernel, dim3(cb), dim3(256), 0, stream, w.counter, nclear);
+    if (!cleared) {
+        size_t nclear;
+        uint32_t* const to = union_clear_range(rows, k, V, ws, &nclear);
+        unsigned cb = (unsigned)((nclear + 1023) / 1024);
+        if (cb > (unsigned)di.cus * 4) cb = (unsigned)di.cus * 4;
+        hipLaunchKernelGGL(clear_kernel, dim3(cb), dim3(256), 0, stream, to, nclear);
+    }
     unsigned mb = (unsigned)((pairs + 1023) / 1024);
     if (mb > (unsigned)di.cus * 8) mb = (unsigned)di.cus * 8;
     hipLaunchKernelGGL(mark_kernel, dim3(mb), dim3(256), 0, stream, idx, pairs, w.flag);
