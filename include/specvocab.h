@@ -302,7 +302,7 @@ int specvocab_dense_logits(const void* h, int64_t rows, int64_t d, int64_t ldh,
  * specvocab_quantize_rows: the rows of x [rows x d] (SV_F32 or SV_BF16, d a multiple of 16) in 8 bits -- the output embedding
  * once, hidden rows per step.  A block's scale is the smallest 2^e, e >= -126, with max|x| <= 448 * 2^e (1 for a block of zeros); a
  * code is x / 2^e, which is exact, rounded to nearest even.  A block with an infinity or a NaN in it has scale 255 and
- * NaN codes.  rows is limited by int32 only. */
+ * NaN codes.  rows is limited by int32 only.  The outputs must not overlap x. */
 int specvocab_quantize_rows(const void* x, int64_t rows, int64_t d, int64_t ldx, int dt,
                             uint8_t* q_out, int64_t ldq, uint8_t* scales_out, int64_t lds, void* stream);
 
@@ -343,12 +343,15 @@ int specvocab_quantized_subset_logits(const void* h, const uint8_t* h_scales, in
  *   4. the first place of those at which the running sum of w exceeds u[r] times the sum over all of them is drawn.
  * T <= 0 or NaN: the first place, with probability 1.  NaN in top_p or min_p: no such step.  temperature, top_k, top_p,
  * min_p: device [rows], or NULL for 1, 0, 1, 0.  Places with a logit of -inf or NaN are masked: they are in none of the steps.
- * Places with w below 2^-64 have no mass and count as masked too.  A +inf logit takes all of a row's mass.
+ * Places with w below 2^-64 (or, in some rows, 2^-88) have no mass and count as masked too.  A +inf logit takes all of a row's
+ * mass.
  * tok_out: device [rows] int32, the place, or idx(r, place) where idx (as in specvocab_subset_logits, padding slots having a logit of
  * -inf) is not NULL; -1 for a row that is masked throughout.  prob_out: device [rows] float32, w over the sum in 4 (0 for such
  * a row), or NULL.
- * Sums are kept as exactly as 64-bit floating point keeps them, whatever n is, and do not depend on the run.  One to three launches.  Thousands of
- * equal logits among the kept ones, or top_k and borders among logits that crowd into few values, cost some tens of passes over the row. */
+ * Sums are kept to 2^-44 of each term (n up to 2^18; a bit less for each doubling of n), and do not depend on the run.  Rows of up to
+ * 16384 logits: one launch; longer ones: one from 256 rows on, else three (and workspace).  A row in which more than 1024 places crowd into one
+ * of the 4096 steps (1024 for short rows) that its range, or 64 octaves of w, is cut into, at a border or where the token is drawn --
+ * thousands of equal logits, clusters far apart --, costs some tens of passes over the row. */
 int specvocab_sample(const float* logits, int64_t ld, int64_t rows, int64_t n, const int32_t* idx, int idx_mode,
                      const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
                      int32_t* tok_out, float* prob_out, void* ws, size_t ws_bytes, void* stream);

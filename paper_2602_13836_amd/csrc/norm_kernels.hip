@@ -50,8 +50,8 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const char* x, const
     }
 }
 
-// ---- the norm: CH pieces of eight values per thread in registers; WAVE: a wavefront per row, else a workgroup.  Rows that do not
-// fit (LOOP) are read again for their second half.
+// ---- the norm: a workgroup per row, CH pieces of eight values per thread in registers.  Rows that do not fit (LOOP) are read again for
+// their second half.
 __device__ __forceinline__ float block_sum(float x, float* s_w) {
     x = wave_sum(x);
     const int waves = (int)(blockDim.x >> 6);
@@ -63,14 +63,12 @@ __device__ __forceinline__ float block_sum(float x, float* s_w) {
     return t;
 }
 
-template <int DT, int CH, bool WAVE, bool LOOP>
-__global__ __launch_bounds__(WAVE ? 256 : 1024) void rms_norm_kernel(const NormArgs a) {
+template <int DT, int CH, bool LOOP>
+__global__ __launch_bounds__(1024) void rms_norm_kernel(const NormArgs a) {
     constexpr int kEs = DT == DT_BF16 ? 2 : 4;
     __shared__ float s_w[16];
-    const int threads = WAVE ? 64 : (int)blockDim.x;
-    const int tid = WAVE ? (int)threadIdx.x & 63 : (int)threadIdx.x;
-    const int64_t r = WAVE ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : (int64_t)blockIdx.x;
-    if (WAVE && r >= a.rows) return;                                 // (whole wavefronts; no barrier in this form)
+    const int threads = (int)blockDim.x, tid = (int)threadIdx.x;
+    const int64_t r = blockIdx.x;
     const int d = a.d;
     const char* x = a.x + r * a.x_row_bytes;
     const char* res = a.residual ? a.residual + r * a.res_row_bytes : nullptr;
@@ -138,7 +136,7 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void rms_norm_kernel(const NormA
             s += squares(t);
             if (a.sum && at < d) e.store(a.sum + r * a.sum_row_bytes + (int64_t)at * kEs);
         }
-        s = WAVE ? wave_sum(s) : block_sum(s, s_w);
+        s = block_sum(s, s_w);
         const float rstd = 1.0f / sqrtf(s / (float)d + a.eps);
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
@@ -177,36 +175,55 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void rms_norm_kernel(const NormA
     }
 }
 
+constexpr int64_t kRowsPerLaunch = 1 << 20;                          // (a launch has less than 2^32 threads)
 template <int DT>
 hipError_t launch_norm(const NormArgs& a, hipStream_t stream) {
     const int pieces = (a.d + 7) / 8;
     const unsigned rows = (unsigned)a.rows;
     const int per = (pieces + 63) / 64 * 64;                         // threads that a piece each takes
-    if (per <= 1024) hipLaunchKernelGGL((rms_norm_kernel<DT, 1, false, false>), dim3(rows), dim3(per), 0, stream, a);
-    else if (per <= 2048) hipLaunchKernelGGL((rms_norm_kernel<DT, 2, false, false>), dim3(rows), dim3((per / 2 + 63) / 64 * 64), 0, stream, a);
-    else if (per <= 4096) hipLaunchKernelGGL((rms_norm_kernel<DT, 4, false, false>), dim3(rows), dim3((per / 4 + 63) / 64 * 64), 0, stream, a);
-    else hipLaunchKernelGGL((rms_norm_kernel<DT, 1, false, true>), dim3(rows), dim3(1024), 0, stream, a);
+    if (per <= 1024) hipLaunchKernelGGL((rms_norm_kernel<DT, 1, false>), dim3(rows), dim3(per), 0, stream, a);
+    else if (per <= 2048) hipLaunchKernelGGL((rms_norm_kernel<DT, 2, false>), dim3(rows), dim3((per / 2 + 63) / 64 * 64), 0, stream, a);
+    else if (per <= 4096) hipLaunchKernelGGL((rms_norm_kernel<DT, 4, false>), dim3(rows), dim3((per / 4 + 63) / 64 * 64), 0, stream, a);
+    else hipLaunchKernelGGL((rms_norm_kernel<DT, 1, true>), dim3(rows), dim3(1024), 0, stream, a);
     return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_rms_norm(int dt, const NormArgs& a, hipStream_t stream) {
-    return dt == DT_BF16 ? launch_norm<DT_BF16>(a, stream) : launch_norm<DT_F32>(a, stream);
+    for (int64_t row0 = 0; row0 < a.rows; row0 += kRowsPerLaunch) {
+        NormArgs b = a;
+        b.rows = a.rows - row0 < kRowsPerLaunch ? a.rows - row0 : kRowsPerLaunch;
+        b.x += row0 * a.x_row_bytes;
+        if (a.residual) b.residual += row0 * a.res_row_bytes;
+        if (a.sum) b.sum += row0 * a.sum_row_bytes;
+        if (a.y) b.y += row0 * a.y_row_bytes;
+        if (a.q) {
+            b.q += row0 * a.ldq;
+            b.scales += row0 * a.lds;
+        }
+        const hipError_t e = dt == DT_BF16 ? launch_norm<DT_BF16>(b, stream) : launch_norm<DT_F32>(b, stream);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_quantize_rows(int dt, const char* x, int64_t row_bytes, int64_t rows, int d, uint8_t* q, int64_t ldq, uint8_t* scales,
                                 int64_t lds, hipStream_t stream) {
     const int units = (d + 511) / 512;
-    const int64_t blocks = (rows * units + 4 * kUnits - 1) / (4 * kUnits);
-    if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-    if (dt == DT_BF16)
-        hipLaunchKernelGGL(quantize_rows_kernel<DT_BF16>, dim3((unsigned)blocks), dim3(256), 0, stream, x, row_bytes, rows, d, units, q, ldq,
-                           scales, lds);
-    else
-        hipLaunchKernelGGL(quantize_rows_kernel<DT_F32>, dim3((unsigned)blocks), dim3(256), 0, stream, x, row_bytes, rows, d, units, q, ldq,
-                           scales, lds);
-    return hipGetLastError();
+    const int64_t most = ((int64_t)1 << 26) / units;                 // rows of a launch
+    for (int64_t row0 = 0; row0 < rows; row0 += most) {
+        const int64_t here = rows - row0 < most ? rows - row0 : most;
+        const unsigned blocks = (unsigned)((here * units + 4 * kUnits - 1) / (4 * kUnits));
+        auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), 0, stream, x + row0 * row_bytes, row_bytes, here, d, units, q + row0 * ldq, ldq,
+                               scales + row0 * lds, lds);
+            return hipGetLastError();
+        };
+        const hipError_t e = dt == DT_BF16 ? go(&quantize_rows_kernel<DT_BF16>) : go(&quantize_rows_kernel<DT_F32>);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace sv

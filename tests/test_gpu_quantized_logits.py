@@ -86,6 +86,7 @@ SHAPES = [
     (1, 20000, 64, 7), (2, 256, 300, 100), (3, 4096, 500, 129), (5, 272, 1000, 64), (15, 2048, 1200, 300), (16, 512, 3000, 1100), (17, 528, 2000, 65),
     (32, 1040, 900, 600), (33, 4096, 600, 520), (60, 2560, 3000, 700), (64, 256, 2049, 300), (65, 512, 1500, 400), (100, 4096, 700, 300),
     (128, 1024, 3000, 900), (129, 144, 4000, 200), (200, 3840, 600, 200), (256, 512, 2000, 300), (300, 272, 1111, 1111), (513, 128, 700, 64),
+    (20, 16, 300, 50), (70, 48, 300, 20), (33, 128, 500, 1),
     (20, 8208, 300, 40), (70, 16400, 200, 50),               # scales of a tile's rows do not fit into LDS
     # lists of every length class of the ring (tiles of 32, 64, 128 and 256 items, the last of a width that fills rounds), ragged
     (3, 400, 9000, 8000), (31, 144, 17001, 12345), (8, 272, 33001, 20000), (32, 128, 70001, 66000), (64, 144, 9001, 8500),

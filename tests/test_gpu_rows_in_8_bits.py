@@ -107,6 +107,16 @@ def test_rms_norm_in_place_and_one_output_at_a_time(d):
     assert torch.equal(x3, sv.rms_norm(x, w, 1e-6)[0]) and t3 is x3
 
 
+def test_more_rows_than_a_launch_takes():
+    rows = (1 << 20) + 3
+    x = torch.randn((rows, 16), generator=torch.Generator(device=DEV).manual_seed(1), device=DEV).to(torch.bfloat16)
+    w = torch.ones(16, dtype=torch.bfloat16, device=DEV)
+    y, total, q = sv.rms_norm(x, w, 1e-5, residual=x, want_quantized=True)
+    tail, t2, q2 = sv.rms_norm(x[-10:], w, 1e-5, residual=x[-10:], want_quantized=True)
+    assert torch.equal(y[-10:], tail) and torch.equal(total[-10:], t2)
+    assert torch.equal(q.q.view(torch.uint8)[-10:], q2.q.view(torch.uint8)) and torch.equal(q.scales.view(torch.uint8)[-10:], q2.scales.view(torch.uint8))
+
+
 def test_rms_norm_of_zeros_infinities_and_nan():
     x = torch.zeros((4, 256), dtype=torch.bfloat16, device=DEV)
     x[1, 5], x[2, 7] = float("inf"), float("nan")
