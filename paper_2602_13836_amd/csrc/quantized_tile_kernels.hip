@@ -107,7 +107,7 @@ __device__ __forceinline__ void store_product(const QuantizedArgs& a, const Tile
     }
 }
 
-// ---- Up to 64 hidden rows: TM = 32 WM of them and TN = 32 WN GN items; KS wavefronts share each group of 32 WN items and split every
+// ---- Up to 64 hidden rows, and short lists of more: TM = 32 WM of them and TN = 32 WN GN items; KS wavefronts share each group of 32 WN items and split every
 // slice of 128 values between them (what a wavefront reads of h from LDS is for more items then: with 64 items a wavefront instead of 32, half
 // as much), their sums being added up at the end.  A ring of D stages in LDS, D - 1 slices on their way, one barrier per slice: behind
 // it everybody has slice s and nobody reads slice s - 1 any more, whose stage takes slice s + D - 1.  Rows of 128 bytes (h's slice as
@@ -436,7 +436,7 @@ hipError_t opt_in(F* kernel) {
     return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLdsBytes);
 }
 
-// the rings: tiles of 32, 64, 128 and 256 items
+// the rings: tiles of 32, 64, 128 and 256 items, by 32 or 64 hidden rows (and 96, by 128 items)
 template <int WM, int TN>
 struct RingOf;
 template <int WM>
@@ -447,6 +447,8 @@ template <int WM>
 struct RingOf<WM, 128> { static constexpr int WN = 2, GN = 2, KS = 4, D = WM == 1 ? 6 : 4; };
 template <int WM>
 struct RingOf<WM, 256> { static constexpr int WN = 2, GN = 4, KS = 2, D = 3; };
+template <>
+struct RingOf<3, 128> { static constexpr int WN = 1, GN = 4, KS = 2, D = 3; };
 template <int WM, int TN, bool FAR>
 constexpr auto ring_kernel() {
     using P = RingOf<WM, TN>;
@@ -504,6 +506,7 @@ hipError_t configure_quantized_tile_lds() {
     both(ring_kernel<2, 64, false>(), ring_kernel<2, 64, true>());
     both(ring_kernel<2, 128, false>(), ring_kernel<2, 128, true>());
     both(ring_kernel<2, 256, false>(), ring_kernel<2, 256, true>());
+    both(ring_kernel<3, 128, false>(), ring_kernel<3, 128, true>());
     both(&quantized_turns_kernel<2, 1, false>, &quantized_turns_kernel<2, 1, true>);
     both(&quantized_turns_kernel<2, 2, false>, &quantized_turns_kernel<2, 2, true>);
     both(&quantized_turns_kernel<4, 2, false>, &quantized_turns_kernel<4, 2, true>);
@@ -527,12 +530,16 @@ hipError_t launch_quantized_tile(const QuantizedArgs& a, hipStream_t stream) {
         if (a.n_items <= 128 * cus) return launch_ring<128>(a, 0, stream);
         return launch_ring<256>(a, di.cus, stream);
     }
-    // Lists so short that tiles of 64 hidden rows by 64 or 128 items fill no more than a round of workgroups: the ring, which splits
-    // the slices among its wavefronts, is done with 4096 elements in 18 to 21 and 27 to 30 us, the alternating loop in 43 to 52 whatever the list's length.
-    const int64_t groups = (a.rows + 63) / 64;
-    if (ring_lds<2, 128>(a) <= kLdsBytes) {
-        if (groups * ((a.n_items + 63) / 64) <= di.cus) return launch_ring<64>(a, 0, stream);
-        if (groups * ((a.n_items + 127) / 128) <= di.cus) return launch_ring<128>(a, 0, stream);
+    // Lists so short that tiles of 64 hidden rows by 64 or 128 items, or 96 by 128, fill no more than a round of workgroups: the ring, which
+    // splits the slices among its wavefronts, is done with 4096 elements in 18 to 21, 27 to 30 and 36 to 37 us, the alternating loop in 43
+    // to 52 whatever the list's length.  (In a second round it takes as long again: 96 rows x 65536 items, 74 us and 67.)
+    auto one_round = [&](int tm, int tn) { return ((int64_t)a.rows + tm - 1) / tm * ((a.n_items + tn - 1) / tn) <= di.cus; };
+    if (ring_lds<2, 128>(a) <= kLdsBytes && ring_lds<3, 128>(a) <= kLdsBytes) {
+        if (one_round(64, 64)) return launch_ring<64>(a, 0, stream);
+        if (one_round(64, 128)) return launch_ring<128>(a, 0, stream);
+        if (one_round(96, 128))
+            return launch<void (*)(QuantizedArgs, int)>(ring_kernel<3, 128, false>(), ring_kernel<3, 128, true>(), a, 96, 128, 0, 512,
+                                                        ring_lds<3, 128>(a), stream);
     }
     switch (tile_shape(a.rows, a.n_items, di.cus, false)) {
         case TILE_128x128: return launch_turns<2, 1>(a, stream);

@@ -75,6 +75,13 @@ def test_rows_gigabytes_apart(rows):
     assert torch.equal(sv.quantized_dense_logits(h, spread(few, 17_000_000 // 16 * 16)).cpu().double(), full[:, :300])
 
 
+@pytest.mark.parametrize("rows, n", [(3, 30000), (20, 30000), (40, 40000), (60, 70000), (90, 30000), (150, 40000), (300, 40000)])
+def test_long_lists_of_rows_gigabytes_apart(rows, n):
+    h, U, full = case(rows, rows, 144, 900, False)
+    idx = torch.randint(0, 900, (n,), generator=torch.Generator().manual_seed(n)).to(torch.int32)
+    assert torch.equal(sv.quantized_subset_logits(h, spread(U, 5_000_000 // 16 * 16), idx.to(DEV)).cpu().double(), picked(full, idx))
+
+
 def picked(full, idx):
     at = idx.long().expand(full.shape[0], -1)
     return full.gather(1, at.clamp(min=0)).masked_fill(at < 0, -np.inf)
@@ -87,6 +94,7 @@ SHAPES = [
     (32, 1040, 900, 600), (33, 4096, 600, 520), (60, 2560, 3000, 700), (64, 256, 2049, 300), (65, 512, 1500, 400), (100, 4096, 700, 300),
     (128, 1024, 3000, 900), (129, 144, 4000, 200), (200, 3840, 600, 200), (256, 512, 2000, 300), (300, 272, 1111, 1111), (513, 128, 700, 64),
     (20, 16, 300, 50), (70, 48, 300, 20), (33, 128, 500, 1),
+    (90, 272, 30000, 26000), (180, 528, 15000, 13000),
     (20, 8208, 300, 40), (70, 16400, 200, 50),               # scales of a tile's rows do not fit into LDS
     # lists of every length class of the ring (tiles of 32, 64, 128 and 256 items, the last of a width that fills rounds), ragged
     (3, 400, 9000, 8000), (31, 144, 17001, 12345), (8, 272, 33001, 20000), (32, 128, 70001, 66000), (64, 144, 9001, 8500),
