@@ -348,8 +348,8 @@ int specvocab_quantized_subset_logits(const void* h, const uint8_t* h_scales, in
  * tok_out: device [rows] int32, the place, or idx(r, place) where idx (as in specvocab_subset_logits, padding slots having a logit of
  * -inf) is not NULL; -1 for a row that is masked throughout.  prob_out: device [rows] float32, w over the sum in 4 (0 for such
  * a row), or NULL.
- * Sums are kept to 2^-44 of each term (n up to 2^18; a bit less for each doubling of n), and do not depend on the run.  Rows of up to
- * 16384 logits: one launch; longer ones: one from 256 rows on, else three (and workspace).  A row in which more than 1024 places crowd into one
+ * Sums are kept to 2^-44 of each term (n up to 2^18; a bit less for each doubling of n), and do not depend on the run.  One launch; four (and
+ * workspace) for up to 64 rows of 49152 logits or more.  A row in which more than 1024 places crowd into one
  * of the 4096 steps (1024 for short rows) that its range, or 64 octaves of w, is cut into, at a border or where the token is drawn --
  * thousands of equal logits, clusters far apart --, costs some tens of passes over the row. */
 int specvocab_sample(const float* logits, int64_t ld, int64_t rows, int64_t n, const int32_t* idx, int idx_mode,

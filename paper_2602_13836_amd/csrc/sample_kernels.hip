@@ -288,6 +288,10 @@ struct RowWork {
     Drawn drawn;
 };
 
+// Where a row's lists come from: it is looked through for each; its first is there already, in memory; or only the first is wanted, of a
+// part of the row, to be added to what other parts found (LISTS_PART: `draw` ends there).
+enum Lists { LISTS_OWN, LISTS_GIVEN, LISTS_PART };
+
 // `places` hands out the row's logits, some threads some of them: quads(f) four at a time as for_quads does, groups(f) several quads at a
 // time for what does little with each.  Whatever is found is found by every wavefront for itself where 64 lanes are enough for it: bins
 // (64 x 64), and places of lists of up to 64.
@@ -374,8 +378,22 @@ struct RowSampler {
     // the places of bins lo0 .. hi0 and lo1 .. hi1 (hi0 <= hi1), and maybe some next to those
     __device__ __forceinline__ void collect(int lo0, int hi0, int lo1, int hi1) {
         const float from0 = lowest(hi0), to0 = highest(lo0), from1 = lowest(hi1), to1 = highest(lo1);
+        lo[0] = lo0;
+        hi[0] = hi0;
+        lo[1] = lo1;
+        hi[1] = hi1;
         if (used > 0) __syncthreads();                               // (an earlier list is read)
         uint32_t* fill = &w.fill[used++];
+        if constexpr (Places::kLists == LISTS_GIVEN) {
+            if (used == 1) {
+                len = *places.count;
+                full = len > (uint32_t)kList;
+                if (full) return;
+                for (uint32_t i = threadIdx.x; i < len; i += NT) w.list[i] = places.list[i];
+                __syncthreads();
+                return;
+            }
+        }
         places.groups([&](auto& v, int64_t p, int64_t step) {
             constexpr int kGroup = sizeof(v) / sizeof(v[0]);
             static_assert(kGroup <= 8, "a bit per logit");
@@ -401,6 +419,16 @@ struct RowSampler {
         });
         __syncthreads();
         len = *fill;
+        if constexpr (Places::kLists == LISTS_PART) {
+            if (threadIdx.x == 0) w.found[1] = (int)atomicAdd(places.count, len);
+            __syncthreads();
+            const uint32_t at = (uint32_t)w.found[1];
+            for (uint32_t i = threadIdx.x; i < len && at + i < (uint32_t)kList; i += NT) {
+                const int32_t place = (int32_t)w.list[i];
+                places.list[at + i] = make_key(places.z[place], place);
+            }
+            return;
+        }
         full = len > (uint32_t)kList;
         if (full) return;
         for (uint32_t i = threadIdx.x; i < len; i += NT) {           // their logits, all at once
@@ -408,10 +436,6 @@ struct RowSampler {
             w.list[i] = make_key(places.z[place], place);
         }
         __syncthreads();
-        lo[0] = lo0;
-        hi[0] = hi0;
-        lo[1] = lo1;
-        hi[1] = hi1;
     }
     // The places of bin b, which the list has, in order, with the running sums of their weights: up to 64 in the lanes of every wavefront,
     // more in LDS
@@ -539,7 +563,8 @@ struct RowSampler {
 #pragma nounroll
         for (int stage = with_k ? TOP_K : with_p ? TOP_P : with_m ? MIN_P : TOKEN; stage <= TOKEN; ++stage) {
             if ((stage == TOP_P && !with_p) || (stage == MIN_P && (!with_m || bin_m > border))) continue;
-            const double goal = (stage == TOP_P ? p : u) * kept;
+            // (p <= 0: the first place stays.  The bins in front of its own may be empty.)
+            const double goal = stage == TOP_P ? fmax(p * kept, 1e-300) : u * kept;
             int b = bin_m;
             if (stage == TOP_K) b = last_bin(BINS - 1, [&](int i) { return places_before(i) < k; });
             else if (stage != MIN_P) b = bin_with_mass(goal, stage == TOKEN, stage == TOKEN && take == 0u ? border - 1 : border);
@@ -553,7 +578,7 @@ struct RowSampler {
                     h = bin_with_mass(u * before(b + 1), true, b);
                 }
                 collect(l, h, b, b);
-                if (full) return false;
+                if (full || Places::kLists == LISTS_PART) return false;
             }
             order(b);
             if (full) return false;
@@ -565,7 +590,7 @@ struct RowSampler {
                 out->prob = weight_of(s, key_value(drawn)) / kept;
                 return true;
             }
-            if (stage == TOP_P) c = umax32(c, 1u);                   // (p <= 0: the first place stays)
+            if (stage == TOP_P) c = umax32(c, 1u);
             if (b < border || c < take) {
                 border = b;
                 take = c;
@@ -828,7 +853,9 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t r, const
     row.slot = 0;
     row.scan(ldexp(1.0, mass_bits(a.n)), in.k > 0u);
     Drawn d;
-    if (!row.draw(in.k, in.p, in.m, in.u, &d)) {
+    const bool drawn = row.draw(in.k, in.p, in.m, in.u, &d);
+    if constexpr (Places::kLists == LISTS_PART) return;
+    if (!drawn) {
         if (threadIdx.x == 0) w.slow = SlowInput{s, row.total, in.p, in.m, in.u, row.all, in.k};
         __syncthreads();
         draw_slowly<NT, BINS>(w, a.logits + r * a.ld, a.n);
@@ -836,9 +863,9 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t r, const
     }
     put_token(a, r, d.place, d.prob);
 }
-// the first place of the largest logit
+// the first place of the largest logit, into w.found[0]
 template <int NT, int BINS, class Places>
-__device__ __forceinline__ void pick_first(const SampleArgs& a, int64_t r, float top, RowWork<NT, BINS>& w, const Places& places) {
+__device__ __forceinline__ void find_first(float top, RowWork<NT, BINS>& w, const Places& places) {
     places.groups([&](auto& v, int64_t p, int64_t step) {
 #pragma unroll
         for (int a = 0; a < (int)(sizeof(v) / sizeof(v[0])); ++a)
@@ -847,6 +874,10 @@ __device__ __forceinline__ void pick_first(const SampleArgs& a, int64_t r, float
                 if (v[a][i] == top) atomicMin(&w.found[0], (int)(p + a * step + i));
     });
     __syncthreads();
+}
+template <int NT, int BINS, class Places>
+__device__ __forceinline__ void pick_first(const SampleArgs& a, int64_t r, float top, RowWork<NT, BINS>& w, const Places& places) {
+    find_first(top, w, places);
     put_token(a, r, w.found[0], 1.0);
 }
 
@@ -858,6 +889,7 @@ struct ShortWork {
 };
 template <int NT>
 struct LdsPlaces {
+    static constexpr Lists kLists = LISTS_OWN;
     const float* z;
     int n;
     template <class F>
@@ -913,12 +945,15 @@ __global__ __launch_bounds__(NT, 4) void sample_short_kernel(const SampleArgs a)
     sample_row<ROW_EXACT>(a, r, in, settings_of(in.t, x.x, x.y, kOctaves, kNarrowBins), w, places);
 }
 
-// ---- longer rows.  A workgroup per row reads it once for its range, once for the histogram and once for each list; where rows are
-// few the first two are spread over the chip: launches of `parts` workgroups per row.
+// ---- longer rows.  A workgroup per row reads it once for the histogram and once for each list; where rows are few, they are spread over
+// the chip: launches of `parts` workgroups per row for the range, the histogram and the first list, and one of a workgroup per row.
 struct SampleScratch {
     unsigned long long* mass;    // [rows][kWideBins]
     uint32_t* cnt;               // [rows][kWideBins]
+    unsigned long long* list;    // [rows][kList]: the first list
     float2* range;               // [rows][parts]
+    uint32_t* list_len;          // [rows]
+    int32_t* first;              // [rows]: the first place of the largest logit
     int parts;
 };
 __device__ __forceinline__ void part_of(int64_t n, int parts, int64_t* from, int64_t* to) {
@@ -954,6 +989,10 @@ __global__ __launch_bounds__(kPartThreads) void sample_range_kernel(const Sample
         s.mass[r * kWideBins + i] = 0ull;
         s.cnt[r * kWideBins + i] = 0u;
     }
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        s.list_len[r] = 0u;
+        s.first[r] = 0x7fffffff;
+    }
     int64_t from, to;
     part_of(a.n, s.parts, &from, &to);
     const float2 x = range_of<kPartThreads>(a.logits + r * a.ld, from, to, sums);
@@ -987,84 +1026,105 @@ __global__ __launch_bounds__(kPartThreads) void sample_count_kernel(const Sample
     }
 }
 
-// (a pass over a row is one CU's: what it has on its way decides how long one that does little takes)
-template <int NT, int GROUP>
+// (a pass over a row, or its part, is one CU's: what it has on its way decides how long one that does little takes)
+template <int NT, int GROUP, Lists LISTS>
 struct RowPlaces {
+    static constexpr Lists kLists = LISTS;
     const float* z;
-    int64_t n;
+    int64_t from, to;
+    unsigned long long* list;
+    uint32_t* count;
     template <class F>
-    __device__ __forceinline__ void groups(F f) const { for_groups<NT, GROUP>(z, 0, n, f); }
+    __device__ __forceinline__ void groups(F f) const { for_groups<NT, GROUP>(z, from, to, f); }
     template <class F>
-    __device__ __forceinline__ void quads(F f) const { for_quads<NT, 2>(z, 0, n, f); }
+    __device__ __forceinline__ void quads(F f) const { for_quads<NT, 2>(z, from, to, f); }
 };
-// (a workgroup per row: two of 512 threads share a CU and fill each other's pauses; rows in parts, which are few, have a CU and twice
-// the registers to themselves)
 constexpr int kRowThreads = 512, kGuessed = 8192;
-template <bool PARTS>
-__global__ __launch_bounds__(kRowThreads, PARTS ? 2 : 4) void sample_long_kernel(const SampleArgs a, const SampleScratch s) {
+using LongWork = RowWork<kRowThreads, kWideBins>;
+// Rows in parts, their histogram in memory.  FIRST: a workgroup per part finds, as each of its row does, where the first list's places
+// lie, and brings its part's together; then a workgroup per row draws.
+template <bool FIRST>
+__global__ __launch_bounds__(kRowThreads, 2) void sample_parts_kernel(const SampleArgs a, const SampleScratch s) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    RowWork<kRowThreads, kWideBins>& w = *reinterpret_cast<RowWork<kRowThreads, kWideBins>*>(smem);
+    LongWork& w = *reinterpret_cast<LongWork*>(smem);
+    const int64_t r = FIRST ? blockIdx.y : blockIdx.x;
+    const RowInput in = input_of(a, r);
+    RowPlaces<kRowThreads, 8, (FIRST ? LISTS_PART : LISTS_GIVEN)> places{a.logits + r * a.ld, 0, a.n, s.list + r * kList, s.list_len + r};
+    if (FIRST) part_of(a.n, s.parts, &places.from, &places.to);
+    clear_work(w, false);
+    const float2 x = range_of_parts(s, r);
+    if (!is_logit(x.x)) {
+        if (!FIRST) put_token(a, r, -1, 0.0);
+        return;
+    }
+    if (in.greedy) {
+        if (!FIRST) return put_token(a, r, s.first[r], 1.0);
+        __syncthreads();
+        find_first(x.x, w, places);
+        if (threadIdx.x == 0) atomicMin(&s.first[r], w.found[0]);
+        return;
+    }
+    for (int i = threadIdx.x; i < kWideBins; i += kRowThreads) {
+        w.mass[i] = s.mass[r * kWideBins + i];
+        w.cnt[i] = s.cnt[r * kWideBins + i];
+    }
+    __syncthreads();
+    sample_row<ROW_COUNTED>(a, r, in, settings_of(in.t, x.x, x.y, kOctaves, kWideBins), w, places);
+}
+// A workgroup per row: of 1024 threads up to a row per CU, else of 512, two on a CU that fill each other's pauses (151936 logits: 255 rows
+// 84 us and 98, 512 rows 156 and 140).  The row's first places say where its logits lie; bins
+// up to 24 octaves above (or as far as those spread) leave room for larger ones.  What lies outside is noticed while the histogram is
+// made, which is then made again: 64 octaves from the largest on.  Saves reading the row once more (512 x 151936: 40 of 186 us).
+template <int NT>
+__global__ __launch_bounds__(NT, 4) void sample_rows_kernel(const SampleArgs a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    RowWork<NT, kWideBins>& w = *reinterpret_cast<RowWork<NT, kWideBins>*>(smem);
     const int64_t r = blockIdx.x;
     const float* z = a.logits + r * a.ld;
     const RowInput in = input_of(a, r);
-    clear_work(w, !PARTS);
-    const RowPlaces<kRowThreads, (PARTS ? 8 : 3)> places{z, a.n};
-    if constexpr (PARTS) {
-        const float2 x = range_of_parts(s, r);
-        for (int i = threadIdx.x; i < kWideBins; i += kRowThreads) {
-            w.mass[i] = s.mass[r * kWideBins + i];
-            w.cnt[i] = s.cnt[r * kWideBins + i];
-        }
-        __syncthreads();
-        if (!is_logit(x.x)) return put_token(a, r, -1, 0.0);
-        if (in.greedy) return pick_first(a, r, x.x, w, places);
-        sample_row<ROW_COUNTED>(a, r, in, settings_of(in.t, x.x, x.y, kOctaves, kWideBins), w, places);
-    } else {
-        // The row's first places say where its logits lie; bins up to 24 octaves above (or as far as those spread) leave room for larger ones.  What
-        // lies outside is noticed while the histogram is made, which is then made again: 64 octaves from the largest on.  Saves reading the row
-        // once more (512 x 151936: 40 of 186 us).
-        const float2 g = range_of<kRowThreads>(z, 0, in.greedy ? a.n : min(a.n, (int64_t)kGuessed), w.sums);
-        if (in.greedy) return is_logit(g.x) ? pick_first(a, r, g.x, w, places) : put_token(a, r, -1, 0.0);
-        float edge = 0.0f, low = 0.0f;
-        if (is_logit(g.x)) {
-            const float spread = fmaxf(g.x - g.y, 1e-30f);
-            edge = g.x + fminf((float)(kAbove * 0.6931472) * in.t, spread);
-            if (edge == __builtin_inff()) edge = g.x;                // (past the largest float)
-            low = g.y - spread;
-        }
-        sample_row<ROW_GUESSED>(a, r, in, settings_of(in.t, edge, low, kOctaves + kAbove, kWideBins), w, places);
+    clear_work(w, true);
+    const RowPlaces<NT, 3, LISTS_OWN> places{z, 0, a.n, nullptr, nullptr};
+    const float2 g = range_of<NT>(z, 0, in.greedy ? a.n : min(a.n, (int64_t)kGuessed), w.sums);
+    if (in.greedy) return is_logit(g.x) ? pick_first(a, r, g.x, w, places) : put_token(a, r, -1, 0.0);
+    float edge = 0.0f, low = 0.0f;
+    if (is_logit(g.x)) {
+        const float spread = fmaxf(g.x - g.y, 1e-30f);
+        edge = g.x + fminf((float)(kAbove * 0.6931472) * in.t, spread);
+        if (edge == __builtin_inff()) edge = g.x;                    // (past the largest float)
+        low = g.y - spread;
     }
+    sample_row<ROW_GUESSED>(a, r, in, settings_of(in.t, edge, low, kOctaves + kAbove, kWideBins), w, places);
 }
 
 constexpr int kShort = 16384;
-// workgroups that share a long row: enough rows to fill the chip need none (a rule of the sizes alone: the workspace depends on it)
-constexpr int64_t kChip = 256;
+// Workgroups that share a row.  A few rows of a whole vocabulary are shared: 8 x 151936 logits 37 us (69 with a workgroup per row), 32
+// 49 (70), 60 59 (73), but 85 79 (74); 8 x 80000 35 (45), 60 48 (48); from 40000 logits down never (1 row 28 and 24, 32 rows 40 and 36).
+// No more parts than there are CUs for: 60 rows in five parts each, 71.  (A rule of the sizes alone: the workspace depends on it.)
+constexpr int64_t kChip = 256, kMostShared = 64, kLeastShared = 49152;
 int parts_of(int64_t rows, int64_t n) {
-    if (n <= kShort || rows >= kChip) return 1;
-    const int64_t want = (kChip + rows - 1) / rows, most = n / 8192;
-    const int64_t p = want < most ? want : most;
-    return (int)(p < kMostParts ? p : kMostParts);
+    if (n < kLeastShared || rows > kMostShared) return 1;
+    const int64_t most = n / 8192 < kMostParts ? n / 8192 : kMostParts;
+    return (int)(kChip / rows < most ? kChip / rows : most);
 }
 
 }  // namespace
 
 size_t sample_scratch_bytes(int64_t rows, int64_t n) {
     const int parts = parts_of(rows, n);
-    return parts > 1 ? (size_t)rows * (kWideBins * 12 + (size_t)parts * sizeof(float2)) : 0;
+    return parts > 1 ? (size_t)rows * (kWideBins * 12 + kList * 8 + (size_t)parts * sizeof(float2) + 8) : 0;
 }
 
 hipError_t configure_sample_lds() {
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&sample_long_kernel<false>),
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RowWork<kRowThreads, kWideBins>));
-    if (e == hipSuccess)
-        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&sample_short_kernel<512, 8192>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                (int)sizeof(ShortWork<512, 8192>));
-    if (e == hipSuccess)
-        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&sample_short_kernel<1024, kShort>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                (int)sizeof(ShortWork<1024, kShort>));
-    if (e == hipSuccess)
-        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&sample_long_kernel<true>),
-                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RowWork<kRowThreads, kWideBins>));
+    hipError_t e = hipSuccess;
+    auto opt_in = [&](auto* kernel, size_t bytes) {
+        if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    };
+    opt_in(&sample_short_kernel<512, 8192>, sizeof(ShortWork<512, 8192>));
+    opt_in(&sample_short_kernel<1024, kShort>, sizeof(ShortWork<1024, kShort>));
+    opt_in(&sample_rows_kernel<512>, sizeof(RowWork<512, kWideBins>));
+    opt_in(&sample_rows_kernel<1024>, sizeof(RowWork<1024, kWideBins>));
+    opt_in(&sample_parts_kernel<true>, sizeof(LongWork));
+    opt_in(&sample_parts_kernel<false>, sizeof(LongWork));
     return e;
 }
 
@@ -1080,13 +1140,19 @@ hipError_t launch_sample(const SampleArgs& a, hipStream_t stream) {
         s.parts = parts_of(a.rows, a.n);
         if (s.parts > 1) {
             s.mass = reinterpret_cast<unsigned long long*>(a.scratch);
-            s.range = reinterpret_cast<float2*>(s.mass + (size_t)a.rows * kWideBins);
+            s.list = s.mass + (size_t)a.rows * kWideBins;
+            s.range = reinterpret_cast<float2*>(s.list + (size_t)a.rows * kList);
             s.cnt = reinterpret_cast<uint32_t*>(s.range + (size_t)a.rows * s.parts);
-            hipLaunchKernelGGL(sample_range_kernel, dim3(s.parts, rows), dim3(kPartThreads), 0, stream, a, s);
-            hipLaunchKernelGGL(sample_count_kernel, dim3(s.parts, rows), dim3(kPartThreads), (size_t)kWideBins * 12, stream, a, s);
-            hipLaunchKernelGGL(sample_long_kernel<true>, dim3(rows), dim3(kRowThreads), sizeof(RowWork<kRowThreads, kWideBins>), stream, a, s);
+            s.list_len = s.cnt + (size_t)a.rows * kWideBins;
+            s.first = reinterpret_cast<int32_t*>(s.list_len + a.rows);
+            const dim3 parts(s.parts, rows);
+            hipLaunchKernelGGL(sample_range_kernel, parts, dim3(kPartThreads), 0, stream, a, s);
+            hipLaunchKernelGGL(sample_count_kernel, parts, dim3(kPartThreads), (size_t)kWideBins * 12, stream, a, s);
+            hipLaunchKernelGGL(sample_parts_kernel<true>, parts, dim3(kRowThreads), sizeof(LongWork), stream, a, s);
+            hipLaunchKernelGGL(sample_parts_kernel<false>, dim3(rows), dim3(kRowThreads), sizeof(LongWork), stream, a, s);
         } else {
-            hipLaunchKernelGGL(sample_long_kernel<false>, dim3(rows), dim3(kRowThreads), sizeof(RowWork<kRowThreads, kWideBins>), stream, a, s);
+            if (a.rows <= kChip) go(&sample_rows_kernel<1024>, 1024, sizeof(RowWork<1024, kWideBins>));
+            else go(&sample_rows_kernel<512>, 512, sizeof(RowWork<512, kWideBins>));
         }
     }
     return hipGetLastError();

@@ -55,7 +55,7 @@ def test_language_like_logits_with_everything(n):
     check(language_like(rng, rows, n), u=s["u"], name="none")
 
 
-@pytest.mark.parametrize("rows, n", [(300, 20000), (256, 128256), (513, 3000), (255, 17000)])
+@pytest.mark.parametrize("rows, n", [(300, 20000), (256, 128256), (513, 3000), (255, 17000), (64, 49152), (64, 49151), (65, 60000), (3, 200003)])
 def test_many_rows(rows, n):
     rng = np.random.default_rng(rows)
     z = torch.randn((rows, n), generator=torch.Generator(device=DEV).manual_seed(rows), device=DEV) * 3
@@ -69,7 +69,7 @@ def test_many_rows(rows, n):
     assert torch.equal(got[0][at], part[0]) and torch.equal(got[1][at], part[1])
 
 
-@pytest.mark.parametrize("n", [5, 300, 3000, 16384, 40000])
+@pytest.mark.parametrize("n", [5, 300, 3000, 16384, 40000, 100001])
 def test_every_border_by_itself(n):
     rng = np.random.default_rng(n + 1)
     for name, kw in [("k", dict(k=[1, 2, 3, n - 1, n, n + 5, 1400, 3000])), ("p", dict(p=[0.0, -1.0, 1e-7, 0.3, 0.5, 0.9, 0.9999, 1 - 2.0 ** -24])),
@@ -82,7 +82,7 @@ def test_every_border_by_itself(n):
             check(language_like(rng, 8, n), u=u, name=name, **kw)
 
 
-@pytest.mark.parametrize("n", [1, 700, 4096, 16384, 16390, 60000])
+@pytest.mark.parametrize("n", [1, 700, 4096, 16384, 16390, 30000, 60000])
 def test_ties_flat_rows_and_clusters(n):
     rng = np.random.default_rng(n + 2)
     few = rng.integers(0, 4, (8, n)).astype(np.float32)                        # four values
@@ -120,7 +120,7 @@ def test_masks(n):
     check(z, u=s["u"], p=np.full(10, 0.9), m=np.full(10, 0.01))
 
 
-@pytest.mark.parametrize("rows, n", [(260, 20000), (257, 100001)])
+@pytest.mark.parametrize("rows, n", [(260, 20000), (257, 100001), (20, 20000), (100, 70001)])
 def test_rows_whose_first_places_are_unlike_the_rest(rows, n):
     """Rows that a workgroup each reads, whose first 8192 places say nothing, little or the wrong thing about the rest."""
     rng = np.random.default_rng(n)
@@ -147,9 +147,18 @@ def test_rows_whose_first_places_are_unlike_the_rest(rows, n):
              p=rng.choice([1.0, 0.9, 0.99], rows), m=rng.choice([0.0, 0.0, 0.05], rows))
     dev = [torch.as_tensor(s[x], dtype=torch.int32 if x == "k" else torch.float32).to(DEV) for x in ("u", "t", "k", "p", "m")]
     tok, prob = (x.cpu().numpy() for x in sv.sample(torch.from_numpy(z).to(DEV), *dev))
-    for r in range(5 * kinds):
+    for r in range(min(rows, 5 * kinds)):
         at, pr = sample_row(z[r], s["u"][r], float(np.float32(s["t"][r])), int(s["k"][r]), float(np.float32(s["p"][r])), float(np.float32(s["m"][r])))
         assert tok[r] == at and abs(prob[r] - pr) <= pr * (2.0 ** -24 + 2.0 ** -40) + 1e-38, (r, r % kinds, tok[r], at, prob[r], pr)
+
+
+@pytest.mark.parametrize("rows, n", [(300, 17000), (100, 20000), (10, 60000), (5, 9000)])
+def test_a_mass_of_zero_keeps_the_first_place(rows, n):
+    rng = np.random.default_rng(rows)
+    z = language_like(rng, rows, n)
+    p = rng.choice([0.0, -0.0, -1.0, -math.inf, 1e-45, 1e-30], rows)
+    tok, prob = sv.sample(z.to(DEV), torch.rand(rows, device=DEV), top_p=torch.as_tensor(p, dtype=torch.float32).to(DEV))
+    assert torch.equal(tok.cpu().long(), z.argmax(dim=1)) and (prob == 1).all()
 
 
 def test_lists_name_the_tokens():

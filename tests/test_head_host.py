@@ -115,7 +115,8 @@ def test_workspace_sizes(lib):
     assert sv.workspace_bytes(sub, 1, 4096, 128256, 8192, dt=sv.SV_E4M3) == 0
     assert sv.workspace_bytes(sv.SV_OP_QUANTIZED_DENSE_LOGITS, 8, 4096, 128256, dt=sv.SV_BF16) == 0
     assert sv.workspace_bytes(sv.SV_OP_QUANTIZED_DENSE_LOGITS, 8, 4096, 128256, dt=sv.SV_E4M3) == 8 * 4096 * 2
-    assert sv.workspace_bytes(sv.SV_OP_SAMPLE, 1, k=16384) == 0 and sv.workspace_bytes(sv.SV_OP_SAMPLE, 1, k=16385) > 0
+    assert sv.workspace_bytes(sv.SV_OP_SAMPLE, 1, k=49151) == 0 and sv.workspace_bytes(sv.SV_OP_SAMPLE, 1, k=49152) > 0
+    assert sv.workspace_bytes(sv.SV_OP_SAMPLE, 64, k=128256) > 0 and sv.workspace_bytes(sv.SV_OP_SAMPLE, 65, k=128256) == 0
     assert sv.workspace_bytes(step, 1, 4096, 128256, 0, dt=sv.SV_E4M3) == sv.workspace_bytes(sv.SV_OP_SAMPLE, 1, k=128256)
     plain = sv.workspace_bytes(sub, 60, 4096, 128256, 4096, dt=sv.SV_BF16)
     assert sv.workspace_bytes(sub, 60, 4096, 128256, 4096, dt=sv.SV_E4M3) == plain + 60 * 4096 * 2
