@@ -126,7 +126,9 @@ __global__ __launch_bounds__(64 * GN * KS) void quantized_ring_kernel(const Quan
     constexpr int TM = R::TM, TN = R::TN, kStage = R::kStage, kPass = R::kPass, LB = R::LB, LX = R::LX;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];     // [D][TN rows of U, TM rows of h twice], scales
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
-    const int wc = wave % GN, kh = wave / GN;                         // its group of items, and its part of every slice
+    // its group of items, and its part of every slice (a SIMD's wavefronts, w and w + 4, are of groups 0 and 2 or 1 and 3 of four: in
+    // a tile of 160 items each SIMD has 64 or 96 to multiply with, none 128)
+    const int wc = wave / KS, kh = wave % KS;
     const Tile t = find_tile<TM, TN>(a, balance_cus);
     if (!t.any) return;
     const int units = a.units, nk = (units + 7) / 8;
@@ -167,9 +169,10 @@ __global__ __launch_bounds__(64 * GN * KS) void quantized_ring_kernel(const Quan
     const int fx0 = TN * 128 + (lane & 31) * 128 + ((((2 * g) ^ swz) * 16) ^ ((4 * (q0 & 1) + k0) * 16)) + (q0 >> 1) * TM * 128;
     const int fu0 = (wc * 32 * WN + (lane & 31)) * 128 + (((g ^ swz) * 16) ^ (q0 * 32));
     // What lies past the tile's width is neither requested nor multiplied.
-    const bool none = wc * 32 * WN >= t.tn;
+    const int my_items = __builtin_amdgcn_readfirstlane(t.tn - wc * 32 * WN);
+    const bool none = my_items <= 0;
     const unsigned char* const my_scales = scales + (wc * 32 * WN + (lane & 31)) * stride;
-    auto walk = [&](auto mine) {
+    auto walk = [&](auto mine, auto some) {
         constexpr int MINE = decltype(mine)::value;
         auto request = [&](int s, int stage) {
             const int e = eff(s);
@@ -212,6 +215,7 @@ __global__ __launch_bounds__(64 * GN * KS) void quantized_ring_kernel(const Quan
                                 base + (fx0 ^ ((4 * (q & 1) + k) * 16)) + (q >> 1) * TM * 128 + 32 * m * 128));
 #pragma unroll
                         for (int n = 0; n < WN; ++n) {
+                            if (decltype(some)::value && 32 * n >= my_items) break;              // uniform
                             const uint32_t lo = NK == 1 && k0 ? raw[n][2] : raw[n][2 * k], hi = NK == 1 && k0 ? raw[n][3] : raw[n][2 * k + 1];
                             const bf16x8_t b = widen_8(lo, hi, scale[n]);
 #pragma unroll
@@ -224,11 +228,15 @@ __global__ __launch_bounds__(64 * GN * KS) void quantized_ring_kernel(const Quan
         }
     };
     const int live = (t.tn - 8 * wave + kPass - 1) / kPass;          // requests for U: 0 .. LB
-    if (LB >= 4 && live >= 4) walk(std::integral_constant<int, (LB < 4 ? LB : 4)>{});
-    else if (LB >= 3 && live == 3) walk(std::integral_constant<int, (LB < 3 ? LB : 3)>{});
-    else if (LB >= 2 && live >= 2) walk(std::integral_constant<int, (LB < 2 ? LB : 2)>{});
-    else if (live >= 1) walk(std::integral_constant<int, 1>{});
-    else walk(std::integral_constant<int, 0>{});
+    auto of_width = [&](auto some) {
+        if (LB >= 4 && live >= 4) walk(std::integral_constant<int, (LB < 4 ? LB : 4)>{}, some);
+        else if (LB >= 3 && live == 3) walk(std::integral_constant<int, (LB < 3 ? LB : 3)>{}, some);
+        else if (LB >= 2 && live >= 2) walk(std::integral_constant<int, (LB < 2 ? LB : 2)>{}, some);
+        else if (live >= 1) walk(std::integral_constant<int, 1>{}, some);
+        else walk(std::integral_constant<int, 0>{}, some);
+    };
+    if (WN > 1 && my_items < 32 * WN) of_width(std::bool_constant<(WN > 1)>{});
+    else of_width(std::false_type{});
     // Everybody has read its last slice, and nothing is on its way into the ring any more (slices past the end: requested, never
     // read): the wavefronts' sums go there, [part][group][value][lane], and each of the KS adds up and stores its share of the group's.
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -515,8 +523,7 @@ hipError_t configure_quantized_tile_lds() {
 
 // True if one of these kernels can: the scales of a tile's rows have to fit into LDS beside its slices.
 bool quantized_tile_supported(const QuantizedArgs& a) {
-    return a.rows > 64 ? turns_fit<4, 2>(a) : ring_lds<2, 64>(a) <= kLdsBytes && ring_lds<2, 128>(a) <= kLdsBytes && ring_lds<2, 256>(a) <= kLdsBytes &&
-                                                  ring_lds<1, 128>(a) <= kLdsBytes;
+    return a.rows > 64 ? turns_fit<4, 2>(a) : ring_lds<2, 64>(a) <= kLdsBytes && ring_lds<2, 128>(a) <= kLdsBytes && ring_lds<1, 128>(a) <= kLdsBytes;
 }
 
 hipError_t launch_quantized_tile(const QuantizedArgs& a, hipStream_t stream) {
@@ -527,7 +534,8 @@ hipError_t launch_quantized_tile(const QuantizedArgs& a, hipStream_t stream) {
         const int64_t cus = di.cus;
         if (a.n_items <= 32 * cus) return launch_ring<32>(a, 0, stream);
         if (a.n_items <= 64 * cus) return launch_ring<64>(a, 0, stream);
-        if (a.n_items <= 128 * cus) return launch_ring<128>(a, 0, stream);
+        // (from 8192 elements on, the scales of 256 items do not fit beside their slices: more rounds of 128)
+        if (a.n_items <= 128 * cus || ring_lds<2, 256>(a) > kLdsBytes) return launch_ring<128>(a, 0, stream);
         return launch_ring<256>(a, di.cus, stream);
     }
     // Lists so short that tiles of 64 hidden rows by 64 or 128 items, or 96 by 128, fill no more than a round of workgroups: the ring, which

@@ -75,11 +75,15 @@ def test_rows_gigabytes_apart(rows):
     assert torch.equal(sv.quantized_dense_logits(h, spread(few, 17_000_000 // 16 * 16)).cpu().double(), full[:, :300])
 
 
-@pytest.mark.parametrize("rows, n", [(3, 30000), (20, 30000), (40, 40000), (60, 70000), (90, 30000), (150, 40000), (300, 40000)])
-def test_long_lists_of_rows_gigabytes_apart(rows, n):
-    h, U, full = case(rows, rows, 144, 900, False)
+@pytest.mark.parametrize("far", [False, True])
+@pytest.mark.parametrize("rows, n, d", [(3, 30000, 144), (20, 30000, 144), (20, 70000, 656), (25, 90000, 144), (40, 40000, 144), (60, 70000, 656),
+                                        (33, 82000, 144), (90, 30000, 144), (150, 40000, 144), (300, 40000, 144), (40, 70000, 8192), (20, 40000, 8192)])
+def test_long_lists_of_near_and_far_rows(rows, n, d, far):
+    """Tokens come several times; rows that 32 bits do not reach."""
+    h, U, full = case(rows, rows, d, 900, False)
     idx = torch.randint(0, 900, (n,), generator=torch.Generator().manual_seed(n)).to(torch.int32)
-    assert torch.equal(sv.quantized_subset_logits(h, spread(U, 5_000_000 // 16 * 16), idx.to(DEV)).cpu().double(), picked(full, idx))
+    got = sv.quantized_subset_logits(h, spread(U, 5_000_000 // 16 * 16) if far else U, idx.to(DEV))
+    assert torch.equal(got, full.to(DEV).float()[:, idx.to(DEV).long()])
 
 
 def picked(full, idx):
