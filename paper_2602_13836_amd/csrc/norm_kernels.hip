@@ -7,7 +7,9 @@
 // addition, a norm and a quantisation of their own would: the selector multiplies y, the 8-bit head q, and both mean the same row.
 // Sums of squares are float32, of at most a few dozen values per lane before the tree over lanes and wavefronts.
 // Memory bounds it: two rows in, two and a half out, nothing read twice.  Eight consecutive values per lane and load, so that 16
-// lanes hold a block of 128 and its largest magnitude is four DPP steps away.
+// lanes hold a block of 128 and its largest magnitude is four DPP steps away.  A workgroup per row, as many threads as the row has
+// pieces of eight (a wavefront per row left too few loads on their way).  Measured: 5000 rows of 3840 bfloat16 values with the
+// residual and all three outputs 28.6 us, 173 MB at 6.0 TB/s; one row of 4096, 2.6 us, a launch.
 #include "quantized_rows.h"
 #include "sv_launch.h"
 
@@ -15,7 +17,8 @@ namespace sv {
 
 namespace {
 
-// ---- 8 bits of given rows: a wavefront takes 512 values (four blocks, one word of scales) at a time, kUnits of them on their way
+// ---- 8 bits of given rows: a wavefront takes 512 values (four blocks, one word of scales) at a time, kUnits of them on their way.
+// 128256 rows of 4096 bfloat16 values: 275 us, 1.6 GB at 5.7 TB/s, two thirds of them reads.
 constexpr int kUnits = 4;
 template <int DT>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const char* x, const int64_t row_bytes, const int64_t rows, const int d,
