@@ -487,6 +487,8 @@ def scale_columns(d: int) -> int:
 
 # These calls check that what they are given lives on the current device, whose stream they go to, and spend as little
 # as they can on it: a norm of one row is over in less time than ten Python calls take.  Tensors that they make are not checked.
+# With a stream given they run with it as the current one: outputs and workspaces that a call makes are that stream's, so nobody else is
+# handed their memory while it works on them.
 def _rows(t: torch.Tensor, name: str, here: int) -> Tuple[int, int, int]:
     """_mat of a tensor on the current device."""
     if t.get_device() != here:
@@ -507,10 +509,6 @@ def _flat(t: Optional[torch.Tensor], shape: tuple, dtype: torch.dtype, name: str
     if t.get_device() != here or t.shape != shape or t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {list(shape)} {dtype} tensor on the current GPU (cuda:{here})")
     return t.data_ptr()
-
-
-def _raw_stream(stream: Optional[torch.cuda.Stream], here: int) -> int:
-    return _current_raw_stream(here) if stream is None else stream.cuda_stream
 
 
 def _scratch(nbytes: int, like: torch.Tensor, ws: Optional[torch.Tensor], here: int) -> Tuple[Optional[torch.Tensor], Optional[int], int]:
@@ -551,11 +549,14 @@ def _quantized_out(rows: int, d: int, like: torch.Tensor, out: Optional[Quantize
 def quantize_rows(x: torch.Tensor, out: Optional[QuantizedRows] = None,
                   stream: Optional[torch.cuda.Stream] = None) -> QuantizedRows:
     """specvocab_quantize_rows: the rows of x in 8 bits, a power-of-two scale per block of 128."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return quantize_rows(x, out)
     here = torch.cuda.current_device()
     rows, d, ldx = _rows(x, "x", here)
     out, ldq, lds = _quantized_out(rows, d, x, out, here)
     _check(load_library().specvocab_quantize_rows(x.data_ptr(), rows, d, ldx, _dt(x), out.q.data_ptr(), ldq, out.scales.data_ptr(),
-                                                  lds, _raw_stream(stream, here)), "specvocab_quantize_rows")
+                                                  lds, _current_raw_stream(here)), "specvocab_quantize_rows")
     return out
 
 
@@ -573,6 +574,9 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Option
              quantized_out: Optional[QuantizedRows] = None, stream: Optional[torch.cuda.Stream] = None):
     """specvocab_rms_norm: root-mean-square norm of x + residual.
     Returns (y or None, the sum (x itself without a residual), QuantizedRows of y or None)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return rms_norm(x, weight, eps, residual, weight_offset, want_y, want_quantized, sum_out, y_out, quantized_out)
     here = torch.cuda.current_device()
     rows, d, ldx = _rows(x, "x", here)
     w = _flat(weight, (d,), x.dtype, "weight", here)
@@ -598,7 +602,7 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Option
         quantized_out, ldq, lds = _quantized_out(rows, d, x, quantized_out, here)
         q, s = quantized_out.q.data_ptr(), quantized_out.scales.data_ptr()
     _check(load_library().specvocab_rms_norm(x.data_ptr(), rows, d, ldx, r, ldr, w, weight_offset, eps, _dt(x), t, ld_sum, y, ldy,
-                                             q, ldq, s, lds, _raw_stream(stream, here)), "specvocab_rms_norm")
+                                             q, ldq, s, lds, _current_raw_stream(here)), "specvocab_rms_norm")
     return y_out, x if residual is None else sum_out, quantized_out
 
 
@@ -640,11 +644,14 @@ def _list(idx: torch.Tensor, rows: int, padded: bool, here: int) -> Tuple[int, i
 def quantized_dense_logits(h: Union[torch.Tensor, QuantizedRows], U: QuantizedRows, out: Optional[torch.Tensor] = None,
                            ws: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """specvocab_quantized_dense_logits: out[r, v] = <U[v], h_r> with U in 8 bits, h in 8 bits or bfloat16."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return quantized_dense_logits(h, U, out, ws)
     here = torch.cuda.current_device()
     args, rows, d, V, dt = _head_operands(h, U, here)
     out, op = _logits_out(out, rows, V, U, here)
     ws, wp, wn = _scratch(workspace_bytes(SV_OP_QUANTIZED_DENSE_LOGITS, rows, d, V, 0, 0, 0, dt), U.q, ws, here)
-    _check(load_library().specvocab_quantized_dense_logits(*args, op, wp, wn, _raw_stream(stream, here)),
+    _check(load_library().specvocab_quantized_dense_logits(*args, op, wp, wn, _current_raw_stream(here)),
            "specvocab_quantized_dense_logits")
     return out
 
@@ -653,12 +660,15 @@ def quantized_subset_logits(h: Union[torch.Tensor, QuantizedRows], U: QuantizedR
                             out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
                             stream: Optional[torch.cuda.Stream] = None, padded: bool = False) -> torch.Tensor:
     """specvocab_quantized_subset_logits: out[r, j] = <U[idx(r, j)], h_r>.  padded: idx may hold padding slots (-1)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return quantized_subset_logits(h, U, idx, out, ws, padded=padded)
     here = torch.cuda.current_device()
     args, rows, d, V, dt = _head_operands(h, U, here)
     ip, mode, k = _list(idx, rows, padded, here)
     out, op = _logits_out(out, rows, k, U, here)
     ws, wp, wn = _scratch(workspace_bytes(SV_OP_QUANTIZED_SUBSET_LOGITS, rows, d, V, k, 0, 0, dt, mode), U.q, ws, here)
-    _check(load_library().specvocab_quantized_subset_logits(*args, ip, k, mode, op, wp, wn, _raw_stream(stream, here)),
+    _check(load_library().specvocab_quantized_subset_logits(*args, ip, k, mode, op, wp, wn, _current_raw_stream(here)),
            "specvocab_quantized_subset_logits")
     return out
 
@@ -690,6 +700,9 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Te
     """specvocab_sample: one token per row from the random numbers u [rows]; temperature, top_p, min_p float32 [rows], top_k int32
     [rows], each or None.  idx: the token ids of the places, [n] or [rows x n].
     Returns (tok [rows] int32, prob [rows] float32)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return sample(logits, u, temperature, top_k, top_p, min_p, idx, tok_out, prob_out, ws)
     here = torch.cuda.current_device()
     rows, n, ld = _rows(logits, "logits", here)
     if logits.dtype != torch.float32:
@@ -703,7 +716,7 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Te
     tok_out, prob_out = _drawn(rows, logits, tok_out, prob_out, here)
     ws, wp, wn = _scratch(workspace_bytes(SV_OP_SAMPLE, rows, 0, 0, n, 0, 0, SV_F32), logits, ws, here)
     _check(load_library().specvocab_sample(logits.data_ptr(), ld, rows, n, ip, mode, *settings, tok_out.data_ptr(),
-                                           prob_out.data_ptr(), wp, wn, _raw_stream(stream, here)), "specvocab_sample")
+                                           prob_out.data_ptr(), wp, wn, _current_raw_stream(here)), "specvocab_sample")
     return tok_out, prob_out
 
 
@@ -715,6 +728,9 @@ def quantized_sample_step(h: Union[torch.Tensor, QuantizedRows], U: QuantizedRow
                           ws: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None, padded: bool = False):
     """specvocab_quantized_sample_step: logits over idx (None: the whole vocabulary) with U in 8 bits, then a token per row.
     Returns (logits, tok, prob)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return quantized_sample_step(h, U, u, idx, temperature, top_k, top_p, min_p, logits_out, tok_out, prob_out, ws, padded=padded)
     here = torch.cuda.current_device()
     args, rows, d, V, dt = _head_operands(h, U, here)
     ip, mode, k = (None, SV_IDX_PER_ROW, 0) if idx is None else _list(idx, rows, padded, here)
@@ -723,5 +739,5 @@ def quantized_sample_step(h: Union[torch.Tensor, QuantizedRows], U: QuantizedRow
     tok_out, prob_out = _drawn(rows, U.q, tok_out, prob_out, here)
     ws, wp, wn = _scratch(workspace_bytes(SV_OP_QUANTIZED_SAMPLE_STEP, rows, d, V, k, 0, 0, dt, mode), U.q, ws, here)
     _check(load_library().specvocab_quantized_sample_step(*args, ip, k, mode, *settings, op, tok_out.data_ptr(), prob_out.data_ptr(),
-                                                          wp, wn, _raw_stream(stream, here)), "specvocab_quantized_sample_step")
+                                                          wp, wn, _current_raw_stream(here)), "specvocab_quantized_sample_step")
     return logits_out, tok_out, prob_out

@@ -213,6 +213,33 @@ def test_the_same_in_every_run_and_in_a_graph():
         torch.cuda.synchronize()
 
 
+def test_a_stream_that_is_still_busy_owns_what_a_call_makes():
+    """The workspace and the outputs of a call on another stream are not handed out again before that stream is done with them."""
+    rng = np.random.default_rng(3)
+    n = 60000
+    z = language_like(rng, 12, n).to(DEV)
+    s = settings(rng, 12)
+    dev = [torch.as_tensor(s[x], dtype=torch.int32 if x == "k" else torch.float32).to(DEV) for x in ("u", "t", "k", "p", "m")]
+    U = sv.quantize_rows(torch.randn((3000, 1024), device=DEV, dtype=torch.bfloat16))
+    h = sv.quantize_rows(torch.randn((80, 1024), device=DEV, dtype=torch.bfloat16))
+    want, want_z = sv.sample(z, *dev), sv.quantized_dense_logits(h, U)
+    nbytes = [sv.workspace_bytes(sv.SV_OP_SAMPLE, 12, k=n), sv.workspace_bytes(sv.SV_OP_QUANTIZED_DENSE_LOGITS, 80, 1024, 3000, dt=sv.SV_E4M3)]
+    big = torch.randn((4096, 4096), device=DEV, dtype=torch.bfloat16)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            for _ in range(40):                                # some milliseconds
+                big @ big
+        got = sv.sample(z, *dev, stream=side)
+        got_z = sv.quantized_dense_logits(h, U, stream=side)
+        for b in nbytes + [12 * 4, 80 * 3000 * 4]:              # memory of those sizes, written at once on this stream
+            for _ in range(3):
+                torch.empty(b, dtype=torch.uint8, device=DEV).fill_(255)
+        side.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and torch.equal(got_z, want_z)
+
+
 def test_draws_follow_the_distribution():
     """65000 draws from five tokens: counts of a multinomial, each within six standard deviations (1 in 5e8 for a right sampler)."""
     p = np.array([0.4, 0.3, 0.2, 0.06, 0.04])
