@@ -213,6 +213,23 @@ def test_the_same_in_every_run_and_in_a_graph():
         torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("rows, n", [(1, 49152), (3, 49155), (64, 60001), (7, 151936)])
+def test_nothing_beside_the_workspace_and_the_outputs_is_written(rows, n):
+    rng = np.random.default_rng(rows)
+    full = torch.full((rows, n + 64), 5.0, device=DEV)
+    z = full[:, 32:32 + n]
+    z.copy_(language_like(rng, rows, n))
+    before = full.clone()
+    size = sv.workspace_bytes(sv.SV_OP_SAMPLE, rows, k=n)
+    ws = torch.full((256 + size + 256,), 0x5A, dtype=torch.uint8, device=DEV)
+    tok, prob = torch.full((rows + 8,), -7, dtype=torch.int32, device=DEV), torch.full((rows + 8,), -7.0, device=DEV)
+    s = settings(rng, rows)
+    dev = [torch.as_tensor(s[x], dtype=torch.int32 if x == "k" else torch.float32).to(DEV) for x in ("u", "t", "k", "p", "m")]
+    sv.sample(z, *dev, tok_out=tok[:rows], prob_out=prob[:rows], ws=ws[256:256 + size])
+    assert torch.equal(full, before) and (ws[:256] == 0x5A).all() and (ws[256 + size:] == 0x5A).all()
+    assert (tok[rows:] == -7).all() and (prob[rows:] == -7).all() and (tok[:rows] >= 0).all()
+
+
 def test_a_stream_that_is_still_busy_owns_what_a_call_makes():
     """The workspace and the outputs of a call on another stream are not handed out again before that stream is done with them."""
     rng = np.random.default_rng(3)
