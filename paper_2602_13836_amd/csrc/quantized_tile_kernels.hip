@@ -12,7 +12,7 @@
 //
 // Two main loops, as in the bfloat16 kernels: the ring for up to 64 hidden rows, where the one pass over U bounds the product, and the
 // loop of wavefronts that take turns for more, where the matrix cores do.  Measured, 4096 elements: 32 hidden rows by 65536 tokens 48 us
-// (5.6 TB/s), 64 by 65536 49, 64 by 128256 112 (4.7 TB/s: LDS reads and the multiplication take turns), 512 by 151936 560 (1.14 PFLOP/s; a
+// (5.6 TB/s), 64 by 65536 49, 64 by 128256 112 (4.7 TB/s), 512 by 151936 560 (1.14 PFLOP/s; a
 // library product of the same sizes in bfloat16, U twice as large, 698).  Sources are named by 32-bit offsets where these reach, else
 // (FAR) by addresses.
 #include "quantized_rows.h"

@@ -18,7 +18,7 @@
 // into a bin all the same (thousands of equal logits, or clusters far apart) takes the slow form: the same borders by digits of the
 // logits' keys, eight bits per pass over the row.
 //
-// What bounds it: a logit takes some 25 instructions, half of them on 64 bits, to be counted, ten times what its four bytes take from
+// What bounds it: a logit takes some 30 instructions, half of them on 64 bits, to be counted, ten times what its four bytes take from
 // memory; then a chain of steps that each need the one before, some 10 us of barriers and LDS round trips a row.  Measured, with settings
 // of every kind: 1 x 8192 logits 5 us (11 with the host's part), 1 x 128256 23, 60 x 128256 52, 512 x 151936 135 (2.3 TB/s).
 #include "sv_device.h"
