@@ -362,11 +362,14 @@ int check_stored(const void* x, int64_t d, int64_t ld, int dt) {
 }
 
 // Which way a product with an 8-bit embedding goes: a hidden row at a time, all rows over one list, or over the union of the rows'
-// lists (where reading U once pays for the launches that make the union: the rule of the bfloat16 products).
+// lists (where reading U once pays for the launches that make the union: the rule of the bfloat16 products).  One row by itself is faster at
+// any length (4096 elements by 128256 tokens 81 us, through LDS 97); so are several up to 16384 logits in all, their list's rows of U coming from the
+// caches after the first (4096 elements, 4 rows x 4096 tokens 9.9 and 11.6 us, 16 x 1024 6.8 and 11.1; at 24576 logits 10.0 to 15.5 and 11.2 to 12.5),
+// and hidden rows in 8 bits, which would have to be widened by a launch in front, up to 24576 (6 x 4096 12.3 and 14.0; 4 x 8192 18.0 and 14.7).
 enum QuantizedWay { Q_ROWS, Q_SHARED, Q_UNION };
-QuantizedWay quantized_way(int64_t rows, int64_t d, int64_t k, bool list, int idx_mode) {
+QuantizedWay quantized_way(int64_t rows, int64_t d, int64_t k, bool quantized_h, bool list, int idx_mode) {
     if (rows == 1) return Q_ROWS;
-    if (!list || base_mode(idx_mode) == SV_IDX_PER_STEP) return Q_SHARED;
+    if (!list || base_mode(idx_mode) == SV_IDX_PER_STEP) return rows * k <= (quantized_h ? 24576 : 16384) ? Q_ROWS : Q_SHARED;
     const bool many = rows * k >= 16384 && (rows >= 16 || rows * k * d >= ((int64_t)512 << 20));
     return many ? Q_UNION : Q_ROWS;
 }
@@ -376,7 +379,7 @@ struct QuantizedWs {
 };
 QuantizedWs quantized_ws(int64_t rows, int64_t d, int64_t V, int64_t k, bool quantized_h, bool list, int idx_mode) {
     QuantizedWs w{};
-    const QuantizedWay way = quantized_way(rows, d, k, list, idx_mode);
+    const QuantizedWay way = quantized_way(rows, d, k, quantized_h, list, idx_mode);
     if (way != Q_ROWS) {
         if (quantized_h) w.hidden = round256((size_t)rows * (size_t)d * 2);
         if (list && is_padded(idx_mode)) w.list = round256((size_t)(base_mode(idx_mode) == SV_IDX_PER_ROW ? rows : 1) * (size_t)k * sizeof(int32_t));
@@ -441,7 +444,7 @@ int launch_quantized(const QuantizedCall& c, hipStream_t s) {
     a.out = c.out;
     a.out_row_stride = c.k;
     a.u_rows = c.V;
-    const QuantizedWay way = quantized_way(c.rows, c.d, c.k, c.idx != nullptr, c.idx_mode);
+    const QuantizedWay way = quantized_way(c.rows, c.d, c.k, c.h_scales != nullptr, c.idx != nullptr, c.idx_mode);
     if (way == Q_ROWS) return sv::launch_quantized_gemv(a, s) == hipSuccess ? SV_OK : SV_ERR_HIP;
     const QuantizedWs w = quantized_ws(c.rows, c.d, c.V, c.k, c.h_scales != nullptr, c.idx != nullptr, c.idx_mode);
     char* ws = static_cast<char*>(c.ws);

@@ -533,6 +533,8 @@ hipError_t launch_quantized_tile(const QuantizedArgs& a, hipStream_t stream) {
     const hipError_t e = device_info(&di);
     if (e != hipSuccess) return e;
     if (a.rows <= 64) {
+        // The narrowest tiles that fill no more than a round.  4096 elements, 48 hidden rows: 8192 items 16.4 us in tiles of 32, 18.5 of 64, 23.7 of 128; 16384
+        // 29.3, 19.6, 23.9 and (256) 24.5; 32768 54.6, 35.9, 28.6 and 29.2; 40000 67.9, 51.5, 48.1 and 33.7.
         const int64_t cus = di.cus;
         if (a.n_items <= 32 * cus) return launch_ring<32>(a, 0, stream);
         if (a.n_items <= 64 * cus) return launch_ring<64>(a, 0, stream);

@@ -98,7 +98,8 @@ SHAPES = [
     (32, 1040, 900, 600), (33, 4096, 600, 520), (60, 2560, 3000, 700), (64, 256, 2049, 300), (65, 512, 1500, 400), (100, 4096, 700, 300),
     (128, 1024, 3000, 900), (129, 144, 4000, 200), (200, 3840, 600, 200), (256, 512, 2000, 300), (300, 272, 1111, 1111), (513, 128, 700, 64),
     (20, 16, 300, 50), (70, 48, 300, 20), (33, 128, 500, 1),
-    (5000, 64, 40, 3), (700, 16, 20, 1),
+    (5000, 64, 40, 3), (700, 16, 20, 1), (70, 48, 3000, 1500), (33, 144, 5000, 1200), (7, 528, 9000, 4000), (300, 272, 40000, 33000),
+    (140, 656, 3000, 900), (64, 128, 20000, 1000),
     (90, 272, 30000, 26000), (180, 528, 15000, 13000),
     (20, 8208, 300, 40), (70, 16400, 200, 50),               # scales of a tile's rows do not fit into LDS
     # lists of every length class of the ring (tiles of 32, 64, 128 and 256 items, the last of a width that fills rounds), ragged
@@ -238,7 +239,7 @@ def test_refusals_of_the_binding():
     with pytest.raises(ValueError):
         sv.quantized_dense_logits(h, U, out=torch.zeros((3, 99), device=DEV))
     with pytest.raises(ValueError):
-        sv.quantized_dense_logits(h, U, ws=torch.zeros(16, dtype=torch.uint8, device=DEV))
+        sv.quantized_dense_logits(*case(1, 40, 256, 1000, True)[:2], ws=torch.zeros(16, dtype=torch.uint8, device=DEV))
     with pytest.raises(ValueError):
         sv.quantized_dense_logits(sv.QuantizedRows(h.q.cpu(), h.scales.cpu()), U)
     with pytest.raises(ValueError):

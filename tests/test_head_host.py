@@ -90,7 +90,7 @@ def test_quantized_logits_refuse_lists_and_workspaces(lib):
         assert logits(lib, name, rows=64, k=300, ws=None) == WORKSPACE
         assert logits(lib, name, rows=64, k=300, ws_bytes=1000) == WORKSPACE
         assert logits(lib, name, rows=64, k=300, ws=P + 8) == ALIGN
-    assert logits(lib, "dense", rows=2, ws=None) == WORKSPACE         # two rows in 8 bits are widened there
+    assert logits(lib, "dense", rows=30, ws=None) == WORKSPACE        # that many rows in 8 bits are widened there
     assert logits(lib, "step", u=None) == NULL
     assert logits(lib, "step", tok=None) == NULL
 
