@@ -335,8 +335,8 @@ int specvocab_quantized_subset_logits(const void* h, const uint8_t* h_scales, in
                                       float* logits_out, void* ws, size_t ws_bytes, void* stream);
 
 /* One token per row, drawn with a given random number u[r] in [0, 1) (smaller ones count as 0, larger ones and 1 as the
- * largest float below 1).  logits: device [rows x n] float32, row stride ld (any alignment).  With T = temperature[r] and the row's places ordered by
- * descending logit, equal logits by place (for ascending lists: by token id), w = exp((logit - largest) / T):
+ * largest float below 1).  logits: device [rows x n] float32, row stride ld (any alignment).  With T = temperature[r] and the
+ * row's places ordered by descending logit, equal logits by place (for ascending lists: by token id), w = exp((logit - largest) / T):
  *   1. top_k[r] > 0:  the first top_k[r] places stay;
  *   2. top_p[r] < 1:  of those, the ones stay that have less than top_p[r] of their mass in front of them (always the first);
  *   3. min_p[r] > 0:  of those, the ones with w >= min_p[r] stay (above 1 counts as 1);
@@ -348,9 +348,8 @@ int specvocab_quantized_subset_logits(const void* h, const uint8_t* h_scales, in
  * tok_out: device [rows] int32, the place, or idx(r, place) where idx (as in specvocab_subset_logits, padding slots having a logit of
  * -inf) is not NULL; -1 for a row that is masked throughout.  prob_out: device [rows] float32, w over the sum in 4 (0 for such
  * a row), or NULL.
- * Sums are kept to 2^-44 of each term (n up to 2^18; a bit less for each doubling of n), and do not depend on the run.  One launch; four (and
- * workspace) for up to 64 rows of 49152 logits or more.  A row in which more than 1024 places crowd into one
- * of the 4096 steps (1024 for short rows) that its range, or 64 octaves of w, is cut into, at a border or where the token is drawn --
+ * Sums are kept to 2^-44 of each term (n up to 2^18; a bit less for each doubling of n), and do not depend on the run.
+ * One launch; four (and workspace) for up to 64 rows of 49152 logits or more.  A row in which more than 1024 places crowd into one of the 4096 steps (1024 for short rows) that its range, or 64 octaves of w, is cut into, at a border or where the token is drawn --
  * thousands of equal logits, clusters far apart --, costs some tens of passes over the row. */
 int specvocab_sample(const float* logits, int64_t ld, int64_t rows, int64_t n, const int32_t* idx, int idx_mode,
                      const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
