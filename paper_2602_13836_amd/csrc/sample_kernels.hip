@@ -839,7 +839,8 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t r, const
                 if (round == 1) break;
                 const float2 x = block_range<NT / 64>(w.sums, 1, top, low);
                 if (!is_logit(x.x)) return put_token(a, r, -1, 0.0);
-                if (x.x <= s.edge && x.y >= s.low) {
+                // (a largest logit below the floor: nothing was counted, and x.y says nothing)
+                if (x.x <= s.edge && x.x >= s.floor && x.y >= s.low) {
                     s.top = x.x;
                     s.top64 = (double)x.x;
                     break;
