@@ -234,14 +234,35 @@ __global__ __launch_bounds__(256) void quantized_skinny_kernel(const QuantizedAr
     }
 }
 
+// The product in launches of `most` items each.  A launch has less than 2^32 threads in a direction: the runtime takes more without an error
+// and runs what the low 32 bits say.
+template <class F>
+hipError_t in_parts(const QuantizedArgs& a, int64_t most, F launch) {
+    for (int64_t first = 0; first < a.n_items; first += most) {
+        QuantizedArgs b = a;
+        b.n_items = a.n_items - first < most ? a.n_items - first : most;
+        b.out += first;
+        if (a.idx) {
+            b.idx += first;
+        } else {
+            b.U += first * a.ldu;
+            b.u_scales += first * a.ldus;
+            b.u_rows -= first;
+        }
+        const hipError_t e = launch(b);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 template <bool H8>
 hipError_t gemv(const QuantizedArgs& a, hipStream_t stream) {
     const int nl = (a.units + 63) / 64;
     auto go = [&](auto kernel, int per) {
-        const int64_t bx = (a.n_items + per - 1) / per;
-        if (bx > 0x7fffffffLL) return hipErrorInvalidValue;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)bx, (unsigned)a.rows), dim3(256), 0, stream, a);
-        return hipGetLastError();
+        return in_parts(a, (int64_t)per << 23, [&](const QuantizedArgs& b) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((b.n_items + per - 1) / per), (unsigned)b.rows), dim3(256), 0, stream, b);
+            return hipGetLastError();
+        });
     };
     switch (nl) {
         case 1: return go(&quantized_gemv_kernel<1, 4, H8>, 16);
@@ -272,9 +293,12 @@ hipError_t launch_quantized_gemv(const QuantizedArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_quantized_product(const QuantizedArgs& a, hipStream_t stream) {
+    constexpr int64_t kMostItems = (int64_t)1 << 28;                 // (up to four threads each)
+    if (a.n_items > kMostItems && !a.n_items_dev)
+        return in_parts(a, kMostItems, [&](const QuantizedArgs& b) { return launch_quantized_product(b, stream); });
     if (quantized_tile_supported(a)) return launch_quantized_tile(a, stream);
     const int64_t bx = (a.n_items + 63) / 64;
-    if (bx > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (bx >= (int64_t)1 << 24) return hipErrorInvalidValue;
     for (int row0 = 0; row0 < a.rows; row0 += 64) {
         const int left = a.rows - row0;
         const dim3 grid((unsigned)bx), block(256);

@@ -479,7 +479,7 @@ hipError_t launch(K kernel_near, K kernel_far, const QuantizedArgs& a, int tm, i
     int64_t IT = (a.n_items + tn - 1) / tn;
     if (balance_cus > 0) IT = (IT + balance_cus - 1) / balance_cus * balance_cus;
     const int64_t bx = (IT + kXcds - 1) / kXcds * RT * kXcds;
-    if (bx > 0x7fffffffLL) return hipErrorInvalidValue;
+    if (bx * threads >= (int64_t)1 << 32) return hipErrorInvalidValue;      // (the runtime would take the low 32 bits)
     K kernel = near(a) ? kernel_near : kernel_far;
     if constexpr (std::is_same<K, void (*)(QuantizedArgs, int)>::value)
         hipLaunchKernelGGL(kernel, dim3((unsigned)bx), dim3(threads), lds, stream, a, balance_cus);

@@ -43,3 +43,40 @@ def test_masked_first_places_and_a_rest_far_below_zero(rows, n):
     check_rows(z, s, range(min(rows, 60)))
     z[:, :9000] = -np.inf
     check_rows(z, dict(s, k=np.zeros(rows), p=np.ones(rows), m=np.zeros(rows)), range(min(rows, 60)))
+
+
+def small_rows(rows, d, seed):
+    """QuantizedRows of small integers, scale 1, and the same in 64 bits: sums are exact in float32."""
+    v = torch.randint(-3, 4, (rows, d), generator=torch.Generator().manual_seed(seed)).float()
+    s = torch.full((rows, sv.scale_columns(d)), 127, dtype=torch.uint8).view(torch.float8_e8m0fnu)
+    return sv.QuantizedRows(v.to(torch.float8_e4m3fn).to(DEV), s.to(DEV)), v.double()
+
+
+def equal_by_parts(got, full, at, part=1 << 24):
+    for j in range(0, got.shape[1], part):
+        assert torch.equal(got[:, j:j + part], full[:, at[j:j + part].long()]), j
+
+
+def test_a_vocabulary_of_more_rows_than_a_launch_has_threads_for():
+    V, d, kinds = (1 << 28) + 37, 16, 1000
+    few, v64 = small_rows(kinds, d, 1)
+    h, h64 = small_rows(1, d, 2)
+    q = torch.empty((V, d), dtype=torch.uint8, device=DEV)
+    at = torch.arange(V, dtype=torch.int32, device=DEV) % kinds
+    for j in range(0, V, 1 << 24):
+        q[j:j + (1 << 24)] = few.q.view(torch.uint8)[at[j:j + (1 << 24)].long()]
+    scales = torch.full((V, 4), 127, dtype=torch.uint8, device=DEV)
+    U = sv.QuantizedRows(q.view(torch.float8_e4m3fn), scales.view(torch.float8_e8m0fnu))
+    equal_by_parts(sv.quantized_dense_logits(h, U), (h64 @ v64.t()).float().to(DEV), at)
+
+
+@pytest.mark.parametrize("rows, k, d", [(1, (1 << 26) + 5, 4112), (2, (1 << 30) + 5, 8208)])
+def test_lists_of_more_tokens_than_a_launch_has_threads_for(rows, k, d):
+    V = 100
+    U, u64 = small_rows(V, d, 3)
+    h, h64 = small_rows(rows, d, 4)
+    idx = torch.empty(k, dtype=torch.int32, device=DEV)
+    for j in range(0, k, 1 << 24):
+        idx[j:j + (1 << 24)] = (torch.arange(j, min(j + (1 << 24), k), device=DEV) * 7 % V).to(torch.int32)
+    idx[-1] = 99
+    equal_by_parts(sv.quantized_subset_logits(h, U, idx), (h64 @ u64.t()).float().to(DEV), idx)
