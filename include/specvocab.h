@@ -314,7 +314,7 @@ int specvocab_quantize_rows(const void* x, int64_t rows, int64_t d, int64_t ldx,
  * q_out.  The selector reads y (specvocab_select), the 8-bit head q.  weight: [d] in `dt`; weight_offset: 0, or 1 for models that store
  * the weight's distance from 1.  Sums are float32.  sum_out and y_out may be x or residual themselves (same base and stride), not
  * otherwise overlap them or each other.  d a multiple of 16; eps >= 0 and finite.  No workspace.  A row with an infinity or a NaN
- * in t gets NaN. */
+ * in t gets NaN throughout; finite rows whose squares are too large or too small for float32 are scaled on the way and get their norm. */
 int specvocab_rms_norm(const void* x, int64_t rows, int64_t d, int64_t ldx, const void* residual, int64_t ldr,
                        const void* weight, float weight_offset, float eps, int dt,
                        void* sum_out, int64_t ld_sum, void* y_out, int64_t ldy,

@@ -66,10 +66,32 @@ __device__ __forceinline__ float block_sum(float x, float* s_w) {
     return t;
 }
 
+__device__ __forceinline__ uint32_t block_max_u32(uint32_t x, uint32_t* s_w) {
+    x = row16_max_u32(x);
+#pragma unroll
+    for (int l = 0; l < 64; l += 16) x = umax32(x, (uint32_t)__builtin_amdgcn_readlane((int)x, l));
+    if ((threadIdx.x & 63) == 0) s_w[threadIdx.x >> 6] = x;
+    __syncthreads();
+    for (int w = 0; w < (int)(blockDim.x >> 6); ++w) x = umax32(x, s_w[w]);
+    return x;
+}
+
+// Squares of values beyond 2^64 are infinite in float32, and those of values below 2^-63 lose bits or are nothing, while the norm itself is
+// an ordinary number: such a row, known by its mean + eps, is brought near 1 by a power of two first, eps by its square, which
+// changes nothing in the result.  Rows with an infinity or a NaN in them come here too, and get NaN.
+__device__ __forceinline__ bool out_of_range(float mean) { return !(mean >= 0x1p-80f && mean <= 0x1p126f); }
+// that power of two, from the bits of the row's largest magnitude and from eps: 2^-126 .. 2^126
+__device__ __forceinline__ float toward_one(uint32_t most, float eps) {
+    const int of_t = (int)umax32(most >> 23, 1u) - 127;
+    const int of_eps = eps > 0.0f ? ((int)umax32(__float_as_uint(eps) >> 23, 1u) - 127) >> 1 : -126;
+    return __uint_as_float((uint32_t)(127 - min(max(of_t, of_eps), 126)) << 23);
+}
+
 template <int DT, int CH, bool LOOP>
 __global__ __launch_bounds__(1024) void rms_norm_kernel(const NormArgs a) {
     constexpr int kEs = DT == DT_BF16 ? 2 : 4;
-    __shared__ float s_w[16];
+    __shared__ float s_w[16], s_w2[16];
+    __shared__ uint32_t s_most[16];
     const int threads = (int)blockDim.x, tid = (int)threadIdx.x;
     const int64_t r = blockIdx.x;
     const int d = a.d;
@@ -90,6 +112,14 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(const NormArgs a) {
         }
         e.put(t);
     };
+    auto largest = [&](const Eight<DT>& e) {                         // bits of the largest magnitude
+        float t[8];
+        e.get(t);
+        uint32_t most = 0u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = umax32(most, __float_as_uint(t[i]) & 0x7FFFFFFFu);
+        return most;
+    };
     auto squares = [&](const float (&t)[8]) {
         float s = 0.f;
 #pragma unroll
@@ -97,11 +127,11 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(const NormArgs a) {
         return s;
     };
     // what leaves for the eight values at `at`; all lanes of a wavefront come here together
-    auto finish = [&](int at, float (&t)[8], const Eight<DT>& ew, float rstd) {
+    auto finish = [&](int at, float (&t)[8], const Eight<DT>& ew, float f, float rstd) {
         float w[8], y[8];
         ew.get(w);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = t[i] * rstd * (w[i] + a.offset);
+        for (int i = 0; i < 8; ++i) y[i] = t[i] * f * rstd * (w[i] + a.offset);     // (f: 1, but for rows out of range)
         if (at >= d) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) y[i] = 0.f;
@@ -128,7 +158,7 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(const NormArgs a) {
         }
 #pragma unroll
         for (int c = 0; c < CH; ++c) ew[c].load(a.weight + (int64_t)min((c * threads + tid) * 8, d - 8) * kEs);
-        float s = 0.f;
+        float s = 0.f, f = 1.0f;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int at = (c * threads + tid) * 8;
@@ -140,28 +170,65 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(const NormArgs a) {
             if (a.sum && at < d) e.store(a.sum + r * a.sum_row_bytes + (int64_t)at * kEs);
         }
         s = block_sum(s, s_w);
-        const float rstd = 1.0f / sqrtf(s / (float)d + a.eps);
+        float mean = s / (float)d + a.eps;
+        if (out_of_range(mean)) {                                    // (uniform)
+            uint32_t most = 0u;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) most = umax32(most, largest(ex[c]));
+            most = block_max_u32(most, s_most);
+            f = toward_one(most, a.eps);
+            s = 0.f;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                float t[8];
+                ex[c].get(t);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t[i] *= f;
+                s += squares(t);
+            }
+            s = block_sum(s, s_w2);
+            mean = most >= 0x7F800000u ? __builtin_nanf("") : s / (float)d + a.eps * f * f;
+        }
+        const float rstd = 1.0f / sqrtf(mean);
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             if ((c * threads + (tid & ~63)) * 8 >= d) break;         // (uniform over the wavefront)
             float t[8];
             ex[c].get(t);
-            finish((c * threads + tid) * 8, t, ew[c], rstd);
+            finish((c * threads + tid) * 8, t, ew[c], f, rstd);
         }
     } else {
         const int pieces = (d / 8 + threads - 1) / threads;
-        float s = 0.f;
-        for (int c = 0; c < pieces; ++c) {
-            const int at = (c * threads + tid) * 8, from = min(at, d - 8);
-            Eight<DT> ex, er, e;
-            ex.load(x + (int64_t)from * kEs);
-            if (res) er.load(res + (int64_t)from * kEs);
-            float t[8];
-            sum_of(at, ex, er, e, t);
-            s += squares(t);
-        }
+        auto each = [&](auto f) {                                    // f(the sum as it is stored)
+            for (int c = 0; c < pieces; ++c) {
+                const int at = (c * threads + tid) * 8, from = min(at, d - 8);
+                Eight<DT> ex, er, e;
+                ex.load(x + (int64_t)from * kEs);
+                if (res) er.load(res + (int64_t)from * kEs);
+                float t[8];
+                sum_of(at, ex, er, e, t);
+                f(e, t);
+            }
+        };
+        float s = 0.f, f = 1.0f;
+        each([&](const Eight<DT>&, float (&t)[8]) { s += squares(t); });
         s = block_sum(s, s_w);
-        const float rstd = 1.0f / sqrtf(s / (float)d + a.eps);
+        float mean = s / (float)d + a.eps;
+        if (out_of_range(mean)) {
+            uint32_t most = 0u;
+            each([&](const Eight<DT>& e, float (&)[8]) { most = umax32(most, largest(e)); });
+            most = block_max_u32(most, s_most);
+            f = toward_one(most, a.eps);
+            s = 0.f;
+            each([&](const Eight<DT>&, float (&t)[8]) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t[i] *= f;
+                s += squares(t);
+            });
+            s = block_sum(s, s_w2);
+            mean = most >= 0x7F800000u ? __builtin_nanf("") : s / (float)d + a.eps * f * f;
+        }
+        const float rstd = 1.0f / sqrtf(mean);
         __syncthreads();                                             // everybody has read: outputs may lie over inputs
         for (int c = 0; c < pieces; ++c) {
             const int at = (c * threads + tid) * 8, from = min(at, d - 8);
@@ -173,7 +240,7 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(const NormArgs a) {
             float t[8];
             sum_of(at, ex, er, e, t);
             if (a.sum && at < d) e.store(a.sum + r * a.sum_row_bytes + (int64_t)at * kEs);
-            finish(at, t, ew, rstd);
+            finish(at, t, ew, f, rstd);
         }
     }
 }

@@ -1,4 +1,6 @@
 """Norm, products and sampling where a value, a range or a size is at its edge."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -43,6 +45,53 @@ def test_masked_first_places_and_a_rest_far_below_zero(rows, n):
     check_rows(z, s, range(min(rows, 60)))
     z[:, :9000] = -np.inf
     check_rows(z, dict(s, k=np.zeros(rows), p=np.ones(rows), m=np.zeros(rows)), range(min(rows, 60)))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [16, 256, 4096, 16400, 40000])
+@pytest.mark.parametrize("residual", [False, True])
+def test_a_norm_of_an_infinity_or_nan_is_nan_throughout(dtype, d, residual):
+    x = torch.randn((6, d), generator=torch.Generator().manual_seed(d)).to(dtype)
+    x[1, d - 1], x[2, 3], x[3, d // 2], x[4, 0] = math.inf, -math.inf, math.nan, math.inf
+    x[4, 1] = -math.inf
+    w = torch.ones(d, dtype=dtype, device=DEV)
+    res = torch.zeros_like(x).to(DEV) if residual else None
+    y, t, q = sv.rms_norm(x.to(DEV), w, 1e-5, residual=res, want_quantized=True)
+    assert y[1:5].isnan().all() and not y[0].isnan().any() and not y[5].isnan().any()
+    blocks = (d + 127) // 128
+    scales = q.scales.view(torch.uint8)
+    assert (scales[1:5, :blocks] == 255).all() and (scales[1:5, blocks:] == 127).all()
+    assert ((q.q.view(torch.uint8)[1:5] & 127) == 127).all() and (scales[[0, 5], :blocks] != 255).all()
+    assert torch.equal(t.cpu().nan_to_num(nan=7.0), x.nan_to_num(nan=7.0))
+    alone = sv.rms_norm(x[:1].to(DEV), w, 1e-5)[0]
+    assert torch.equal(y[:1], alone)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [16, 272, 4096, 16400, 40000])
+@pytest.mark.parametrize("eps", [0.0, 1e-5, 1e-37, 1e38])
+def test_a_norm_whose_squares_leave_the_range_of_float32(dtype, d, eps):
+    """Values whose squares are too large or too small for float32; the norm itself is an ordinary number."""
+    rng = np.random.default_rng(d)
+    base = torch.from_numpy(rng.standard_normal(d))
+    largest = torch.finfo(dtype).max
+    x = torch.stack([(base * s).clamp(-largest, largest).to(dtype) for s in (1e19, 1e30, 1e38, 1e-19, 1e-25, 1e-36, 1.0)] +
+                    [torch.full((d,), largest, dtype=dtype), torch.full((d,), -torch.finfo(dtype).tiny, dtype=dtype)])
+    x[5, 1::2] = 0.0
+    w = torch.from_numpy(rng.standard_normal(d)).to(dtype)
+    y, t, q = sv.rms_norm(x.to(DEV), w.to(DEV), eps, residual=torch.zeros_like(x).to(DEV), want_quantized=True)
+    assert torch.equal(t.cpu(), x)
+    t64 = x.double().numpy()
+    ref = t64 / np.sqrt((t64 * t64).mean(axis=1, keepdims=True) + float(np.float32(eps))) * w.double().numpy()
+    # the steps counted at test_rms_norm, and two more for eps's factors; results below the smallest normal number are off by half a
+    # step of it, whatever they are multiplied with afterwards (|w| < 8)
+    chain = 8 * -(-d // 8192) if d > 8192 else 8 * 4
+    rel = (0.5 * (2 * chain + 22 + 4) + 6) * 2.0 ** -24
+    half = torch.finfo(dtype).eps / 2
+    err = np.abs(y.double().cpu().numpy() - ref)
+    assert (err <= np.abs(ref) * (rel + half * (1 + rel)) + 8 * torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps).all()
+    alone = sv.quantize_rows(y)
+    assert torch.equal(q.q.view(torch.uint8), alone.q.view(torch.uint8)) and torch.equal(q.scales.view(torch.uint8), alone.scales.view(torch.uint8))
 
 
 def small_rows(rows, d, seed):
