@@ -629,7 +629,37 @@ __device__ __forceinline__ void put_token(const SampleArgs& a, int64_t r, int64_
     a.tok_out[r] = place < 0 ? -1 : a.idx ? a.idx[r * a.idx_row_stride + place] : (int32_t)place;
     if (a.prob_out) a.prob_out[r] = (float)prob;
 }
-// ---- the slow form: borders as (key, how many of the places with that key), found digit by digit, from the row in memory
+// ---- the slow form: borders as (key, how many of the places with that key), found digit by digit, from the row in memory.
+// A digit's places may weigh anything between 2^-88 and 1, so its mass is an integer in units of 2^-131, exact for weights from 2^-79 on, to 2^-44
+// of the term below; four parts of 33 bits, of which a weight's 53 bits touch at most three, each added up in 64 bits by itself (n < 2^31).
+// (One part of 64 bits, 2^-44 of the largest weight, would lose crowds of far places, and save up to a fifth: 60 x 128256 logits in two
+// crowds 1960 us instead of 2360, four values 2520 instead of 2880, all equal 2370 instead of 2410.)
+constexpr int kPartBits = 33, kMassParts = 4;
+struct WeightParts {
+    unsigned long long v[3];
+    int first;           // the part that v[0] goes to
+};
+__device__ __forceinline__ WeightParts parts_of_weight(double weight) {
+    const unsigned long long bits = (unsigned long long)__double_as_longlong(weight), one = 1ull, mask = (one << kPartBits) - one;
+    unsigned long long m = (bits & ((one << 52) - one)) | one << 52;
+    int shift = (int)(bits >> 52) - 1023 - 52 + 131;                 // weight = m 2^(shift - 131)
+    if (shift < 0) {
+        const int off = min(-shift, 63);
+        m = (m + (one << (off - 1))) >> off;
+        shift = 0;
+    }
+    WeightParts p;
+    p.first = shift / kPartBits;
+    const int off = shift - p.first * kPartBits;
+    p.v[0] = m << off & mask;
+    m >>= kPartBits - off;
+    p.v[1] = m & mask;
+    p.v[2] = m >> kPartBits;                                         // (zero where there is no such part: a weight is at most 1)
+    return p;
+}
+__device__ __forceinline__ double mass_of_parts(const unsigned long long* v) {
+    return (double)v[0] * 0x1p-131 + (double)v[1] * 0x1p-98 + (double)v[2] * 0x1p-65 + (double)v[3] * 0x1p-32;
+}
 template <int NT, int BINS>
 struct SlowSampler {
     using Work = RowWork<NT, BINS>;
@@ -643,16 +673,17 @@ struct SlowSampler {
         uint32_t key, ties, places_above;
         double above;                    // mass of the places with larger keys
     };
-    __device__ double units_of(float v, double unit) const { return floor(weight_of(s, v) * unit + 0.5); }
+    static_assert(BINS >= 256 * kMassParts, "a digit's mass");
+    __device__ double weight_of_key(uint32_t key) const { return weight_of(s, ord_to_f32(key)); }
     // by rank (the place with `rank` places in front of it) or by mass (the last key with less than, or `reached`: no more
     // than, `goal` in front of it), among the keys from `least` on
-    __device__ __noinline__ Edge descend(bool by_rank, uint32_t rank, double goal, bool reached, uint32_t least, double unit) {
+    __device__ __noinline__ Edge descend(bool by_rank, uint32_t rank, double goal, bool reached, uint32_t least) {
         Edge e{0u, 0u, 0u, 0.0};
         for (int shift = 24; shift >= 0; shift -= 8) {
             __syncthreads();
-            for (int i = threadIdx.x; i < 256; i += NT) {
+            for (int i = threadIdx.x; i < 256 * kMassParts; i += NT) {
                 w.mass[i] = 0ull;
-                w.cnt[i] = 0u;
+                if (i < 256) w.cnt[i] = 0u;
             }
             __syncthreads();
             for_quads<NT, 2>(z, 0, n, [&](const f32x4_t& q, int64_t) {
@@ -662,22 +693,24 @@ struct SlowSampler {
                 if (!(v >= s.floor)) continue;
                 const uint32_t key = f32_to_ord(v);
                 if (key < least || (shift < 24 && key >> (shift + 8) != e.key)) continue;
-                unsigned long long m = (unsigned long long)units_of(v, unit);
+                const WeightParts m = parts_of_weight(weight_of(s, v));
                 uint32_t one = 1u;
                 const uint64_t active = __builtin_amdgcn_ballot_w64(true);
                 if (__builtin_amdgcn_ballot_w64(key == (uint32_t)__builtin_amdgcn_readfirstlane((int)key)) == active) {
                     one = (uint32_t)__popcll(active);
-                    m *= one;
                     if ((threadIdx.x & 63) != (unsigned)__ffsll((unsigned long long)active) - 1u) continue;
                 }
-                atomicAdd(&w.mass[key >> shift & 255u], m);
-                atomicAdd(&w.cnt[key >> shift & 255u], one);
+                const uint32_t digit = key >> shift & 255u;
+#pragma unroll
+                for (int j = 0; j < 3; ++j)
+                    if (m.v[j]) atomicAdd(&w.mass[digit * kMassParts + m.first + j], m.v[j] * one);
+                atomicAdd(&w.cnt[digit], one);
               }
             });
             __syncthreads();
             const int digit = 255 - (int)threadIdx.x;
             const uint32_t c = digit >= 0 ? w.cnt[digit] : 0u;
-            const double m = digit >= 0 ? (double)w.mass[digit] / unit : 0.0;
+            const double m = digit >= 0 ? mass_of_parts(&w.mass[digit * kMassParts]) : 0.0;
             double in, msum;
             uint32_t cin, csum;
             block_scan<Work::kWaves>(w.sums, (shift >> 3) & 1, m, c, &in, &cin, &msum, &csum);
@@ -699,12 +732,12 @@ struct SlowSampler {
                 at = w.found[0];
             }
             if ((int)threadIdx.x == at) {
-                w.mass[256] = (unsigned long long)__double_as_longlong(in);
+                w.bin[0] = (unsigned long long)__double_as_longlong(in);
                 w.found[1] = (int)cin;
                 w.found[2] = (int)c;
             }
             __syncthreads();
-            e.above = __longlong_as_double((long long)w.mass[256]);
+            e.above = __longlong_as_double((long long)w.bin[0]);
             e.places_above = (uint32_t)w.found[1];
             e.ties = (uint32_t)w.found[2];
             e.key = e.key << 8 | (uint32_t)(255 - at);
@@ -712,7 +745,6 @@ struct SlowSampler {
         return e;
     }
     __device__ void draw(uint32_t k, double p, double m, double u, Drawn* out) {
-        const double unit = ldexp(1.0, mass_bits(n));
         uint32_t edge = 0u, take = 0u;          // kept: keys above `edge`, and `take` of its own
         auto shorten = [&](uint32_t key, uint32_t t) {
             if (key > edge || (key == edge && t < take)) {
@@ -722,36 +754,38 @@ struct SlowSampler {
         };
         double kept = total;
         if (k > 0u && k < all) {
-            const Edge e = descend(true, k - 1u, 0.0, false, 0u, unit);
+            const Edge e = descend(true, k - 1u, 0.0, false, 0u);
             shorten(e.key, k - e.places_above);
-            kept = e.above + (k - e.places_above) * (units_of(ord_to_f32(e.key), unit) / unit);
+            kept = e.above + (k - e.places_above) * weight_of_key(e.key);
         }
         if (p < 1.0) {
             const double goal = p * kept;
-            const Edge e = descend(false, 0u, goal, false, 0u, unit);
-            const double each = units_of(ord_to_f32(e.key), unit) / unit;
-            const double t = each > 0.0 ? ceil((goal - e.above) / each) : 1.0;
+            const Edge e = descend(false, 0u, goal, false, 0u);
+            const double t = ceil((goal - e.above) / weight_of_key(e.key));
             shorten(e.key, (uint32_t)fmin(fmax(t, 1.0), (double)e.ties));
         }
         if (m > 0.0) shorten(least_key(s, fmin(m, 1.0)) - 1u, 0u);
         // what is kept
-        unsigned long long sum = 0ull;
+        unsigned long long sum[kMassParts] = {0ull, 0ull, 0ull, 0ull};
         for_quads<NT, 2>(z, 0, n, [&](const f32x4_t& q, int64_t) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (q[i] >= s.floor && f32_to_ord(q[i]) > edge) sum += (unsigned long long)units_of(q[i], unit);
+            for (int i = 0; i < 4; ++i) {
+                if (!(q[i] >= s.floor && f32_to_ord(q[i]) > edge)) continue;
+                const WeightParts x = parts_of_weight(weight_of(s, q[i]));
+#pragma unroll
+                for (int l = 0; l < kMassParts; ++l) sum[l] += l == x.first ? x.v[0] : l == x.first + 1 ? x.v[1] : l == x.first + 2 ? x.v[2] : 0ull;
+            }
         });
         __syncthreads();
-        if (threadIdx.x == 0) w.mass[0] = 0ull;
+        if (threadIdx.x < kMassParts) w.mass[threadIdx.x] = 0ull;
         __syncthreads();
-        atomicAdd(&w.mass[0], sum);                                  // (integers: in any order)
+#pragma unroll
+        for (int l = 0; l < kMassParts; ++l) atomicAdd(&w.mass[l], sum[l]);      // (integers: in any order)
         __syncthreads();
-        sum = w.mass[0];
-        kept = (double)sum / unit + (take ? take * (units_of(ord_to_f32(edge), unit) / unit) : 0.0);
+        kept = mass_of_parts(w.mass) + (take ? take * weight_of_key(edge) : 0.0);
         const double goal = u * kept;
-        const Edge e = descend(false, 0u, goal, true, take ? edge : edge + 1u, unit);
-        const double each = units_of(ord_to_f32(e.key), unit) / unit;
-        const double t = each > 0.0 ? floor((goal - e.above) / each) : 0.0;
+        const Edge e = descend(false, 0u, goal, true, take ? edge : edge + 1u);
+        const double t = floor((goal - e.above) / weight_of_key(e.key));
         const uint32_t most = e.key == edge ? min(take, e.ties) : e.ties;
         uint32_t j = (uint32_t)fmin(fmax(t, 0.0), (double)(most - 1u));
         // the j-th of the places with that key: every wavefront counts them in a part of the row, and one looks for it

@@ -1,5 +1,6 @@
 """Norm, products and sampling where a value, a range or a size is at its edge."""
 import math
+from fractions import Fraction
 
 import numpy as np
 import pytest
@@ -45,6 +46,31 @@ def test_masked_first_places_and_a_rest_far_below_zero(rows, n):
     check_rows(z, s, range(min(rows, 60)))
     z[:, :9000] = -np.inf
     check_rows(z, dict(s, k=np.zeros(rows), p=np.ones(rows), m=np.zeros(rows)), range(min(rows, 60)))
+
+
+@pytest.mark.parametrize("rows, n", [(1, 1 << 22), (66, 1 << 21)])
+@pytest.mark.parametrize("octaves", [39.4, 40.6, 42.0])
+def test_a_crowd_of_far_places_has_its_mass(rows, n, octaves):
+    """One place of mass 1 and millions of equal ones whose masses only together are something: against exact fractions."""
+    z = torch.full((rows, n), -octaves * math.log(2.0), device=DEV)
+    first = 1000
+    z[:, first] = 0.0
+    w = Fraction(math.exp(float(z[0, 0])))
+    most = Fraction(1) - Fraction(1, 1 << 24)
+    for p in (None, most):
+        u = [most] * rows if p is None else [Fraction(3, 4)] + [most] * (rows - 1)
+        tok, prob = drawn(z, [float(x) for x in u], p=None if p is None else [float(p)] * rows)
+        kept = 1 + (n - 1) * w
+        if p is not None:
+            count = max(math.ceil((p * kept - 1) / w), 0)
+            kept = 1 + count * w
+        for r in range(0, rows, 13):
+            j = math.floor((u[r] * kept - 1) / w) if u[r] * kept >= 1 else -1
+            place = first if j < 0 else (j if j < first else j + 1)
+            # w is right to 2^-46 (an exponent up to 64, rounded twice), the product u * kept to 2^-53: less than one of 2^22 places
+            assert abs(int(tok[r]) - place) <= 1, (r, p, int(tok[r]), place)
+            want = float((1 if j < 0 else w) / kept)
+            assert abs(prob[r] - want) <= want * (2.0 ** -24 + 2.0 ** -40), (r, p, prob[r], want)
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
