@@ -273,7 +273,7 @@ struct Drawn {
 
 struct SlowInput {
     RowSettings s;
-    double total, p, m, u;
+    double p, m, u;
     uint32_t all, k;
 };
 // What one workgroup needs for a row.
@@ -667,18 +667,18 @@ struct SlowSampler {
     const RowSettings s;
     const float* z;
     const int64_t n;
-    double total;
     uint32_t all;
     struct Edge {
         uint32_t key, ties, places_above;
         double above;                    // mass of the places with larger keys
+        double goal;                     // that was looked for
     };
     static_assert(BINS >= 256 * kMassParts, "a digit's mass");
     __device__ double weight_of_key(uint32_t key) const { return weight_of(s, ord_to_f32(key)); }
     // by rank (the place with `rank` places in front of it) or by mass (the last key with less than, or `reached`: no more
-    // than, `goal` in front of it), among the keys from `least` on
-    __device__ __noinline__ Edge descend(bool by_rank, uint32_t rank, double goal, bool reached, uint32_t least) {
-        Edge e{0u, 0u, 0u, 0.0};
+    // than, `goal` in front of it; share: than that part of all mass), among the keys from `least` on
+    __device__ __noinline__ Edge descend(bool by_rank, uint32_t rank, double goal, bool share, bool reached, uint32_t least) {
+        Edge e{0u, 0u, 0u, 0.0, 0.0};
         for (int shift = 24; shift >= 0; shift -= 8) {
             __syncthreads();
             for (int i = threadIdx.x; i < 256 * kMassParts; i += NT) {
@@ -714,6 +714,7 @@ struct SlowSampler {
             double in, msum;
             uint32_t cin, csum;
             block_scan<Work::kWaves>(w.sums, (shift >> 3) & 1, m, c, &in, &cin, &msum, &csum);
+            if (shift == 24 && share) goal *= msum;
             in += e.above;
             cin += e.places_above;
             __syncthreads();
@@ -742,6 +743,7 @@ struct SlowSampler {
             e.ties = (uint32_t)w.found[2];
             e.key = e.key << 8 | (uint32_t)(255 - at);
         }
+        e.goal = goal;
         return e;
     }
     __device__ void draw(uint32_t k, double p, double m, double u, Drawn* out) {
@@ -752,16 +754,16 @@ struct SlowSampler {
                 take = t;
             }
         };
-        double kept = total;
-        if (k > 0u && k < all) {
-            const Edge e = descend(true, k - 1u, 0.0, false, 0u);
+        double kept = 0.0;
+        const bool with_k = k > 0u && k < all;
+        if (with_k) {
+            const Edge e = descend(true, k - 1u, 0.0, false, false, 0u);
             shorten(e.key, k - e.places_above);
             kept = e.above + (k - e.places_above) * weight_of_key(e.key);
         }
         if (p < 1.0) {
-            const double goal = p * kept;
-            const Edge e = descend(false, 0u, goal, false, 0u);
-            const double t = ceil((goal - e.above) / weight_of_key(e.key));
+            const Edge e = descend(false, 0u, with_k ? p * kept : p, !with_k, false, 0u);
+            const double t = ceil((e.goal - e.above) / weight_of_key(e.key));
             shorten(e.key, (uint32_t)fmin(fmax(t, 1.0), (double)e.ties));
         }
         if (m > 0.0) shorten(least_key(s, fmin(m, 1.0)) - 1u, 0u);
@@ -784,7 +786,7 @@ struct SlowSampler {
         __syncthreads();
         kept = mass_of_parts(w.mass) + (take ? take * weight_of_key(edge) : 0.0);
         const double goal = u * kept;
-        const Edge e = descend(false, 0u, goal, true, take ? edge : edge + 1u);
+        const Edge e = descend(false, 0u, goal, false, true, take ? edge : edge + 1u);
         const double t = floor((goal - e.above) / weight_of_key(e.key));
         const uint32_t most = e.key == edge ? min(take, e.ties) : e.ties;
         uint32_t j = (uint32_t)fmin(fmax(t, 0.0), (double)(most - 1u));
@@ -827,7 +829,7 @@ struct SlowSampler {
 template <int NT, int BINS>
 __device__ __noinline__ void draw_slowly(RowWork<NT, BINS>& w, const float* z, int64_t n) {
     const SlowInput in = w.slow;
-    SlowSampler<NT, BINS> slow{w, in.s, z, n, in.total, in.all};
+    SlowSampler<NT, BINS> slow{w, in.s, z, n, in.all};
     Drawn d;
     slow.draw(in.k, in.p, in.m, in.u, &d);
     __syncthreads();
@@ -896,7 +898,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, int64_t r, const
     const bool drawn = row.draw(in.k, in.p, in.m, in.u, &d);
     if constexpr (Places::kLists == LISTS_PART) return;
     if (!drawn) {
-        if (threadIdx.x == 0) w.slow = SlowInput{s, row.total, in.p, in.m, in.u, row.all, in.k};
+        if (threadIdx.x == 0) w.slow = SlowInput{s, in.p, in.m, in.u, row.all, in.k};
         __syncthreads();
         draw_slowly<NT, BINS>(w, a.logits + r * a.ld, a.n);
         d = w.drawn;

@@ -50,16 +50,18 @@ def test_masked_first_places_and_a_rest_far_below_zero(rows, n):
 
 @pytest.mark.parametrize("rows, n", [(1, 1 << 22), (66, 1 << 21)])
 @pytest.mark.parametrize("octaves", [39.4, 40.6, 42.0])
-def test_a_crowd_of_far_places_has_its_mass(rows, n, octaves):
+@pytest.mark.parametrize("t", [1.0, 0.37, 1.7])
+def test_a_crowd_of_far_places_has_its_mass(rows, n, octaves, t):
     """One place of mass 1 and millions of equal ones whose masses only together are something: against exact fractions."""
-    z = torch.full((rows, n), -octaves * math.log(2.0), device=DEV)
+    t = float(np.float32(t))
+    z = torch.full((rows, n), -octaves * math.log(2.0) * t, device=DEV)
     first = 1000
     z[:, first] = 0.0
-    w = Fraction(math.exp(float(z[0, 0])))
+    w = Fraction(math.exp(float(z[0, 0]) / t))
     most = Fraction(1) - Fraction(1, 1 << 24)
     for p in (None, most):
         u = [most] * rows if p is None else [Fraction(3, 4)] + [most] * (rows - 1)
-        tok, prob = drawn(z, [float(x) for x in u], p=None if p is None else [float(p)] * rows)
+        tok, prob = drawn(z, [float(x) for x in u], t=[t] * rows, p=None if p is None else [float(p)] * rows)
         kept = 1 + (n - 1) * w
         if p is not None:
             count = max(math.ceil((p * kept - 1) / w), 0)
