@@ -45,7 +45,7 @@ struct RowSettings {
     double edge64, top64;
     float edge;         // no logit is larger: bins are counted from here
     float top;          // the row's largest logit: weights are relative to it
-    float floor;        // the smallest logit that has mass: 64 octaves below it, or a little more
+    float floor;        // the smallest logit that has mass: 64 octaves below it, 88 below a guessed edge
     float low;          // no logit that has mass may be smaller, for the bins to hold them all
 };
 
@@ -71,7 +71,11 @@ __device__ __forceinline__ RowSettings settings_of(float t, float edge, float lo
     const double range = edge < __builtin_inff() ? s.edge64 - (double)low : __builtin_inf();
     s.width = fmax(fmin(limit, range * (1.0 + 0x1p-30)) / bins, 1e-290);
     s.inv = 1.0 / s.width;
-    s.floor = fmaxf((float)(s.edge64 - limit), -3.402823466e38f);
+    // (rounded upwards: a logit below the last bin's end would be counted with a weight that the series is not meant for)
+    const double end = s.edge64 - limit;
+    s.floor = (float)end;
+    if ((double)s.floor < end) s.floor = nextafterf(s.floor, __builtin_inff());
+    s.floor = fmaxf(s.floor, -3.402823466e38f);
     return s;
 }
 
@@ -1131,7 +1135,10 @@ __global__ __launch_bounds__(NT, 4) void sample_rows_kernel(const SampleArgs a) 
     float edge = 0.0f, low = 0.0f;
     if (is_logit(g.x)) {
         const float spread = fmaxf(g.x - g.y, 1e-30f);
-        edge = g.x + fminf((float)(kAbove * 0.6931472) * in.t, spread);
+        const float above = fminf((float)(kAbove * 0.69314) * in.t, spread);      // (ln 2, rounded down)
+        edge = g.x + above;
+        // (rounded downwards: where floats are octaves apart, a step further up would leave places with mass below the floor)
+        if ((double)edge - (double)g.x > (double)above) edge = nextafterf(edge, -__builtin_inff());
         if (edge == __builtin_inff()) edge = g.x;                    // (past the largest float)
         low = g.y - spread;
     }

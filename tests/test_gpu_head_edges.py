@@ -48,6 +48,23 @@ def test_masked_first_places_and_a_rest_far_below_zero(rows, n):
     check_rows(z, dict(s, k=np.zeros(rows), p=np.ones(rows), m=np.zeros(rows)), range(min(rows, 60)))
 
 
+@pytest.mark.parametrize("rows, n", [(3, 20000), (70, 50000)])
+@pytest.mark.parametrize("top, t", [(1e8, 0.243), (-1e8, 0.245), (16777216.0, 0.07), (1000.0, 1.9e-6)])
+def test_logits_whose_neighbours_are_dozens_of_octaves_away(rows, n, top, t):
+    """Steps of a float between 24 and 48 octaves of weight: what lies one below the largest has little mass, but neither none nor more."""
+    rng = np.random.default_rng(rows)
+    top = np.float32(top)
+    next_down = np.nextafter(top, np.float32(-np.inf))
+    z = np.full((rows, n), -np.inf, np.float32)
+    for r in range(rows):                                     # a few, whose places are ranked, or a crowd
+        z[r, rng.permutation(n)[:n if r % 3 == 2 else 1000]] = next_down
+    z[:, 100] = top
+    z[1::2, 12000:][z[1::2, 12000:] == next_down] = np.nextafter(next_down, np.float32(-np.inf))
+    ones = np.ones(rows)
+    s = dict(u=np.where(np.arange(rows) % 2 == 0, np.float32(0.5), np.float32(1 - 2.0 ** -24)), t=ones * t, k=0 * ones, p=ones, m=0 * ones)
+    check_rows(z, s, range(min(rows, 6)))
+
+
 @pytest.mark.parametrize("rows, n", [(1, 1 << 22), (66, 1 << 21)])
 @pytest.mark.parametrize("octaves", [39.4, 40.6, 42.0])
 @pytest.mark.parametrize("t", [1.0, 0.37, 1.7])
