@@ -489,8 +489,14 @@ def scale_columns(d: int) -> int:
 # as they can on it: a norm of one row is over in less time than ten Python calls take.  Tensors that they make are not checked.
 # With a stream given they run with it as the current one: outputs and workspaces that a call makes are that stream's, so nobody else is
 # handed their memory while it works on them.
+def _tensor(t, name: str) -> None:
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a tensor, got {type(t).__name__}")
+
+
 def _rows(t: torch.Tensor, name: str, here: int) -> Tuple[int, int, int]:
     """_mat of a tensor on the current device."""
+    _tensor(t, name)
     if t.get_device() != here:
         raise ValueError(f"{name} must live on the current GPU (cuda:{here}), not on {t.device}")
     if t.dim() != 2:
@@ -506,6 +512,7 @@ def _flat(t: Optional[torch.Tensor], shape: tuple, dtype: torch.dtype, name: str
     """Pointer of a contiguous tensor of this shape and type on the current device, or None."""
     if t is None:
         return None
+    _tensor(t, name)
     if t.get_device() != here or t.shape != shape or t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {list(shape)} {dtype} tensor on the current GPU (cuda:{here})")
     return t.data_ptr()
@@ -517,13 +524,17 @@ def _scratch(nbytes: int, like: torch.Tensor, ws: Optional[torch.Tensor], here: 
         if nbytes == 0:
             return None, None, 0
         ws = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
-    elif ws.get_device() != here or ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.numel() < nbytes:
+        return ws, ws.data_ptr(), nbytes
+    _tensor(ws, "workspace")
+    if ws.get_device() != here or ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.numel() < nbytes:
         raise ValueError(f"workspace must be a contiguous uint8 tensor of >= {nbytes} bytes on the current GPU (cuda:{here})")
     return ws, ws.data_ptr(), ws.numel()
 
 
 def _quantized(t: QuantizedRows, name: str, here: int) -> Tuple[int, int, int, int]:
     """(rows, d, row stride of the codes, row stride of the scales)."""
+    if not isinstance(t, QuantizedRows):
+        raise TypeError(f"{name} must be QuantizedRows, got {type(t).__name__}")
     q, scales = t
     rows, d, ld = _rows(q, name, here)
     if q.dtype != torch.float8_e4m3fn or scales.dtype != torch.float8_e8m0fnu:
@@ -631,6 +642,7 @@ def _logits_out(out: Optional[torch.Tensor], rows: int, n: int, U: QuantizedRows
 
 def _list(idx: torch.Tensor, rows: int, padded: bool, here: int) -> Tuple[int, int, int]:
     """(pointer, idx_mode, length) of an index list."""
+    _tensor(idx, "idx")
     if idx.get_device() != here or idx.dtype != torch.int32 or not idx.is_contiguous():
         raise ValueError(f"idx must be a contiguous int32 tensor on the current GPU (cuda:{here})")
     flag = SV_IDX_PADDED if padded else 0

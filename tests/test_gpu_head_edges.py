@@ -174,3 +174,19 @@ def test_lists_of_more_tokens_than_a_launch_has_threads_for(rows, k, d):
         idx[j:j + (1 << 24)] = (torch.arange(j, min(j + (1 << 24), k), device=DEV) * 7 % V).to(torch.int32)
     idx[-1] = 99
     equal_by_parts(sv.quantized_subset_logits(h, U, idx), (h64 @ u64.t()).float().to(DEV), idx)
+
+
+def test_what_is_no_tensor_is_named():
+    z, u = torch.zeros((2, 8), device=DEV), torch.zeros(2, device=DEV)
+    x = torch.zeros((2, 256), dtype=torch.bfloat16, device=DEV)
+    U = sv.quantize_rows(x)
+    for name, call in [("temperature", lambda: sv.sample(z, u, temperature=0.8)), ("top_k", lambda: sv.sample(z, u, top_k=5)),
+                       ("top_p", lambda: sv.sample(z, u, top_p=0.9)), ("min_p", lambda: sv.sample(z, u, min_p=0.1)),
+                       ("u", lambda: sv.sample(z, 0.5)), ("logits", lambda: sv.sample([[0.0]], u)), ("idx", lambda: sv.sample(z, u, idx=[1])),
+                       ("workspace", lambda: sv.sample(z, u, ws=100)), ("tok_out", lambda: sv.sample(z, u, tok_out=[0, 0])),
+                       ("x", lambda: sv.quantize_rows(None)), ("weight", lambda: sv.rms_norm(x, 1.0, 1e-5)),
+                       ("residual", lambda: sv.rms_norm(x, x[0], 1e-5, residual=0.0)), ("U", lambda: sv.quantized_dense_logits(x, U.q)),
+                       ("U", lambda: sv.quantized_dense_logits(x, None)), ("h", lambda: sv.quantized_dense_logits([1.0], U)),
+                       ("the quantized output", lambda: sv.quantize_rows(x, U.q)), ("idx", lambda: sv.quantized_subset_logits(x, U, [1, 2]))]:
+        with pytest.raises(TypeError, match=name + " must be"):
+            call()
