@@ -324,8 +324,8 @@ int specvocab_rms_norm(const void* x, int64_t rows, int64_t d, int64_t ldx, cons
  *     logits_out[r, j] = < U[row(j), :], h[r, :] >     over the values that codes and scales stand for, accumulated in float32
  * h: rows in 8 bits (h_scales not NULL; ldh in codes, ldhs in scale bytes), or bfloat16 rows (h_scales NULL; ldh in elements,
  * ldhs ignored).  d a multiple of 16.  idx, k, idx_mode as in specvocab_subset_logits (SV_IDX_SORTED makes no difference).  A
- * NaN code or scale makes the logits that use it NaN.  The values are widened to bfloat16, which is exact, and multiplied as such (h_scales so
- * small that a value lies below 2^-126 lose it). */
+ * NaN code or scale makes the logits that use it NaN.  The values are widened to bfloat16, which is exact, and multiplied as such: values of
+ * h or U below 2^-126 may count as 0, and |h| beyond 2^100 may overflow (some forms apply U's scale to sums of 16 products). */
 int specvocab_quantized_dense_logits(const void* h, const uint8_t* h_scales, int64_t rows, int64_t d, int64_t ldh, int64_t ldhs,
                                      const uint8_t* U, const uint8_t* U_scales, int64_t V, int64_t ldu, int64_t ldus,
                                      float* logits_out, void* ws, size_t ws_bytes, void* stream);
@@ -348,8 +348,10 @@ int specvocab_quantized_subset_logits(const void* h, const uint8_t* h_scales, in
  * tok_out: device [rows] int32, the place, or idx(r, place) where idx (as in specvocab_subset_logits, padding slots having a logit of
  * -inf) is not NULL; -1 for a row that is masked throughout.  prob_out: device [rows] float32, w over the sum in 4 (0 for such
  * a row), or NULL.
- * Sums are kept to 2^-44 of each term (n up to 2^18; a bit less for each doubling of n), and do not depend on the run.
- * One launch; four (and workspace) for up to 64 rows of 49152 logits or more.  A row in which more than 1024 places crowd into one of the 4096 steps (1024 for short rows) that its range, or 64 octaves of w, is cut into, at a border or where the token is drawn --
+ * Sums are kept to 2^-44 of each term (n up to 2^18; a bit less for each doubling of n), and do not depend on the run.  How they are
+ * rounded below that depends on the form that serves the row, which goes by rows and n.
+ * One launch; four (and workspace) for up to 64 rows of 49152 logits or more.  A row in which more than 1024 places crowd into one of
+ * the 4096 steps (1024 for short rows) that its range, or 64 octaves of w, is cut into, at a border or where the token is drawn --
  * thousands of equal logits, clusters far apart --, costs some tens of passes over the row. */
 int specvocab_sample(const float* logits, int64_t ld, int64_t rows, int64_t n, const int32_t* idx, int idx_mode,
                      const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, const float* u,

@@ -366,6 +366,7 @@ int check_stored(const void* x, int64_t d, int64_t ld, int dt) {
 // any length (4096 elements by 128256 tokens 81 us, through LDS 97); so are several up to 16384 logits in all, their list's rows of U coming from the
 // caches after the first (4096 elements, 4 rows x 4096 tokens 9.9 and 11.6 us, 16 x 1024 6.8 and 11.1; at 24576 logits 10.0 to 15.5 and 11.2 to 12.5),
 // and hidden rows in 8 bits, which would have to be widened by a launch in front, up to 24576 (6 x 4096 12.3 and 14.0; 4 x 8192 18.0 and 14.7).
+// The borders are those of 4096 elements, whatever d is: 6 x 4096 takes 25 us a row at a time at 8192 elements, 36 at 12288, 47 at 16384.
 enum QuantizedWay { Q_ROWS, Q_SHARED, Q_UNION };
 QuantizedWay quantized_way(int64_t rows, int64_t d, int64_t k, bool quantized_h, bool list, int idx_mode) {
     if (rows == 1) return Q_ROWS;

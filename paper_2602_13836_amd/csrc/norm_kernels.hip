@@ -5,11 +5,12 @@
 //
 // The norm reads the sum as it is stored, and the 8 bits are those of y as it is stored, so the one call leaves, bit for bit, what an
 // addition, a norm and a quantisation of their own would: the selector multiplies y, the 8-bit head q, and both mean the same row.
-// Sums of squares are float32, of at most a few dozen values per lane before the tree over lanes and wavefronts.
+// Sums of squares are float32, of at most 32 values per lane (rows of more than 32768 values: of d / 1024) before the tree over lanes and
+// wavefronts.
 // Memory bounds it: two rows in, two and a half out, nothing read twice.  Eight consecutive values per lane and load, so that 16
 // lanes hold a block of 128 and its largest magnitude is four DPP steps away.  A workgroup per row, as many threads as the row has
 // pieces of eight (a wavefront per row left too few loads on their way).  Measured: 5000 rows of 3840 bfloat16 values with the
-// residual and all three outputs 28.6 us, 173 MB at 6.0 TB/s; one row of 4096, 2.6 us, a launch.
+// residual and all three outputs 29 us, 173 MB at 6.0 TB/s; one row of 4096, 2.6 us, a launch.
 #include "quantized_rows.h"
 #include "sv_launch.h"
 

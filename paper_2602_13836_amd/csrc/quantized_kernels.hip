@@ -142,7 +142,8 @@ __global__ __launch_bounds__(256) void quantized_gemv_kernel(const QuantizedArgs
     }
 }
 
-// rows of more than 8192 values: a wavefront per row of U, in pieces
+// Rows of more than 8192 values: a wavefront per row of U, in pieces.  By 128256 tokens: 12288 values 256 us (bfloat16 hidden rows 317),
+// 1.6 GB at 6.2 TB/s; 16384 350 (442), 6.0 TB/s.
 template <bool H8>
 __global__ __launch_bounds__(256) void quantized_gemv_long_kernel(const QuantizedArgs a) {
     const int lane = threadIdx.x & 63;
@@ -173,7 +174,8 @@ __global__ __launch_bounds__(256) void quantized_gemv_long_kernel(const Quantize
 
 // ---- several hidden rows (bfloat16) on one set of rows of U, where they are so long that the scales of a tile's rows do not fit into
 // LDS beside its slices (from about 16000 elements on; the tiles of quantized_tile_kernels.hip take the rest: at 4096 elements 512 rows by
-// 151936 tokens 560 us, this form 2650).  A wavefront owns 16 rows of U, reads 64 values of each per step straight into operand
+// 151936 tokens 560 us, this form 2650).  16384 elements by 128256 tokens: 8 rows 660 us, 32 720, 64 920, 512 7400, where the tiles take 270,
+// 290, 340 and 1280 at 12288.  A wavefront owns 16 rows of U, reads 64 values of each per step straight into operand
 // registers (lane = row i, 16-byte piece g: two steps of v_mfma_f32_16x16x32_bf16 whose reduction order is the pieces'), the hidden
 // rows come through LDS, 256 values at a time.
 constexpr int kSlice = 256;                       // values of the reduction per LDS slice

@@ -26,7 +26,7 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t amax_bits) {
     const int e = (int)(amax_bits >> 23) - 127 - 8 + ((amax_bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);      // 448 = 1.75 * 2^8
     return (uint32_t)(max(e, -126) + 127);
 }
-__device__ __forceinline__ float inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }   // byte 1 .. 246
+__device__ __forceinline__ float inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }   // byte 1 .. 247
 
 // largest bits of the 16 lanes of a DPP row, in every lane
 __device__ __forceinline__ uint32_t row16_max_u32(uint32_t x) {

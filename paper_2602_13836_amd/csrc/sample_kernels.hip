@@ -20,7 +20,8 @@
 //
 // What bounds it: a logit takes some 30 instructions, half of them on 64 bits, to be counted, ten times what its four bytes take from
 // memory; then a chain of steps that each need the one before, some 10 us of barriers and LDS round trips a row.  Measured, with settings
-// of every kind: 1 x 8192 logits 5 us (11 with the host's part), 1 x 128256 23, 60 x 128256 52, 512 x 151936 135 (2.3 TB/s).
+// of every kind: 1 x 8192 logits 5 us (11 to 16 with the host's part), 1 x 128256 23 to 32 (29 of them kernels in a trace), 60 x 128256 52,
+// 512 x 151936 135 (2.3 TB/s).
 #include "sv_device.h"
 #include "sv_launch.h"
 

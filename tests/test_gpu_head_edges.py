@@ -146,6 +146,28 @@ def small_rows(rows, d, seed):
     return sv.QuantizedRows(v.to(torch.float8_e4m3fn).to(DEV), s.to(DEV)), v.double()
 
 
+@pytest.mark.parametrize("d", [256, 4096, 8208, 16400])
+@pytest.mark.parametrize("rows", [1, 3, 40, 70])
+@pytest.mark.parametrize("h8", [True, False], ids=["h8", "hbf16"])
+def test_large_hidden_values_by_small_embeddings_and_the_reverse(rows, d, h8):
+    """Codes of +-448 at scales of 2^91 and 2^-110, and of 2^-90 and 2^110: every sum is a multiple of 2^12 * 2^(e + f), below 2^24 of them."""
+    gen = torch.Generator().manual_seed(d + rows)
+    signs = lambda n: torch.randint(0, 2, (n, d), generator=gen).float() * 2 - 1  # noqa: E731
+    hv, uv = signs(rows), signs(300)
+
+    def rows8(v, e):
+        s = torch.full((v.shape[0], sv.scale_columns(d)), 127 + e, dtype=torch.uint8).view(torch.float8_e8m0fnu)
+        return sv.QuantizedRows((v * 448).to(torch.float8_e4m3fn).to(DEV), s.to(DEV))
+
+    for e, f in ((91, -110), (-90, 110)):
+        h = rows8(hv, e) if h8 else (hv.double() * 448 * 2.0 ** e).to(torch.bfloat16).to(DEV)
+        ref = (hv.double() @ uv.double().t()) * (448.0 ** 2 * 2.0 ** (e + f))
+        U = rows8(uv, f)
+        assert torch.equal(sv.quantized_dense_logits(h, U).cpu().double(), ref)
+        idx = torch.arange(299, -1, -1, dtype=torch.int32)
+        assert torch.equal(sv.quantized_subset_logits(h, U, idx.to(DEV)).cpu().double(), ref.flip(1))
+
+
 def equal_by_parts(got, full, at, part=1 << 24):
     for j in range(0, got.shape[1], part):
         assert torch.equal(got[:, j:j + part], full[:, at[j:j + part].long()]), j
