@@ -200,7 +200,7 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(const NormArgs a) {
         }
     } else {
         const int pieces = (d / 8 + threads - 1) / threads;
-        auto each = [&](auto f) {                                    // f(the sum as it is stored)
+        auto each = [&](auto use) {                                  // use(the sum as it is stored, the same widened)
             for (int c = 0; c < pieces; ++c) {
                 const int at = (c * threads + tid) * 8, from = min(at, d - 8);
                 Eight<DT> ex, er, e;
@@ -208,7 +208,7 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(const NormArgs a) {
                 if (res) er.load(res + (int64_t)from * kEs);
                 float t[8];
                 sum_of(at, ex, er, e, t);
-                f(e, t);
+                use(e, t);
             }
         };
         float s = 0.f, f = 1.0f;
