@@ -109,11 +109,24 @@ typedef enum {
     SV_OP_QUANTIZED_DENSE_LOGITS = 7,  /* dt: what h is, SV_BF16 or SV_E4M3 */
     SV_OP_QUANTIZED_SUBSET_LOGITS = 8, /* the same */
     SV_OP_QUANTIZED_SAMPLE_STEP = 9,   /* the same; k: 0 for the whole vocabulary */
-    SV_OP_SAMPLE = 10                  /* k: logits of a row (n) */
+    SV_OP_SAMPLE = 10,                 /* k: logits of a row (n) */
+    SV_OP_TOKEN_LOGPROBS = 11,         /* k: logits of a row (n); kd: alternatives (top); dt: type of the logits */
+    SV_OP_DISTILL = 12                 /* k: logits of a row (n); dt: type of the logits */
 } sv_op;
+
+/* What a teacher's list holds (specvocab_distill). */
+typedef enum {
+    SV_TEACHER_LOGITS = 0,   /* logits: its probabilities are their softmax over the list, at the call's temperature */
+    SV_TEACHER_LOGPROBS = 1, /* log probabilities at that temperature; the mass that the list leaves counts nothing */
+    SV_TEACHER_REST = 2      /* the same; the mass that the list leaves counts as one more token */
+} sv_teacher;
 
 /* Largest kd the draft top-kd accepts. */
 #define SPECVOCAB_MAX_KD 64
+/* Most alternatives and most given tokens of a row in specvocab_token_logprobs, and most entries of a teacher's list. */
+#define SPECVOCAB_MAX_TOP 64
+#define SPECVOCAB_MAX_GIVEN 64
+#define SPECVOCAB_MAX_TEACHER 512
 
 /* SPECVOCAB_VERSION of the loaded library. */
 int specvocab_version(void);
@@ -365,6 +378,67 @@ int specvocab_quantized_sample_step(const void* h, const uint8_t* h_scales, int6
                                     const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
                                     const float* u, float* logits_out, int32_t* tok_out, float* prob_out,
                                     void* ws, size_t ws_bytes, void* stream);
+
+/* ---- Over finished rows of logits: what a token's probability is, and what a draft model learns from a teacher -------------------
+ *
+ * logits: device [rows x n] in `dt` (SV_F32: what the products of this library leave; SV_BF16: a training program's), row stride ld in
+ * elements, aligned to an element.  -inf masks a place: it has probability 0 and no gradient.  Any other value is a logit, the type's
+ * lowest too.  A row with a NaN or +inf has NaN throughout, and no alternatives (-1).  A row that is masked throughout has log probabilities of -inf, entropy
+ * 0 and no gradient.  grad_out: device [rows x n] in `grad_dt` (SV_F32 or SV_BF16, rounded to nearest even), row stride ld_grad, every
+ * place written; it may be the logits themselves (same base, stride and type) and must not overlap them otherwise.
+ * Results do not depend on the run.  Sums are float32, relative to the largest logit; probabilities below 2^-126 count as 0.
+ * `state` is what a gradient needs of the forward call: device [rows x 4] float32, 16-byte aligned. */
+
+/* Log probabilities of given tokens, the entropy and the largest alternatives of every row, natural logarithms at temperature T =
+ * temperature[r] (device [rows] float32, or NULL for 1; kept within 2^-20 .. 2^20; T <= 0 and NaN count as 1):
+ *     logprob_out[r, j] = z[t_j] / T - log sum_v exp(z[v] / T),  t_j = tokens[r, j]     device [rows x given] float32
+ *     entropy_out[r]    = - sum_v p_v log p_v                                           device [rows] float32, or NULL
+ *     top_tok_out, top_logprob_out: the `top` largest places and their log probabilities, by descending logit, equal logits by
+ *                          place, -1 with -inf where the row has no more              device [rows x top] int32, float32
+ *     state_out[r]      = (largest logit, sum_v exp((z[v] - largest) / T), entropy, 0), or NULL
+ * tokens: device [rows x given] int32, 0 <= given <= SPECVOCAB_MAX_GIVEN (0: none, tokens and logprob_out NULL); a token that names no place
+ * (-1, a place past the row, an id that is not in the list) has -inf.  0 <= top <= min(n, SPECVOCAB_MAX_TOP); top > 0 with n above
+ * 8388608 is SV_ERR_UNSUPPORTED.
+ * idx, idx_mode: the token ids of the places, as in specvocab_sample (any order), or NULL: a token is its place.  Of equal ids
+ * the first place counts.
+ * One launch, two (and workspace) where there are few rows for their length.  Rows in which more than 1024 places may be among the
+ * largest (equal logits in their hundreds) take some ten passes over the row. */
+int specvocab_token_logprobs(const void* logits, int64_t ld, int64_t rows, int64_t n, int dt,
+                             const int32_t* idx, int idx_mode, const float* temperature,
+                             const int32_t* tokens, int64_t given, int64_t top,
+                             float* logprob_out, float* entropy_out, int32_t* top_tok_out, float* top_logprob_out, float* state_out,
+                             void* ws, size_t ws_bytes, void* stream);
+
+/* The logits' gradient of specvocab_token_logprobs without a list (cross entropy, policy gradients, entropy bonuses):
+ *     grad_out[r, v] = (sum_j grad_logprob[r, j] ([v = t_j] - p_v) - grad_entropy[r] p_v (log p_v + entropy[r])) / T
+ * grad_logprob: device [rows x given] float32, or NULL (then tokens may be NULL); grad_entropy: device [rows] float32, or NULL; not both NULL.
+ * state: what the forward call at the same temperature wrote.  A token that is given several times gets the sum; one that names no place, nothing.  No workspace. */
+int specvocab_token_logprobs_grad(const void* logits, int64_t ld, int64_t rows, int64_t n, int dt, const float* temperature,
+                                  const int32_t* tokens, int64_t given, const float* state,
+                                  const float* grad_logprob, const float* grad_entropy,
+                                  void* grad_out, int64_t ld_grad, int grad_dt, void* stream);
+
+/* Distillation (Section 3.4's losses, for a teacher of whose rows the largest logits were kept): the divergence of q = softmax(z / T) from
+ * the teacher's probabilities p_j of the tokens t_j = tok[r, j] that it lists, times weight[r],
+ *     loss_out[r] = weight[r] (sum_j p_j (log p_j - log q[t_j])  [+ p' (log p' - log q')])         device [rows] float32
+ *     grad_out[r, v] = weight[r] / T (m q[v] - sum_{j: t_j = v} p_j  [- p' q[v] / q', v not listed])
+ * with m the mass that counts, sum_j p_j [+ p'].  In brackets: SV_TEACHER_REST only; p' = 1 - sum_j p_j (at least 0) and q' the mass
+ * of all places that are not listed (left out where there is no such place).  tok, teacher: device [rows x known] int32 and float32, 1 <= known <=
+ * SPECVOCAB_MAX_TEACHER, in any order; an entry whose token lies outside [0, n) (-1: padding) is not there, one of -inf has no mass, and a
+ * token that is listed twice has both masses.  specvocab_token_logprobs writes such lists (top_tok_out, top_logprob_out).  A listed token with mass at a
+ * masked place makes the loss +inf.  temperature: T, finite, within 2^-20 .. 2^20; weight: device [rows] float32, or NULL for 1; a row of weight 0
+ * is not read: loss 0, gradient 0.  A mean over tokens or a factor T^2 goes into the weight.
+ * state_out[r] = (largest logit, sum_v exp((z[v] - largest) / T), the same two over the places that are not listed), or NULL.
+ * grad_out may be NULL: the loss alone (or its gradient later, when the factors are known, by specvocab_distill_grad with the same arguments and
+ * the state; weight[r] is then whatever factor the row's divergence has).  Both at once read the logits from memory once.
+ * One launch; two, three with the gradient, and workspace where there are few rows for their length, or more than 2^18 places. */
+int specvocab_distill(const void* logits, int64_t ld, int64_t rows, int64_t n, int dt,
+                      const int32_t* tok, const float* teacher, int64_t known, int kind, float temperature, const float* weight,
+                      float* loss_out, float* state_out, void* grad_out, int64_t ld_grad, int grad_dt,
+                      void* ws, size_t ws_bytes, void* stream);
+int specvocab_distill_grad(const void* logits, int64_t ld, int64_t rows, int64_t n, int dt,
+                           const int32_t* tok, const float* teacher, int64_t known, int kind, float temperature, const float* weight,
+                           const float* state, void* grad_out, int64_t ld_grad, int grad_dt, void* stream);
 
 #ifdef __cplusplus
 }

@@ -23,10 +23,12 @@ SV_OP_SELECT, SV_OP_SUBSET_LOGITS, SV_OP_DRAFT_TOPK, SV_OP_DENSE_LOGITS, SV_OP_D
 SV_OP_INDEXED_HEAD_NAIVE = 5
 SV_OP_AUX_LOG_SOFTMAX = 6
 SV_OP_QUANTIZED_DENSE_LOGITS, SV_OP_QUANTIZED_SUBSET_LOGITS, SV_OP_QUANTIZED_SAMPLE_STEP, SV_OP_SAMPLE = 7, 8, 9, 10
+SV_OP_TOKEN_LOGPROBS, SV_OP_DISTILL = 11, 12
 SV_E4M3 = 2              # rows in 8 bits, where a workspace size is asked for
 SV_IDX_PADDED = 4        # OR into idx_mode: the list may hold padding slots (-1)
 SV_IDX_SORTED = 8        # OR into idx_mode: every list is sorted by ascending id (what select emits)
 MAX_KD = 64
+MAX_TOP, MAX_GIVEN, MAX_TEACHER = 64, 64, 512
 SELECT_SAMPLE = 8192     # sampled tokens of a batch's selection, d' > 512: ids floor(j * V / SELECT_SAMPLE)
 SELECT_CODE_SAMPLE = 4096            # ... with one byte per score in memory: floor(j * V / SELECT_CODE_SAMPLE), every second one of those
 
@@ -52,6 +54,10 @@ EXPORTS = (
     "specvocab_quantized_subset_logits",
     "specvocab_sample",
     "specvocab_quantized_sample_step",
+    "specvocab_token_logprobs",
+    "specvocab_token_logprobs_grad",
+    "specvocab_distill",
+    "specvocab_distill_grad",
 )
 
 
@@ -125,6 +131,14 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.specvocab_sample.argtypes = [vp, i64, i64, i64, vp, ci, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.specvocab_quantized_sample_step.restype = ci
     lib.specvocab_quantized_sample_step.argtypes = head + [vp, i64, ci, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.specvocab_token_logprobs.restype = ci
+    lib.specvocab_token_logprobs.argtypes = [vp, i64, i64, i64, ci, vp, ci, vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.specvocab_token_logprobs_grad.restype = ci
+    lib.specvocab_token_logprobs_grad.argtypes = [vp, i64, i64, i64, ci, vp, vp, i64, vp, vp, vp, vp, i64, ci, vp]
+    lib.specvocab_distill.restype = ci
+    lib.specvocab_distill.argtypes = [vp, i64, i64, i64, ci, vp, vp, i64, ci, cf, vp, vp, vp, vp, i64, ci, vp, sz, vp]
+    lib.specvocab_distill_grad.restype = ci
+    lib.specvocab_distill_grad.argtypes = [vp, i64, i64, i64, ci, vp, vp, i64, ci, cf, vp, vp, vp, i64, ci, vp]
     if path is None:
         _lib = lib
     return lib
@@ -753,3 +767,188 @@ def quantized_sample_step(h: Union[torch.Tensor, QuantizedRows], U: QuantizedRow
     _check(load_library().specvocab_quantized_sample_step(*args, ip, k, mode, *settings, op, tok_out.data_ptr(), prob_out.data_ptr(),
                                                           wp, wn, _current_raw_stream(here)), "specvocab_quantized_sample_step")
     return logits_out, tok_out, prob_out
+
+
+# ---- over finished rows of logits: log probabilities of given tokens, distillation from a teacher's largest logits
+
+class TokenLogprobs(NamedTuple):
+    """logprob [rows] or [rows x given] (None without tokens), entropy [rows], top_tok int32 and top_logprob [rows x top] (None for top
+    0), state [rows x 4] (None unless asked for); float32 where nothing else is said."""
+    logprob: Optional[torch.Tensor]
+    entropy: torch.Tensor
+    top_tok: Optional[torch.Tensor]
+    top_logprob: Optional[torch.Tensor]
+    state: Optional[torch.Tensor]
+
+
+class Distilled(NamedTuple):
+    """loss [rows] float32, grad [rows x n] (None unless asked for), state [rows x 4] float32 (None unless asked for)."""
+    loss: torch.Tensor
+    grad: Optional[torch.Tensor]
+    state: Optional[torch.Tensor]
+
+
+_TEACHER_KINDS = {"logits": 0, "logprobs": 1, "rest": 2}
+
+
+def _out(t: Optional[torch.Tensor], shape: tuple, dtype: torch.dtype, name: str, like: torch.Tensor, here: int) -> Tuple[torch.Tensor, int]:
+    """(the caller's output or a new one, its pointer)."""
+    if t is None:
+        t = torch.empty(shape, dtype=dtype, device=like.device)
+        return t, t.data_ptr()
+    return t, _flat(t, shape, dtype, name, here)
+
+
+def _gradient(out: Optional[torch.Tensor], dtype: Optional[torch.dtype], logits: torch.Tensor, here: int) -> Tuple[torch.Tensor, int, int]:
+    """(where a gradient goes, its row stride, its type)."""
+    if out is None:
+        out = torch.empty(logits.shape, dtype=dtype or logits.dtype, device=logits.device)
+        return out, out.shape[1], _dt(out)
+    ld = _rows(out, "grad_out", here)[2]
+    if out.shape != logits.shape:
+        raise ValueError("grad_out must have the logits' shape")
+    if dtype is not None and out.dtype != dtype:
+        raise ValueError(f"grad_out is {out.dtype}, not {dtype}")
+    return out, ld, _dt(out)
+
+
+def _given(tokens: torch.Tensor, rows: int, here: int) -> Tuple[int, int]:
+    """(pointer, tokens of a row)."""
+    _tensor(tokens, "tokens")
+    if tokens.dim() not in (1, 2):
+        raise ValueError("tokens must be [rows] or [rows x given]")
+    shape = (rows,) if tokens.dim() == 1 else (rows, tokens.shape[1])
+    return _flat(tokens, shape, torch.int32, "tokens", here), 1 if tokens.dim() == 1 else tokens.shape[1]
+
+
+def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top: int = 0,
+                   temperature: Optional[torch.Tensor] = None, idx: Optional[torch.Tensor] = None, want_state: bool = False,
+                   logprob_out: Optional[torch.Tensor] = None, entropy_out: Optional[torch.Tensor] = None,
+                   top_tok_out: Optional[torch.Tensor] = None, top_logprob_out: Optional[torch.Tensor] = None,
+                   state_out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                   stream: Optional[torch.cuda.Stream] = None) -> TokenLogprobs:
+    """specvocab_token_logprobs: log probabilities of the given tokens (int32 [rows] or [rows x given]), the entropy and the `top` largest
+    alternatives of every row of logits (float32 or bfloat16), at temperature [rows] float32 (None: 1).  idx: the token ids of the places,
+    [n] or [rows x n].  state: what token_logprobs_grad needs."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return token_logprobs(logits, tokens, top, temperature, idx, want_state, logprob_out, entropy_out, top_tok_out, top_logprob_out,
+                                  state_out, ws)
+    here = torch.cuda.current_device()
+    rows, n, ld = _rows(logits, "logits", here)
+    dt, f32 = _dt(logits), torch.float32
+    tp, given = (None, 0) if tokens is None else _given(tokens, rows, here)
+    t = _flat(temperature, (rows,), f32, "temperature", here)
+    ip, mode = None, SV_IDX_PER_ROW
+    if idx is not None:
+        ip, mode, k = _list(idx, rows, False, here)
+        if k != n:
+            raise ValueError("idx and logits disagree on n")
+    lp = kp = vp = sp = None
+    if tokens is not None:
+        logprob_out, lp = _out(logprob_out, tuple(tokens.shape), f32, "logprob_out", logits, here)
+    elif logprob_out is not None:
+        raise ValueError("logprob_out needs tokens")
+    entropy_out, ep = _out(entropy_out, (rows,), f32, "entropy_out", logits, here)
+    if top > 0:
+        top_tok_out, kp = _out(top_tok_out, (rows, top), torch.int32, "top_tok_out", logits, here)
+        top_logprob_out, vp = _out(top_logprob_out, (rows, top), f32, "top_logprob_out", logits, here)
+    elif top_tok_out is not None or top_logprob_out is not None:
+        raise ValueError("top_tok_out and top_logprob_out need top > 0")
+    if want_state or state_out is not None:
+        state_out, sp = _out(state_out, (rows, 4), f32, "state_out", logits, here)
+    ws, wp, wn = _scratch(workspace_bytes(SV_OP_TOKEN_LOGPROBS, rows, 0, 0, n, 0, top, dt), logits, ws, here)
+    _check(load_library().specvocab_token_logprobs(logits.data_ptr(), ld, rows, n, dt, ip, mode, t, tp, given, top, lp, ep, kp, vp, sp,
+                                                   wp, wn, _current_raw_stream(here)), "specvocab_token_logprobs")
+    return TokenLogprobs(logprob_out, entropy_out, top_tok_out, top_logprob_out, state_out)
+
+
+def token_logprobs_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor], state: torch.Tensor,
+                        grad_logprob: Optional[torch.Tensor] = None, grad_entropy: Optional[torch.Tensor] = None,
+                        temperature: Optional[torch.Tensor] = None, grad_dtype: Optional[torch.dtype] = None,
+                        grad_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """specvocab_token_logprobs_grad: the logits' gradient [rows x n] from those of token_logprobs' log probabilities (the tokens' shape)
+    and entropy [rows].  grad_dtype: float32 or bfloat16 (None: the logits' type); grad_out may be the logits themselves."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return token_logprobs_grad(logits, tokens, state, grad_logprob, grad_entropy, temperature, grad_dtype, grad_out)
+    here = torch.cuda.current_device()
+    rows, n, ld = _rows(logits, "logits", here)
+    dt, f32 = _dt(logits), torch.float32
+    tp, given = (None, 0) if tokens is None else _given(tokens, rows, here)
+    t = _flat(temperature, (rows,), f32, "temperature", here)
+    if state is None:
+        raise ValueError("state must be given")
+    sp = _flat(state, (rows, 4), f32, "state", here)
+    if grad_logprob is not None and tokens is None:
+        raise ValueError("grad_logprob needs tokens")
+    gp = None if grad_logprob is None else _flat(grad_logprob, tuple(tokens.shape), f32, "grad_logprob", here)
+    ge = _flat(grad_entropy, (rows,), f32, "grad_entropy", here)
+    grad_out, ldg, gdt = _gradient(grad_out, grad_dtype, logits, here)
+    _check(load_library().specvocab_token_logprobs_grad(logits.data_ptr(), ld, rows, n, dt, t, tp, given, sp, gp, ge, grad_out.data_ptr(),
+                                                        ldg, gdt, _current_raw_stream(here)), "specvocab_token_logprobs_grad")
+    return grad_out
+
+
+def _teacher(logits: torch.Tensor, tok: torch.Tensor, teacher: torch.Tensor, kind: str, weight: Optional[torch.Tensor], here: int):
+    """(leading arguments of a distillation but for the temperature and the weight, the weight's pointer, rows, n, dtype)."""
+    rows, n, ld = _rows(logits, "logits", here)
+    dt = _dt(logits)
+    _tensor(tok, "tok")
+    _tensor(teacher, "teacher")
+    if tok.dim() != 2:
+        raise ValueError("tok must be [rows x known]")
+    known = tok.shape[1]
+    tp = _flat(tok, (rows, known), torch.int32, "tok", here)
+    vp = _flat(teacher, (rows, known), torch.float32, "teacher", here)
+    if kind not in _TEACHER_KINDS:
+        raise ValueError(f"kind must be one of {sorted(_TEACHER_KINDS)}, got {kind!r}")
+    w = _flat(weight, (rows,), torch.float32, "weight", here)
+    return (logits.data_ptr(), ld, rows, n, dt, tp, vp, known, _TEACHER_KINDS[kind]), w, rows, n, dt
+
+
+def distill(logits: torch.Tensor, tok: torch.Tensor, teacher: torch.Tensor, kind: str = "logits", temperature: float = 1.0,
+            weight: Optional[torch.Tensor] = None, want_grad: bool = False, grad_dtype: Optional[torch.dtype] = None,
+            want_state: bool = False, loss_out: Optional[torch.Tensor] = None, grad_out: Optional[torch.Tensor] = None,
+            state_out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+            stream: Optional[torch.cuda.Stream] = None) -> Distilled:
+    """specvocab_distill: every row's divergence from a teacher that lists tokens tok [rows x known] int32 (-1: padding) with values teacher
+    [rows x known] float32 -- kind "logits", "logprobs" (what the list leaves counts nothing) or "rest" (it counts as one more token) --
+    times weight [rows].  want_grad, grad_dtype or grad_out: the logits' gradient of the sum of the losses too, in float32 or bfloat16 (the
+    logits' type unless said); grad_out may be the logits themselves.  state: what distill_grad needs."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return distill(logits, tok, teacher, kind, temperature, weight, want_grad, grad_dtype, want_state, loss_out, grad_out, state_out, ws)
+    here = torch.cuda.current_device()
+    args, w, rows, n, dt = _teacher(logits, tok, teacher, kind, weight, here)
+    loss_out, lp = _out(loss_out, (rows,), torch.float32, "loss_out", logits, here)
+    sp = gp = None
+    ldg, gdt = 0, SV_F32
+    if want_state or state_out is not None:
+        state_out, sp = _out(state_out, (rows, 4), torch.float32, "state_out", logits, here)
+    if want_grad or grad_dtype is not None or grad_out is not None:
+        grad_out, ldg, gdt = _gradient(grad_out, grad_dtype, logits, here)
+        gp = grad_out.data_ptr()
+    ws, wp, wn = _scratch(workspace_bytes(SV_OP_DISTILL, rows, 0, 0, n, 0, 0, dt), logits, ws, here)
+    _check(load_library().specvocab_distill(*args, temperature, w, lp, sp, gp, ldg, gdt, wp, wn, _current_raw_stream(here)),
+           "specvocab_distill")
+    return Distilled(loss_out, grad_out, state_out)
+
+
+def distill_grad(logits: torch.Tensor, tok: torch.Tensor, teacher: torch.Tensor, state: torch.Tensor, kind: str = "logits",
+                 temperature: float = 1.0, weight: Optional[torch.Tensor] = None, grad_dtype: Optional[torch.dtype] = None,
+                 grad_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """specvocab_distill_grad: the logits' gradient of distill's losses from the state that it left; weight: whatever factor each row's
+    divergence has by now."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return distill_grad(logits, tok, teacher, state, kind, temperature, weight, grad_dtype, grad_out)
+    here = torch.cuda.current_device()
+    args, w, rows, _, _ = _teacher(logits, tok, teacher, kind, weight, here)
+    if state is None:
+        raise ValueError("state must be given")
+    sp = _flat(state, (rows, 4), torch.float32, "state", here)
+    grad_out, ldg, gdt = _gradient(grad_out, grad_dtype, logits, here)
+    _check(load_library().specvocab_distill_grad(*args, temperature, w, sp, grad_out.data_ptr(), ldg, gdt, _current_raw_stream(here)),
+           "specvocab_distill_grad")
+    return grad_out

@@ -497,6 +497,57 @@ int check_sample(const float* logits, int64_t ld, int64_t rows, int64_t n, const
     }
     return SV_OK;
 }
+
+// finished rows of logits, of either type
+int check_finished(int64_t rows, int64_t n, int64_t ld, int dt) {
+    if (!dtype_ok(dt)) return SV_ERR_DTYPE;
+    return rows < 1 || rows > kMaxVocab || n < 1 || n > kMaxVocab || ld < n ? SV_ERR_SHAPE : SV_OK;
+}
+int check_token_shape(int64_t rows, int64_t n, int64_t ld, int dt, int64_t given, int64_t top) {
+    const int st = check_finished(rows, n, ld, dt);
+    if (st != SV_OK) return st;
+    if (given < 0 || given > SPECVOCAB_MAX_GIVEN || top < 0 || top > SPECVOCAB_MAX_TOP || top > n) return SV_ERR_SHAPE;
+    return top > 0 && n > sv::kTopVocab ? SV_ERR_UNSUPPORTED : SV_OK;
+}
+inline bool aligned_to(const void* p, int dt) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(esize_of(dt) - 1)) == 0; }
+int check_gradient(const void* grad, int64_t ld_grad, int grad_dt, int64_t n) {
+    if (!dtype_ok(grad_dt)) return SV_ERR_DTYPE;
+    if (ld_grad < n) return SV_ERR_SHAPE;
+    return aligned_to(grad, grad_dt) ? SV_OK : SV_ERR_ALIGN;
+}
+int check_scratch(size_t need, const void* ws, size_t ws_bytes) {
+    if (!need) return SV_OK;
+    if (!ws || ws_bytes < need) return SV_ERR_WORKSPACE;
+    return aligned16(ws) ? SV_OK : SV_ERR_ALIGN;
+}
+// what the two calls of a distillation have in common; `tok` is looked at in the debug mode only
+int check_distill(const sv::DistillArgs& a, int64_t ld, int dt, int64_t known) {
+    if (!a.logits || !a.tok || !a.teacher) return SV_ERR_NULL;
+    const int st = check_finished(a.rows, a.n, ld, dt);
+    if (st != SV_OK) return st;
+    if (a.kind != SV_TEACHER_LOGITS && a.kind != SV_TEACHER_LOGPROBS && a.kind != SV_TEACHER_REST) return SV_ERR_DTYPE;
+    if (known < 1 || known > SPECVOCAB_MAX_TEACHER || !(a.temperature >= 0x1p-20f) || !(a.temperature <= 0x1p20f)) return SV_ERR_SHAPE;
+    return aligned_to(a.logits, dt) && aligned16(a.state) ? SV_OK : SV_ERR_ALIGN;
+}
+sv::DistillArgs distill_args(const void* logits, int64_t ld, int64_t rows, int64_t n, int dt, const int32_t* tok, const float* teacher,
+                             int64_t known, int kind, float temperature, const float* weight, const float* state, void* grad_out,
+                             int64_t ld_grad, int grad_dt) {
+    sv::DistillArgs a{};
+    a.logits = static_cast<const char*>(logits);
+    a.row_bytes = ld * esize_of(dt);
+    a.n = n;
+    a.rows = rows;
+    a.tok = tok;
+    a.teacher = teacher;
+    a.known = (int)(known > SPECVOCAB_MAX_TEACHER ? 0 : known);
+    a.kind = kind;
+    a.temperature = temperature;
+    a.weight = weight;
+    a.state = reinterpret_cast<float4*>(const_cast<float*>(state));
+    a.grad = static_cast<char*>(grad_out);
+    a.grad_row_bytes = ld_grad * esize_of(grad_dt);
+    return a;
+}
 sv::SampleArgs sample_args(const float* logits, int64_t ld, int64_t rows, int64_t n, const int32_t* idx, int idx_mode, const float* temperature,
                            const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* tok_out, float* prob_out, void* ws) {
     sv::SampleArgs a{};
@@ -540,7 +591,6 @@ const char* specvocab_status_string(int status) {
 
 int specvocab_workspace_bytes(int op, int64_t rows, int64_t d, int64_t V, int64_t k, int64_t d_prime,
                               int64_t kd, int dt, int idx_mode, size_t* bytes_out) {
-    (void)kd;
     if (!bytes_out) return SV_ERR_NULL;
     *bytes_out = 0;
     switch (op) {
@@ -586,6 +636,18 @@ int specvocab_workspace_bytes(int op, int64_t rows, int64_t d, int64_t V, int64_
             if (rows < 1 || rows > kMaxRows || k < 1 || k > kMaxVocab) return SV_ERR_SHAPE;
             *bytes_out = sv::sample_scratch_bytes(rows, k);
             return SV_OK;
+        case SV_OP_TOKEN_LOGPROBS: {
+            const int st = check_token_shape(rows, k, k, dt, 0, kd);
+            if (st != SV_OK) return st;
+            *bytes_out = sv::token_scratch_bytes(rows, k, (int)kd);
+            return SV_OK;
+        }
+        case SV_OP_DISTILL: {
+            const int st = check_finished(rows, k, k, dt);
+            if (st != SV_OK) return st;
+            *bytes_out = sv::distill_scratch_bytes(rows, k);
+            return SV_OK;
+        }
         case SV_OP_DRAFT_TOPK:
         case SV_OP_DENSE_LOGITS:
             return SV_OK;
@@ -1040,6 +1102,106 @@ int specvocab_quantized_sample_step(const void* h, const uint8_t* h_scales, int6
     // (in the same workspace: the logits are done with it)
     const sv::SampleArgs a = sample_args(logits_out, n, rows, n, idx, idx_mode, temperature, top_k, top_p, min_p, u, tok_out, prob_out, ws);
     return sv::launch_sample(a, s) == hipSuccess ? SV_OK : SV_ERR_HIP;
+}
+
+int specvocab_token_logprobs(const void* logits, int64_t ld, int64_t rows, int64_t n, int dt, const int32_t* idx, int idx_mode,
+                             const float* temperature, const int32_t* tokens, int64_t given, int64_t top, float* logprob_out,
+                             float* entropy_out, int32_t* top_tok_out, float* top_logprob_out, float* state_out, void* ws, size_t ws_bytes,
+                             void* stream) {
+    if (!logits || (given > 0 && (!tokens || !logprob_out)) || (top > 0 && (!top_tok_out || !top_logprob_out))) return SV_ERR_NULL;
+    if (given == 0 && top == 0 && !entropy_out && !state_out) return SV_ERR_NULL;
+    int st = check_token_shape(rows, n, ld, dt, given, top);
+    if (st != SV_OK) return st;
+    if (idx && !mode_ok(idx_mode)) return SV_ERR_DTYPE;
+    if (!aligned_to(logits, dt) || !aligned16(state_out)) return SV_ERR_ALIGN;
+    st = check_scratch(sv::token_scratch_bytes(rows, n, (int)top), ws, ws_bytes);
+    if (st != SV_OK) return st;
+    if (ensure_device() != SV_OK) return SV_ERR_HIP;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (!idx && given > 0) st = validate_indices(tokens, rows * given, n, s, true);
+    if (st != SV_OK) return st;
+    sv::TokenArgs a{};
+    a.logits = static_cast<const char*>(logits);
+    a.row_bytes = ld * esize_of(dt);
+    a.n = n;
+    a.rows = rows;
+    a.idx = idx;
+    a.idx_row_stride = idx && base_mode(idx_mode) == SV_IDX_PER_ROW ? n : 0;
+    a.temperature = temperature;
+    a.tokens = tokens;
+    a.given = (int)given;
+    a.top = (int)top;
+    a.logprob = logprob_out;
+    a.entropy = entropy_out;
+    a.top_tok = top_tok_out;
+    a.top_logprob = top_logprob_out;
+    a.state = reinterpret_cast<float4*>(state_out);
+    a.scratch = static_cast<char*>(ws);
+    return sv::launch_token_logprobs(dt, a, s) == hipSuccess ? SV_OK : SV_ERR_HIP;
+}
+
+int specvocab_token_logprobs_grad(const void* logits, int64_t ld, int64_t rows, int64_t n, int dt, const float* temperature,
+                                  const int32_t* tokens, int64_t given, const float* state, const float* grad_logprob,
+                                  const float* grad_entropy, void* grad_out, int64_t ld_grad, int grad_dt, void* stream) {
+    if (!logits || !state || !grad_out || (!grad_logprob && !grad_entropy) || (grad_logprob && !tokens)) return SV_ERR_NULL;
+    int st = check_token_shape(rows, n, ld, dt, given, 0);
+    if (st != SV_OK) return st;
+    if (grad_logprob && given < 1) return SV_ERR_SHAPE;
+    st = check_gradient(grad_out, ld_grad, grad_dt, n);
+    if (st != SV_OK) return st;
+    if (!aligned_to(logits, dt) || !aligned16(state)) return SV_ERR_ALIGN;
+    if (ensure_device() != SV_OK) return SV_ERR_HIP;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (grad_logprob) st = validate_indices(tokens, rows * given, n, s, true);
+    if (st != SV_OK) return st;
+    sv::TokenGradArgs a{};
+    a.logits = static_cast<const char*>(logits);
+    a.row_bytes = ld * esize_of(dt);
+    a.n = n;
+    a.rows = rows;
+    a.temperature = temperature;
+    a.tokens = tokens;
+    a.given = (int)given;
+    a.state = reinterpret_cast<const float4*>(state);
+    a.grad_logprob = grad_logprob;
+    a.grad_entropy = grad_entropy;
+    a.grad = static_cast<char*>(grad_out);
+    a.grad_row_bytes = ld_grad * esize_of(grad_dt);
+    return sv::launch_token_grad(dt, grad_dt, a, s) == hipSuccess ? SV_OK : SV_ERR_HIP;
+}
+
+int specvocab_distill(const void* logits, int64_t ld, int64_t rows, int64_t n, int dt, const int32_t* tok, const float* teacher,
+                      int64_t known, int kind, float temperature, const float* weight, float* loss_out, float* state_out, void* grad_out,
+                      int64_t ld_grad, int grad_dt, void* ws, size_t ws_bytes, void* stream) {
+    sv::DistillArgs a = distill_args(logits, ld, rows, n, dt, tok, teacher, known, kind, temperature, weight, state_out, grad_out, ld_grad, grad_dt);
+    a.loss = loss_out;
+    a.scratch = static_cast<char*>(ws);
+    if (!loss_out) return SV_ERR_NULL;
+    int st = check_distill(a, ld, dt, known);
+    if (st == SV_OK && grad_out) st = check_gradient(grad_out, ld_grad, grad_dt, n);
+    if (st == SV_OK) st = check_scratch(sv::distill_scratch_bytes(rows, n), ws, ws_bytes);
+    if (st != SV_OK) return st;
+    if (ensure_device() != SV_OK) return SV_ERR_HIP;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    st = validate_indices(tok, rows * known, n, s, true);
+    if (st != SV_OK) return st;
+    return sv::launch_distill(dt, grad_dt, a, s) == hipSuccess ? SV_OK : SV_ERR_HIP;
+}
+
+int specvocab_distill_grad(const void* logits, int64_t ld, int64_t rows, int64_t n, int dt, const int32_t* tok, const float* teacher,
+                           int64_t known, int kind, float temperature, const float* weight, const float* state, void* grad_out,
+                           int64_t ld_grad, int grad_dt, void* stream) {
+    const sv::DistillArgs a =
+        distill_args(logits, ld, rows, n, dt, tok, teacher, known, kind, temperature, weight, state, grad_out, ld_grad, grad_dt);
+    if (!state || !grad_out) return SV_ERR_NULL;
+    int st = check_distill(a, ld, dt, known);
+    if (st == SV_OK) st = check_gradient(grad_out, ld_grad, grad_dt, n);
+    if (st != SV_OK) return st;
+    if (ensure_device() != SV_OK) return SV_ERR_HIP;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    st = validate_indices(tok, rows * known, n, s, true);
+    if (st != SV_OK) return st;
+    return sv::launch_distill_grad(dt, grad_dt, a, s) == hipSuccess ? SV_OK : SV_ERR_HIP;
 }
 
 int specvocab_stream_read_probe(const void* buf, size_t bytes, void* ws, size_t ws_bytes, void* stream) {

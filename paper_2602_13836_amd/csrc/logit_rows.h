@@ -1,0 +1,326 @@
+// What the operators over finished rows of logits share: a row, or a part of one, read in 16-byte vectors from any alignment, and the
+// running softmax sums of a thread, a workgroup and a row's parts.
+#pragma once
+#include "sv_device.h"
+#include "sv_launch.h"
+
+#include <math.h>
+
+#include <type_traits>
+
+namespace sv {
+
+constexpr float kLowestF32 = -3.402823466e38f;
+constexpr float kNoMass = -1000.0f;                       // 2^-1000 is 0: an exponent that has to stay finite is cut off here
+
+// rows begin at any element: bfloat16 ones at any even address
+typedef unsigned int u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef unsigned int u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+
+template <int DT>
+constexpr int kVec = DT == DT_BF16 ? 8 : 4;               // logits of a vector
+template <int DT>
+constexpr int kBytes = DT == DT_BF16 ? 2 : 4;
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }      // within an ulp; below 2^-126: 0
+
+template <int DT>
+__device__ __forceinline__ u32x4 masked_vector() {
+    const uint32_t w = DT == DT_BF16 ? 0xFF80FF80u : 0xFF800000u;
+    return u32x4{w, w, w, w};
+}
+
+template <int DT>
+__device__ __forceinline__ void widen(const u32x4 v, float* f) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w = v[i];
+        if constexpr (DT == DT_BF16) {
+            f[2 * i] = __uint_as_float(w << 16);
+            f[2 * i + 1] = __uint_as_float(w & 0xFFFF0000u);
+        } else {
+            f[i] = __uint_as_float(w);
+        }
+    }
+}
+
+template <int DT>
+__device__ __forceinline__ float logit_at(const char* row, int64_t place) {
+    if constexpr (DT == DT_BF16) return __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(row)[place] << 16);
+    else return reinterpret_cast<const float*>(row)[place];
+}
+
+// A row's places [first, first + n): a part begins at a multiple of 32 places (a word of the bitmaps) and has at most 2^18 of them.
+struct Part {
+    const char* p;       // of its first logit
+    int64_t first;
+    int n;
+    int full;            // whole vectors
+    int vectors;         // with the one that the row ends in
+};
+
+template <int DT>
+__device__ __forceinline__ Part part_of(const char* row, int64_t n, int64_t first, int64_t most) {
+    Part t;
+    t.first = first;
+    t.n = (int)(n - first < most ? n - first : most);
+    t.p = row + first * kBytes<DT>;
+    t.full = t.n / kVec<DT>;
+    t.vectors = (t.n + kVec<DT> - 1) / kVec<DT>;
+    return t;
+}
+
+// (of a vector behind the part's end: masked places)
+template <int DT>
+__device__ __forceinline__ u32x4 load_guarded(const Part& t, int iv) {
+    if (iv < t.full) return *reinterpret_cast<const u32x4_any*>(t.p + (uint32_t)iv * 16u);
+    u32x4 v = masked_vector<DT>();
+    if (iv < t.vectors) {
+        const int left = t.n - iv * kVec<DT>;
+        const char* p = t.p + (uint32_t)iv * 16u;
+#pragma unroll
+        for (int i = 0; i < kVec<DT>; ++i) {
+            if (i >= left) continue;
+            if constexpr (DT == DT_BF16) {
+                const uint32_t x = reinterpret_cast<const uint16_t*>(p)[i];
+                v[i / 2] = (i & 1) ? (v[i / 2] & 0xFFFFu) | (x << 16) : (v[i / 2] & 0xFFFF0000u) | x;
+            } else {
+                v[i] = reinterpret_cast<const uint32_t*>(p)[i];
+            }
+        }
+    }
+    return v;
+}
+
+// f(chunk, v[U]) for every chunk of U x NT vectors of the part: thread t has vectors t, t + NT, ... of it
+template <int DT, int NT, int U, class F>
+__device__ __forceinline__ void for_chunks(const Part& t, F&& f) {
+    const int chunks = (t.vectors + U * NT - 1) / (U * NT), whole = t.full / (U * NT);
+    for (int c = 0; c < chunks; ++c) {
+        const int at = c * (U * NT) + (int)threadIdx.x;
+        u32x4 v[U];
+        if (c < whole) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const u32x4_any*>(t.p + (uint32_t)(at + u * NT) * 16u);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = load_guarded<DT>(t, at + u * NT);
+        }
+        f(c, v);
+    }
+}
+
+// ---- softmax sums, in octaves: with a = log2(e) / T, s = sum of 2^(a z - c) and, for entropies, e = sum of 2^(a z - c) (a z - c)
+//
+// The reference c is a times the largest logit so far, rounded: whatever it is rounded to, the sums are exactly those of that reference, so a
+// logit takes one fused multiply-add and no error grows with the logits' size.  Where a z leaves float32's range (logits of the
+// type's lowest value, of 2^127 and more, tiny temperatures) the sums come out as 0, infinite or NaN, and the row is summed again by
+// differences (EXACT): 2^(a (z - m)).
+struct RowSums {
+    float m;        // largest logit, -inf where there is none; NaNs are not in it
+    float s, e;     // relative to m
+};
+
+template <bool ENTROPY, bool EXACT>
+struct Running {
+    float m = -INFINITY, c = kLowestF32, s = 0.0f, e = 0.0f;
+
+    template <int N>
+    __device__ __forceinline__ float add(const float (&z)[N], float a) {
+        float most = z[0];
+#pragma unroll
+        for (int i = 1; i < N; ++i) most = fmaxf(most, z[i]);
+        m = fmaxf(m, most);
+        float now, d;
+        if constexpr (EXACT) {
+            now = fmaxf(m, kLowestF32);
+            d = (c - now) * a;
+        } else {
+            now = fminf(fmaxf(m * a, kLowestF32), -kLowestF32);
+            d = c - now;
+        }
+        d = fmaxf(d, kNoMass);
+        const float r = exp2_fast(d);
+        if constexpr (ENTROPY) e = r * fmaf(d, s, e);
+        s *= r;
+        c = now;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float y = EXACT ? (z[i] - now) * a : fmaf(z[i], a, -now);
+            const float p = exp2_fast(y);
+            s += p;
+            if constexpr (ENTROPY) e = fmaf(p, fmaxf(y, kNoMass), e);
+        }
+        return most;
+    }
+};
+
+// sums of two sets of places
+template <bool ENTROPY>
+__device__ __forceinline__ RowSums joined(const RowSums& x, const RowSums& y, float a) {
+    RowSums r;
+    r.m = fmaxf(x.m, y.m);
+    const float m = fmaxf(r.m, kLowestF32);
+    const float dx = fmaxf((fmaxf(x.m, kLowestF32) - m) * a, kNoMass), dy = fmaxf((fmaxf(y.m, kLowestF32) - m) * a, kNoMass);
+    const float rx = exp2_fast(dx), ry = exp2_fast(dy);
+    r.s = x.s * rx + y.s * ry;
+    r.e = ENTROPY ? rx * fmaf(dx, x.s, x.e) + ry * fmaf(dy, y.s, y.e) : 0.0f;
+    return r;
+}
+
+// The workgroup's sums, the same for every thread and in the same order every time.  scratch: 4 * NT / 64 floats.
+template <bool ENTROPY, bool EXACT, int NT>
+__device__ __forceinline__ RowSums block_sums(const Running<ENTROPY, EXACT>& t, float a, float* scratch) {
+    constexpr int kWaves = NT / 64;
+    const float c = wave_max_f32(t.c);
+    const float d = fmaxf(EXACT ? (t.c - c) * a : t.c - c, kNoMass);
+    const float r = exp2_fast(d);
+    float s = wave_sum(t.s * r), e = 0.0f;
+    if constexpr (ENTROPY) e = wave_sum(r * fmaf(d, t.s, t.e));
+    const float m = wave_max_f32(t.m);
+    const int wave = threadIdx.x >> 6;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) {
+        scratch[4 * wave] = m;
+        scratch[4 * wave + 1] = c;
+        scratch[4 * wave + 2] = s;
+        scratch[4 * wave + 3] = e;
+    }
+    __syncthreads();
+    RowSums out;
+    out.m = -INFINITY;
+    float top = kLowestF32;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        out.m = fmaxf(out.m, scratch[4 * w]);
+        top = fmaxf(top, scratch[4 * w + 1]);
+    }
+    out.s = out.e = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        const float dw = fmaxf(EXACT ? (scratch[4 * w + 1] - top) * a : scratch[4 * w + 1] - top, kNoMass);
+        const float rw = exp2_fast(dw);
+        out.s = fmaf(scratch[4 * w + 2], rw, out.s);
+        if constexpr (ENTROPY) out.e += rw * fmaf(dw, scratch[4 * w + 2], scratch[4 * w + 3]);
+    }
+    // from the reference to the largest logit itself (EXACT: they are the same)
+    if (!EXACT && out.s > 0.0f) {
+        const float shift = -fmaf(fmaxf(out.m, kLowestF32), a, -top);
+        const float rs = exp2_fast(shift);
+        if constexpr (ENTROPY) out.e = rs * fmaf(shift, out.s, out.e);
+        out.s *= rs;
+    }
+    return out;
+}
+
+// true if sums by reference may be those of a row that float32 does not hold so: it is summed again
+__device__ __forceinline__ bool sum_again(const RowSums& r) { return !(r.s < INFINITY) || (!(r.s > 0.0f) && r.m > -INFINITY); }
+
+template <int NT>
+__device__ __forceinline__ double block_sum_f64(double x, double* scratch) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = x;
+    __syncthreads();
+    double sum = 0.0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) sum += scratch[w];
+    return sum;
+}
+
+template <int NT>
+__device__ __forceinline__ float block_max_f32(float x, float* scratch) {
+    x = wave_max_f32(x);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = x;
+    __syncthreads();
+    float m = scratch[0];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) m = fmaxf(m, scratch[w]);
+    return m;
+}
+
+// ---- places that are marked: a bitmap of a part's places, and a table from place to number
+template <int NT>
+__device__ __forceinline__ void clear_words(uint32_t* p, int words, uint32_t value = 0u) {
+    for (int i = threadIdx.x; i < words; i += NT) p[i] = value;
+}
+
+// the marks of vector iv
+template <int DT>
+__device__ __forceinline__ uint32_t marks_of(const uint32_t* bits, int iv) {
+    if constexpr (DT == DT_BF16) return reinterpret_cast<const uint8_t*>(bits)[iv];
+    else return (reinterpret_cast<const uint8_t*>(bits)[iv >> 1] >> ((iv & 1) * 4)) & 15u;
+}
+
+constexpr int32_t kEmptySlot = -1;
+template <int SLOTS>
+__device__ __forceinline__ uint32_t slot_of(int32_t place) { return ((uint32_t)place * 2654435761u) >> (32 - __builtin_ctz(SLOTS)); }
+
+// equal places get the same slot (`again`: it was there); there are at most SLOTS / 2 of them
+template <int SLOTS>
+__device__ __forceinline__ uint32_t insert_place(int32_t* keys, int32_t place, bool& again) {
+    uint32_t s = slot_of<SLOTS>(place);
+    for (;;) {
+        const int32_t was = atomicCAS(&keys[s], kEmptySlot, place);
+        again = was == place;
+        if (was == kEmptySlot || was == place) return s;
+        s = (s + 1) & (SLOTS - 1);
+    }
+}
+template <int SLOTS>
+__device__ __forceinline__ uint32_t find_place(const int32_t* keys, int32_t place) {
+    uint32_t s = slot_of<SLOTS>(place);
+    while (keys[s] != place) s = (s + 1) & (SLOTS - 1);
+    return s;
+}
+
+// launches of less than 2^32 threads, a range of rows each: f(first row, rows)
+template <class F>
+hipError_t over_rows(int64_t rows, int64_t threads_of_row, F&& f) {
+    const int64_t most = 0xFFFFFFFFLL / threads_of_row;
+    for (int64_t at = 0; at < rows; at += most) {
+        f(at, rows - at < most ? rows - at : most);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+// ---- gradients: a vector's worth of them, rounded to nearest even, at any alignment
+template <int GDT, int N>
+__device__ __forceinline__ void store_gradient(char* row, int64_t place, const float (&g)[N], int left) {
+    if constexpr (GDT == DT_BF16) {
+        typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+        uint32_t w[N / 2];
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            const bf16x2_t b = {(__bf16)g[2 * i], (__bf16)g[2 * i + 1]};
+            w[i] = __builtin_bit_cast(uint32_t, b);
+        }
+        char* p = row + place * 2;
+        if (left >= N) {
+            if constexpr (N == 8) *reinterpret_cast<u32x4_any*>(p) = u32x4{w[0], w[1], w[2], w[3]};
+            else *reinterpret_cast<u32x2_any*>(p) = u32x2_any{w[0], w[1]};
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i < left) reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+        }
+    } else {
+        float* p = reinterpret_cast<float*>(row) + place;
+        if (left >= N) {
+#pragma unroll
+            for (int q = 0; q < N / 4; ++q)
+                *reinterpret_cast<u32x4_any*>(p + 4 * q) = u32x4{__float_as_uint(g[4 * q]), __float_as_uint(g[4 * q + 1]),
+                                                                 __float_as_uint(g[4 * q + 2]), __float_as_uint(g[4 * q + 3])};
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i < left) p[i] = g[i];
+        }
+    }
+}
+
+}  // namespace sv

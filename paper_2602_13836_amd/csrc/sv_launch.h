@@ -420,4 +420,63 @@ size_t sample_scratch_bytes(int64_t rows, int64_t n);
 hipError_t configure_sample_lds();
 hipError_t launch_sample(const SampleArgs& a, hipStream_t stream);
 
+// ---- log probabilities of given tokens, entropy, largest alternatives; their gradient (token_kernels.hip)
+struct TokenArgs {
+    const char* logits;      // rows of n in `dt`, row_bytes apart
+    int64_t row_bytes;
+    int64_t n;
+    int64_t rows;
+    const int32_t* idx;      // token ids of a row's places, or nullptr
+    int64_t idx_row_stride;  // n (per row) or 0 (one list)
+    const float* temperature;      // [rows], or nullptr
+    const int32_t* tokens;   // [rows x given]
+    int given, top;
+    float* logprob;          // [rows x given]
+    float* entropy;          // [rows], or nullptr
+    int32_t* top_tok;        // [rows x top]
+    float* top_logprob;
+    float4* state;           // [rows], or nullptr
+    char* scratch;           // token_scratch_bytes
+};
+constexpr int64_t kTopVocab = 1 << 23;         // places of a row of which the largest are looked for
+size_t token_scratch_bytes(int64_t rows, int64_t n, int top);
+hipError_t launch_token_logprobs(int dt, const TokenArgs& a, hipStream_t stream);
+struct TokenGradArgs {
+    const char* logits;
+    int64_t row_bytes;
+    int64_t n;
+    int64_t rows;
+    const float* temperature;
+    const int32_t* tokens;
+    int given;
+    const float4* state;
+    const float* grad_logprob;     // [rows x given], or nullptr
+    const float* grad_entropy;     // [rows], or nullptr
+    char* grad;              // rows of n, grad_row_bytes apart; may be the logits
+    int64_t grad_row_bytes;
+};
+hipError_t launch_token_grad(int dt, int grad_dt, const TokenGradArgs& a, hipStream_t stream);
+
+// ---- divergence from a teacher of which the largest logits are known, and its gradient (distill_kernels.hip)
+struct DistillArgs {
+    const char* logits;      // rows of n in `dt`, row_bytes apart
+    int64_t row_bytes;
+    int64_t n;
+    int64_t rows;
+    const int32_t* tok;      // [rows x known]
+    const float* teacher;    // [rows x known]
+    int known;
+    int kind;                // sv_teacher
+    float temperature;
+    const float* weight;     // [rows], or nullptr
+    float* loss;             // [rows]
+    float4* state;           // [rows], or nullptr (not where only the gradient is asked for)
+    char* grad;              // rows of n, grad_row_bytes apart, or nullptr; may be the logits
+    int64_t grad_row_bytes;
+    char* scratch;           // distill_scratch_bytes
+};
+size_t distill_scratch_bytes(int64_t rows, int64_t n);
+hipError_t launch_distill(int dt, int grad_dt, const DistillArgs& a, hipStream_t stream);
+hipError_t launch_distill_grad(int dt, int grad_dt, const DistillArgs& a, hipStream_t stream);
+
 }  // namespace sv

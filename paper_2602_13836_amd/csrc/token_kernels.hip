@@ -1,0 +1,510 @@
+// Log probabilities of given tokens, entropy and largest alternatives of finished rows of logits, and the logits' gradient of them.
+//
+// With T a row's temperature, M its largest logit and S = sum of exp((z - M) / T):
+//     log p_v = (z_v - M) / T - log S,     H = log S - sum of exp((z - M) / T) (z - M) / T / S,
+//     d/dz_v = (sum over given tokens j of g_j ([v = t_j] - p_v) - g_H p_v (log p_v + H)) / T.
+//
+// Forward, one pass: every thread keeps the largest logit and the sums relative to it (logit_rows.h).  The alternatives come from what the
+// pass has seen anyway: a thread's largest logit of each chunk (16 or 32 logits) goes to LDS, the `top`-th largest of the threads'
+// largest logits is a bound that at least `top` logits reach, and only the chunks that reach it -- about `top` of them -- are read
+// again and their places ranked.  A row in which more than 1024 places reach the bound (equal logits) is selected by digits of the keys.
+// Few rows are cut into parts, whose sums and alternatives a second launch joins.
+#include "logit_rows.h"
+
+namespace sv {
+
+namespace {
+
+constexpr int kMaxTop = 64, kMaxGiven = 64;
+constexpr int kCandidates = 1024;
+constexpr int64_t kTopPart = 1 << 17, kSumPart = 1 << 18;      // places of a part: 32 KB of chunks' largest logits; 32-bit offsets
+constexpr int kMaxTopParts = 64;
+constexpr int kRowThreads = 512, kChunkVectors = 4;
+constexpr int kMergeThreads = 256;
+constexpr uint32_t kLowestKey = 0x00800000u;               // of the lowest finite float
+
+__device__ __forceinline__ float row_temperature(const float* temperature, int64_t row) {
+    if (!temperature) return 1.0f;
+    const float t = temperature[row];
+    return t > 0.0f ? fminf(fmaxf(t, 0x1p-20f), 0x1p20f) : 1.0f;
+}
+__device__ __forceinline__ float octaves_per_logit(float t) { return 1.4426950408889634f / t; }
+
+// what a part leaves for the launch that joins a row's parts
+struct PartSums {
+    float m, s, e, pad;
+};
+
+struct TokenScratch {
+    PartSums* sums;          // [rows x parts]
+    uint64_t* top;           // [rows x parts x top], largest first; 0: none
+    int parts;
+    int64_t part;            // places of a part
+};
+
+// A bound that at least `want` of the keys reach and, unless equal keys prevent it, no more than `enough`.  Every wavefront finds it for itself.
+template <int N, class K>
+__device__ __forceinline__ K bound_of(const K (&k)[N], K least, K most, int want, int enough) {
+    K lo = least, hi = most + 1;                           // all keys reach lo, none hi
+    while (hi - lo > 1) {
+        const K mid = lo + (hi - lo) / 2;
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) n += __popcll(__builtin_amdgcn_ballot_w64(k[i] >= mid));
+        if (n >= want) {
+            lo = mid;
+            if (n <= enough) break;
+        } else {
+            hi = mid;
+        }
+    }
+    return lo;
+}
+
+template <int NT>
+struct TopWork {
+    uint64_t found[kCandidates];
+    uint64_t best[kMaxTop];
+    uint32_t keys[NT];           // the threads' largest logits; later the chunks that are read again
+    uint32_t scan[NT / 64];
+    uint32_t bins[256];
+    uint32_t n_chunks, n_found, digit, above;
+};
+
+// best[0 .. top): the largest of found[0 .. n), largest first, 0 where there are no more.  The keys differ.
+template <int NT>
+__device__ __forceinline__ void rank_found(const uint64_t* found, int n, uint64_t* best, int top) {
+    for (int i = threadIdx.x; i < top; i += NT) best[i] = 0ull;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += NT) {
+        const uint64_t mine = found[i];
+        int larger = 0;
+        for (int j = 0; j < n; ++j) larger += found[j] > mine ? 1 : 0;
+        if (larger < top) best[larger] = mine;
+    }
+    __syncthreads();
+}
+
+// The part's largest places by digits of their keys: any number of equal logits.  w.found[0 .. return) are the `top` largest.
+template <int DT, int NT>
+__device__ __forceinline__ int select_by_digits(const Part& t, int top, TopWork<NT>& w) {
+    uint32_t prefix = 0, want = (uint32_t)top;              // of the keys with the prefix, `want` are still looked for
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        clear_words<NT>(w.bins, 256);
+        __syncthreads();
+        for_chunks<DT, NT, 1>(t, [&](int, const u32x4(&v)[1]) {
+            float z[kVec<DT>];
+            widen<DT>(v[0], z);
+#pragma unroll
+            for (int i = 0; i < kVec<DT>; ++i) {
+                const uint32_t key = f32_to_ord(z[i]);
+                const bool in = key >= kLowestKey && (shift == 24 || (key >> (shift + 8)) == prefix);
+                const uint32_t bin = (key >> shift) & 255u;
+                // (equal logits all meet in one bin: one lane adds for those that agree with it)
+                const uint64_t some = __builtin_amdgcn_ballot_w64(in);
+                if (some == 0ull) continue;
+                const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)bin, __ffsll((unsigned long long)some) - 1);
+                const uint64_t same = __builtin_amdgcn_ballot_w64(in && bin == first);
+                if (in && bin != first) atomicAdd(&w.bins[bin], 1u);
+                if ((int)(threadIdx.x & 63) == __ffsll((unsigned long long)some) - 1) atomicAdd(&w.bins[first], (uint32_t)__popcll(same));
+            }
+        });
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            uint32_t above = 0;
+            int d = 255;
+            for (; d > 0 && above + w.bins[d] < want; --d) above += w.bins[d];
+            w.digit = (uint32_t)d;
+            w.above = above;
+        }
+        __syncthreads();
+        prefix = (prefix << 8) | w.digit;
+        want -= w.above;
+        __syncthreads();
+    }
+    // the keys above the one that was found, in any order, and the first `want` places that have it
+    if (threadIdx.x == 0) w.n_found = 0;
+    __syncthreads();
+    for_chunks<DT, NT, 1>(t, [&](int c, const u32x4(&v)[1]) {
+        float z[kVec<DT>];
+        widen<DT>(v[0], z);
+        const int at = (c * NT + (int)threadIdx.x) * kVec<DT>;
+#pragma unroll
+        for (int i = 0; i < kVec<DT>; ++i)
+            if (f32_to_ord(z[i]) > prefix && f32_to_ord(z[i]) >= kLowestKey) {
+                const uint32_t slot = atomicAdd(&w.n_found, 1u);
+                if (slot < (uint32_t)kMaxTop) w.found[slot] = make_key(z[i], (int32_t)(t.first + at + i));
+            }
+    });
+    __syncthreads();
+    const uint32_t above = min(w.n_found, (uint32_t)kMaxTop);
+    if (prefix < kLowestKey) return (int)above;             // the part has fewer places than are looked for
+    uint32_t taken = 0;
+    for (int at = 0; at < t.vectors && taken < want; at += NT) {
+        const u32x4 v = load_guarded<DT>(t, at + (int)threadIdx.x);
+        float z[kVec<DT>];
+        widen<DT>(v, z);
+        uint32_t n = 0;
+#pragma unroll
+        for (int i = 0; i < kVec<DT>; ++i) n += f32_to_ord(z[i]) == prefix ? 1u : 0u;
+        uint32_t slot = taken + block_prefix_exclusive<NT / 64>(n, w.scan);
+#pragma unroll
+        for (int i = 0; i < kVec<DT>; ++i)
+            if (f32_to_ord(z[i]) == prefix) {
+                if (slot < want) w.found[above + slot] = make_key(z[i], (int32_t)(t.first + (at + (int)threadIdx.x) * kVec<DT> + i));
+                ++slot;
+            }
+        if (threadIdx.x == NT - 1) w.above = slot;
+        __syncthreads();
+        taken = w.above;
+        __syncthreads();
+    }
+    return (int)(above + min(taken, want));
+}
+
+// w.best: the part's `top` largest places.  chunk_most: a thread's largest logit of each chunk, NT of them after the other.
+template <int DT, int NT>
+__device__ __forceinline__ void select_top(const Part& t, int top, float thread_most, const float* chunk_most, TopWork<NT>& w) {
+    constexpr int kEach = NT / 64;
+    const int tid = threadIdx.x;
+    w.keys[tid] = f32_to_ord(thread_most);
+    if (tid == 0) w.n_chunks = w.n_found = 0;
+    __syncthreads();
+    uint32_t k[kEach], most = 0, least = 0xFFFFFFFEu;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        k[i] = w.keys[i * 64 + (tid & 63)];
+        most = max(most, k[i]);
+        least = min(least, k[i]);
+    }
+    most = min(wave_max_u32(most), 0xFFFFFFFEu);
+    least = ~wave_max_u32(~least);
+    // (-inf is below every key that counts)
+    const uint32_t bound = max(bound_of(k, least, most, top, top + top / 2 + 8), kLowestKey);
+    const float least_logit = ord_to_f32(bound);
+    __syncthreads();                                       // the keys' array takes the chunks
+    const int chunks = (t.vectors + kChunkVectors * NT - 1) / (kChunkVectors * NT);
+    for (int i = tid; i < chunks * NT; i += NT)
+        if (chunk_most[i] >= least_logit) {
+            const uint32_t slot = atomicAdd(&w.n_chunks, 1u);
+            if (slot < NT) w.keys[slot] = (uint32_t)i;
+        }
+    __syncthreads();
+    const int listed = (int)w.n_chunks;
+    int n;
+    bool fits = listed <= NT;
+    if (fits) {
+        for (int i = tid; i < listed * kChunkVectors; i += NT) {
+            const int chunk = (int)w.keys[i / kChunkVectors];
+            const int iv = (chunk / NT) * (kChunkVectors * NT) + (i % kChunkVectors) * NT + chunk % NT;
+            float z[kVec<DT>];
+            widen<DT>(load_guarded<DT>(t, iv), z);
+#pragma unroll
+            for (int e = 0; e < kVec<DT>; ++e)
+                if (z[e] >= least_logit) {
+                    const uint32_t slot = atomicAdd(&w.n_found, 1u);
+                    if (slot < (uint32_t)kCandidates) w.found[slot] = make_key(z[e], (int32_t)(t.first + iv * kVec<DT> + e));
+                }
+        }
+        __syncthreads();
+        n = (int)w.n_found;
+        fits = n <= kCandidates;
+    }
+    if (!fits) n = select_by_digits<DT, NT>(t, top, w);
+    __syncthreads();
+    rank_found<NT>(w.found, n, w.best, top);
+}
+
+// ---- a row's results, by one workgroup
+struct FindWork {
+    uint32_t bits[256];
+    int32_t token[kMaxGiven];
+    int32_t place[kMaxGiven];
+};
+
+// w.place[j]: the first place whose id is the j-th given token, n where there is none
+template <int NT>
+__device__ __forceinline__ void find_tokens(const TokenArgs& a, int64_t row, FindWork& w) {
+    const int tid = threadIdx.x, n = (int)a.n;
+    clear_words<NT>(w.bits, 256);
+    __syncthreads();
+    if (tid < a.given) {
+        const int32_t t = a.tokens[row * a.given + tid];
+        w.token[tid] = t;
+        w.place[tid] = n;
+        const uint32_t h = slot_of<8192>(t);
+        atomicOr(&w.bits[h >> 5], 1u << (h & 31));
+    }
+    __syncthreads();
+    const int32_t* ids = a.idx + row * a.idx_row_stride;
+    for (int i = tid; i < n; i += NT) {
+        const int32_t id = ids[i];
+        const uint32_t h = slot_of<8192>(id);
+        if ((w.bits[h >> 5] >> (h & 31)) & 1u)
+            for (int j = 0; j < a.given; ++j)
+                if (w.token[j] == id && id >= 0) atomicMin(&w.place[j], i);
+    }
+    __syncthreads();
+}
+
+// r: the row's sums, e relative to the largest logit in octaves.  best: LDS
+template <int DT, int NT>
+__device__ __forceinline__ void write_row(const TokenArgs& a, int64_t row, float t, const RowSums& r, const uint64_t* best, FindWork& fw) {
+    const int tid = threadIdx.x;
+    const bool empty = r.s == 0.0f;
+    const float m = empty ? 0.0f : r.m, log_s = logf(r.s);
+    if (a.idx && a.given > 0) find_tokens<NT>(a, row, fw);
+    if (tid < a.given) {
+        const int64_t i = row * a.given + tid;
+        int64_t place = a.tokens[i];
+        if (a.idx) place = fw.place[tid];
+        float out = -INFINITY;
+        if (place >= 0 && place < a.n && !empty) out = (logit_at<DT>(a.logits + row * a.row_bytes, place) - m) / t - log_s;
+        a.logprob[i] = r.s != r.s ? r.s : out;
+    }
+    if (tid < a.top) {
+        const uint64_t key = best[tid];
+        const bool some = key != 0ull && r.s == r.s;
+        const int32_t place = key_token(key);
+        a.top_tok[row * a.top + tid] = !some ? -1 : a.idx ? a.idx[row * a.idx_row_stride + place] : place;
+        a.top_logprob[row * a.top + tid] = r.s != r.s ? r.s : some ? (key_value(key) - m) / t - log_s : -INFINITY;
+    }
+    if (tid == 0) {
+        const float h = empty ? 0.0f : log_s - 0.6931471805599453f * (r.e / r.s);
+        if (a.entropy) a.entropy[row] = h;
+        if (a.state) a.state[row] = make_float4(m, r.s, h, 0.0f);
+    }
+}
+
+// One workgroup per part of a row (WHOLE: per row, which it finishes).
+template <int DT, int NT, bool TOP, bool WHOLE>
+__global__ __launch_bounds__(NT) void token_rows_kernel(const TokenArgs a, const TokenScratch x, const int64_t first_row) {
+    extern __shared__ float chunk_most[];
+    __shared__ float sums[4 * NT / 64];
+    __shared__ std::conditional_t<TOP, TopWork<NT>, char> top_work;
+    __shared__ std::conditional_t<WHOLE, FindWork, char> find_work;
+    const int64_t row = first_row + (WHOLE ? blockIdx.x : blockIdx.x / (unsigned)x.parts);
+    const int part_at = WHOLE ? 0 : (int)(blockIdx.x % (unsigned)x.parts);
+    const char* logits = a.logits + row * a.row_bytes;
+    const Part t = part_of<DT>(logits, a.n, (int64_t)part_at * x.part, x.part);
+    const float temp = row_temperature(a.temperature, row);
+    const float c = octaves_per_logit(temp);
+    constexpr int kN = kChunkVectors * kVec<DT>;
+    RowSums r;
+    float thread_most;
+    auto pass = [&](auto exact) {
+        Running<true, decltype(exact)::value> run;
+        for_chunks<DT, NT, kChunkVectors>(t, [&](int chunk, const u32x4(&v)[kChunkVectors]) {
+            float z[kN];
+#pragma unroll
+            for (int u = 0; u < kChunkVectors; ++u) widen<DT>(v[u], z + u * kVec<DT>);
+            const float most = run.add(z, c);
+            if constexpr (TOP) chunk_most[chunk * NT + (int)threadIdx.x] = most;
+        });
+        thread_most = run.m;
+        r = block_sums<true, decltype(exact)::value, NT>(run, c, sums);
+    };
+    pass(std::false_type{});
+    if (sum_again(r)) pass(std::true_type{});
+    const uint64_t* best = nullptr;
+    if constexpr (TOP) {
+        if (r.s == r.s) select_top<DT, NT>(t, a.top, thread_most, chunk_most, top_work);
+        best = top_work.best;
+    }
+    if constexpr (WHOLE) {
+        write_row<DT, NT>(a, row, temp, r, best, find_work);
+    } else {
+        const int64_t at = row * x.parts + part_at;
+        if (threadIdx.x == 0) x.sums[at] = PartSums{r.m, r.s, r.e, 0.0f};
+        if constexpr (TOP)
+            if ((int)threadIdx.x < a.top) x.top[at * a.top + threadIdx.x] = r.s == r.s ? best[threadIdx.x] : 0ull;
+    }
+}
+
+template <int DT, bool TOP>
+__global__ __launch_bounds__(kMergeThreads) void token_join_kernel(const TokenArgs a, const TokenScratch x, const int64_t first_row) {
+    constexpr int NT = kMergeThreads, kEach = kMaxTopParts * kMaxTop / NT;
+    __shared__ RowSums sums[NT / 64];
+    __shared__ FindWork find_work;
+    __shared__ uint64_t best[kMaxTop];
+    __shared__ uint64_t found[TOP ? kMaxTopParts * kMaxTop : 1];
+    __shared__ uint64_t most_of[TOP ? NT : 1];
+    __shared__ uint32_t n_found;
+    const int tid = threadIdx.x;
+    const int64_t row = first_row + blockIdx.x;
+    const float temp = row_temperature(a.temperature, row);
+    const float c = octaves_per_logit(temp);
+    RowSums r{-INFINITY, 0.0f, 0.0f};
+    for (int p = tid; p < x.parts; p += NT) {
+        const PartSums y = x.sums[row * x.parts + p];
+        r = joined<true>(r, RowSums{y.m, y.s, y.e}, c);
+    }
+    uint64_t keys[kEach];
+    if constexpr (TOP) {
+        const uint64_t* list = x.top + row * x.parts * a.top;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) keys[i] = tid + i * NT < x.parts * a.top ? list[tid + i * NT] : 0ull;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) r = joined<true>(r, RowSums{__shfl_xor(r.m, o), __shfl_xor(r.s, o), __shfl_xor(r.e, o)}, c);
+    if ((tid & 63) == 0) sums[tid >> 6] = r;
+    if constexpr (TOP) {
+        uint64_t mine = 0ull;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) mine = umax64(mine, keys[i]);
+        most_of[tid] = mine;
+        if (tid == 0) n_found = 0;
+    }
+    __syncthreads();
+    r = sums[0];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) r = joined<true>(r, sums[w], c);
+    if constexpr (TOP) {
+        uint64_t k[NT / 64], most = 0ull;
+#pragma unroll
+        for (int i = 0; i < NT / 64; ++i) {
+            k[i] = most_of[i * 64 + (tid & 63)];
+            most = umax64(most, k[i]);
+        }
+        // keys that are there differ, so the bound lets few pass: at most kEach from each thread
+        const uint64_t bound = umax64(bound_of(k, (uint64_t)0, wave_max_u64(most), a.top, a.top + a.top / 2 + 8), 1ull);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (keys[i] >= bound) found[atomicAdd(&n_found, 1u)] = keys[i];
+        __syncthreads();
+        rank_found<NT>(found, (int)n_found, best, a.top);
+    }
+    write_row<DT, NT>(a, row, temp, r, best, find_work);
+}
+
+// ---- gradient: grad_v = e (k0 + k1 x) with x = (z_v - M) / T in octaves and e = 2^x, and g_j / T more at the given tokens
+constexpr int kGradThreads = 256, kGradVectors = 4;
+constexpr int64_t kGradPart = 1 << 14;
+constexpr int kGradSlots = 128;
+
+template <int DT, int GDT>
+__global__ __launch_bounds__(kGradThreads) void token_grad_kernel(const TokenGradArgs a, const int64_t first_row, const int parts) {
+    constexpr int NT = kGradThreads, V = kVec<DT>;
+    __shared__ uint32_t bits[kGradPart / 32];
+    __shared__ int32_t keys[kGradSlots];
+    __shared__ float value[kGradSlots];
+    __shared__ float g_of[kMaxGiven];
+    __shared__ int32_t token[kMaxGiven];
+    const int tid = threadIdx.x;
+    const int64_t row = first_row + blockIdx.x / (unsigned)parts;
+    const Part t = part_of<DT>(a.logits + row * a.row_bytes, a.n, (int64_t)(blockIdx.x % (unsigned)parts) * kGradPart, kGradPart);
+    const float4 st = a.state[row];
+    const float temp = row_temperature(a.temperature, row), inv_t = 1.0f / temp;
+    const float c = octaves_per_logit(temp);
+    const bool tokens = a.grad_logprob != nullptr;
+    clear_words<NT>(bits, (t.n + 31) / 32);
+    if (tid < kGradSlots) keys[tid] = kEmptySlot;
+    if (tokens && tid < a.given) {
+        token[tid] = a.tokens[row * a.given + tid];
+        g_of[tid] = a.grad_logprob[row * a.given + tid];
+    }
+    __syncthreads();
+    float g_sum = 0.0f;
+    if (tokens) {
+        for (int j = 0; j < a.given; ++j) g_sum += token[j] >= 0 && token[j] < a.n ? g_of[j] : 0.0f;
+        const int64_t at = tid < a.given ? token[tid] - t.first : -1;
+        if (at >= 0 && at < t.n) {
+            atomicOr(&bits[at >> 5], 1u << (at & 31));
+            // a token that is given several times has the sum
+            float mine = 0.0f;
+            for (int j = 0; j < a.given; ++j) mine += token[j] == token[tid] ? g_of[j] : 0.0f;
+            bool again;
+            value[insert_place<kGradSlots>(keys, (int32_t)at, again)] = mine * inv_t;
+        }
+    }
+    __syncthreads();
+    const float gh = a.grad_entropy ? a.grad_entropy[row] : 0.0f;
+    const bool empty = st.y == 0.0f;
+    const float scale = empty ? 0.0f : -inv_t / st.y;
+    const float k0 = empty ? 0.0f : scale * (g_sum + gh * (st.z - logf(st.y))), k1 = scale * gh * 0.6931471805599453f;
+    char* out = a.grad + row * a.grad_row_bytes;
+    for_chunks<DT, NT, kGradVectors>(t, [&](int chunk, const u32x4(&v)[kGradVectors]) {
+#pragma unroll
+        for (int u = 0; u < kGradVectors; ++u) {
+            const int iv = chunk * (kGradVectors * NT) + u * NT + tid;
+            if (iv >= t.vectors) continue;
+            float z[V], g[V];
+            widen<DT>(v[u], z);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float y = (z[i] - st.x) * c;
+                g[i] = exp2_fast(y) * fmaf(k1, fmaxf(y, kNoMass), k0);
+            }
+            const uint32_t marks = marks_of<DT>(bits, iv);
+            if (marks != 0u) {
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (((marks >> i) & 1u) && !(z[i] == -INFINITY)) g[i] += value[find_place<kGradSlots>(keys, iv * V + i)];
+            }
+            store_gradient<GDT>(out, t.first + (int64_t)iv * V, g, t.n - iv * V);
+        }
+    });
+}
+
+// Parts that a row is cut into: enough workgroups for the chip, 2048 places at least each.
+constexpr int64_t kWantBlocks = 1024;
+TokenScratch scratch_of(int64_t rows, int64_t n, int top, char* at) {
+    TokenScratch x{};
+    const int64_t most = top > 0 ? kTopPart : kSumPart;
+    int64_t parts = (n + most - 1) / most;
+    int64_t wanted = (kWantBlocks + rows - 1) / rows;
+    if (wanted > kMaxTopParts) wanted = kMaxTopParts;
+    if (wanted > n / 2048) wanted = n / 2048;
+    if (wanted > parts) parts = wanted;
+    x.part = (n + parts - 1) / parts;
+    x.part = (x.part + 31) / 32 * 32;
+    x.parts = (int)((n + x.part - 1) / x.part);
+    x.sums = reinterpret_cast<PartSums*>(at);
+    x.top = reinterpret_cast<uint64_t*>(at + (size_t)rows * x.parts * sizeof(PartSums));
+    return x;
+}
+
+}  // namespace
+
+size_t token_scratch_bytes(int64_t rows, int64_t n, int top) {
+    const TokenScratch x = scratch_of(rows, n, top, nullptr);
+    return x.parts > 1 ? (size_t)rows * x.parts * (sizeof(PartSums) + (size_t)top * sizeof(uint64_t)) : 0;
+}
+
+hipError_t launch_token_logprobs(int dt, const TokenArgs& a, hipStream_t stream) {
+    const TokenScratch x = scratch_of(a.rows, a.n, a.top, a.scratch);
+    const int vec = dt == DT_BF16 ? 8 : 4;
+    constexpr int NT = kRowThreads;
+    const int64_t vectors = (x.part + vec - 1) / vec;
+    const int64_t chunks = (vectors + kChunkVectors * NT - 1) / (kChunkVectors * NT);
+    const size_t lds = a.top > 0 ? (size_t)chunks * NT * sizeof(float) : 0;
+    auto rows_launch = [&](auto kernel) {
+        return over_rows(a.rows, (int64_t)x.parts * NT, [&](int64_t first, int64_t rows) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * x.parts)), dim3(NT), lds, stream, a, x, first);
+        });
+    };
+    auto of_type = [&](auto type) {
+        constexpr int DT = decltype(type)::value;
+        if (x.parts == 1) return a.top > 0 ? rows_launch(&token_rows_kernel<DT, NT, true, true>) : rows_launch(&token_rows_kernel<DT, NT, false, true>);
+        const hipError_t e = a.top > 0 ? rows_launch(&token_rows_kernel<DT, NT, true, false>) : rows_launch(&token_rows_kernel<DT, NT, false, false>);
+        if (e != hipSuccess) return e;
+        return over_rows(a.rows, kMergeThreads, [&](int64_t first, int64_t rows) {
+            if (a.top > 0) hipLaunchKernelGGL((token_join_kernel<DT, true>), dim3((unsigned)rows), dim3(kMergeThreads), 0, stream, a, x, first);
+            else hipLaunchKernelGGL((token_join_kernel<DT, false>), dim3((unsigned)rows), dim3(kMergeThreads), 0, stream, a, x, first);
+        });
+    };
+    return dt == DT_BF16 ? of_type(std::integral_constant<int, DT_BF16>{}) : of_type(std::integral_constant<int, DT_F32>{});
+}
+
+hipError_t launch_token_grad(int dt, int grad_dt, const TokenGradArgs& a, hipStream_t stream) {
+    const int parts = (int)((a.n + kGradPart - 1) / kGradPart);
+    auto go = [&](auto kernel) {
+        return over_rows(a.rows, (int64_t)parts * kGradThreads, [&](int64_t first, int64_t rows) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * parts)), dim3(kGradThreads), 0, stream, a, first, parts);
+        });
+    };
+    if (dt == DT_BF16) return grad_dt == DT_BF16 ? go(&token_grad_kernel<DT_BF16, DT_BF16>) : go(&token_grad_kernel<DT_BF16, DT_F32>);
+    return grad_dt == DT_BF16 ? go(&token_grad_kernel<DT_F32, DT_BF16>) : go(&token_grad_kernel<DT_F32, DT_F32>);
+}
+
+}  // namespace sv
