@@ -6,12 +6,12 @@
 // m the mass that counts: sum_j p_j [+ p'].  In brackets: the mass p' = 1 - sum_j p_j that the list leaves, against the mass q' of all places
 // that are not listed.
 //
-// One pass sums exp((z - M) / T) over the places that are NOT listed (a bitmap of the row in LDS tells; a vector of 4 or 8 places costs one LDS
-// byte), so q' is a sum of its own and not the small difference of two large ones; the listed places are gathered and added.  The
-// gradient of every other place is then one factor times exp((z - M') / T).  A listed place finds its sum of p_j in a hash table in LDS: no
-// place is written twice, and a token that is listed twice has both its masses, whatever the order.
+// One pass sums exp((z - M) / T).  With the rest as one more token it sums over the places that are NOT listed (a bitmap of the row in LDS
+// tells; a vector of 4 or 8 places costs one LDS byte), so q' is a sum of its own and not the small difference of two large ones, and the
+// listed places are gathered and added.  The gradient of every place that is not listed is then one factor times 2^(a z - c).  Listed places are
+// written once more when the workgroup has written its part; a token that is listed twice has both its masses, whatever the order.
 //
-// Loss and gradient at once: the workgroup that has summed a row walks it again, out of the caches mostly.  Few rows are cut into parts.
+// Loss and gradient at once: the workgroup that has summed a row walks it again, backwards.  Few rows are cut into parts.
 #include "logit_rows.h"
 
 namespace sv {
@@ -22,7 +22,7 @@ constexpr int kThreads = 512, kVectors = 4;
 constexpr int kMaxKnown = 512, kSlots = 1024;
 constexpr int64_t kWholeRow = 1 << 18;                  // places of a part at most: 32 KB of marks
 constexpr int kRest = 2;                               // SV_TEACHER_REST
-static_assert(kMaxKnown <= kThreads, "an entry of the list per thread");
+static_assert(kMaxKnown == kThreads, "an entry of the list per thread");
 
 struct DistillScratch {
     float2* sums;            // [rows x parts]: largest logit that is not listed, sum relative to it
@@ -33,11 +33,12 @@ struct DistillScratch {
 
 struct ListWork {
     int32_t keys[kSlots];
-    float value[kSlots];
     double p[kMaxKnown];
     int32_t id[kMaxKnown];
     double sums[kThreads / 64];
     float scratch[4 * kThreads / 64];
+    double teacher_sums[kThreads / 64];      // of a wavefront's entries
+    float teacher_most[kThreads / 64];
     uint32_t again;          // a token is listed twice
 };
 
@@ -64,46 +65,75 @@ struct Teacher {
     double p, log_p, mass, left;
 };
 __device__ __forceinline__ Teacher teacher_of(const DistillArgs& a, const Entry& e, ListWork& w) {
-    Teacher t;
+    Teacher t{0.0, 0.0, 0.0, 0.0};
     const bool none = e.value == -INFINITY;              // (a NaN counts, and spreads)
-    if (a.kind == 0) {
-        const float most = block_max_f32<kThreads>(e.value, w.scratch);
-        const double x = ((double)e.value - (double)most) / (double)a.temperature;
+    const int wave = threadIdx.x >> 6, waves = (a.known + 63) >> 6;
+    float most = 0.0f;
+    // exponentials in 64 bits, for what the list leaves of 1; wavefronts without entries have none to take
+    if (wave < waves) {
+        double x = (double)e.value;
+        if (a.kind == 0) {
+            most = fmaxf(wave_max_f32(e.value), kLowestF32);
+            x = (x - (double)most) / (double)a.temperature;
+        }
+        t.log_p = x;
         t.p = none ? 0.0 : exp(x);
-        const double sum = block_sum_f64<kThreads>(t.p, w.sums);
-        t.log_p = x - log(sum);
-        t.p = none ? 0.0 : t.p / sum;
-    } else {
-        t.p = none ? 0.0 : exp((double)e.value);
-        t.log_p = (double)e.value;
+        double sum = t.p;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+        if ((threadIdx.x & 63) == 0) {
+            w.teacher_sums[wave] = sum;
+            w.teacher_most[wave] = most;
+        }
     }
-    t.mass = block_sum_f64<kThreads>(t.p, w.sums);
-    t.left = a.kind == kRest ? fmax(1.0 - t.mass, 0.0) : 0.0;
+    __syncthreads();
+    if (a.kind == 0) {
+        float top = w.teacher_most[0];
+        for (int i = 1; i < waves; ++i) top = fmaxf(top, w.teacher_most[i]);
+        double total = 0.0;
+        for (int i = 0; i < waves; ++i) total += waves == 1 ? w.teacher_sums[i] : w.teacher_sums[i] * exp(((double)w.teacher_most[i] - (double)top) / (double)a.temperature);
+        if (wave < waves) {
+            const double down = waves == 1 ? 0.0 : ((double)most - (double)top) / (double)a.temperature;
+            t.log_p += down - log(total);
+            t.p = none ? 0.0 : t.p * (waves == 1 ? 1.0 : exp(down)) / total;
+        }
+        t.mass = total == 0.0 ? 0.0 : total != total ? total : 1.0;
+    } else {
+        for (int i = 0; i < waves; ++i) t.mass += w.teacher_sums[i];
+        t.left = a.kind == kRest ? fmax(1.0 - t.mass, 0.0) : 0.0;
+    }
     return t;
 }
 
-// The row's loss and state from the sums over the places that are not listed.  z: the logit at this thread's entry.
+// The row's loss and state.  sums: over the places that are not listed where the rest counts, else over all.  z: the logit at this thread's entry.
 __device__ __forceinline__ float4 finish_row(const DistillArgs& a, int64_t row, float weight, const Entry& e, const Teacher& t, float z,
-                                             const RowSums& rest, float c, ListWork& w) {
-    // each token once
-    bool first = e.there;
-    if (w.again != 0u && e.there)
-        for (int i = 0; i < (int)threadIdx.x; ++i) first = first && w.id[i] != e.id;
-    const float m = fmaxf(block_max_f32<kThreads>(e.there ? z : -INFINITY, w.scratch), rest.m);
-    const float ref = fmaxf(m, kLowestF32);
-    const double of_rest = exp2(fmax(((double)fmaxf(rest.m, kLowestF32) - (double)ref) * c, (double)kNoMass));
-    const double of_list = block_sum_f64<kThreads>(first ? (double)exp2_fast((z - ref) * c) : 0.0, w.sums);
-    const double s = (double)rest.s * of_rest + of_list, log_s = log(s);
+                                             const RowSums& sums, float c, ListWork& w) {
+    float m = sums.m;
+    double s = (double)sums.s;
+    if (a.kind == kRest) {
+        // each token once
+        bool first = e.there;
+        if (w.again != 0u && e.there)
+            for (int i = 0; i < (int)threadIdx.x; ++i) first = first && w.id[i] != e.id;
+        m = fmaxf(block_max_f32<kThreads>(z, w.scratch), sums.m);
+        const float ref = fmaxf(m, kLowestF32);
+        s *= exp2(fmax(((double)fmaxf(sums.m, kLowestF32) - (double)ref) * c, (double)kNoMass));
+        s += block_sum_f64<kThreads>(first ? (double)exp2_fast((z - ref) * c) : 0.0, w.sums);
+    }
+    const double ref = (double)fmaxf(m, kLowestF32), log_s = log(s);
     double part = 0.0;
     if (t.p != 0.0) {
-        const double log_q = z == -INFINITY || s == 0.0 ? -INFINITY : ((double)z - (double)ref) / (double)a.temperature - log_s;
+        const double log_q = z == -INFINITY || s == 0.0 ? -INFINITY : ((double)z - ref) / (double)a.temperature - log_s;
         part = t.p * (t.log_p - log_q);
     }
     double loss = block_sum_f64<kThreads>(part, w.sums);
     if (s != s) loss = s;
-    if (t.left > 0.0 && rest.s != 0.0f)
-        loss += t.left * (log(t.left) - (((double)rest.m - (double)ref) / (double)a.temperature + log((double)rest.s) - log_s));
-    const float4 state = make_float4(s == 0.0 ? 0.0f : m, (float)s, rest.s == 0.0f ? 0.0f : rest.m, rest.s);
+    float4 state = make_float4(s == 0.0 ? 0.0f : m, (float)s, 0.0f, 0.0f);
+    if (a.kind == kRest && sums.s != 0.0f) {
+        state.z = sums.m;
+        state.w = sums.s;
+        if (t.left > 0.0) loss += t.left * (log(t.left) - (((double)sums.m - ref) / (double)a.temperature + log((double)sums.s) - log_s));
+    }
     if (threadIdx.x == 0) {
         a.loss[row] = (float)((double)weight * loss);
         if (a.state) a.state[row] = state;
@@ -113,73 +143,81 @@ __device__ __forceinline__ float4 finish_row(const DistillArgs& a, int64_t row, 
 
 // the factors of a row's gradient
 struct Factors {
-    float m, of_listed;      // listed places: of_listed * 2^(c (z - m)) - their sum of p w / T
-    float rest_m, of_rest;   // others: of_rest * 2^(c (z - rest_m))
-    double scale;            // w / T
+    float m, of_listed;      // listed places: of_listed * 2^(c (z - m)) - scale * their sum of p
+    Exponent x;
+    float of_rest;           // others: of_rest * 2^(octaves_at(x, z))
+    float scale;             // w / T
 };
 __device__ __forceinline__ Factors factors_of(const DistillArgs& a, float weight, const Teacher& t, const float4 st, float c) {
     Factors f;
-    f.scale = (double)weight / (double)a.temperature;
-    const bool rest = st.w != 0.0f, some = st.y != 0.0f;
-    const double left = rest ? t.left : 0.0, of_row = some ? (t.mass + left) / (double)st.y : 0.0;
+    f.scale = weight / a.temperature;
+    const bool some = st.y != 0.0f, rest = a.kind == kRest, other = rest && st.w != 0.0f;
+    const float left = other ? (float)t.left : 0.0f, of_row = some ? f.scale * (float)(t.mass + (double)left) / st.y : 0.0f;
     f.m = st.x;
-    f.of_listed = (float)(f.scale * of_row);
-    f.rest_m = st.z;
-    const double share = exp2(fmax(((double)st.z - (double)st.x) * c, (double)kNoMass));
-    f.of_rest = rest ? (float)(f.scale * (of_row * share - left / (double)st.w)) : 0.0f;
+    f.of_listed = of_row;
+    f.x = exponent_of(rest ? st.z : st.x, c);
+    float of_rest = of_row;
+    if (rest) of_rest = other ? of_row * exp2_fast(fmaxf((st.z - st.x) * c, kNoMass)) - f.scale * (left / st.w) : 0.0f;
+    f.of_rest = of_rest * exp2_fast(f.x.shift);
     return f;
 }
+// the gradient at a listed place that holds z, of a token with mass p
+__device__ __forceinline__ float listed_gradient(const Factors& f, float z, double p) {
+    return z == -INFINITY ? f.of_listed * 0.0f : (float)((double)(f.of_listed * exp2_fast((z - f.m) * f.x.a)) - (double)f.scale * p);
+}
 
-// marks, table and sums of p w / T of the entries inside a part; every thread calls
-__device__ __forceinline__ void enter_list(const Part& part, const Entry& e, uint32_t* bits, ListWork& w) {
-    clear_words<kThreads>(bits, (part.n + 31) / 32);
+// the list into LDS, and whether a token is in it twice; every thread calls
+__device__ __forceinline__ void enter_list(const Entry& e, ListWork& w) {
     clear_words<kThreads>(reinterpret_cast<uint32_t*>(w.keys), kSlots, (uint32_t)kEmptySlot);
     if (threadIdx.x == 0) w.again = 0u;
     __syncthreads();
-    const int64_t at = e.there ? e.id - part.first : -1;
-    if (at >= 0 && at < part.n) {
-        bool again;
-        insert_place<kSlots>(w.keys, (int32_t)at, again);
-        if (again) w.again = 1u;
-        atomicOr(&bits[at >> 5], 1u << (at & 31));
-    }
-    if ((int)threadIdx.x < kMaxKnown) w.id[threadIdx.x] = e.there ? e.id : -1;
+    if (e.there && enter_place<kSlots>(w.keys, e.id)) w.again = 1u;
+    w.id[threadIdx.x] = e.there ? e.id : -1;
     __syncthreads();
 }
-__device__ __forceinline__ void enter_masses(const Part& part, const Entry& e, const Teacher& t, double scale, int known, ListWork& w) {
-    if ((int)threadIdx.x < kMaxKnown) w.p[threadIdx.x] = t.p;
+// marks of the entries inside a part; every thread calls
+__device__ __forceinline__ void mark_list(const Part& part, const Entry& e, uint32_t* bits) {
+    clear_words<kThreads>(bits, (part.n + 31) / 32);
     __syncthreads();
     const int64_t at = e.there ? e.id - part.first : -1;
-    if (at >= 0 && at < part.n) {
-        double p = t.p;
-        if (w.again != 0u) {
-            p = 0.0;
-            for (int i = 0; i < known; ++i) p += w.id[i] == e.id ? w.p[i] : 0.0;
-        }
-        w.value[find_place<kSlots>(w.keys, (int32_t)at)] = (float)(scale * p);
-    }
+    if (at >= 0 && at < part.n) atomicOr(&bits[at >> 5], 1u << (at & 31));
     __syncthreads();
+}
+// the mass of this thread's token, from all entries that name it; every thread calls
+__device__ __forceinline__ double mass_of_token(const Entry& e, const Teacher& t, int known, ListWork& w) {
+    if (w.again == 0u) return t.p;                          // (the same for all)
+    w.p[threadIdx.x] = t.p;
+    __syncthreads();
+    double p = 0.0;
+    if (e.there)
+        for (int i = 0; i < known; ++i) p += w.id[i] == e.id ? w.p[i] : 0.0;
+    return p;
 }
 
-template <int DT>
-__device__ __forceinline__ RowSums sum_rest(const Part& t, float c, const uint32_t* bits, float* scratch) {
-    constexpr int kN = kVectors * kVec<DT>;
+// sums of a part: of all its places, or (REST) of those that are not marked.  AGAIN: the part is read once more soon
+template <int DT, bool REST, bool AGAIN>
+__device__ __forceinline__ RowSums sum_part(const Part& t, float c, const uint32_t* bits, float* scratch) {
+    constexpr int V = kVec<DT>, kN = kVectors * V;
     auto pass = [&](auto exact) {
         Running<false, decltype(exact)::value> run;
-        for_chunks<DT, kThreads, kVectors>(t, [&](int chunk, const u32x4(&v)[kVectors]) {
+        for_chunks<DT, kThreads, kVectors, !AGAIN>(t, [&](int chunk, const u32x4(&v)[kVectors]) {
             float z[kN];
-            uint32_t marks[kVectors], any = 0;
 #pragma unroll
-            for (int u = 0; u < kVectors; ++u) {
-                const int iv = chunk * (kVectors * kThreads) + u * kThreads + (int)threadIdx.x;
-                marks[u] = iv < t.vectors ? marks_of<DT>(bits, iv) : 0u;
-                any |= marks[u];
-                widen<DT>(v[u], z + u * kVec<DT>);
-            }
-            if (any != 0u) {
+            for (int u = 0; u < kVectors; ++u) widen<DT>(v[u], z + u * V);
+            if constexpr (REST) {
+                uint32_t marks[kVectors];
 #pragma unroll
-                for (int i = 0; i < kN; ++i)
-                    if ((marks[i / kVec<DT>] >> (i % kVec<DT>)) & 1u) z[i] = -INFINITY;
+                for (int u = 0; u < kVectors; ++u) {
+                    const int iv = chunk * (kVectors * kThreads) + u * kThreads + (int)threadIdx.x;
+                    marks[u] = iv < t.vectors ? marks_of<DT>(bits, iv) : 0u;
+                }
+#pragma unroll
+                for (int u = 0; u < kVectors; ++u)
+                    if (marks[u] != 0u) {
+#pragma unroll
+                        for (int i = 0; i < V; ++i)
+                            if ((marks[u] >> i) & 1u) z[u * V + i] = -INFINITY;
+                    }
             }
             run.add(z, c);
         });
@@ -189,29 +227,29 @@ __device__ __forceinline__ RowSums sum_rest(const Part& t, float c, const uint32
     return sum_again(r) ? pass(std::true_type{}) : r;
 }
 
+// The part's gradient; z, p: the logit and the mass of this thread's token, where it lies in the part.  Every thread calls.
 template <int DT, int GDT>
-__device__ __forceinline__ void write_gradient(const Part& t, const Factors& f, float c, const uint32_t* bits, const ListWork& w, char* out) {
+__device__ __forceinline__ void write_gradient(const Part& t, const Factors& f, const Entry& e, float z_listed, double p, char* out) {
     constexpr int V = kVec<DT>;
-    for_chunks<DT, kThreads, kVectors>(t, [&](int chunk, const u32x4(&v)[kVectors]) {
+    auto pass = [&](auto exact) {
+        for_chunks<DT, kThreads, kVectors, true, true>(t, [&](int chunk, const u32x4(&v)[kVectors]) {
 #pragma unroll
-        for (int u = 0; u < kVectors; ++u) {
-            const int iv = chunk * (kVectors * kThreads) + u * kThreads + (int)threadIdx.x;
-            if (iv >= t.vectors) continue;
-            float z[V], g[V];
-            widen<DT>(v[u], z);
+            for (int u = 0; u < kVectors; ++u) {
+                const int iv = chunk * (kVectors * kThreads) + u * kThreads + (int)threadIdx.x;
+                if (iv >= t.vectors) continue;
+                float z[V], g[V];
+                widen<DT>(v[u], z);
 #pragma unroll
-            for (int i = 0; i < V; ++i) g[i] = f.of_rest * exp2_fast((z[i] - f.rest_m) * c);
-            const uint32_t marks = marks_of<DT>(bits, iv);
-            if (marks != 0u) {
-#pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if ((marks >> i) & 1u)
-                        g[i] = z[i] == -INFINITY ? f.of_listed * 0.0f
-                                                 : fmaf(f.of_listed, exp2_fast((z[i] - f.m) * c), -w.value[find_place<kSlots>(w.keys, iv * V + i)]);
+                for (int i = 0; i < V; ++i) g[i] = f.of_rest * exp2_fast(octaves_at<decltype(exact)::value>(f.x, z[i]));
+                store_gradient<GDT>(out, t.first + (int64_t)iv * V, g, t.n - iv * V);
             }
-            store_gradient<GDT>(out, t.first + (int64_t)iv * V, g, t.n - iv * V);
-        }
-    });
+        });
+    };
+    if (f.x.exact) pass(std::true_type{});
+    else pass(std::false_type{});
+    __syncthreads();
+    const int64_t at = e.there ? e.id - t.first : -1;
+    if (at >= 0 && at < t.n) store_one<GDT>(out, e.id, listed_gradient(f, z_listed, p));
 }
 template <int DT, int GDT>
 __device__ __forceinline__ void write_zeros(const Part& t, char* out) {
@@ -240,18 +278,24 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(const DistillArg
     const float c = 1.4426950408889634f / a.temperature;
     const Entry e = entry_of(a, row);
     const float z = e.there ? logit_at<DT>(logits, e.id) : -INFINITY;
-    enter_list(t, e, bits, w);
-    const RowSums rest = sum_rest<DT>(t, c, bits, w.scratch);
+    enter_list(e, w);
+    RowSums sums;
+    if (a.kind == kRest) {
+        mark_list(t, e, bits);
+        sums = sum_part<DT, true, GDT >= 0>(t, c, bits, w.scratch);
+    } else {
+        sums = sum_part<DT, false, GDT >= 0>(t, c, bits, w.scratch);
+    }
     const Teacher teacher = teacher_of(a, e, w);
-    const float4 st = finish_row(a, row, weight, e, teacher, z, rest, c, w);
+    const float4 st = finish_row(a, row, weight, e, teacher, z, sums, c, w);
     if constexpr (GDT >= 0) {
         const Factors f = factors_of(a, weight, teacher, st, c);
-        enter_masses(t, e, teacher, f.scale, a.known, w);
-        write_gradient<DT, GDT>(t, f, c, bits, w, a.grad + row * a.grad_row_bytes);
+        const double p = mass_of_token(e, teacher, a.known, w);
+        write_gradient<DT, GDT>(t, f, e, z, p, a.grad + row * a.grad_row_bytes);
     }
 }
 
-// One workgroup per part of a row: the sums over the places that are not listed.
+// One workgroup per part of a row: its sums.
 template <int DT>
 __global__ __launch_bounds__(kThreads) void distill_parts_kernel(const DistillArgs a, const DistillScratch x, const int64_t first_row) {
     extern __shared__ uint32_t bits[];
@@ -260,13 +304,14 @@ __global__ __launch_bounds__(kThreads) void distill_parts_kernel(const DistillAr
     const int at = (int)(blockIdx.x % (unsigned)x.parts);
     if (weight_of_row(a, row) == 0.0f) return;
     const Part t = part_of<DT>(a.logits + row * a.row_bytes, a.n, at * x.part, x.part);
-    const Entry e = entry_of(a, row);
-    clear_words<kThreads>(bits, (t.n + 31) / 32);
-    __syncthreads();
-    const int64_t place = e.there ? e.id - t.first : -1;
-    if (place >= 0 && place < t.n) atomicOr(&bits[place >> 5], 1u << (place & 31));
-    __syncthreads();
-    const RowSums r = sum_rest<DT>(t, 1.4426950408889634f / a.temperature, bits, scratch);
+    const float c = 1.4426950408889634f / a.temperature;
+    RowSums r;
+    if (a.kind == kRest) {
+        mark_list(t, entry_of(a, row), bits);
+        r = sum_part<DT, true, false>(t, c, bits, scratch);
+    } else {
+        r = sum_part<DT, false, false>(t, c, bits, scratch);
+    }
     if (threadIdx.x == 0) x.sums[row * x.parts + at] = make_float2(r.m, r.s);
 }
 
@@ -288,15 +333,7 @@ __global__ __launch_bounds__(kThreads) void distill_join_kernel(const DistillArg
     const float c = 1.4426950408889634f / a.temperature;
     const Entry e = entry_of(a, row);
     const float z = e.there ? logit_at<DT>(a.logits + row * a.row_bytes, e.id) : -INFINITY;
-    clear_words<kThreads>(reinterpret_cast<uint32_t*>(w.keys), kSlots, (uint32_t)kEmptySlot);
-    if (tid == 0) w.again = 0u;
-    __syncthreads();
-    if (e.there) {
-        bool again;
-        insert_place<kSlots>(w.keys, e.id, again);
-        if (again) w.again = 1u;
-    }
-    if (tid < kMaxKnown) w.id[tid] = e.there ? e.id : -1;
+    enter_list(e, w);
     RowSums r{-INFINITY, 0.0f, 0.0f};
     for (int p = tid; p < x.parts; p += kThreads) {
         const float2 y = x.sums[row * x.parts + p];
@@ -313,12 +350,15 @@ __global__ __launch_bounds__(kThreads) void distill_join_kernel(const DistillArg
     finish_row(a, row, weight, e, teacher, z, r, c, w);
 }
 
-// One workgroup per part of a row: its gradient from the row's state.
-constexpr int64_t kGradPart = 1 << 15;
+// One workgroup per part of a row: its gradient from the row's state.  Small parts, asked for before anything else is looked at (2048 x 128256
+// bfloat16, a fifth of the rows without weight: 167 us).
+constexpr int64_t kGradPart = 1 << 13;
 template <int DT, int GDT>
 __global__ __launch_bounds__(kThreads) void distill_grad_kernel(const DistillArgs a, const int64_t first_row, const int parts) {
+    constexpr int V = kVec<DT>, U = (int)kGradPart / (kThreads * V);
     __shared__ uint32_t bits[kGradPart / 32];
     __shared__ ListWork w;
+    const int tid = threadIdx.x;
     const int64_t row = first_row + blockIdx.x / (unsigned)parts;
     const float weight = weight_of_row(a, row);
     const Part t = part_of<DT>(a.logits + row * a.row_bytes, a.n, (int64_t)(blockIdx.x % (unsigned)parts) * kGradPart, kGradPart);
@@ -327,14 +367,46 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(const DistillArg
         write_zeros<DT, GDT>(t, out);
         return;
     }
+    u32x4 v[U];
+    load_chunk<DT, kThreads, U, true>(t, 0, v);
     const float c = 1.4426950408889634f / a.temperature;
     const float4 st = a.state[row];
     const Entry e = entry_of(a, row);
-    enter_list(t, e, bits, w);
-    const Teacher teacher = teacher_of(a, e, w);
+    const int64_t at = e.there ? e.id - t.first : -1;
+    const bool here = at >= 0 && at < t.n;
+    const float z_listed = here ? logit_at<DT>(t.p, at) : -INFINITY;
+    if (tid < (int)kGradPart / 32) bits[tid] = 0u;
+    if (tid == 0) w.again = 0u;
+    const Teacher teacher = teacher_of(a, e, w);            // (a barrier)
+    if (here && ((atomicOr(&bits[at >> 5], 1u << (at & 31)) >> (at & 31)) & 1u)) w.again = 1u;
+    w.id[tid] = e.there ? e.id : -1;
+    w.p[tid] = teacher.p;
     const Factors f = factors_of(a, weight, teacher, st, c);
-    enter_masses(t, e, teacher, f.scale, a.known, w);
-    write_gradient<DT, GDT>(t, f, c, bits, w, out);
+    // every read of the part is done before any of its places is written: the gradient may replace the logits
+    __syncthreads();
+    auto pass = [&](auto exact) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int iv = u * kThreads + tid;
+            if (iv >= t.vectors) continue;
+            float z[V], g[V];
+            widen<DT>(v[u], z);
+#pragma unroll
+            for (int i = 0; i < V; ++i) g[i] = f.of_rest * exp2_fast(octaves_at<decltype(exact)::value>(f.x, z[i]));
+            store_gradient<GDT>(out, t.first + (int64_t)iv * V, g, t.n - iv * V);
+        }
+    };
+    if (f.x.exact) pass(std::true_type{});
+    else pass(std::false_type{});
+    __syncthreads();
+    if (here) {
+        double p = teacher.p;
+        if (w.again != 0u) {                               // a token that is listed several times has all its masses
+            p = 0.0;
+            for (int i = 0; i < a.known; ++i) p += w.id[i] == e.id ? w.p[i] : 0.0;
+        }
+        store_one<GDT>(out, e.id, listed_gradient(f, z_listed, p));
+    }
 }
 
 // Parts that a row is cut into: enough workgroups for the chip, 4096 places at least each.

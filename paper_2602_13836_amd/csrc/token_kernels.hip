@@ -79,6 +79,7 @@ __device__ __forceinline__ void rank_found(const uint64_t* found, int n, uint64_
     for (int i = threadIdx.x; i < n; i += NT) {
         const uint64_t mine = found[i];
         int larger = 0;
+#pragma unroll 8
         for (int j = 0; j < n; ++j) larger += found[j] > mine ? 1 : 0;
         if (larger < top) best[larger] = mine;
     }
@@ -222,46 +223,57 @@ struct FindWork {
     int32_t place[kMaxGiven];
 };
 
-// w.place[j]: the first place whose id is the j-th given token, n where there is none
-template <int NT>
-__device__ __forceinline__ void find_tokens(const TokenArgs& a, int64_t row, FindWork& w) {
+// The logit of this thread's given token; `there`: it has a place.  Every thread calls.
+struct Given {
+    bool there;
+    float z;
+};
+template <int DT, int NT>
+__device__ __forceinline__ Given given_token(const TokenArgs& a, int64_t row, FindWork& w) {
     const int tid = threadIdx.x, n = (int)a.n;
-    clear_words<NT>(w.bits, 256);
-    __syncthreads();
-    if (tid < a.given) {
-        const int32_t t = a.tokens[row * a.given + tid];
-        w.token[tid] = t;
-        w.place[tid] = n;
-        const uint32_t h = slot_of<8192>(t);
-        atomicOr(&w.bits[h >> 5], 1u << (h & 31));
+    Given g{false, -INFINITY};
+    int32_t place = tid < a.given ? a.tokens[row * a.given + tid] : -1;
+    if (a.idx && a.given > 0) {
+        // the first place whose id is the token's: the tokens' hashes in a bitmap tell which of the list's ids to look at
+        clear_words<NT>(w.bits, 256);
+        __syncthreads();
+        if (tid < a.given) {
+            w.token[tid] = place;
+            w.place[tid] = n;
+            const uint32_t h = slot_of<8192>(place);
+            atomicOr(&w.bits[h >> 5], 1u << (h & 31));
+        }
+        __syncthreads();
+        typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+        const int32_t* ids = a.idx + row * a.idx_row_stride;
+        auto look = [&](int32_t id, int at) {
+            const uint32_t h = slot_of<8192>(id);
+            if ((w.bits[h >> 5] >> (h & 31)) & 1u)
+                for (int j = 0; j < a.given; ++j)
+                    if (w.token[j] == id && id >= 0) atomicMin(&w.place[j], at);
+        };
+#pragma unroll 4
+        for (int i = 4 * tid; i + 3 < n; i += 4 * NT) {
+            const i32x4_any id = *reinterpret_cast<const i32x4_any*>(ids + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) look(id[e], i + e);
+        }
+        if (tid < (n & 3)) look(ids[(n & ~3) + tid], (n & ~3) + tid);
+        __syncthreads();
+        place = tid < a.given ? w.place[tid] : -1;
     }
-    __syncthreads();
-    const int32_t* ids = a.idx + row * a.idx_row_stride;
-    for (int i = tid; i < n; i += NT) {
-        const int32_t id = ids[i];
-        const uint32_t h = slot_of<8192>(id);
-        if ((w.bits[h >> 5] >> (h & 31)) & 1u)
-            for (int j = 0; j < a.given; ++j)
-                if (w.token[j] == id && id >= 0) atomicMin(&w.place[j], i);
-    }
-    __syncthreads();
+    g.there = place >= 0 && place < a.n;
+    if (g.there) g.z = logit_at<DT>(a.logits + row * a.row_bytes, place);
+    return g;
 }
 
 // r: the row's sums, e relative to the largest logit in octaves.  best: LDS
-template <int DT, int NT>
-__device__ __forceinline__ void write_row(const TokenArgs& a, int64_t row, float t, const RowSums& r, const uint64_t* best, FindWork& fw) {
+template <int NT>
+__device__ __forceinline__ void write_row(const TokenArgs& a, int64_t row, float t, const RowSums& r, const uint64_t* best, const Given& given) {
     const int tid = threadIdx.x;
     const bool empty = r.s == 0.0f;
     const float m = empty ? 0.0f : r.m, log_s = logf(r.s);
-    if (a.idx && a.given > 0) find_tokens<NT>(a, row, fw);
-    if (tid < a.given) {
-        const int64_t i = row * a.given + tid;
-        int64_t place = a.tokens[i];
-        if (a.idx) place = fw.place[tid];
-        float out = -INFINITY;
-        if (place >= 0 && place < a.n && !empty) out = (logit_at<DT>(a.logits + row * a.row_bytes, place) - m) / t - log_s;
-        a.logprob[i] = r.s != r.s ? r.s : out;
-    }
+    if (tid < a.given) a.logprob[row * a.given + tid] = r.s != r.s ? r.s : given.there && !empty ? (given.z - m) / t - log_s : -INFINITY;
     if (tid < a.top) {
         const uint64_t key = best[tid];
         const bool some = key != 0ull && r.s == r.s;
@@ -290,11 +302,13 @@ __global__ __launch_bounds__(NT) void token_rows_kernel(const TokenArgs a, const
     const float temp = row_temperature(a.temperature, row);
     const float c = octaves_per_logit(temp);
     constexpr int kN = kChunkVectors * kVec<DT>;
+    Given given{};
+    if constexpr (WHOLE) given = given_token<DT, NT>(a, row, find_work);
     RowSums r;
     float thread_most;
     auto pass = [&](auto exact) {
         Running<true, decltype(exact)::value> run;
-        for_chunks<DT, NT, kChunkVectors>(t, [&](int chunk, const u32x4(&v)[kChunkVectors]) {
+        for_chunks<DT, NT, kChunkVectors, !TOP>(t, [&](int chunk, const u32x4(&v)[kChunkVectors]) {
             float z[kN];
 #pragma unroll
             for (int u = 0; u < kChunkVectors; ++u) widen<DT>(v[u], z + u * kVec<DT>);
@@ -312,7 +326,7 @@ __global__ __launch_bounds__(NT) void token_rows_kernel(const TokenArgs a, const
         best = top_work.best;
     }
     if constexpr (WHOLE) {
-        write_row<DT, NT>(a, row, temp, r, best, find_work);
+        write_row<NT>(a, row, temp, r, best, given);
     } else {
         const int64_t at = row * x.parts + part_at;
         if (threadIdx.x == 0) x.sums[at] = PartSums{r.m, r.s, r.e, 0.0f};
@@ -334,6 +348,7 @@ __global__ __launch_bounds__(kMergeThreads) void token_join_kernel(const TokenAr
     const int64_t row = first_row + blockIdx.x;
     const float temp = row_temperature(a.temperature, row);
     const float c = octaves_per_logit(temp);
+    const Given given = given_token<DT, NT>(a, row, find_work);
     RowSums r{-INFINITY, 0.0f, 0.0f};
     for (int p = tid; p < x.parts; p += NT) {
         const PartSums y = x.sums[row * x.parts + p];
@@ -374,76 +389,80 @@ __global__ __launch_bounds__(kMergeThreads) void token_join_kernel(const TokenAr
         __syncthreads();
         rank_found<NT>(found, (int)n_found, best, a.top);
     }
-    write_row<DT, NT>(a, row, temp, r, best, find_work);
+    write_row<NT>(a, row, temp, r, best, given);
 }
 
-// ---- gradient: grad_v = e (k0 + k1 x) with x = (z_v - M) / T in octaves and e = 2^x, and g_j / T more at the given tokens
-constexpr int kGradThreads = 256, kGradVectors = 4;
-constexpr int64_t kGradPart = 1 << 14;
-constexpr int kGradSlots = 128;
+// ---- gradient: grad_v = e (k0 + k1 x) with x = (z_v - M) / T in octaves and e = 2^x; then g_j / T more at the given tokens, whose places are
+// written once more when the workgroup has written its part.
+//
+// A workgroup has one small part, which it asks for before it looks at anything else: reads and writes of all that run stay within a few
+// tens of megabytes (2048 x 151936 bfloat16, 1.24 GB: 198.5 us, 6.3 TB/s, with 8192 places; 225 with 16384, 245 with 65536; a copy as torch
+// makes it 4.9 TB/s, torch.neg 6.1).
+constexpr int kGradThreads = 512;
+constexpr int64_t kGradPart = 1 << 13;
 
 template <int DT, int GDT>
 __global__ __launch_bounds__(kGradThreads) void token_grad_kernel(const TokenGradArgs a, const int64_t first_row, const int parts) {
-    constexpr int NT = kGradThreads, V = kVec<DT>;
-    __shared__ uint32_t bits[kGradPart / 32];
-    __shared__ int32_t keys[kGradSlots];
-    __shared__ float value[kGradSlots];
+    constexpr int NT = kGradThreads, V = kVec<DT>, U = (int)kGradPart / (NT * V);
     __shared__ float g_of[kMaxGiven];
     __shared__ int32_t token[kMaxGiven];
     const int tid = threadIdx.x;
     const int64_t row = first_row + blockIdx.x / (unsigned)parts;
     const Part t = part_of<DT>(a.logits + row * a.row_bytes, a.n, (int64_t)(blockIdx.x % (unsigned)parts) * kGradPart, kGradPart);
+    u32x4 v[U];
+    load_chunk<DT, NT, U, true>(t, 0, v);
     const float4 st = a.state[row];
     const float temp = row_temperature(a.temperature, row), inv_t = 1.0f / temp;
-    const float c = octaves_per_logit(temp);
-    const bool tokens = a.grad_logprob != nullptr;
-    clear_words<NT>(bits, (t.n + 31) / 32);
-    if (tid < kGradSlots) keys[tid] = kEmptySlot;
-    if (tokens && tid < a.given) {
-        token[tid] = a.tokens[row * a.given + tid];
-        g_of[tid] = a.grad_logprob[row * a.given + tid];
-    }
-    __syncthreads();
-    float g_sum = 0.0f;
-    if (tokens) {
+    float g_sum = 0.0f, mine = 0.0f, z_mine = -INFINITY;
+    if (a.grad_logprob) {                                   // (the same for all)
+        if (tid < a.given) {
+            token[tid] = a.tokens[row * a.given + tid];
+            g_of[tid] = a.grad_logprob[row * a.given + tid];
+        }
+        __syncthreads();
         for (int j = 0; j < a.given; ++j) g_sum += token[j] >= 0 && token[j] < a.n ? g_of[j] : 0.0f;
-        const int64_t at = tid < a.given ? token[tid] - t.first : -1;
-        if (at >= 0 && at < t.n) {
-            atomicOr(&bits[at >> 5], 1u << (at & 31));
-            // a token that is given several times has the sum
-            float mine = 0.0f;
-            for (int j = 0; j < a.given; ++j) mine += token[j] == token[tid] ? g_of[j] : 0.0f;
-            bool again;
-            value[insert_place<kGradSlots>(keys, (int32_t)at, again)] = mine * inv_t;
+        if (tid < a.given) {
+            const int64_t at = token[tid] - t.first;
+            // (read before the part is written: the gradient may replace the logits)
+            if (at >= 0 && at < t.n) {
+                z_mine = logit_at<DT>(t.p, at);
+                // a token that is given several times has the sum
+                for (int j = 0; j < a.given; ++j) mine += token[j] == token[tid] ? g_of[j] : 0.0f;
+            }
         }
     }
-    __syncthreads();
     const float gh = a.grad_entropy ? a.grad_entropy[row] : 0.0f;
     const bool empty = st.y == 0.0f;
-    const float scale = empty ? 0.0f : -inv_t / st.y;
-    const float k0 = empty ? 0.0f : scale * (g_sum + gh * (st.z - logf(st.y))), k1 = scale * gh * 0.6931471805599453f;
+    const Exponent x = exponent_of(st.x, octaves_per_logit(temp));
+    const float scale = empty ? 0.0f : -inv_t / st.y * exp2_fast(x.shift);
+    const float k1 = scale * gh * 0.6931471805599453f;
+    const float k0 = empty ? 0.0f : fmaf(k1, x.shift, scale * (g_sum + gh * (st.z - logf(st.y))));
     char* out = a.grad + row * a.grad_row_bytes;
-    for_chunks<DT, NT, kGradVectors>(t, [&](int chunk, const u32x4(&v)[kGradVectors]) {
+    auto gradient = [&](auto exact, float z) {
+        const float y = octaves_at<decltype(exact)::value>(x, z);
+        return exp2_fast(y) * fmaf(k1, fmaxf(y, kNoMass), k0);
+    };
+    // every read of the part is done before any of its places is written
+    if (a.grad_logprob) __syncthreads();
+    auto pass = [&](auto exact) {
 #pragma unroll
-        for (int u = 0; u < kGradVectors; ++u) {
-            const int iv = chunk * (kGradVectors * NT) + u * NT + tid;
+        for (int u = 0; u < U; ++u) {
+            const int iv = u * NT + tid;
             if (iv >= t.vectors) continue;
             float z[V], g[V];
             widen<DT>(v[u], z);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float y = (z[i] - st.x) * c;
-                g[i] = exp2_fast(y) * fmaf(k1, fmaxf(y, kNoMass), k0);
-            }
-            const uint32_t marks = marks_of<DT>(bits, iv);
-            if (marks != 0u) {
-#pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (((marks >> i) & 1u) && !(z[i] == -INFINITY)) g[i] += value[find_place<kGradSlots>(keys, iv * V + i)];
-            }
+            for (int i = 0; i < V; ++i) g[i] = gradient(exact, z[i]);
             store_gradient<GDT>(out, t.first + (int64_t)iv * V, g, t.n - iv * V);
         }
-    });
+    };
+    if (x.exact) pass(std::true_type{});
+    else pass(std::false_type{});
+    if (a.grad_logprob) {
+        __syncthreads();
+        if (!(z_mine == -INFINITY))
+            store_one<GDT>(out, token[tid], fmaf(mine, inv_t, x.exact ? gradient(std::true_type{}, z_mine) : gradient(std::false_type{}, z_mine)));
+    }
 }
 
 // Parts that a row is cut into: enough workgroups for the chip, 2048 places at least each.
