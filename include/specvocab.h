@@ -386,7 +386,7 @@ int specvocab_quantized_sample_step(const void* h, const uint8_t* h_scales, int6
  * lowest too.  A row with a NaN or +inf has NaN throughout, and no alternatives (-1).  A row that is masked throughout has log probabilities of -inf, entropy
  * 0 and no gradient.  grad_out: device [rows x n] in `grad_dt` (SV_F32 or SV_BF16, rounded to nearest even), row stride ld_grad, every
  * place written; it may be the logits themselves (same base, stride and type) and must not overlap them otherwise.
- * Results do not depend on the run.  Sums are float32, relative to the largest logit; probabilities below 2^-126 count as 0.
+ * Results do not depend on the run.  Sums are float32, relative to a logit near the largest; probabilities below 2^-126 count as 0.
  * `state` is what a gradient needs of the forward call: device [rows x 4] float32, 16-byte aligned. */
 
 /* Log probabilities of given tokens, the entropy and the largest alternatives of every row, natural logarithms at temperature T =
@@ -395,7 +395,7 @@ int specvocab_quantized_sample_step(const void* h, const uint8_t* h_scales, int6
  *     entropy_out[r]    = - sum_v p_v log p_v                                           device [rows] float32, or NULL
  *     top_tok_out, top_logprob_out: the `top` largest places and their log probabilities, by descending logit, equal logits by
  *                          place, -1 with -inf where the row has no more              device [rows x top] int32, float32
- *     state_out[r]      = (largest logit, sum_v exp((z[v] - largest) / T), entropy, 0), or NULL
+ *     state_out[r]      = (m, sum_v exp((z[v] - m) / T), entropy, 0), m a logit near the row's largest, or NULL
  * tokens: device [rows x given] int32, 0 <= given <= SPECVOCAB_MAX_GIVEN (0: none, tokens and logprob_out NULL); a token that names no place
  * (-1, a place past the row, an id that is not in the list) has -inf.  0 <= top <= min(n, SPECVOCAB_MAX_TOP); top > 0 with n above
  * 8388608 is SV_ERR_UNSUPPORTED.
@@ -428,8 +428,8 @@ int specvocab_token_logprobs_grad(const void* logits, int64_t ld, int64_t rows, 
  * token that is listed twice has both masses.  specvocab_token_logprobs writes such lists (top_tok_out, top_logprob_out).  A listed token with mass at a
  * masked place makes the loss +inf.  temperature: T, finite, within 2^-20 .. 2^20; weight: device [rows] float32, or NULL for 1; a row of weight 0
  * is not read: loss 0, gradient 0.  A mean over tokens or a factor T^2 goes into the weight.
- * state_out[r] = (largest logit, sum_v exp((z[v] - largest) / T), the same two over the places that are not listed (SV_TEACHER_REST only, else
- * 0)), or NULL.
+ * state_out[r] = (m, sum_v exp((z[v] - m) / T), the same two over the places that are not listed (SV_TEACHER_REST only, else 0)), m a logit near
+ * the largest, or NULL.
  * grad_out may be NULL: the loss alone (or its gradient later, when the factors are known, by specvocab_distill_grad with the same arguments and
  * the state; weight[r] is then whatever factor the row's divergence has).  Both at once read the logits from memory once.
  * One launch; two, three with the gradient, and workspace where there are few rows for their length, or more than 2^18 places. */

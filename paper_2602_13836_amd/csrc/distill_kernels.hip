@@ -175,13 +175,34 @@ __device__ __forceinline__ void enter_list(const Entry& e, ListWork& w) {
     w.id[threadIdx.x] = e.there ? e.id : -1;
     __syncthreads();
 }
-// marks of the entries inside a part; every thread calls
-__device__ __forceinline__ void mark_list(const Part& part, const Entry& e, uint32_t* bits) {
-    clear_words<kThreads>(bits, (part.n + 31) / 32);
+// Marks of the entries inside a part: a byte for each chunk of each thread that says whether to look, and a bit for each place.
+struct Marks {
+    uint8_t* chunk;
+    uint32_t* place;
+};
+template <int DT>
+constexpr int kChunkPlaces = kVectors * kThreads * kVec<DT>;
+// of a part of so many places, in bytes; the bits are whole chunks'
+template <int DT>
+__host__ __device__ inline size_t marks_bytes(int64_t places) {
+    const int64_t chunks = (places + kChunkPlaces<DT> - 1) / kChunkPlaces<DT>;
+    return (size_t)chunks * (kThreads + kChunkPlaces<DT> / 8);
+}
+// every thread calls
+template <int DT>
+__device__ __forceinline__ Marks mark_list(const Part& part, const Entry& e, uint32_t* at) {
+    constexpr int V = kVec<DT>;
+    const int chunks = (part.n + kChunkPlaces<DT> - 1) / kChunkPlaces<DT>;
+    clear_words<kThreads>(at, chunks * (kThreads + kChunkPlaces<DT> / 8) / 4);
+    const Marks m{reinterpret_cast<uint8_t*>(at), at + chunks * kThreads / 4};
     __syncthreads();
-    const int64_t at = e.there ? e.id - part.first : -1;
-    if (at >= 0 && at < part.n) atomicOr(&bits[at >> 5], 1u << (at & 31));
+    const int64_t place = e.there ? e.id - part.first : -1;
+    if (place >= 0 && place < part.n) {
+        atomicOr(&m.place[place >> 5], 1u << (place & 31));
+        m.chunk[(int)place / kChunkPlaces<DT> * kThreads + (int)place / V % kThreads] = 1;
+    }
     __syncthreads();
+    return m;
 }
 // the mass of this thread's token, from all entries that name it; every thread calls
 __device__ __forceinline__ double mass_of_token(const Entry& e, const Teacher& t, int known, ListWork& w) {
@@ -194,37 +215,30 @@ __device__ __forceinline__ double mass_of_token(const Entry& e, const Teacher& t
     return p;
 }
 
-// sums of a part: of all its places, or (REST) of those that are not marked.  AGAIN: the part is read once more soon
-template <int DT, bool REST, bool AGAIN>
-__device__ __forceinline__ RowSums sum_part(const Part& t, float c, const uint32_t* bits, float* scratch) {
+// sums of a part, of those places that are not marked.  AGAIN: the part is read once more soon
+template <int DT, bool AGAIN>
+__device__ __forceinline__ RowSums sum_rest(const Part& t, float c, const Marks& m, float* scratch) {
     constexpr int V = kVec<DT>, kN = kVectors * V;
-    auto pass = [&](auto exact) {
-        Running<false, decltype(exact)::value> run;
-        for_chunks<DT, kThreads, kVectors, !AGAIN>(t, [&](int chunk, const u32x4(&v)[kVectors]) {
-            float z[kN];
+    return sum_part<false, DT, kThreads, kVectors, !AGAIN>(
+        t, c, scratch,
+        [&](int chunk, float(&z)[kN]) {
+            if (m.chunk[chunk * kThreads + (int)threadIdx.x] == 0) return;
 #pragma unroll
-            for (int u = 0; u < kVectors; ++u) widen<DT>(v[u], z + u * V);
-            if constexpr (REST) {
-                uint32_t marks[kVectors];
+            for (int u = 0; u < kVectors; ++u) {
+                const uint32_t marks = marks_of<DT>(m.place, chunk * (kVectors * kThreads) + u * kThreads + (int)threadIdx.x);
+                if (marks != 0u) {
 #pragma unroll
-                for (int u = 0; u < kVectors; ++u) {
-                    const int iv = chunk * (kVectors * kThreads) + u * kThreads + (int)threadIdx.x;
-                    marks[u] = iv < t.vectors ? marks_of<DT>(bits, iv) : 0u;
+                    for (int i = 0; i < V; ++i)
+                        if ((marks >> i) & 1u) z[u * V + i] = -INFINITY;
                 }
-#pragma unroll
-                for (int u = 0; u < kVectors; ++u)
-                    if (marks[u] != 0u) {
-#pragma unroll
-                        for (int i = 0; i < V; ++i)
-                            if ((marks[u] >> i) & 1u) z[u * V + i] = -INFINITY;
-                    }
             }
-            run.add(z, c);
-        });
-        return block_sums<false, decltype(exact)::value, kThreads>(run, c, scratch);
-    };
-    const RowSums r = pass(std::false_type{});
-    return sum_again(r) ? pass(std::true_type{}) : r;
+        },
+        [](int, const u32x4(&)[kVectors], const float(&)[kN]) {});
+}
+template <int DT, bool AGAIN>
+__device__ __forceinline__ RowSums sum_all(const Part& t, float c, float* scratch) {
+    constexpr int kN = kVectors * kVec<DT>;
+    return sum_part<false, DT, kThreads, kVectors, !AGAIN>(t, c, scratch, [](int, float(&)[kN]) {}, [](int, const u32x4(&)[kVectors], const float(&)[kN]) {});
 }
 
 // The part's gradient; z, p: the logit and the mass of this thread's token, where it lies in the part.  Every thread calls.
@@ -236,12 +250,11 @@ __device__ __forceinline__ void write_gradient(const Part& t, const Factors& f, 
 #pragma unroll
             for (int u = 0; u < kVectors; ++u) {
                 const int iv = chunk * (kVectors * kThreads) + u * kThreads + (int)threadIdx.x;
-                if (iv >= t.vectors) continue;
                 float z[V], g[V];
                 widen<DT>(v[u], z);
 #pragma unroll
                 for (int i = 0; i < V; ++i) g[i] = f.of_rest * exp2_fast(octaves_at<decltype(exact)::value>(f.x, z[i]));
-                store_gradient<GDT>(out, t.first + (int64_t)iv * V, g, t.n - iv * V);
+                store_vector<GDT>(out, t, iv, (chunk + 1) * (kVectors * kThreads) <= t.full, g);
             }
         });
     };
@@ -255,7 +268,7 @@ template <int DT, int GDT>
 __device__ __forceinline__ void write_zeros(const Part& t, char* out) {
     constexpr int V = kVec<DT>;
     const float g[V] = {};
-    for (int iv = threadIdx.x; iv < t.vectors; iv += kThreads) store_gradient<GDT>(out, t.first + (int64_t)iv * V, g, t.n - iv * V);
+    for (int iv = threadIdx.x; iv < t.vectors; iv += kThreads) store_vector<GDT>(out, t, iv, false, g);
 }
 
 // One workgroup per row: the loss, and (GDT >= 0) the gradient.
@@ -281,10 +294,10 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(const DistillArg
     enter_list(e, w);
     RowSums sums;
     if (a.kind == kRest) {
-        mark_list(t, e, bits);
-        sums = sum_part<DT, true, GDT >= 0>(t, c, bits, w.scratch);
+        const Marks marks = mark_list<DT>(t, e, bits);
+        sums = sum_rest<DT, GDT >= 0>(t, c, marks, w.scratch);
     } else {
-        sums = sum_part<DT, false, GDT >= 0>(t, c, bits, w.scratch);
+        sums = sum_all<DT, GDT >= 0>(t, c, w.scratch);
     }
     const Teacher teacher = teacher_of(a, e, w);
     const float4 st = finish_row(a, row, weight, e, teacher, z, sums, c, w);
@@ -307,10 +320,10 @@ __global__ __launch_bounds__(kThreads) void distill_parts_kernel(const DistillAr
     const float c = 1.4426950408889634f / a.temperature;
     RowSums r;
     if (a.kind == kRest) {
-        mark_list(t, entry_of(a, row), bits);
-        r = sum_part<DT, true, false>(t, c, bits, scratch);
+        const Marks marks = mark_list<DT>(t, entry_of(a, row), bits);
+        r = sum_rest<DT, false>(t, c, marks, scratch);
     } else {
-        r = sum_part<DT, false, false>(t, c, bits, scratch);
+        r = sum_all<DT, false>(t, c, scratch);
     }
     if (threadIdx.x == 0) x.sums[row * x.parts + at] = make_float2(r.m, r.s);
 }
@@ -387,13 +400,11 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(const DistillArg
     auto pass = [&](auto exact) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int iv = u * kThreads + tid;
-            if (iv >= t.vectors) continue;
             float z[V], g[V];
             widen<DT>(v[u], z);
 #pragma unroll
             for (int i = 0; i < V; ++i) g[i] = f.of_rest * exp2_fast(octaves_at<decltype(exact)::value>(f.x, z[i]));
-            store_gradient<GDT>(out, t.first + (int64_t)iv * V, g, t.n - iv * V);
+            store_vector<GDT>(out, t, u * kThreads + tid, U * kThreads <= t.full, g);
         }
     };
     if (f.x.exact) pass(std::true_type{});
@@ -409,22 +420,25 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(const DistillArg
     }
 }
 
-// Parts that a row is cut into: enough workgroups for the chip, 4096 places at least each.
-constexpr int64_t kWantBlocks = 512;
+// Parts that a row is cut into: up to 128 rows of more than 65536 places only, 4096 places at least each, as many as 256 workgroups ask for
+// (128256 float32 places, graph replays, loss alone and with the gradient: 1 row 9.5 us instead of 15.3 and 13.3 instead of 30.7, 60 rows 15.0 instead
+// of 17.9 and 23.9 instead of 35.4, 128 rows 18.3 instead of 20.2 and 38.6 instead of 41.4, 256 rows 28.1 instead of 24.5; 60 x 32003 11.0 instead of 9.8
+// and 15.7 instead of 14.4).
+constexpr int64_t kWantBlocks = 256, kLongRow = 65536, kFewRows = 128;
 DistillScratch scratch_of(int64_t rows, int64_t n, char* at) {
     DistillScratch x{};
     int64_t parts = (n + kWholeRow - 1) / kWholeRow;
-    int64_t wanted = (kWantBlocks + rows - 1) / rows;
-    if (wanted > n / 4096) wanted = n / 4096;
-    if (wanted > parts) parts = wanted;
+    if (n > kLongRow && rows <= kFewRows) {
+        int64_t wanted = kWantBlocks / rows;
+        if (wanted > n / 4096) wanted = n / 4096;
+        if (wanted > parts) parts = wanted;
+    }
     x.part = ((n + parts - 1) / parts + 31) / 32 * 32;
     x.parts = (int)((n + x.part - 1) / x.part);
     x.state = reinterpret_cast<float4*>(at);
     x.sums = reinterpret_cast<float2*>(at + (size_t)rows * sizeof(float4));
     return x;
 }
-
-inline size_t marks_bytes(int64_t places) { return (size_t)((places + 31) / 32) * 4; }
 
 }  // namespace
 
@@ -435,10 +449,11 @@ size_t distill_scratch_bytes(int64_t rows, int64_t n) {
 
 hipError_t launch_distill(int dt, int grad_dt, const DistillArgs& a, hipStream_t stream) {
     const DistillScratch x = scratch_of(a.rows, a.n, a.scratch);
+    const size_t lds = a.kind != kRest ? 0 : dt == DT_BF16 ? marks_bytes<DT_BF16>(x.part) : marks_bytes<DT_F32>(x.part);
     if (x.parts == 1) {
         auto go = [&](auto kernel) {
             return over_rows(a.rows, kThreads, [&](int64_t first, int64_t rows) {
-                hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(kThreads), marks_bytes(a.n), stream, a, first);
+                hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(kThreads), lds, stream, a, first);
             });
         };
         if (dt == DT_BF16) {
@@ -452,8 +467,8 @@ hipError_t launch_distill(int dt, int grad_dt, const DistillArgs& a, hipStream_t
     if (!b.state) b.state = x.state;
     hipError_t e = over_rows(a.rows, (int64_t)x.parts * kThreads, [&](int64_t first, int64_t rows) {
         const dim3 grid((unsigned)(rows * x.parts));
-        if (dt == DT_BF16) hipLaunchKernelGGL((distill_parts_kernel<DT_BF16>), grid, dim3(kThreads), marks_bytes(x.part), stream, b, x, first);
-        else hipLaunchKernelGGL((distill_parts_kernel<DT_F32>), grid, dim3(kThreads), marks_bytes(x.part), stream, b, x, first);
+        if (dt == DT_BF16) hipLaunchKernelGGL((distill_parts_kernel<DT_BF16>), grid, dim3(kThreads), lds, stream, b, x, first);
+        else hipLaunchKernelGGL((distill_parts_kernel<DT_F32>), grid, dim3(kThreads), lds, stream, b, x, first);
     });
     if (e != hipSuccess) return e;
     e = over_rows(a.rows, kThreads, [&](int64_t first, int64_t rows) {

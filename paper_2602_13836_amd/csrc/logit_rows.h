@@ -124,66 +124,73 @@ __device__ __forceinline__ void for_chunks(const Part& t, F&& f) {
     }
 }
 
-// ---- softmax sums, in octaves: with a = log2(e) / T, s = sum of 2^(a z - c) and, for entropies, e = sum of 2^(a z - c) (a z - c)
-//
-// The reference c is a times the largest logit so far, rounded: whatever it is rounded to, the sums are exactly those of that reference, so a
-// logit takes one fused multiply-add and no error grows with the logits' size.  Where a z leaves float32's range (logits of the
-// type's lowest value, of 2^127 and more, tiny temperatures) the sums come out as 0, infinite or NaN, and the row is summed again by
-// differences (EXACT): 2^(a (z - m)).
+// ---- softmax sums, in octaves: with a = log2(e) / T, s = sum of 2^(a (z - m)) and, for entropies, e = sum of 2^(a (z - m)) a (z - m)
 struct RowSums {
-    float m;        // largest logit, -inf where there is none; NaNs are not in it
-    float s, e;     // relative to m
+    float m;        // the reference: a logit of the row near its largest; -inf where all places are masked
+    float s, e;     // 0 then
 };
 
-template <bool ENTROPY, bool EXACT>
-struct Running {
-    float m = -INFINITY, c = kLowestF32, s = 0.0f, e = 0.0f;
+// The reference is the largest logit of the first chunk (16 or 32 logits of every thread): what lies above it, up to 2^90
+// times, float32 holds as well.  So a logit takes one fused multiply-add, an exponential and an addition: c = a m is rounded, but the sums are exactly those
+// of the rounded reference, and block_sums moves them to m itself.
+template <bool ENTROPY>
+struct Sums {
+    float s = 0.0f, e = 0.0f;
     bool masks = false;      // (the same for a wavefront) there have been places of -inf: their 0 * -inf is kept out of e
 
     template <int N>
-    __device__ __forceinline__ float add(const float (&z)[N], float a) {
-        float most = z[0];
-#pragma unroll
-        for (int i = 1; i < N; ++i) most = fmaxf(most, z[i]);
-        m = fmaxf(m, most);
-        float now, d;
-        if constexpr (EXACT) {
-            now = fmaxf(m, kLowestF32);
-            d = (c - now) * a;
-        } else {
-            now = fminf(fmaxf(m * a, kLowestF32), -kLowestF32);
-            d = c - now;
-        }
-        d = fmaxf(d, kNoMass);
-        const float r = exp2_fast(d);
-        if constexpr (ENTROPY) e = r * fmaf(d, s, e);
-        s *= r;
-        c = now;
-        auto terms = [&](auto cut, float& sum, float& esum) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float y = EXACT ? (z[i] - now) * a : fmaf(z[i], a, -now);
-                const float p = exp2_fast(y);
-                sum += p;
-                if constexpr (ENTROPY) esum = fmaf(p, decltype(cut)::value ? fmaxf(y, kNoMass) : y, esum);
-            }
-        };
+    __device__ __forceinline__ void add(const float (&z)[N], float a, float c) {
         if constexpr (ENTROPY) {
             if (!masks) {
-                float sum = s, esum = e;
-                terms(std::false_type{}, sum, esum);
+                float esum = e;
+                add_terms<false>(z, a, c, s, esum);
                 masks = __builtin_amdgcn_ballot_w64(esum != esum) != 0ull;
                 if (!masks) {
-                    s = sum;
                     e = esum;
-                    return most;
+                    return;
                 }
+                float again = 0.0f;
+                add_terms<true>(z, a, c, again, e);
+            } else {
+                add_terms<true>(z, a, c, s, e);
             }
-            terms(std::true_type{}, s, e);
         } else {
-            terms(std::false_type{}, s, e);
+            add_terms<false>(z, a, c, s, e);
         }
-        return most;
+    }
+
+private:
+    template <bool CUT, int N>
+    static __device__ __forceinline__ void add_terms(const float (&z)[N], float a, float c, float& s, float& e) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float y = fmaf(z[i], a, -c), p = exp2_fast(y);
+            s += p;
+            if constexpr (ENTROPY) e = fmaf(p, CUT ? fmaxf(y, kNoMass) : y, e);
+        }
+    }
+};
+
+// The same by differences from the largest logit so far: for rows whose a z leaves float32's range (logits of 2^100 and more, of the type's
+// lowest value throughout), whose first chunk is masked, or that rise further above it than float32 can count.  NaN and +inf end here too, as NaN.
+template <bool ENTROPY>
+struct Running {
+    float m = -INFINITY, s = 0.0f, e = 0.0f;
+
+    template <int N>
+    __device__ __forceinline__ void add(const float (&z)[N], float a) {
+        const float was = fmaxf(m, kLowestF32);
+#pragma unroll
+        for (int i = 0; i < N; ++i) m = fmaxf(m, z[i]);
+        const float now = fmaxf(m, kLowestF32), d = fmaxf((was - now) * a, kNoMass), r = exp2_fast(d);
+        if constexpr (ENTROPY) e = r * fmaf(d, s, e);
+        s *= r;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float y = (z[i] - now) * a, p = exp2_fast(y);
+            s += p;
+            if constexpr (ENTROPY) e = fmaf(p, fmaxf(y, kNoMass), e);
+        }
     }
 };
 
@@ -200,53 +207,100 @@ __device__ __forceinline__ RowSums joined(const RowSums& x, const RowSums& y, fl
     return r;
 }
 
-// The workgroup's sums, the same for every thread and in the same order every time.  scratch: 4 * NT / 64 floats.
-template <bool ENTROPY, bool EXACT, int NT>
-__device__ __forceinline__ RowSums block_sums(const Running<ENTROPY, EXACT>& t, float a, float* scratch) {
-    constexpr int kWaves = NT / 64;
-    const float c = wave_max_f32(t.c);
-    const float d = fmaxf(EXACT ? (t.c - c) * a : t.c - c, kNoMass);
-    const float r = exp2_fast(d);
-    float s = wave_sum(t.s * r), e = 0.0f;
-    if constexpr (ENTROPY) e = wave_sum(r * fmaf(d, t.s, t.e));
-    const float m = wave_max_f32(t.m);
-    const int wave = threadIdx.x >> 6;
+template <int NT>
+__device__ __forceinline__ float block_max_f32(float x, float* scratch) {
+    x = wave_max_f32(x);
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) {
-        scratch[4 * wave] = m;
-        scratch[4 * wave + 1] = c;
-        scratch[4 * wave + 2] = s;
-        scratch[4 * wave + 3] = e;
-    }
+    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = x;
     __syncthreads();
-    RowSums out;
-    out.m = -INFINITY;
-    float top = kLowestF32;
+    float m = scratch[0];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        out.m = fmaxf(out.m, scratch[4 * w]);
-        top = fmaxf(top, scratch[4 * w + 1]);
-    }
-    out.s = out.e = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        const float dw = fmaxf(EXACT ? (scratch[4 * w + 1] - top) * a : scratch[4 * w + 1] - top, kNoMass);
-        const float rw = exp2_fast(dw);
-        out.s = fmaf(scratch[4 * w + 2], rw, out.s);
-        if constexpr (ENTROPY) out.e += rw * fmaf(dw, scratch[4 * w + 2], scratch[4 * w + 3]);
-    }
-    // from the reference to the largest logit itself (EXACT: they are the same)
-    if (!EXACT && out.s > 0.0f) {
-        const float shift = -fmaf(fmaxf(out.m, kLowestF32), a, -top);
-        const float rs = exp2_fast(shift);
-        if constexpr (ENTROPY) out.e = rs * fmaf(shift, out.s, out.e);
-        out.s *= rs;
-    }
-    return out;
+    for (int w = 1; w < NT / 64; ++w) m = fmaxf(m, scratch[w]);
+    return m;
 }
 
-// true if sums by reference may be those of a row that float32 does not hold so: it is summed again
-__device__ __forceinline__ bool sum_again(const RowSums& r) { return !(r.s < INFINITY) || (!(r.s > 0.0f) && r.m > -INFINITY); }
+// The sums of a part, the same for every thread and in the same order every time.  mask(chunk, z) may set places to -inf; seen(chunk, v, z)
+// looks at a chunk on the way.  scratch: 4 * NT / 64 floats.
+template <bool ENTROPY, int DT, int NT, int U, bool ONCE, class Mask, class Seen>
+__device__ __forceinline__ RowSums sum_part(const Part& t, float a, float* scratch, Mask&& mask, Seen&& seen) {
+    constexpr int N = U * kVec<DT>, kWaves = NT / 64;
+    const int chunks = (t.vectors + U * NT - 1) / (U * NT), wave = threadIdx.x >> 6;
+    auto widened = [&](int chunk, const u32x4(&v)[U], float(&z)[N]) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) widen<DT>(v[u], z + u * kVec<DT>);
+        mask(chunk, z);
+    };
+    u32x4 v[U], next[U];
+    load_chunk<DT, NT, U, ONCE>(t, 0, v);
+    if (chunks > 1) load_chunk<DT, NT, U, ONCE>(t, U * NT, next);
+    RowSums r;
+    {
+        float z[N];
+        widened(0, v, z);
+        float most = z[0];
+#pragma unroll
+        for (int i = 1; i < N; ++i) most = fmaxf(most, z[i]);
+        r.m = block_max_f32<NT>(most, scratch);
+    }
+    const float c = r.m * a;
+    bool done = fabsf(c) < 0x1p100f;
+    if (done) {
+        Sums<ENTROPY> run;
+        for (int chunk = 0; chunk < chunks; ++chunk) {
+            float z[N];
+            widened(chunk, v, z);
+            seen(chunk, v, z);
+            run.add(z, a, c);
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = next[u];
+            if (chunk + 2 < chunks) load_chunk<DT, NT, U, ONCE>(t, (chunk + 2) * (U * NT), next);
+        }
+        r.s = wave_sum(run.s);
+        r.e = ENTROPY ? wave_sum(run.e) : 0.0f;
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) {
+            scratch[2 * wave] = r.s;
+            scratch[2 * wave + 1] = r.e;
+        }
+        __syncthreads();
+        r.s = r.e = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            r.s += scratch[2 * w];
+            r.e += scratch[2 * w + 1];
+        }
+        // from the rounded reference to m
+        const float shift = -fmaf(r.m, a, -c), rs = exp2_fast(shift);
+        r.e = rs * fmaf(shift, r.s, r.e);
+        r.s *= rs;
+        done = r.s < 0x1p90f && fabsf(r.e) < 0x1p100f;
+    }
+    if (!done) {
+        Running<ENTROPY> run;
+        for_chunks<DT, NT, U>(t, [&](int chunk, const u32x4(&w)[U]) {
+            float z[N];
+            widened(chunk, w, z);
+            seen(chunk, w, z);
+            run.add(z, a);
+        });
+        r.m = block_max_f32<NT>(run.m, scratch);
+        const float d = fmaxf((fmaxf(run.m, kLowestF32) - fmaxf(r.m, kLowestF32)) * a, kNoMass), rd = exp2_fast(d);
+        r.s = wave_sum(run.s * rd);
+        r.e = ENTROPY ? wave_sum(rd * fmaf(d, run.s, run.e)) : 0.0f;
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) {
+            scratch[2 * wave] = r.s;
+            scratch[2 * wave + 1] = r.e;
+        }
+        __syncthreads();
+        r.s = r.e = 0.0f;
+        for (int w = 0; w < kWaves; ++w) {
+            r.s += scratch[2 * w];
+            r.e += scratch[2 * w + 1];
+        }
+    }
+    return r;
+}
 
 template <int NT>
 __device__ __forceinline__ double block_sum_f64(double x, double* scratch) {
@@ -259,18 +313,6 @@ __device__ __forceinline__ double block_sum_f64(double x, double* scratch) {
 #pragma unroll
     for (int w = 0; w < NT / 64; ++w) sum += scratch[w];
     return sum;
-}
-
-template <int NT>
-__device__ __forceinline__ float block_max_f32(float x, float* scratch) {
-    x = wave_max_f32(x);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = x;
-    __syncthreads();
-    float m = scratch[0];
-#pragma unroll
-    for (int w = 1; w < NT / 64; ++w) m = fmaxf(m, scratch[w]);
-    return m;
 }
 
 // ---- places that are marked: a bitmap of a part's places; a table of places that have been met
@@ -336,9 +378,12 @@ __device__ __forceinline__ void store_one(char* row, int64_t place, float g) {
     else reinterpret_cast<float*>(row)[place] = g;
 }
 
-// a vector's worth of gradients, rounded to nearest even, at any alignment; nobody here reads them again
+// The gradients of vector iv of a part, rounded to nearest even; nobody here reads them again.  whole: (the same for all) vectors up to it and its
+// neighbours' are whole ones.  One behind the part's end is not stored.
 template <int GDT, int N>
-__device__ __forceinline__ void store_gradient(char* row, int64_t place, const float (&g)[N], int left) {
+__device__ __forceinline__ void store_vector(char* row, const Part& t, int iv, bool whole, const float (&g)[N]) {
+    const int64_t place = t.first + (int64_t)iv * N;
+    const int left = whole ? N : t.n - iv * N;
     if constexpr (GDT == DT_BF16) {
         typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
         uint32_t w[N / 2];
@@ -348,7 +393,7 @@ __device__ __forceinline__ void store_gradient(char* row, int64_t place, const f
             w[i] = __builtin_bit_cast(uint32_t, b);
         }
         char* p = row + place * 2;
-        if (left >= N) {
+        if (whole || left >= N) {
             if constexpr (N == 8) __builtin_nontemporal_store(u32x4_any{w[0], w[1], w[2], w[3]}, reinterpret_cast<u32x4_any*>(p));
             else __builtin_nontemporal_store(u32x2_any{w[0], w[1]}, reinterpret_cast<u32x2_any*>(p));
         } else {
@@ -358,7 +403,7 @@ __device__ __forceinline__ void store_gradient(char* row, int64_t place, const f
         }
     } else {
         float* p = reinterpret_cast<float*>(row) + place;
-        if (left >= N) {
+        if (whole || left >= N) {
 #pragma unroll
             for (int q = 0; q < N / 4; ++q)
                 __builtin_nontemporal_store(u32x4_any{__float_as_uint(g[4 * q]), __float_as_uint(g[4 * q + 1]), __float_as_uint(g[4 * q + 2]),

@@ -1,11 +1,11 @@
 // Log probabilities of given tokens, entropy and largest alternatives of finished rows of logits, and the logits' gradient of them.
 //
-// With T a row's temperature, M its largest logit and S = sum of exp((z - M) / T):
+// With T a row's temperature, M a reference near its largest logit and S = sum of exp((z - M) / T):
 //     log p_v = (z_v - M) / T - log S,     H = log S - sum of exp((z - M) / T) (z - M) / T / S,
 //     d/dz_v = (sum over given tokens j of g_j ([v = t_j] - p_v) - g_H p_v (log p_v + H)) / T.
 //
-// Forward, one pass: every thread keeps the largest logit and the sums relative to it (logit_rows.h).  The alternatives come from what the
-// pass has seen anyway: a thread's largest logit of each chunk (16 or 32 logits) goes to LDS, the `top`-th largest of the threads'
+// Forward, one pass (sum_part, logit_rows.h).  The alternatives come from what the
+// pass has seen anyway: a thread's largest logit of every 32 goes to LDS, the `top`-th largest of the threads'
 // largest logits is a bound that at least `top` logits reach, and only the chunks that reach it -- about `top` of them -- are read
 // again and their places ranked.  A row in which more than 1024 places reach the bound (equal logits) is selected by digits of the keys.
 // Few rows are cut into parts, whose sums and alternatives a second launch joins.
@@ -17,9 +17,10 @@ namespace {
 
 constexpr int kMaxTop = 64, kMaxGiven = 64;
 constexpr int kCandidates = 1024;
-constexpr int64_t kTopPart = 1 << 17, kSumPart = 1 << 18;      // places of a part: 32 KB of chunks' largest logits; 32-bit offsets
+constexpr int64_t kMostPart = 1 << 18;                         // places of a part: 32 KB of chunks' largest logits, 32-bit offsets
 constexpr int kMaxTopParts = 64;
-constexpr int kRowThreads = 512, kChunkVectors = 4;
+template <int DT>
+constexpr int kChunkVectors = 16 / kVec<DT>;               // a chunk: 16 logits of a thread
 constexpr int kMergeThreads = 256;
 constexpr uint32_t kLowestKey = 0x00800000u;               // of the lowest finite float
 
@@ -163,10 +164,12 @@ __device__ __forceinline__ int select_by_digits(const Part& t, int top, TopWork<
     return (int)(above + min(taken, want));
 }
 
-// w.best: the part's `top` largest places.  chunk_most: a thread's largest logit of each chunk, NT of them after the other.
+// w.best: the part's `top` largest places.  chunk_most: a thread's largest logit of each two chunks, NT of them after the other.
+// only: the thread's logits, where it has no more than one chunk.
 template <int DT, int NT>
-__device__ __forceinline__ void select_top(const Part& t, int top, float thread_most, const float* chunk_most, TopWork<NT>& w) {
-    constexpr int kEach = NT / 64;
+__device__ __forceinline__ void select_top(const Part& t, int top, float thread_most, const float* chunk_most, const u32x4 (&only)[kChunkVectors<DT>],
+                                           TopWork<NT>& w) {
+    constexpr int kEach = NT / 64, V = kVec<DT>, U = kChunkVectors<DT>;
     const int tid = threadIdx.x;
     w.keys[tid] = f32_to_ord(thread_most);
     if (tid == 0) w.n_chunks = w.n_found = 0;
@@ -183,34 +186,43 @@ __device__ __forceinline__ void select_top(const Part& t, int top, float thread_
     // (-inf is below every key that counts)
     const uint32_t bound = max(bound_of(k, least, most, top, top + top / 2 + 8), kLowestKey);
     const float least_logit = ord_to_f32(bound);
-    __syncthreads();                                       // the keys' array takes the chunks
-    const int chunks = (t.vectors + kChunkVectors * NT - 1) / (kChunkVectors * NT);
-    for (int i = tid; i < chunks * NT; i += NT)
-        if (chunk_most[i] >= least_logit) {
-            const uint32_t slot = atomicAdd(&w.n_chunks, 1u);
-            if (slot < NT) w.keys[slot] = (uint32_t)i;
-        }
-    __syncthreads();
-    const int listed = (int)w.n_chunks;
-    int n;
-    bool fits = listed <= NT;
-    if (fits) {
-        for (int i = tid; i < listed * kChunkVectors; i += NT) {
-            const int chunk = (int)w.keys[i / kChunkVectors];
-            const int iv = (chunk / NT) * (kChunkVectors * NT) + (i % kChunkVectors) * NT + chunk % NT;
-            float z[kVec<DT>];
-            widen<DT>(load_guarded<DT>(t, iv), z);
+    auto take = [&](const u32x4 v, int iv) {
+        float z[V];
+        widen<DT>(v, z);
 #pragma unroll
-            for (int e = 0; e < kVec<DT>; ++e)
-                if (z[e] >= least_logit) {
-                    const uint32_t slot = atomicAdd(&w.n_found, 1u);
-                    if (slot < (uint32_t)kCandidates) w.found[slot] = make_key(z[e], (int32_t)(t.first + iv * kVec<DT> + e));
-                }
+        for (int e = 0; e < V; ++e)
+            if (z[e] >= least_logit) {
+                const uint32_t slot = atomicAdd(&w.n_found, 1u);
+                if (slot < (uint32_t)kCandidates) w.found[slot] = make_key(z[e], (int32_t)(t.first + iv * V + e));
+            }
+    };
+    bool fits = true;
+    if (t.vectors <= U * NT) {
+        if (thread_most >= least_logit) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) take(only[u], u * NT + tid);
         }
+    } else {
+        __syncthreads();                                   // the keys' array takes the chunks
+        const int pairs = (t.vectors + 2 * U * NT - 1) / (2 * U * NT);
+        for (int i = tid; i < pairs * NT; i += NT)
+            if (chunk_most[i] >= least_logit) {
+                const uint32_t slot = atomicAdd(&w.n_chunks, 1u);
+                if (slot < NT) w.keys[slot] = (uint32_t)i;
+            }
         __syncthreads();
-        n = (int)w.n_found;
-        fits = n <= kCandidates;
+        const int listed = (int)w.n_chunks;
+        fits = listed <= NT;
+        if (fits)
+            for (int i = tid; i < listed * 2 * U; i += NT) {
+                const int pair = (int)w.keys[i / (2 * U)];
+                const int iv = (pair / NT) * (2 * U * NT) + (i % (2 * U)) * NT + pair % NT;
+                take(load_guarded<DT>(t, iv), iv);
+            }
     }
+    __syncthreads();
+    int n = (int)w.n_found;
+    fits = fits && n <= kCandidates;
     if (!fits) n = select_by_digits<DT, NT>(t, top, w);
     __syncthreads();
     rank_found<NT>(w.found, n, w.best, top);
@@ -252,11 +264,21 @@ __device__ __forceinline__ Given given_token(const TokenArgs& a, int64_t row, Fi
                 for (int j = 0; j < a.given; ++j)
                     if (w.token[j] == id && id >= 0) atomicMin(&w.place[j], at);
         };
-#pragma unroll 4
-        for (int i = 4 * tid; i + 3 < n; i += 4 * NT) {
-            const i32x4_any id = *reinterpret_cast<const i32x4_any*>(ids + i);
+        constexpr int kAtOnce = 4;
+        int at = 4 * tid;
+        for (; at + 4 * NT * (kAtOnce - 1) + 3 < n; at += 4 * NT * kAtOnce) {
+            i32x4_any id[kAtOnce];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) look(id[e], i + e);
+            for (int u = 0; u < kAtOnce; ++u) id[u] = *reinterpret_cast<const i32x4_any*>(ids + at + 4 * NT * u);
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) look(id[u][e], at + 4 * NT * u + e);
+        }
+        for (; at + 3 < n; at += 4 * NT) {
+            const i32x4_any id = *reinterpret_cast<const i32x4_any*>(ids + at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) look(id[e], at + e);
         }
         if (tid < (n & 3)) look(ids[(n & ~3) + tid], (n & ~3) + tid);
         __syncthreads();
@@ -267,7 +289,7 @@ __device__ __forceinline__ Given given_token(const TokenArgs& a, int64_t row, Fi
     return g;
 }
 
-// r: the row's sums, e relative to the largest logit in octaves.  best: LDS
+// r: the row's sums.  best: LDS
 template <int NT>
 __device__ __forceinline__ void write_row(const TokenArgs& a, int64_t row, float t, const RowSums& r, const uint64_t* best, const Given& given) {
     const int tid = threadIdx.x;
@@ -301,28 +323,30 @@ __global__ __launch_bounds__(NT) void token_rows_kernel(const TokenArgs a, const
     const Part t = part_of<DT>(logits, a.n, (int64_t)part_at * x.part, x.part);
     const float temp = row_temperature(a.temperature, row);
     const float c = octaves_per_logit(temp);
-    constexpr int kN = kChunkVectors * kVec<DT>;
+    constexpr int U = kChunkVectors<DT>, kN = U * kVec<DT>;
     Given given{};
     if constexpr (WHOLE) given = given_token<DT, NT>(a, row, find_work);
-    RowSums r;
-    float thread_most;
-    auto pass = [&](auto exact) {
-        Running<true, decltype(exact)::value> run;
-        for_chunks<DT, NT, kChunkVectors, !TOP>(t, [&](int chunk, const u32x4(&v)[kChunkVectors]) {
-            float z[kN];
+    float thread_most = -INFINITY;
+    u32x4 only[U];
+    const RowSums r = sum_part<true, DT, NT, U, !TOP>(
+        t, c, sums, [](int, float(&)[kN]) {},
+        [&](int chunk, const u32x4(&v)[U], const float(&z)[kN]) {
+            if constexpr (TOP) {
+                float most = z[0];
 #pragma unroll
-            for (int u = 0; u < kChunkVectors; ++u) widen<DT>(v[u], z + u * kVec<DT>);
-            const float most = run.add(z, c);
-            if constexpr (TOP) chunk_most[chunk * NT + (int)threadIdx.x] = most;
+                for (int i = 1; i < kN; ++i) most = fmaxf(most, z[i]);
+                float* slot = chunk_most + (chunk >> 1) * NT + (int)threadIdx.x;
+                *slot = chunk & 1 ? fmaxf(*slot, most) : most;
+                thread_most = fmaxf(thread_most, most);
+                if (chunk == 0) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) only[u] = v[u];
+                }
+            }
         });
-        thread_most = run.m;
-        r = block_sums<true, decltype(exact)::value, NT>(run, c, sums);
-    };
-    pass(std::false_type{});
-    if (sum_again(r)) pass(std::true_type{});
     const uint64_t* best = nullptr;
     if constexpr (TOP) {
-        if (r.s == r.s) select_top<DT, NT>(t, a.top, thread_most, chunk_most, top_work);
+        if (r.s == r.s) select_top<DT, NT>(t, a.top, thread_most, chunk_most, only, top_work);
         best = top_work.best;
     }
     if constexpr (WHOLE) {
@@ -447,13 +471,11 @@ __global__ __launch_bounds__(kGradThreads) void token_grad_kernel(const TokenGra
     auto pass = [&](auto exact) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int iv = u * NT + tid;
-            if (iv >= t.vectors) continue;
             float z[V], g[V];
             widen<DT>(v[u], z);
 #pragma unroll
             for (int i = 0; i < V; ++i) g[i] = gradient(exact, z[i]);
-            store_gradient<GDT>(out, t.first + (int64_t)iv * V, g, t.n - iv * V);
+            store_vector<GDT>(out, t, u * NT + tid, U * NT <= t.full, g);
         }
     };
     if (x.exact) pass(std::true_type{});
@@ -465,18 +487,23 @@ __global__ __launch_bounds__(kGradThreads) void token_grad_kernel(const TokenGra
     }
 }
 
-// Parts that a row is cut into: enough workgroups for the chip, 2048 places at least each.
-constexpr int64_t kWantBlocks = 1024;
+// Parts that a row is cut into: up to 64 rows of more than 98304 places only, 4096 places at least each, as many as 256 workgroups ask for
+// (1 x 128256 float32, graph replays: 6.1 us instead of 10.2, with 20 alternatives 12.5 instead of 15.0; 60 rows 10.1 instead of 12.5 and 16.2
+// instead of 17.8; 128 rows 14.9 instead of 17.0 but 22.5 instead of 19.3; 16 x 65537 6.5 instead of 7.6 but 13.1 instead of 11.5).
+constexpr int64_t kWantBlocks = 256, kLongRow = 98304, kFewRows = 64;
+// 256 threads work on a part of up to 8192 places, and where there are workgroups for every place on the chip, else 512 (60 rows with 20 alternatives, 256
+// and 512 threads: of 2048 places 6.8 and 7.7 us, 8192 6.7 and 6.9, 32003 10.2 and 8.7; 1024 rows: 2048 places 8.7 and 15.9, 32003 25.7 and 30.0).
+constexpr int64_t kShortPart = 8192, kManyBlocks = 1024;
 TokenScratch scratch_of(int64_t rows, int64_t n, int top, char* at) {
     TokenScratch x{};
-    const int64_t most = top > 0 ? kTopPart : kSumPart;
-    int64_t parts = (n + most - 1) / most;
-    int64_t wanted = (kWantBlocks + rows - 1) / rows;
-    if (wanted > kMaxTopParts) wanted = kMaxTopParts;
-    if (wanted > n / 2048) wanted = n / 2048;
-    if (wanted > parts) parts = wanted;
-    x.part = (n + parts - 1) / parts;
-    x.part = (x.part + 31) / 32 * 32;
+    int64_t parts = (n + kMostPart - 1) / kMostPart;
+    if (n > kLongRow && rows <= kFewRows) {
+        int64_t wanted = kWantBlocks / rows;
+        if (wanted > kMaxTopParts) wanted = kMaxTopParts;
+        if (wanted > n / 4096) wanted = n / 4096;
+        if (wanted > parts) parts = wanted;
+    }
+    x.part = ((n + parts - 1) / parts + 31) / 32 * 32;
     x.parts = (int)((n + x.part - 1) / x.part);
     x.sums = reinterpret_cast<PartSums*>(at);
     x.top = reinterpret_cast<uint64_t*>(at + (size_t)rows * x.parts * sizeof(PartSums));
@@ -492,18 +519,15 @@ size_t token_scratch_bytes(int64_t rows, int64_t n, int top) {
 
 hipError_t launch_token_logprobs(int dt, const TokenArgs& a, hipStream_t stream) {
     const TokenScratch x = scratch_of(a.rows, a.n, a.top, a.scratch);
-    const int vec = dt == DT_BF16 ? 8 : 4;
-    constexpr int NT = kRowThreads;
-    const int64_t vectors = (x.part + vec - 1) / vec;
-    const int64_t chunks = (vectors + kChunkVectors * NT - 1) / (kChunkVectors * NT);
-    const size_t lds = a.top > 0 ? (size_t)chunks * NT * sizeof(float) : 0;
-    auto rows_launch = [&](auto kernel) {
-        return over_rows(a.rows, (int64_t)x.parts * NT, [&](int64_t first, int64_t rows) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * x.parts)), dim3(NT), lds, stream, a, x, first);
-        });
-    };
-    auto of_type = [&](auto type) {
-        constexpr int DT = decltype(type)::value;
+    auto of_rows = [&](auto type, auto threads) {
+        constexpr int DT = decltype(type)::value, NT = decltype(threads)::value;
+        const int64_t pair = 2 * kChunkVectors<DT> * kVec<DT> * NT;
+        const size_t lds = a.top > 0 ? (size_t)((x.part + pair - 1) / pair) * NT * sizeof(float) : 0;
+        auto rows_launch = [&](auto kernel) {
+            return over_rows(a.rows, (int64_t)x.parts * NT, [&](int64_t first, int64_t rows) {
+                hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * x.parts)), dim3(NT), lds, stream, a, x, first);
+            });
+        };
         if (x.parts == 1) return a.top > 0 ? rows_launch(&token_rows_kernel<DT, NT, true, true>) : rows_launch(&token_rows_kernel<DT, NT, false, true>);
         const hipError_t e = a.top > 0 ? rows_launch(&token_rows_kernel<DT, NT, true, false>) : rows_launch(&token_rows_kernel<DT, NT, false, false>);
         if (e != hipSuccess) return e;
@@ -511,6 +535,10 @@ hipError_t launch_token_logprobs(int dt, const TokenArgs& a, hipStream_t stream)
             if (a.top > 0) hipLaunchKernelGGL((token_join_kernel<DT, true>), dim3((unsigned)rows), dim3(kMergeThreads), 0, stream, a, x, first);
             else hipLaunchKernelGGL((token_join_kernel<DT, false>), dim3((unsigned)rows), dim3(kMergeThreads), 0, stream, a, x, first);
         });
+    };
+    auto of_type = [&](auto type) {
+        if (x.part <= kShortPart || a.rows * x.parts >= kManyBlocks) return of_rows(type, std::integral_constant<int, 256>{});
+        return of_rows(type, std::integral_constant<int, 512>{});
     };
     return dt == DT_BF16 ? of_type(std::integral_constant<int, DT_BF16>{}) : of_type(std::integral_constant<int, DT_F32>{});
 }
