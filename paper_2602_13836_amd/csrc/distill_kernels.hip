@@ -18,9 +18,12 @@ namespace sv {
 
 namespace {
 
-constexpr int kThreads = 512, kVectors = 4;
+constexpr int kThreads = 512;
+template <int DT>
+constexpr int kVectors = 16 / kVec<DT>;                   // of a chunk of a thread: 16 logits
 constexpr int kMaxKnown = 512, kSlots = 1024;
 constexpr int64_t kWholeRow = 1 << 18;                  // places of a part at most: 32 KB of marks
+constexpr int kLdsBytes = 160 * 1024;                   // of a CU
 constexpr int kRest = 2;                               // SV_TEACHER_REST
 static_assert(kMaxKnown == kThreads, "an entry of the list per thread");
 
@@ -32,7 +35,6 @@ struct DistillScratch {
 };
 
 struct ListWork {
-    int32_t keys[kSlots];
     double p[kMaxKnown];
     int32_t id[kMaxKnown];
     double sums[kThreads / 64];
@@ -166,43 +168,44 @@ __device__ __forceinline__ float listed_gradient(const Factors& f, float z, doub
     return z == -INFINITY ? f.of_listed * 0.0f : (float)((double)(f.of_listed * exp2_fast((z - f.m) * f.x.a)) - (double)f.scale * p);
 }
 
-// the list into LDS, and whether a token is in it twice; every thread calls
-__device__ __forceinline__ void enter_list(const Entry& e, ListWork& w) {
-    clear_words<kThreads>(reinterpret_cast<uint32_t*>(w.keys), kSlots, (uint32_t)kEmptySlot);
+// the list into LDS, and whether a token is in it twice; keys: kSlots words.  Every thread calls.
+__device__ __forceinline__ void enter_list(const Entry& e, int32_t* keys, ListWork& w) {
+    clear_words<kThreads>(reinterpret_cast<uint32_t*>(keys), kSlots, (uint32_t)kEmptySlot);
     if (threadIdx.x == 0) w.again = 0u;
     __syncthreads();
-    if (e.there && enter_place<kSlots>(w.keys, e.id)) w.again = 1u;
+    if (e.there && enter_place<kSlots>(keys, e.id)) w.again = 1u;
     w.id[threadIdx.x] = e.there ? e.id : -1;
     __syncthreads();
 }
-// Marks of the entries inside a part: a byte for each chunk of each thread that says whether to look, and a bit for each place.
-struct Marks {
-    uint8_t* chunk;
-    uint32_t* place;
-};
-template <int DT>
-constexpr int kChunkPlaces = kVectors * kThreads * kVec<DT>;
-// of a part of so many places, in bytes; the bits are whole chunks'
+// Marks of the entries inside a part: a bit for each of its places, whole chunks of them.
 template <int DT>
 __host__ __device__ inline size_t marks_bytes(int64_t places) {
-    const int64_t chunks = (places + kChunkPlaces<DT> - 1) / kChunkPlaces<DT>;
-    return (size_t)chunks * (kThreads + kChunkPlaces<DT> / 8);
+    constexpr int64_t kPlaces = (int64_t)kThreads * 16;
+    return (size_t)((places + kPlaces - 1) / kPlaces) * (kPlaces / 8);
 }
 // every thread calls
 template <int DT>
-__device__ __forceinline__ Marks mark_list(const Part& part, const Entry& e, uint32_t* at) {
-    constexpr int V = kVec<DT>;
-    const int chunks = (part.n + kChunkPlaces<DT> - 1) / kChunkPlaces<DT>;
-    clear_words<kThreads>(at, chunks * (kThreads + kChunkPlaces<DT> / 8) / 4);
-    const Marks m{reinterpret_cast<uint8_t*>(at), at + chunks * kThreads / 4};
+__device__ __forceinline__ void mark_list(const Part& part, const Entry& e, uint32_t* bits) {
+    clear_words<kThreads>(bits, (int)(marks_bytes<DT>(part.n) / 4));
     __syncthreads();
     const int64_t place = e.there ? e.id - part.first : -1;
-    if (place >= 0 && place < part.n) {
-        atomicOr(&m.place[place >> 5], 1u << (place & 31));
-        m.chunk[(int)place / kChunkPlaces<DT> * kThreads + (int)place / V % kThreads] = 1;
-    }
+    if (place >= 0 && place < part.n) atomicOr(&bits[place >> 5], 1u << (place & 31));
     __syncthreads();
-    return m;
+}
+// vectors layer * kThreads + thread, (layer + 1) * kThreads + thread, ... without their marked places
+template <int DT, int U>
+__device__ __forceinline__ void without_marked(const uint32_t* bits, int layer, float (&z)[U * kVec<DT>]) {
+    constexpr int V = kVec<DT>;
+    uint32_t marks[U], any = 0u;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        marks[u] = marks_of<DT>(bits, (layer + u) * kThreads + (int)threadIdx.x);
+        any |= marks[u];
+    }
+    if (any == 0u) return;
+#pragma unroll
+    for (int i = 0; i < U * V; ++i)
+        if ((marks[i / V] >> (i % V)) & 1u) z[i] = -INFINITY;
 }
 // the mass of this thread's token, from all entries that name it; every thread calls
 __device__ __forceinline__ double mass_of_token(const Entry& e, const Teacher& t, int known, ListWork& w) {
@@ -215,55 +218,18 @@ __device__ __forceinline__ double mass_of_token(const Entry& e, const Teacher& t
     return p;
 }
 
-// sums of a part, of those places that are not marked.  AGAIN: the part is read once more soon
-template <int DT, bool AGAIN>
-__device__ __forceinline__ RowSums sum_rest(const Part& t, float c, const Marks& m, float* scratch) {
-    constexpr int V = kVec<DT>, kN = kVectors * V;
-    return sum_part<false, DT, kThreads, kVectors, !AGAIN>(
+// sums of a part; REST: of those places that are not marked
+template <int DT, bool REST>
+__device__ __forceinline__ RowSums sums_of(const Part& t, float c, const uint32_t* bits, float* scratch) {
+    constexpr int U = kVectors<DT>, kN = U * kVec<DT>;
+    return sum_part<false, DT, kThreads, U, true>(
         t, c, scratch,
         [&](int chunk, float(&z)[kN]) {
-            if (m.chunk[chunk * kThreads + (int)threadIdx.x] == 0) return;
-#pragma unroll
-            for (int u = 0; u < kVectors; ++u) {
-                const uint32_t marks = marks_of<DT>(m.place, chunk * (kVectors * kThreads) + u * kThreads + (int)threadIdx.x);
-                if (marks != 0u) {
-#pragma unroll
-                    for (int i = 0; i < V; ++i)
-                        if ((marks >> i) & 1u) z[u * V + i] = -INFINITY;
-                }
-            }
+            if constexpr (REST) without_marked<DT, U>(bits, chunk * U, z);
         },
-        [](int, const u32x4(&)[kVectors], const float(&)[kN]) {});
-}
-template <int DT, bool AGAIN>
-__device__ __forceinline__ RowSums sum_all(const Part& t, float c, float* scratch) {
-    constexpr int kN = kVectors * kVec<DT>;
-    return sum_part<false, DT, kThreads, kVectors, !AGAIN>(t, c, scratch, [](int, float(&)[kN]) {}, [](int, const u32x4(&)[kVectors], const float(&)[kN]) {});
+        [](int, const u32x4(&)[U], const float(&)[kN]) {});
 }
 
-// The part's gradient; z, p: the logit and the mass of this thread's token, where it lies in the part.  Every thread calls.
-template <int DT, int GDT>
-__device__ __forceinline__ void write_gradient(const Part& t, const Factors& f, const Entry& e, float z_listed, double p, char* out) {
-    constexpr int V = kVec<DT>;
-    auto pass = [&](auto exact) {
-        for_chunks<DT, kThreads, kVectors, true, true>(t, [&](int chunk, const u32x4(&v)[kVectors]) {
-#pragma unroll
-            for (int u = 0; u < kVectors; ++u) {
-                const int iv = chunk * (kVectors * kThreads) + u * kThreads + (int)threadIdx.x;
-                float z[V], g[V];
-                widen<DT>(v[u], z);
-#pragma unroll
-                for (int i = 0; i < V; ++i) g[i] = f.of_rest * exp2_fast(octaves_at<decltype(exact)::value>(f.x, z[i]));
-                store_vector<GDT>(out, t, iv, (chunk + 1) * (kVectors * kThreads) <= t.full, g);
-            }
-        });
-    };
-    if (f.x.exact) pass(std::true_type{});
-    else pass(std::false_type{});
-    __syncthreads();
-    const int64_t at = e.there ? e.id - t.first : -1;
-    if (at >= 0 && at < t.n) store_one<GDT>(out, e.id, listed_gradient(f, z_listed, p));
-}
 template <int DT, int GDT>
 __device__ __forceinline__ void write_zeros(const Part& t, char* out) {
     constexpr int V = kVec<DT>;
@@ -271,45 +237,195 @@ __device__ __forceinline__ void write_zeros(const Part& t, char* out) {
     for (int iv = threadIdx.x; iv < t.vectors; iv += kThreads) store_vector<GDT>(out, t, iv, false, g);
 }
 
-// One workgroup per row: the loss, and (GDT >= 0) the gradient.
-template <int DT, int GDT>
+// a row that does not count; true if it is one
+__device__ __forceinline__ bool skipped_row(const DistillArgs& a, int64_t row, float weight) {
+    if (weight != 0.0f) return false;
+    if (threadIdx.x == 0) {
+        a.loss[row] = 0.0f;
+        if (a.state) a.state[row] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
+    return true;
+}
+
+// One workgroup per row: the loss.
+template <int DT, bool REST>
 __global__ __launch_bounds__(kThreads) void distill_rows_kernel(const DistillArgs a, const int64_t first_row) {
     extern __shared__ uint32_t bits[];
     __shared__ ListWork w;
+    __shared__ int32_t keys[kSlots];
     const int64_t row = first_row + blockIdx.x;
     const float weight = weight_of_row(a, row);
+    if (skipped_row(a, row, weight)) return;
     const char* logits = a.logits + row * a.row_bytes;
     const Part t = part_of<DT>(logits, a.n, 0, a.n);
-    if (weight == 0.0f) {
-        if (threadIdx.x == 0) {
-            a.loss[row] = 0.0f;
-            if (a.state) a.state[row] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        }
-        if constexpr (GDT >= 0) write_zeros<DT, GDT>(t, a.grad + row * a.grad_row_bytes);
-        return;
-    }
     const float c = 1.4426950408889634f / a.temperature;
     const Entry e = entry_of(a, row);
     const float z = e.there ? logit_at<DT>(logits, e.id) : -INFINITY;
-    enter_list(e, w);
-    RowSums sums;
-    if (a.kind == kRest) {
-        const Marks marks = mark_list<DT>(t, e, bits);
-        sums = sum_rest<DT, GDT >= 0>(t, c, marks, w.scratch);
-    } else {
-        sums = sum_all<DT, GDT >= 0>(t, c, w.scratch);
+    if constexpr (REST) {
+        enter_list(e, keys, w);
+        mark_list<DT>(t, e, bits);
     }
+    const RowSums sums = sums_of<DT, REST>(t, c, bits, w.scratch);
     const Teacher teacher = teacher_of(a, e, w);
-    const float4 st = finish_row(a, row, weight, e, teacher, z, sums, c, w);
-    if constexpr (GDT >= 0) {
-        const Factors f = factors_of(a, weight, teacher, st, c);
-        const double p = mass_of_token(e, teacher, a.known, w);
-        write_gradient<DT, GDT>(t, f, e, z, p, a.grad + row * a.grad_row_bytes);
+    finish_row(a, row, weight, e, teacher, z, sums, c, w);
+}
+
+// One workgroup per row: loss and gradient, that is two passes over the row.  The fabric moves 7 TB/s whether the lines come from the last-level
+// cache or from memory, so the second pass reads as little as it can: a thread keeps its first 16 vectors in registers and some more in
+// LDS (`stored` chunks of two), 70 per cent of 128256 bfloat16 logits, and walks the others backwards.  Two workgroups share a CU, so that one's
+// reads fill the time of the other's sums.
+constexpr int kKept = 16, kStep = 2;
+constexpr size_t kStoredBytes = (size_t)kStep * kThreads * 16;
+template <int DT, int GDT, bool REST>
+__global__ __launch_bounds__(kThreads, 4) void distill_step_kernel(const DistillArgs a, const int64_t first_row, const int stored) {
+    constexpr int V = kVec<DT>, kN = kStep * V, NT = kThreads;
+    extern __shared__ u32x4 store[];                       // stored * kStep * NT vectors, then the marks
+    __shared__ ListWork w;
+    const int tid = threadIdx.x;
+    const int64_t row = first_row + blockIdx.x;
+    const float weight = weight_of_row(a, row);
+    const char* logits = a.logits + row * a.row_bytes;
+    char* out = a.grad + row * a.grad_row_bytes;
+    const Part t = part_of<DT>(logits, a.n, 0, a.n);
+    if (skipped_row(a, row, weight)) {
+        write_zeros<DT, GDT>(t, out);
+        return;
     }
+    uint32_t* bits = reinterpret_cast<uint32_t*>(store + stored * kStep * NT);
+    u32x4 kept[kKept];
+#pragma unroll
+    for (int k = 0; k < kKept; k += kStep) {
+        u32x4 v[kStep];
+        load_chunk<DT, NT, kStep, true>(t, k * NT, v);
+        kept[k] = v[0];
+        kept[k + 1] = v[1];
+    }
+    const float c = 1.4426950408889634f / a.temperature;
+    const Entry e = entry_of(a, row);
+    const float z_listed = e.there ? logit_at<DT>(logits, e.id) : -INFINITY;
+    // (the table of places lies where chunks will be stored later: a barrier of the sums is in between)
+    enter_list(e, reinterpret_cast<int32_t*>(store), w);
+    if constexpr (REST) mark_list<DT>(t, e, bits);
+
+    const int chunks = (t.vectors + kStep * NT - 1) / (kStep * NT);       // the first kKept / kStep of them are kept
+    auto logits_of = [&](int chunk, const u32x4 v0, const u32x4 v1, float(&z)[kN]) {
+        widen<DT>(v0, z);
+        widen<DT>(v1, z + V);
+        if constexpr (REST) without_marked<DT, kStep>(bits, chunk * kStep, z);
+    };
+    bool is_stored = false;
+    // f(z) of every chunk; the first time the chunks to be stored are
+    auto pass = [&](auto&& f) {
+#pragma unroll
+        for (int k = 0; k < kKept; k += kStep) {
+            if (k * NT >= t.vectors) continue;
+            // (or the widened logits would live on to the next pass, in twice the registers)
+            asm volatile("" : "+v"(kept[k]), "+v"(kept[k + 1]));
+            float z[kN];
+            logits_of(k / kStep, kept[k], kept[k + 1], z);
+            f(z);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        u32x4 next[kStep];
+        auto fetch = [&](int chunk) {
+            const int at = chunk - kKept / kStep;
+            if (at < stored && is_stored) {
+#pragma unroll
+                for (int u = 0; u < kStep; ++u) next[u] = store[(at * kStep + u) * NT + tid];
+            } else {
+                load_chunk<DT, NT, kStep, false>(t, chunk * (kStep * NT), next);
+            }
+        };
+        if (chunks > kKept / kStep) fetch(kKept / kStep);
+        for (int chunk = kKept / kStep; chunk < chunks; ++chunk) {
+            const u32x4 v0 = next[0], v1 = next[1];
+            if (chunk + 1 < chunks) fetch(chunk + 1);
+            const int at = chunk - kKept / kStep;
+            if (at < stored && !is_stored) {
+                store[at * kStep * NT + tid] = v0;
+                store[(at * kStep + 1) * NT + tid] = v1;
+            }
+            float z[kN];
+            logits_of(chunk, v0, v1, z);
+            f(z);
+        }
+        is_stored = true;
+    };
+    RowSums sums;
+    {
+        // (of as many logits as the loss alone takes it from: the same bits)
+        float most = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < kVectors<DT>; k += kStep) {
+            float z[kN];
+            logits_of(k / kStep, kept[k], kept[k + 1], z);
+#pragma unroll
+            for (int i = 0; i < kN; ++i) most = fmaxf(most, z[i]);
+        }
+        sums.m = block_max_f32<NT>(most, w.scratch);
+    }
+    const float ref = sums.m * c;
+    bool done = fabsf(ref) < 0x1p100f;
+    if (done) {
+        Sums<false> run;
+        pass([&](const float(&z)[kN]) { run.add(z, c, ref); });
+        sums = sums_by_reference<false, NT>(run, sums.m, c, w.scratch);
+        done = sums_hold(sums);
+    }
+    if (!done) {
+        Running<false> run;
+        pass([&](const float(&z)[kN]) { run.add(z, c); });
+        sums = sums_by_differences<false, NT>(run, c, w.scratch);
+    }
+
+    const Teacher teacher = teacher_of(a, e, w);
+    const float4 st = finish_row(a, row, weight, e, teacher, z_listed, sums, c, w);
+    const Factors f = factors_of(a, weight, teacher, st, c);
+    const double p = mass_of_token(e, teacher, a.known, w);
+    auto write = [&](auto exact, int chunk, const u32x4 v0, const u32x4 v1) {
+        const bool whole = (chunk + 1) * (kStep * NT) <= t.full;
+#pragma unroll
+        for (int u = 0; u < kStep; ++u) {
+            float z[V], g[V];
+            widen<DT>(u == 0 ? v0 : v1, z);
+#pragma unroll
+            for (int i = 0; i < V; ++i) g[i] = f.of_rest * exp2_fast(octaves_at<decltype(exact)::value>(f.x, z[i]));
+            store_vector<GDT>(out, t, (chunk * kStep + u) * NT + tid, whole, g);
+        }
+    };
+    auto write_all = [&](auto exact) {
+        u32x4 next[kStep];
+        auto fetch = [&](int chunk) {
+            const int at = chunk - kKept / kStep;
+            if (at < stored) {
+#pragma unroll
+                for (int u = 0; u < kStep; ++u) next[u] = store[(at * kStep + u) * NT + tid];
+            } else {
+                load_chunk<DT, NT, kStep, true>(t, chunk * (kStep * NT), next);
+            }
+        };
+        if (chunks > kKept / kStep) fetch(chunks - 1);
+        for (int chunk = chunks - 1; chunk >= kKept / kStep; --chunk) {
+            const u32x4 v0 = next[0], v1 = next[1];
+            if (chunk > kKept / kStep) fetch(chunk - 1);
+            write(exact, chunk, v0, v1);
+        }
+#pragma unroll
+        for (int k = 0; k < kKept; k += kStep) {
+            if (k * NT >= t.vectors) continue;
+            asm volatile("" : "+v"(kept[k]), "+v"(kept[k + 1]));
+            write(exact, k / kStep, kept[k], kept[k + 1]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    if (f.x.exact) write_all(std::true_type{});
+    else write_all(std::false_type{});
+    __syncthreads();
+    if (e.there) store_one<GDT>(out, e.id, listed_gradient(f, z_listed, p));
 }
 
 // One workgroup per part of a row: its sums.
-template <int DT>
+template <int DT, bool REST>
 __global__ __launch_bounds__(kThreads) void distill_parts_kernel(const DistillArgs a, const DistillScratch x, const int64_t first_row) {
     extern __shared__ uint32_t bits[];
     __shared__ float scratch[4 * kThreads / 64];
@@ -318,13 +434,8 @@ __global__ __launch_bounds__(kThreads) void distill_parts_kernel(const DistillAr
     if (weight_of_row(a, row) == 0.0f) return;
     const Part t = part_of<DT>(a.logits + row * a.row_bytes, a.n, at * x.part, x.part);
     const float c = 1.4426950408889634f / a.temperature;
-    RowSums r;
-    if (a.kind == kRest) {
-        const Marks marks = mark_list<DT>(t, entry_of(a, row), bits);
-        r = sum_rest<DT, false>(t, c, marks, scratch);
-    } else {
-        r = sum_all<DT, false>(t, c, scratch);
-    }
+    if constexpr (REST) mark_list<DT>(t, entry_of(a, row), bits);
+    const RowSums r = sums_of<DT, REST>(t, c, bits, scratch);
     if (threadIdx.x == 0) x.sums[row * x.parts + at] = make_float2(r.m, r.s);
 }
 
@@ -333,20 +444,15 @@ template <int DT>
 __global__ __launch_bounds__(kThreads) void distill_join_kernel(const DistillArgs a, const DistillScratch x, const int64_t first_row) {
     __shared__ ListWork w;
     __shared__ RowSums sums[kThreads / 64];
+    __shared__ int32_t keys[kSlots];
     const int64_t row = first_row + blockIdx.x;
     const int tid = threadIdx.x;
     const float weight = weight_of_row(a, row);
-    if (weight == 0.0f) {
-        if (tid == 0) {
-            a.loss[row] = 0.0f;
-            if (a.state) a.state[row] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        }
-        return;
-    }
+    if (skipped_row(a, row, weight)) return;
     const float c = 1.4426950408889634f / a.temperature;
     const Entry e = entry_of(a, row);
     const float z = e.there ? logit_at<DT>(a.logits + row * a.row_bytes, e.id) : -INFINITY;
-    enter_list(e, w);
+    if (a.kind == kRest) enter_list(e, keys, w);
     RowSums r{-INFINITY, 0.0f, 0.0f};
     for (int p = tid; p < x.parts; p += kThreads) {
         const float2 y = x.sums[row * x.parts + p];
@@ -449,27 +555,46 @@ size_t distill_scratch_bytes(int64_t rows, int64_t n) {
 
 hipError_t launch_distill(int dt, int grad_dt, const DistillArgs& a, hipStream_t stream) {
     const DistillScratch x = scratch_of(a.rows, a.n, a.scratch);
-    const size_t lds = a.kind != kRest ? 0 : dt == DT_BF16 ? marks_bytes<DT_BF16>(x.part) : marks_bytes<DT_F32>(x.part);
+    const bool rest = a.kind == kRest;
+    const size_t marks = rest ? marks_bytes<DT_F32>(x.part) : 0;
     if (x.parts == 1) {
-        auto go = [&](auto kernel) {
+        // chunks that the kept ones leave, as many as half a CU's LDS holds beside the rest
+        const int64_t chunk = (int64_t)kStep * kThreads * (dt == DT_BF16 ? 8 : 4), left = (a.n + chunk - 1) / chunk - kKept / kStep;
+        const int64_t room = (int64_t)((kLdsBytes / 2 - sizeof(ListWork) - 256 - marks) / kStoredBytes);
+        const int stored = (int)(left < 0 ? 0 : left < room ? left : room);
+        size_t lds = (size_t)stored * kStoredBytes;
+        if (lds < kSlots * sizeof(int32_t)) lds = kSlots * sizeof(int32_t);
+        auto step = [&](auto kernel) {
             return over_rows(a.rows, kThreads, [&](int64_t first, int64_t rows) {
-                hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(kThreads), lds, stream, a, first);
+                hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(kThreads), lds + marks, stream, a, first, stored);
             });
         };
-        if (dt == DT_BF16) {
-            if (!a.grad) return go(&distill_rows_kernel<DT_BF16, -1>);
-            return grad_dt == DT_BF16 ? go(&distill_rows_kernel<DT_BF16, DT_BF16>) : go(&distill_rows_kernel<DT_BF16, DT_F32>);
-        }
-        if (!a.grad) return go(&distill_rows_kernel<DT_F32, -1>);
-        return grad_dt == DT_BF16 ? go(&distill_rows_kernel<DT_F32, DT_BF16>) : go(&distill_rows_kernel<DT_F32, DT_F32>);
+        auto loss = [&](auto kernel) {
+            return over_rows(a.rows, kThreads, [&](int64_t first, int64_t rows) {
+                hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(kThreads), marks, stream, a, first);
+            });
+        };
+        auto of = [&](auto type, auto with_rest) {
+            constexpr int DT = decltype(type)::value;
+            constexpr bool REST = decltype(with_rest)::value;
+            if (!a.grad) return loss(&distill_rows_kernel<DT, REST>);
+            return grad_dt == DT_BF16 ? step(&distill_step_kernel<DT, DT_BF16, REST>) : step(&distill_step_kernel<DT, DT_F32, REST>);
+        };
+        constexpr std::integral_constant<int, DT_BF16> bf16{};
+        constexpr std::integral_constant<int, DT_F32> f32{};
+        if (dt == DT_BF16) return rest ? of(bf16, std::true_type{}) : of(bf16, std::false_type{});
+        return rest ? of(f32, std::true_type{}) : of(f32, std::false_type{});
     }
     DistillArgs b = a;
     if (!b.state) b.state = x.state;
-    hipError_t e = over_rows(a.rows, (int64_t)x.parts * kThreads, [&](int64_t first, int64_t rows) {
-        const dim3 grid((unsigned)(rows * x.parts));
-        if (dt == DT_BF16) hipLaunchKernelGGL((distill_parts_kernel<DT_BF16>), grid, dim3(kThreads), lds, stream, b, x, first);
-        else hipLaunchKernelGGL((distill_parts_kernel<DT_F32>), grid, dim3(kThreads), lds, stream, b, x, first);
-    });
+    auto parts = [&](auto kernel) {
+        return over_rows(a.rows, (int64_t)x.parts * kThreads, [&](int64_t first, int64_t rows) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * x.parts)), dim3(kThreads), marks, stream, b, x, first);
+        });
+    };
+    hipError_t e;
+    if (dt == DT_BF16) e = rest ? parts(&distill_parts_kernel<DT_BF16, true>) : parts(&distill_parts_kernel<DT_BF16, false>);
+    else e = rest ? parts(&distill_parts_kernel<DT_F32, true>) : parts(&distill_parts_kernel<DT_F32, false>);
     if (e != hipSuccess) return e;
     e = over_rows(a.rows, kThreads, [&](int64_t first, int64_t rows) {
         if (dt == DT_BF16) hipLaunchKernelGGL((distill_join_kernel<DT_BF16>), dim3((unsigned)rows), dim3(kThreads), 0, stream, b, x, first);
@@ -477,6 +602,24 @@ hipError_t launch_distill(int dt, int grad_dt, const DistillArgs& a, hipStream_t
     });
     if (e != hipSuccess || !a.grad) return e;
     return launch_distill_grad(dt, grad_dt, b, stream);
+}
+
+// the kernels of loss and gradient want up to half a CU's LDS
+hipError_t configure_distill_lds() {
+    hipError_t e = hipSuccess;
+    auto opt_in = [&](auto kernel) {
+        if (e == hipSuccess)
+            e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes / 2);
+    };
+    opt_in(&distill_step_kernel<DT_BF16, DT_BF16, true>);
+    opt_in(&distill_step_kernel<DT_BF16, DT_BF16, false>);
+    opt_in(&distill_step_kernel<DT_BF16, DT_F32, true>);
+    opt_in(&distill_step_kernel<DT_BF16, DT_F32, false>);
+    opt_in(&distill_step_kernel<DT_F32, DT_BF16, true>);
+    opt_in(&distill_step_kernel<DT_F32, DT_BF16, false>);
+    opt_in(&distill_step_kernel<DT_F32, DT_F32, true>);
+    opt_in(&distill_step_kernel<DT_F32, DT_F32, false>);
+    return e;
 }
 
 hipError_t launch_distill_grad(int dt, int grad_dt, const DistillArgs& a, hipStream_t stream) {

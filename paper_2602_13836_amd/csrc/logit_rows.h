@@ -110,16 +110,13 @@ __device__ __forceinline__ void load_chunk(const Part& t, int first, u32x4 (&v)[
     }
 }
 
-// f(chunk, v[U]) for every chunk of U x NT vectors of the part.  BACKWARDS: the last chunk first, for a part that was read a moment ago: what
-// came last is what the caches still hold (the second pass over 4096 x 128256 bfloat16 logits, whose rows in flight are as large as the
-// last-level cache: 453 us instead of 466 for both).
-template <int DT, int NT, int U, bool ONCE = true, bool BACKWARDS = false, class F>
+// f(chunk, v[U]) for every chunk of U x NT vectors of the part
+template <int DT, int NT, int U, class F>
 __device__ __forceinline__ void for_chunks(const Part& t, F&& f) {
     const int chunks = (t.vectors + U * NT - 1) / (U * NT);
-    for (int i = 0; i < chunks; ++i) {
-        const int c = BACKWARDS ? chunks - 1 - i : i;
+    for (int c = 0; c < chunks; ++c) {
         u32x4 v[U];
-        load_chunk<DT, NT, U, ONCE>(t, c * (U * NT), v);
+        load_chunk<DT, NT, U, true>(t, c * (U * NT), v);
         f(c, v);
     }
 }
@@ -219,12 +216,53 @@ __device__ __forceinline__ float block_max_f32(float x, float* scratch) {
     return m;
 }
 
+// the threads' sums into the workgroup's, the same for every thread
+template <int NT>
+__device__ __forceinline__ void block_sum_pair(float& s, float& e, float* scratch) {
+    const int wave = threadIdx.x >> 6;
+    s = wave_sum(s);
+    e = wave_sum(e);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) {
+        scratch[2 * wave] = s;
+        scratch[2 * wave + 1] = e;
+    }
+    __syncthreads();
+    s = e = 0.0f;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+        s += scratch[2 * w];
+        e += scratch[2 * w + 1];
+    }
+}
+template <bool ENTROPY, int NT>
+__device__ __forceinline__ RowSums sums_by_reference(const Sums<ENTROPY>& run, float m, float a, float* scratch) {
+    RowSums r{m, run.s, run.e};
+    block_sum_pair<NT>(r.s, r.e, scratch);
+    // from the rounded reference to m
+    const float shift = -fmaf(m, a, -(m * a)), rs = exp2_fast(shift);
+    r.e = rs * fmaf(shift, r.s, r.e);
+    r.s *= rs;
+    return r;
+}
+__device__ __forceinline__ bool sums_hold(const RowSums& r) { return r.s < 0x1p90f && fabsf(r.e) < 0x1p100f; }
+template <bool ENTROPY, int NT>
+__device__ __forceinline__ RowSums sums_by_differences(const Running<ENTROPY>& run, float a, float* scratch) {
+    RowSums r;
+    r.m = block_max_f32<NT>(run.m, scratch);
+    const float d = fmaxf((fmaxf(run.m, kLowestF32) - fmaxf(r.m, kLowestF32)) * a, kNoMass), rd = exp2_fast(d);
+    r.s = run.s * rd;
+    r.e = ENTROPY ? rd * fmaf(d, run.s, run.e) : 0.0f;
+    block_sum_pair<NT>(r.s, r.e, scratch);
+    return r;
+}
+
 // The sums of a part, the same for every thread and in the same order every time.  mask(chunk, z) may set places to -inf; seen(chunk, v, z)
 // looks at a chunk on the way.  scratch: 4 * NT / 64 floats.
 template <bool ENTROPY, int DT, int NT, int U, bool ONCE, class Mask, class Seen>
 __device__ __forceinline__ RowSums sum_part(const Part& t, float a, float* scratch, Mask&& mask, Seen&& seen) {
-    constexpr int N = U * kVec<DT>, kWaves = NT / 64;
-    const int chunks = (t.vectors + U * NT - 1) / (U * NT), wave = threadIdx.x >> 6;
+    constexpr int N = U * kVec<DT>;
+    const int chunks = (t.vectors + U * NT - 1) / (U * NT);
     auto widened = [&](int chunk, const u32x4(&v)[U], float(&z)[N]) {
 #pragma unroll
         for (int u = 0; u < U; ++u) widen<DT>(v[u], z + u * kVec<DT>);
@@ -255,25 +293,8 @@ __device__ __forceinline__ RowSums sum_part(const Part& t, float a, float* scrat
             for (int u = 0; u < U; ++u) v[u] = next[u];
             if (chunk + 2 < chunks) load_chunk<DT, NT, U, ONCE>(t, (chunk + 2) * (U * NT), next);
         }
-        r.s = wave_sum(run.s);
-        r.e = ENTROPY ? wave_sum(run.e) : 0.0f;
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) {
-            scratch[2 * wave] = r.s;
-            scratch[2 * wave + 1] = r.e;
-        }
-        __syncthreads();
-        r.s = r.e = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            r.s += scratch[2 * w];
-            r.e += scratch[2 * w + 1];
-        }
-        // from the rounded reference to m
-        const float shift = -fmaf(r.m, a, -c), rs = exp2_fast(shift);
-        r.e = rs * fmaf(shift, r.s, r.e);
-        r.s *= rs;
-        done = r.s < 0x1p90f && fabsf(r.e) < 0x1p100f;
+        r = sums_by_reference<ENTROPY, NT>(run, r.m, a, scratch);
+        done = sums_hold(r);
     }
     if (!done) {
         Running<ENTROPY> run;
@@ -283,21 +304,7 @@ __device__ __forceinline__ RowSums sum_part(const Part& t, float a, float* scrat
             seen(chunk, w, z);
             run.add(z, a);
         });
-        r.m = block_max_f32<NT>(run.m, scratch);
-        const float d = fmaxf((fmaxf(run.m, kLowestF32) - fmaxf(r.m, kLowestF32)) * a, kNoMass), rd = exp2_fast(d);
-        r.s = wave_sum(run.s * rd);
-        r.e = ENTROPY ? wave_sum(rd * fmaf(d, run.s, run.e)) : 0.0f;
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) {
-            scratch[2 * wave] = r.s;
-            scratch[2 * wave + 1] = r.e;
-        }
-        __syncthreads();
-        r.s = r.e = 0.0f;
-        for (int w = 0; w < kWaves; ++w) {
-            r.s += scratch[2 * w];
-            r.e += scratch[2 * w + 1];
-        }
+        r = sums_by_differences<ENTROPY, NT>(run, a, scratch);
     }
     return r;
 }
