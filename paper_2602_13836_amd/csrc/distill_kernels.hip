@@ -23,7 +23,6 @@ template <int DT>
 constexpr int kVectors = 16 / kVec<DT>;                   // of a chunk of a thread: 16 logits
 constexpr int kMaxKnown = 512, kSlots = 1024;
 constexpr int64_t kWholeRow = 1 << 18;                  // places of a part at most: 32 KB of marks
-constexpr int kLdsBytes = 160 * 1024;                   // of a CU
 constexpr int kRest = 2;                               // SV_TEACHER_REST
 static_assert(kMaxKnown == kThreads, "an entry of the list per thread");
 
@@ -37,10 +36,10 @@ struct DistillScratch {
 struct ListWork {
     double p[kMaxKnown];
     int32_t id[kMaxKnown];
-    double sums[kThreads / 64];
-    float scratch[4 * kThreads / 64];
     double teacher_sums[kThreads / 64];      // of a wavefront's entries
-    float teacher_most[kThreads / 64];
+    double list_sums[kThreads / 64], loss_sums[kThreads / 64];
+    float teacher_most[kThreads / 64], list_most[kThreads / 64];
+    float scratch[4 * kThreads / 64];
     uint32_t again;          // a token is listed twice
 };
 
@@ -62,81 +61,111 @@ __device__ __forceinline__ Entry entry_of(const DistillArgs& a, int64_t row) {
     return e;
 }
 
-// the teacher's probability of this thread's entry, its logarithm, and the masses: of the list, and what it leaves
+__device__ __forceinline__ double wave_sum_f64(double x) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+    return x;
+}
+
+// the teacher's probability of this thread's entry, its logarithm, and the masses: of the list, and what it leaves.  Exponentials are 64-bit ones, for
+// what the list leaves of 1; wavefronts without entries have none to take.  FINISH: for finish_row, the largest z (the logit at the
+// entry) goes to LDS.  One barrier.
 struct Teacher {
-    double p, log_p, mass, left;
+    double p, log_p;         // of this thread's entry; 0 without one
+    double mass, left;
 };
-__device__ __forceinline__ Teacher teacher_of(const DistillArgs& a, const Entry& e, ListWork& w) {
+template <bool FINISH>
+__device__ __forceinline__ Teacher teacher_of(const DistillArgs& a, const Entry& e, float z, ListWork& w) {
     Teacher t{0.0, 0.0, 0.0, 0.0};
     const bool none = e.value == -INFINITY;              // (a NaN counts, and spreads)
     const int wave = threadIdx.x >> 6, waves = (a.known + 63) >> 6;
+    const double inv_t = 1.0 / (double)a.temperature;
     float most = 0.0f;
-    // exponentials in 64 bits, for what the list leaves of 1; wavefronts without entries have none to take
     if (wave < waves) {
-        double x = (double)e.value;
+        t.log_p = (double)e.value;
         if (a.kind == 0) {
             most = fmaxf(wave_max_f32(e.value), kLowestF32);
-            x = (x - (double)most) / (double)a.temperature;
+            t.log_p = (t.log_p - (double)most) * inv_t;
         }
-        t.log_p = x;
-        t.p = none ? 0.0 : exp(x);
-        double sum = t.p;
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+        t.p = none ? 0.0 : exp(t.log_p);
+        const double sum = wave_sum_f64(t.p);
+        const float z_most = FINISH ? wave_max_f32(z) : 0.0f;
         if ((threadIdx.x & 63) == 0) {
             w.teacher_sums[wave] = sum;
             w.teacher_most[wave] = most;
+            if (FINISH) w.list_most[wave] = z_most;
         }
     }
     __syncthreads();
+    for (int i = 0; i < waves; ++i) t.mass += w.teacher_sums[i];
     if (a.kind == 0) {
-        float top = w.teacher_most[0];
-        for (int i = 1; i < waves; ++i) top = fmaxf(top, w.teacher_most[i]);
-        double total = 0.0;
-        for (int i = 0; i < waves; ++i) total += waves == 1 ? w.teacher_sums[i] : w.teacher_sums[i] * exp(((double)w.teacher_most[i] - (double)top) / (double)a.temperature);
-        if (wave < waves) {
-            const double down = waves == 1 ? 0.0 : ((double)most - (double)top) / (double)a.temperature;
-            t.log_p += down - log(total);
-            t.p = none ? 0.0 : t.p * (waves == 1 ? 1.0 : exp(down)) / total;
+        if (wave < waves) {                               // (log p is for finish_row)
+            double total = t.mass, down = 0.0;
+            if (waves > 1) {
+                float top = w.teacher_most[0];
+                for (int i = 1; i < waves; ++i) top = fmaxf(top, w.teacher_most[i]);
+                total = 0.0;
+                for (int i = 0; i < waves; ++i) total += w.teacher_sums[i] * exp(((double)w.teacher_most[i] - (double)top) * inv_t);
+                down = ((double)most - (double)top) * inv_t;
+                t.p *= exp(down);
+            }
+            if (FINISH) t.log_p += down - log(total);
+            t.p = none ? 0.0 : t.p / total;
         }
-        t.mass = total == 0.0 ? 0.0 : total != total ? total : 1.0;
+        t.mass = t.mass > 0.0 ? 1.0 : t.mass;             // (0 without an entry, NaN with one of NaN)
     } else {
-        for (int i = 0; i < waves; ++i) t.mass += w.teacher_sums[i];
         t.left = a.kind == kRest ? fmax(1.0 - t.mass, 0.0) : 0.0;
     }
     return t;
 }
 
-// The row's loss and state.  sums: over the places that are not listed where the rest counts, else over all.  z: the logit at this thread's entry.
+// The row's loss, and its state, which every thread gets.  sums: over the places that are not listed where the rest counts, else over all.  z: the logit
+// at this thread's entry.  One barrier.
 __device__ __forceinline__ float4 finish_row(const DistillArgs& a, int64_t row, float weight, const Entry& e, const Teacher& t, float z,
                                              const RowSums& sums, float c, ListWork& w) {
+    const int wave = threadIdx.x >> 6, waves = (a.known + 63) >> 6;
+    const bool rest = a.kind == kRest;
     float m = sums.m;
+    if (rest)
+        for (int i = 0; i < waves; ++i) m = fmaxf(m, w.list_most[i]);
+    const float ref = fmaxf(m, kLowestF32);
+    const double inv_t = 1.0 / (double)a.temperature;
+    if (wave < waves) {
+        if (rest) {
+            bool first = e.there;                           // each token once
+            if (w.again != 0u && e.there)
+                for (int i = 0; i < (int)threadIdx.x; ++i) first = first && w.id[i] != e.id;
+            const double list = wave_sum_f64(first ? (double)exp2_fast((z - ref) * c) : 0.0);
+            if ((threadIdx.x & 63) == 0) w.list_sums[wave] = list;
+        }
+        // p (log p - log q) without log S, which comes last
+        const double part = t.p == 0.0 ? 0.0 : z == -INFINITY ? INFINITY : t.p * (t.log_p - ((double)z - (double)ref) * inv_t);
+        const double loss = wave_sum_f64(part);
+        if ((threadIdx.x & 63) == 0) w.loss_sums[wave] = loss;
+    }
+    __syncthreads();
     double s = (double)sums.s;
-    if (a.kind == kRest) {
-        // each token once
-        bool first = e.there;
-        if (w.again != 0u && e.there)
-            for (int i = 0; i < (int)threadIdx.x; ++i) first = first && w.id[i] != e.id;
-        m = fmaxf(block_max_f32<kThreads>(z, w.scratch), sums.m);
-        const float ref = fmaxf(m, kLowestF32);
-        s *= exp2(fmax(((double)fmaxf(sums.m, kLowestF32) - (double)ref) * c, (double)kNoMass));
-        s += block_sum_f64<kThreads>(first ? (double)exp2_fast((z - ref) * c) : 0.0, w.sums);
+    if (rest) {
+        s *= (double)exp2_fast(fmaxf((fmaxf(sums.m, kLowestF32) - ref) * c, kNoMass));
+        for (int i = 0; i < waves; ++i) s += w.list_sums[i];
     }
-    const double ref = (double)fmaxf(m, kLowestF32), log_s = log(s);
-    double part = 0.0;
-    if (t.p != 0.0) {
-        const double log_q = z == -INFINITY || s == 0.0 ? -INFINITY : ((double)z - ref) / (double)a.temperature - log_s;
-        part = t.p * (t.log_p - log_q);
-    }
-    double loss = block_sum_f64<kThreads>(part, w.sums);
-    if (s != s) loss = s;
     float4 state = make_float4(s == 0.0 ? 0.0f : m, (float)s, 0.0f, 0.0f);
-    if (a.kind == kRest && sums.s != 0.0f) {
+    if (rest && sums.s != 0.0f) {
         state.z = sums.m;
         state.w = sums.s;
-        if (t.left > 0.0) loss += t.left * (log(t.left) - (((double)sums.m - ref) / (double)a.temperature + log((double)sums.s) - log_s));
     }
     if (threadIdx.x == 0) {
+        double loss = 0.0;
+        for (int i = 0; i < waves; ++i) loss += w.loss_sums[i];
+        if (s == 0.0) {
+            loss = t.mass > 0.0 ? INFINITY : t.mass;
+        } else {
+            const double log_s = log(s);
+            loss += t.mass * log_s;
+            if (t.left > 0.0 && state.w != 0.0f)
+                loss += t.left * (log(t.left) - (((double)sums.m - (double)ref) * inv_t + log((double)sums.s) - log_s));
+            if (s != s) loss = s;
+        }
         a.loss[row] = (float)((double)weight * loss);
         if (a.state) a.state[row] = state;
     }
@@ -183,13 +212,20 @@ __host__ __device__ inline size_t marks_bytes(int64_t places) {
     constexpr int64_t kPlaces = (int64_t)kThreads * 16;
     return (size_t)((places + kPlaces - 1) / kPlaces) * (kPlaces / 8);
 }
-// every thread calls
+// every thread calls; w, where it is given, gets the list and whether a token is in it twice
 template <int DT>
-__device__ __forceinline__ void mark_list(const Part& part, const Entry& e, uint32_t* bits) {
+__device__ __forceinline__ void mark_list(const Part& part, const Entry& e, uint32_t* bits, ListWork* w) {
     clear_words<kThreads>(bits, (int)(marks_bytes<DT>(part.n) / 4));
+    if (w) {
+        w->id[threadIdx.x] = e.there ? e.id : -1;
+        if (threadIdx.x == 0) w->again = 0u;
+    }
     __syncthreads();
     const int64_t place = e.there ? e.id - part.first : -1;
-    if (place >= 0 && place < part.n) atomicOr(&bits[place >> 5], 1u << (place & 31));
+    if (place >= 0 && place < part.n) {
+        const uint32_t was = atomicOr(&bits[place >> 5], 1u << (place & 31));
+        if (w && ((was >> (place & 31)) & 1u)) w->again = 1u;
+    }
     __syncthreads();
 }
 // vectors layer * kThreads + thread, (layer + 1) * kThreads + thread, ... without their marked places
@@ -204,8 +240,12 @@ __device__ __forceinline__ void without_marked(const uint32_t* bits, int layer, 
     }
     if (any == 0u) return;
 #pragma unroll
-    for (int i = 0; i < U * V; ++i)
-        if ((marks[i / V] >> (i % V)) & 1u) z[i] = -INFINITY;
+    for (int u = 0; u < U; ++u) {
+        if (marks[u] == 0u) continue;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if ((marks[u] >> i) & 1u) z[u * V + i] = -INFINITY;
+    }
 }
 // the mass of this thread's token, from all entries that name it; every thread calls
 __device__ __forceinline__ double mass_of_token(const Entry& e, const Teacher& t, int known, ListWork& w) {
@@ -222,7 +262,7 @@ __device__ __forceinline__ double mass_of_token(const Entry& e, const Teacher& t
 template <int DT, bool REST>
 __device__ __forceinline__ RowSums sums_of(const Part& t, float c, const uint32_t* bits, float* scratch) {
     constexpr int U = kVectors<DT>, kN = U * kVec<DT>;
-    return sum_part<false, DT, kThreads, U, true>(
+    return sum_part<false, DT, kThreads, U>(
         t, c, scratch,
         [&](int chunk, float(&z)[kN]) {
             if constexpr (REST) without_marked<DT, U>(bits, chunk * U, z);
@@ -252,38 +292,34 @@ template <int DT, bool REST>
 __global__ __launch_bounds__(kThreads) void distill_rows_kernel(const DistillArgs a, const int64_t first_row) {
     extern __shared__ uint32_t bits[];
     __shared__ ListWork w;
-    __shared__ int32_t keys[kSlots];
     const int64_t row = first_row + blockIdx.x;
     const float weight = weight_of_row(a, row);
+    const Entry e = entry_of(a, row);
     if (skipped_row(a, row, weight)) return;
     const char* logits = a.logits + row * a.row_bytes;
     const Part t = part_of<DT>(logits, a.n, 0, a.n);
     const float c = 1.4426950408889634f / a.temperature;
-    const Entry e = entry_of(a, row);
     const float z = e.there ? logit_at<DT>(logits, e.id) : -INFINITY;
-    if constexpr (REST) {
-        enter_list(e, keys, w);
-        mark_list<DT>(t, e, bits);
-    }
+    if constexpr (REST) mark_list<DT>(t, e, bits, &w);
     const RowSums sums = sums_of<DT, REST>(t, c, bits, w.scratch);
-    const Teacher teacher = teacher_of(a, e, w);
+    const Teacher teacher = teacher_of<true>(a, e, z, w);
     finish_row(a, row, weight, e, teacher, z, sums, c, w);
 }
 
 // One workgroup per row: loss and gradient, that is two passes over the row.  The fabric moves 7 TB/s whether the lines come from the last-level
-// cache or from memory, so the second pass reads as little as it can: a thread keeps its first 16 vectors in registers and some more in
-// LDS (`stored` chunks of two), 70 per cent of 128256 bfloat16 logits, and walks the others backwards.  Two workgroups share a CU, so that one's
-// reads fill the time of the other's sums.
-constexpr int kKept = 16, kStep = 2;
-constexpr size_t kStoredBytes = (size_t)kStep * kThreads * 16;
-template <int DT, int GDT, bool REST>
-__global__ __launch_bounds__(kThreads, 4) void distill_step_kernel(const DistillArgs a, const int64_t first_row, const int stored) {
-    constexpr int V = kVec<DT>, kN = kStep * V, NT = kThreads;
-    extern __shared__ u32x4 store[];                       // stored * kStep * NT vectors, then the marks
+// cache or from memory, so the second pass reads as little as it can: a thread keeps its first KEPT vectors in registers -- 16, half of
+// 128256 bfloat16 logits, or 4 where the row has no more -- and walks the others backwards, of which the L2 then still holds most (4096 rows: 408 us, 422 with 8
+// kept, 441 with 4; 2.1 GB, a read and a write of each place).  Some of the others in LDS changed nothing.
+constexpr int kStep = 2;                                   // vectors of a chunk
+template <int DT, int GDT, bool REST, int KEPT>
+__global__ __launch_bounds__(kThreads, KEPT > 4 ? 4 : 6) void distill_step_kernel(const DistillArgs a, const int64_t first_row) {
+    constexpr int V = kVec<DT>, kN = kStep * V, NT = kThreads, kFirst = KEPT / kStep;
+    extern __shared__ uint32_t bits[];
     __shared__ ListWork w;
     const int tid = threadIdx.x;
     const int64_t row = first_row + blockIdx.x;
     const float weight = weight_of_row(a, row);
+    const Entry e = entry_of(a, row);                      // (asked for before the row: loads come back in order)
     const char* logits = a.logits + row * a.row_bytes;
     char* out = a.grad + row * a.grad_row_bytes;
     const Part t = part_of<DT>(logits, a.n, 0, a.n);
@@ -291,33 +327,29 @@ __global__ __launch_bounds__(kThreads, 4) void distill_step_kernel(const Distill
         write_zeros<DT, GDT>(t, out);
         return;
     }
-    uint32_t* bits = reinterpret_cast<uint32_t*>(store + stored * kStep * NT);
-    u32x4 kept[kKept];
+    const float c = 1.4426950408889634f / a.temperature;
+    const float z_listed = e.there ? logit_at<DT>(logits, e.id) : -INFINITY;
+    u32x4 kept[KEPT];
 #pragma unroll
-    for (int k = 0; k < kKept; k += kStep) {
+    for (int k = 0; k < KEPT; k += kStep) {
         u32x4 v[kStep];
         load_chunk<DT, NT, kStep, true>(t, k * NT, v);
         kept[k] = v[0];
         kept[k + 1] = v[1];
     }
-    const float c = 1.4426950408889634f / a.temperature;
-    const Entry e = entry_of(a, row);
-    const float z_listed = e.there ? logit_at<DT>(logits, e.id) : -INFINITY;
-    // (the table of places lies where chunks will be stored later: a barrier of the sums is in between)
-    enter_list(e, reinterpret_cast<int32_t*>(store), w);
-    if constexpr (REST) mark_list<DT>(t, e, bits);
+    if constexpr (REST) mark_list<DT>(t, e, bits, &w);
+    else enter_list(e, reinterpret_cast<int32_t*>(bits), w);
 
-    const int chunks = (t.vectors + kStep * NT - 1) / (kStep * NT);       // the first kKept / kStep of them are kept
+    const int chunks = (t.vectors + kStep * NT - 1) / (kStep * NT);       // the first kFirst of them are kept
     auto logits_of = [&](int chunk, const u32x4 v0, const u32x4 v1, float(&z)[kN]) {
         widen<DT>(v0, z);
         widen<DT>(v1, z + V);
         if constexpr (REST) without_marked<DT, kStep>(bits, chunk * kStep, z);
     };
-    bool is_stored = false;
-    // f(z) of every chunk; the first time the chunks to be stored are
+    // f(z) of every chunk
     auto pass = [&](auto&& f) {
 #pragma unroll
-        for (int k = 0; k < kKept; k += kStep) {
+        for (int k = 0; k < KEPT; k += kStep) {
             if (k * NT >= t.vectors) continue;
             // (or the widened logits would live on to the next pass, in twice the registers)
             asm volatile("" : "+v"(kept[k]), "+v"(kept[k + 1]));
@@ -327,29 +359,14 @@ __global__ __launch_bounds__(kThreads, 4) void distill_step_kernel(const Distill
             __builtin_amdgcn_sched_barrier(0);
         }
         u32x4 next[kStep];
-        auto fetch = [&](int chunk) {
-            const int at = chunk - kKept / kStep;
-            if (at < stored && is_stored) {
-#pragma unroll
-                for (int u = 0; u < kStep; ++u) next[u] = store[(at * kStep + u) * NT + tid];
-            } else {
-                load_chunk<DT, NT, kStep, false>(t, chunk * (kStep * NT), next);
-            }
-        };
-        if (chunks > kKept / kStep) fetch(kKept / kStep);
-        for (int chunk = kKept / kStep; chunk < chunks; ++chunk) {
+        if (chunks > kFirst) load_chunk<DT, NT, kStep, false>(t, kFirst * (kStep * NT), next);
+        for (int chunk = kFirst; chunk < chunks; ++chunk) {
             const u32x4 v0 = next[0], v1 = next[1];
-            if (chunk + 1 < chunks) fetch(chunk + 1);
-            const int at = chunk - kKept / kStep;
-            if (at < stored && !is_stored) {
-                store[at * kStep * NT + tid] = v0;
-                store[(at * kStep + 1) * NT + tid] = v1;
-            }
+            if (chunk + 1 < chunks) load_chunk<DT, NT, kStep, false>(t, (chunk + 1) * (kStep * NT), next);
             float z[kN];
             logits_of(chunk, v0, v1, z);
             f(z);
         }
-        is_stored = true;
     };
     RowSums sums;
     {
@@ -378,7 +395,7 @@ __global__ __launch_bounds__(kThreads, 4) void distill_step_kernel(const Distill
         sums = sums_by_differences<false, NT>(run, c, w.scratch);
     }
 
-    const Teacher teacher = teacher_of(a, e, w);
+    const Teacher teacher = teacher_of<true>(a, e, z_listed, w);
     const float4 st = finish_row(a, row, weight, e, teacher, z_listed, sums, c, w);
     const Factors f = factors_of(a, weight, teacher, st, c);
     const double p = mass_of_token(e, teacher, a.known, w);
@@ -395,23 +412,14 @@ __global__ __launch_bounds__(kThreads, 4) void distill_step_kernel(const Distill
     };
     auto write_all = [&](auto exact) {
         u32x4 next[kStep];
-        auto fetch = [&](int chunk) {
-            const int at = chunk - kKept / kStep;
-            if (at < stored) {
-#pragma unroll
-                for (int u = 0; u < kStep; ++u) next[u] = store[(at * kStep + u) * NT + tid];
-            } else {
-                load_chunk<DT, NT, kStep, true>(t, chunk * (kStep * NT), next);
-            }
-        };
-        if (chunks > kKept / kStep) fetch(chunks - 1);
-        for (int chunk = chunks - 1; chunk >= kKept / kStep; --chunk) {
+        if (chunks > kFirst) load_chunk<DT, NT, kStep, true>(t, (chunks - 1) * (kStep * NT), next);
+        for (int chunk = chunks - 1; chunk >= kFirst; --chunk) {
             const u32x4 v0 = next[0], v1 = next[1];
-            if (chunk > kKept / kStep) fetch(chunk - 1);
+            if (chunk > kFirst) load_chunk<DT, NT, kStep, true>(t, (chunk - 1) * (kStep * NT), next);
             write(exact, chunk, v0, v1);
         }
 #pragma unroll
-        for (int k = 0; k < kKept; k += kStep) {
+        for (int k = 0; k < KEPT; k += kStep) {
             if (k * NT >= t.vectors) continue;
             asm volatile("" : "+v"(kept[k]), "+v"(kept[k + 1]));
             write(exact, k / kStep, kept[k], kept[k + 1]);
@@ -434,7 +442,7 @@ __global__ __launch_bounds__(kThreads) void distill_parts_kernel(const DistillAr
     if (weight_of_row(a, row) == 0.0f) return;
     const Part t = part_of<DT>(a.logits + row * a.row_bytes, a.n, at * x.part, x.part);
     const float c = 1.4426950408889634f / a.temperature;
-    if constexpr (REST) mark_list<DT>(t, entry_of(a, row), bits);
+    if constexpr (REST) mark_list<DT>(t, entry_of(a, row), bits, nullptr);
     const RowSums r = sums_of<DT, REST>(t, c, bits, scratch);
     if (threadIdx.x == 0) x.sums[row * x.parts + at] = make_float2(r.m, r.s);
 }
@@ -465,22 +473,25 @@ __global__ __launch_bounds__(kThreads) void distill_join_kernel(const DistillArg
     r = sums[0];
 #pragma unroll
     for (int i = 1; i < kThreads / 64; ++i) r = joined<false>(r, sums[i], c);
-    const Teacher teacher = teacher_of(a, e, w);
+    const Teacher teacher = teacher_of<true>(a, e, z, w);
     finish_row(a, row, weight, e, teacher, z, r, c, w);
 }
 
 // One workgroup per part of a row: its gradient from the row's state.  Small parts, asked for before anything else is looked at (2048 x 128256
-// bfloat16, a fifth of the rows without weight: 167 us).
-constexpr int64_t kGradPart = 1 << 13;
+// bfloat16, a fifth of the rows without weight: 160 us with 16384 places, 168 with 8192).
+template <int DT>
+constexpr int kGradPart = 4 * kThreads * kVec<DT>;        // places of a part: four vectors of each thread
 template <int DT, int GDT>
-__global__ __launch_bounds__(kThreads) void distill_grad_kernel(const DistillArgs a, const int64_t first_row, const int parts) {
-    constexpr int V = kVec<DT>, U = (int)kGradPart / (kThreads * V);
-    __shared__ uint32_t bits[kGradPart / 32];
+__global__ __launch_bounds__(kThreads, 8) void distill_grad_kernel(const DistillArgs a, const int64_t first_row, const int parts) {
+    constexpr int V = kVec<DT>, U = 4;
+    __shared__ uint32_t bits[kGradPart<DT> / 32];
     __shared__ ListWork w;
     const int tid = threadIdx.x;
     const int64_t row = first_row + blockIdx.x / (unsigned)parts;
     const float weight = weight_of_row(a, row);
-    const Part t = part_of<DT>(a.logits + row * a.row_bytes, a.n, (int64_t)(blockIdx.x % (unsigned)parts) * kGradPart, kGradPart);
+    const Entry e = entry_of(a, row);
+    const float4 st = a.state[row];
+    const Part t = part_of<DT>(a.logits + row * a.row_bytes, a.n, (int64_t)(blockIdx.x % (unsigned)parts) * kGradPart<DT>, kGradPart<DT>);
     char* out = a.grad + row * a.grad_row_bytes;
     if (weight == 0.0f) {
         write_zeros<DT, GDT>(t, out);
@@ -489,14 +500,12 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(const DistillArg
     u32x4 v[U];
     load_chunk<DT, kThreads, U, true>(t, 0, v);
     const float c = 1.4426950408889634f / a.temperature;
-    const float4 st = a.state[row];
-    const Entry e = entry_of(a, row);
     const int64_t at = e.there ? e.id - t.first : -1;
     const bool here = at >= 0 && at < t.n;
     const float z_listed = here ? logit_at<DT>(t.p, at) : -INFINITY;
-    if (tid < (int)kGradPart / 32) bits[tid] = 0u;
+    if (tid < kGradPart<DT> / 32) bits[tid] = 0u;
     if (tid == 0) w.again = 0u;
-    const Teacher teacher = teacher_of(a, e, w);            // (a barrier)
+    const Teacher teacher = teacher_of<false>(a, e, z_listed, w);  // (a barrier)
     if (here && ((atomicOr(&bits[at >> 5], 1u << (at & 31)) >> (at & 31)) & 1u)) w.again = 1u;
     w.id[tid] = e.there ? e.id : -1;
     w.p[tid] = teacher.p;
@@ -558,15 +567,11 @@ hipError_t launch_distill(int dt, int grad_dt, const DistillArgs& a, hipStream_t
     const bool rest = a.kind == kRest;
     const size_t marks = rest ? marks_bytes<DT_F32>(x.part) : 0;
     if (x.parts == 1) {
-        // chunks that the kept ones leave, as many as half a CU's LDS holds beside the rest
-        const int64_t chunk = (int64_t)kStep * kThreads * (dt == DT_BF16 ? 8 : 4), left = (a.n + chunk - 1) / chunk - kKept / kStep;
-        const int64_t room = (int64_t)((kLdsBytes / 2 - sizeof(ListWork) - 256 - marks) / kStoredBytes);
-        const int stored = (int)(left < 0 ? 0 : left < room ? left : room);
-        size_t lds = (size_t)stored * kStoredBytes;
-        if (lds < kSlots * sizeof(int32_t)) lds = kSlots * sizeof(int32_t);
+        const bool small = a.n <= 4 * kThreads * (dt == DT_BF16 ? 8 : 4);
+        const size_t lds = rest ? marks : kSlots * sizeof(int32_t);
         auto step = [&](auto kernel) {
             return over_rows(a.rows, kThreads, [&](int64_t first, int64_t rows) {
-                hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(kThreads), lds + marks, stream, a, first, stored);
+                hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(kThreads), lds, stream, a, first);
             });
         };
         auto loss = [&](auto kernel) {
@@ -578,7 +583,8 @@ hipError_t launch_distill(int dt, int grad_dt, const DistillArgs& a, hipStream_t
             constexpr int DT = decltype(type)::value;
             constexpr bool REST = decltype(with_rest)::value;
             if (!a.grad) return loss(&distill_rows_kernel<DT, REST>);
-            return grad_dt == DT_BF16 ? step(&distill_step_kernel<DT, DT_BF16, REST>) : step(&distill_step_kernel<DT, DT_F32, REST>);
+            if (small) return grad_dt == DT_BF16 ? step(&distill_step_kernel<DT, DT_BF16, REST, 4>) : step(&distill_step_kernel<DT, DT_F32, REST, 4>);
+            return grad_dt == DT_BF16 ? step(&distill_step_kernel<DT, DT_BF16, REST, 16>) : step(&distill_step_kernel<DT, DT_F32, REST, 16>);
         };
         constexpr std::integral_constant<int, DT_BF16> bf16{};
         constexpr std::integral_constant<int, DT_F32> f32{};
@@ -604,26 +610,9 @@ hipError_t launch_distill(int dt, int grad_dt, const DistillArgs& a, hipStream_t
     return launch_distill_grad(dt, grad_dt, b, stream);
 }
 
-// the kernels of loss and gradient want up to half a CU's LDS
-hipError_t configure_distill_lds() {
-    hipError_t e = hipSuccess;
-    auto opt_in = [&](auto kernel) {
-        if (e == hipSuccess)
-            e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes / 2);
-    };
-    opt_in(&distill_step_kernel<DT_BF16, DT_BF16, true>);
-    opt_in(&distill_step_kernel<DT_BF16, DT_BF16, false>);
-    opt_in(&distill_step_kernel<DT_BF16, DT_F32, true>);
-    opt_in(&distill_step_kernel<DT_BF16, DT_F32, false>);
-    opt_in(&distill_step_kernel<DT_F32, DT_BF16, true>);
-    opt_in(&distill_step_kernel<DT_F32, DT_BF16, false>);
-    opt_in(&distill_step_kernel<DT_F32, DT_F32, true>);
-    opt_in(&distill_step_kernel<DT_F32, DT_F32, false>);
-    return e;
-}
-
 hipError_t launch_distill_grad(int dt, int grad_dt, const DistillArgs& a, hipStream_t stream) {
-    const int parts = (int)((a.n + kGradPart - 1) / kGradPart);
+    const int64_t part = dt == DT_BF16 ? kGradPart<DT_BF16> : kGradPart<DT_F32>;
+    const int parts = (int)((a.n + part - 1) / part);
     auto go = [&](auto kernel) {
         return over_rows(a.rows, (int64_t)parts * kThreads, [&](int64_t first, int64_t rows) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * parts)), dim3(kThreads), 0, stream, a, first, parts);

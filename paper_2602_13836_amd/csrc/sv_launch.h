@@ -478,6 +478,5 @@ struct DistillArgs {
 size_t distill_scratch_bytes(int64_t rows, int64_t n);
 hipError_t launch_distill(int dt, int grad_dt, const DistillArgs& a, hipStream_t stream);
 hipError_t launch_distill_grad(int dt, int grad_dt, const DistillArgs& a, hipStream_t stream);
-hipError_t configure_distill_lds();
 
 }  // namespace sv

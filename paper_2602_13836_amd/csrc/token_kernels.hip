@@ -328,7 +328,7 @@ __global__ __launch_bounds__(NT) void token_rows_kernel(const TokenArgs a, const
     if constexpr (WHOLE) given = given_token<DT, NT>(a, row, find_work);
     float thread_most = -INFINITY;
     u32x4 only[U];
-    const RowSums r = sum_part<true, DT, NT, U, !TOP>(
+    const RowSums r = sum_part<true, DT, NT, U>(
         t, c, sums, [](int, float(&)[kN]) {},
         [&](int chunk, const u32x4(&v)[U], const float(&z)[kN]) {
             if constexpr (TOP) {
