@@ -267,7 +267,7 @@ __device__ __forceinline__ RowSums sums_of(const Part& t, float c, const uint32_
         [&](int chunk, float(&z)[kN]) {
             if constexpr (REST) without_marked<DT, U>(bits, chunk * U, z);
         },
-        [](int, const u32x4(&)[U], const float(&)[kN]) {});
+        [](int, const u32x4(&)[U], float) {});
 }
 
 template <int DT, int GDT>
@@ -384,9 +384,9 @@ __global__ __launch_bounds__(kThreads, KEPT > 4 ? 4 : 6) void distill_step_kerne
     const float ref = sums.m * c;
     bool done = fabsf(ref) < 0x1p100f;
     if (done) {
-        Sums<false> run;
+        Sums run;
         pass([&](const float(&z)[kN]) { run.add(z, c, ref); });
-        sums = sums_by_reference<false, NT>(run, sums.m, c, w.scratch);
+        sums = sums_by_reference<NT>(run, sums.m, c, w.scratch);
         done = sums_hold(sums);
     }
     if (!done) {

@@ -124,37 +124,46 @@ __device__ __forceinline__ void for_chunks(const Part& t, F&& f) {
 
 // ---- softmax sums, in octaves: with a = log2(e) / T, s = sum of 2^(a (z - m)) and, for entropies, e = sum of 2^(a (z - m)) a (z - m)
 struct RowSums {
-    float m;        // the reference: a logit of the row near its largest; -inf where all places are masked
+    float m;        // the reference: a logit of the row near its largest, with entropies the largest; -inf where all places are masked
     float s, e;     // 0 then
 };
 
-// The reference is the largest logit of the first chunk (16 or 32 logits of every thread): what lies above it, up to 2^90
-// times, float32 holds as well.  So a logit takes one fused multiply-add, an exponential and an addition: c = a m is rounded, but the sums are exactly those
-// of the rounded reference, and block_sums moves them to m itself.
-template <bool ENTROPY>
+// The sums of a thread.  The reference is c = a m, rounded; the sums are exactly those of the rounded c, so a logit takes one fused
+// multiply-add, an exponential and an addition, and no error grows with the logits' size.  The block's sums are moved to m itself.
+//
+// Without entropies m is the largest logit of the first chunk (16 logits of every thread): what lies above it, up to 2^90 times, float32 holds as well.
 struct Sums {
-    float s = 0.0f, e = 0.0f;
-    bool masks = false;      // (the same for a wavefront) there have been places of -inf: their 0 * -inf is kept out of e
+    float s = 0.0f;
 
     template <int N>
     __device__ __forceinline__ void add(const float (&z)[N], float a, float c) {
-        if constexpr (ENTROPY) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) s += exp2_fast(fmaf(z[i], a, -c));
+    }
+};
+// With entropies m is the thread's largest logit so far, or e / s and log s would cancel.
+struct EntropySums {
+    float m = -INFINITY, c = kLowestF32, s = 0.0f, e = 0.0f;
+    bool masks = false;      // (the same for a wavefront) there have been places of -inf: their 0 * -inf is kept out of e
+
+    template <int N>
+    __device__ __forceinline__ void add(const float (&z)[N], float most, float a) {
+        m = fmaxf(m, most);
+        const float now = fminf(fmaxf(m * a, kLowestF32), -kLowestF32), d = fmaxf(c - now, kNoMass), r = exp2_fast(d);
+        e = r * fmaf(d, s, e);
+        s *= r;
+        c = now;
+        if (!masks) {
+            float sum = s, esum = e;
+            add_terms<false>(z, a, now, sum, esum);
+            masks = __builtin_amdgcn_ballot_w64(esum != esum) != 0ull;
             if (!masks) {
-                float esum = e;
-                add_terms<false>(z, a, c, s, esum);
-                masks = __builtin_amdgcn_ballot_w64(esum != esum) != 0ull;
-                if (!masks) {
-                    e = esum;
-                    return;
-                }
-                float again = 0.0f;
-                add_terms<true>(z, a, c, again, e);
-            } else {
-                add_terms<true>(z, a, c, s, e);
+                s = sum;
+                e = esum;
+                return;
             }
-        } else {
-            add_terms<false>(z, a, c, s, e);
         }
+        add_terms<true>(z, a, now, s, e);
     }
 
 private:
@@ -164,7 +173,7 @@ private:
         for (int i = 0; i < N; ++i) {
             const float y = fmaf(z[i], a, -c), p = exp2_fast(y);
             s += p;
-            if constexpr (ENTROPY) e = fmaf(p, CUT ? fmaxf(y, kNoMass) : y, e);
+            e = fmaf(p, CUT ? fmaxf(y, kNoMass) : y, e);
         }
     }
 };
@@ -191,6 +200,17 @@ struct Running {
         }
     }
 };
+
+// log s, in 64 bits as far as its size goes: with (z - m) / T in 64 bits the log probability of a likely token keeps its digits
+__device__ __forceinline__ double log_of_sum(float s) {
+    int k;
+    float f = frexpf(s, &k);
+    if (f < 0.70710678f) {                                 // (around 1, where its logarithm is near 0 and has its digits)
+        f *= 2.0f;
+        --k;
+    }
+    return fma((double)k, 0.69314718055994530942, (double)logf(f));
+}
 
 // sums of two sets of places
 template <bool ENTROPY>
@@ -236,17 +256,32 @@ __device__ __forceinline__ void block_sum_pair(float& s, float& e, float* scratc
         e += scratch[2 * w + 1];
     }
 }
-template <bool ENTROPY, int NT>
-__device__ __forceinline__ RowSums sums_by_reference(const Sums<ENTROPY>& run, float m, float a, float* scratch) {
-    RowSums r{m, run.s, run.e};
+template <int NT>
+__device__ __forceinline__ RowSums sums_by_reference(const Sums& run, float m, float a, float* scratch) {
+    RowSums r{m, run.s, 0.0f};
     block_sum_pair<NT>(r.s, r.e, scratch);
-    // from the rounded reference to m
-    const float shift = -fmaf(m, a, -(m * a)), rs = exp2_fast(shift);
-    r.e = rs * fmaf(shift, r.s, r.e);
-    r.s *= rs;
+    r.s *= exp2_fast(-fmaf(m, a, -(m * a)));               // from the rounded reference to m
     return r;
 }
-__device__ __forceinline__ bool sums_hold(const RowSums& r) { return r.s < 0x1p90f && fabsf(r.e) < 0x1p100f; }
+template <int NT>
+__device__ __forceinline__ RowSums sums_by_reference(const EntropySums& run, float a, float* scratch) {
+    RowSums r;
+    r.m = block_max_f32<NT>(run.m, scratch);
+    const float c = fminf(fmaxf(r.m * a, kLowestF32), -kLowestF32), d = fmaxf(run.c - c, kNoMass), rd = exp2_fast(d);
+    r.s = run.s * rd;
+    r.e = rd * fmaf(d, run.s, run.e);
+    block_sum_pair<NT>(r.s, r.e, scratch);
+    if (r.s > 0.0f) {
+        const float shift = -fmaf(r.m, a, -c), rs = exp2_fast(shift);
+        r.e = rs * fmaf(shift, r.s, r.e);
+        r.s *= rs;
+    }
+    return r;
+}
+// false: sums by reference may be those of a row that float32 does not hold so
+__device__ __forceinline__ bool sums_hold(const RowSums& r) {
+    return r.s < 0x1p90f && fabsf(r.e) < 0x1p100f && (r.s > 0.0f || r.m == -INFINITY);
+}
 template <bool ENTROPY, int NT>
 __device__ __forceinline__ RowSums sums_by_differences(const Running<ENTROPY>& run, float a, float* scratch) {
     RowSums r;
@@ -258,8 +293,8 @@ __device__ __forceinline__ RowSums sums_by_differences(const Running<ENTROPY>& r
     return r;
 }
 
-// The sums of a part, the same for every thread and in the same order every time.  mask(chunk, z) may set places to -inf; seen(chunk, v, z)
-// looks at a chunk on the way.  scratch: 4 * NT / 64 floats.
+// The sums of a part, the same for every thread and in the same order every time.  mask(chunk, z) may set places to -inf; seen(chunk, v, most)
+// gets a chunk and its largest logit (with entropies).  scratch: 2 * NT / 64 floats.
 template <bool ENTROPY, int DT, int NT, int U, class Mask, class Seen>
 __device__ __forceinline__ RowSums sum_part(const Part& t, float a, float* scratch, Mask&& mask, Seen&& seen) {
     constexpr int N = U * kVec<DT>;
@@ -269,40 +304,52 @@ __device__ __forceinline__ RowSums sum_part(const Part& t, float a, float* scrat
         for (int u = 0; u < U; ++u) widen<DT>(v[u], z + u * kVec<DT>);
         mask(chunk, z);
     };
-    u32x4 v[U], next[U];
-    load_chunk<DT, NT, U, true>(t, 0, v);
-    if (chunks > 1) load_chunk<DT, NT, U, true>(t, U * NT, next);
-    RowSums r;
-    {
-        float z[N];
-        widened(0, v, z);
+    auto most_of = [](const float(&z)[N]) {
         float most = z[0];
 #pragma unroll
         for (int i = 1; i < N; ++i) most = fmaxf(most, z[i]);
-        r.m = block_max_f32<NT>(most, scratch);
-    }
-    const float c = r.m * a;
-    bool done = fabsf(c) < 0x1p100f;
-    if (done) {
-        Sums<ENTROPY> run;
-        for (int chunk = 0; chunk < chunks; ++chunk) {
+        return most;
+    };
+    RowSums r;
+    bool done;
+    if constexpr (ENTROPY) {
+        EntropySums run;
+        for_chunks<DT, NT, U>(t, [&](int chunk, const u32x4(&w)[U]) {
             float z[N];
-            widened(chunk, v, z);
-            seen(chunk, v, z);
-            run.add(z, a, c);
-#pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = next[u];
-            if (chunk + 2 < chunks) load_chunk<DT, NT, U, true>(t, (chunk + 2) * (U * NT), next);
-        }
-        r = sums_by_reference<ENTROPY, NT>(run, r.m, a, scratch);
+            widened(chunk, w, z);
+            const float most = most_of(z);
+            seen(chunk, w, most);
+            run.add(z, most, a);
+        });
+        r = sums_by_reference<NT>(run, a, scratch);
         done = sums_hold(r);
+    } else {
+        u32x4 v[U], next[U];
+        load_chunk<DT, NT, U, true>(t, 0, v);
+        if (chunks > 1) load_chunk<DT, NT, U, true>(t, U * NT, next);
+        float z[N];
+        widened(0, v, z);
+        r.m = block_max_f32<NT>(most_of(z), scratch);
+        const float c = r.m * a;
+        done = fabsf(c) < 0x1p100f;
+        if (done) {
+            Sums run;
+            for (int chunk = 0; chunk < chunks; ++chunk) {
+                widened(chunk, v, z);
+                run.add(z, a, c);
+#pragma unroll
+                for (int u = 0; u < U; ++u) v[u] = next[u];
+                if (chunk + 2 < chunks) load_chunk<DT, NT, U, true>(t, (chunk + 2) * (U * NT), next);
+            }
+            r = sums_by_reference<NT>(run, r.m, a, scratch);
+            done = sums_hold(r);
+        }
     }
     if (!done) {
         Running<ENTROPY> run;
         for_chunks<DT, NT, U>(t, [&](int chunk, const u32x4(&w)[U]) {
             float z[N];
             widened(chunk, w, z);
-            seen(chunk, w, z);
             run.add(z, a);
         });
         r = sums_by_differences<ENTROPY, NT>(run, a, scratch);

@@ -1,6 +1,6 @@
 // Log probabilities of given tokens, entropy and largest alternatives of finished rows of logits, and the logits' gradient of them.
 //
-// With T a row's temperature, M a reference near its largest logit and S = sum of exp((z - M) / T):
+// With T a row's temperature, M its largest logit and S = sum of exp((z - M) / T):
 //     log p_v = (z_v - M) / T - log S,     H = log S - sum of exp((z - M) / T) (z - M) / T / S,
 //     d/dz_v = (sum over given tokens j of g_j ([v = t_j] - p_v) - g_H p_v (log p_v + H)) / T.
 //
@@ -15,7 +15,7 @@ namespace sv {
 
 namespace {
 
-constexpr int kMaxTop = 64, kMaxGiven = 64;
+constexpr int kMaxTop = 64, kMaxGiven = 64;                // (one wavefront writes a row's results)
 constexpr int kCandidates = 1024;
 constexpr int64_t kMostPart = 1 << 18;                         // places of a part: 32 KB of chunks' largest logits, 32-bit offsets
 constexpr int kMaxTopParts = 64;
@@ -293,18 +293,21 @@ __device__ __forceinline__ Given given_token(const TokenArgs& a, int64_t row, Fi
 template <int NT>
 __device__ __forceinline__ void write_row(const TokenArgs& a, int64_t row, float t, const RowSums& r, const uint64_t* best, const Given& given) {
     const int tid = threadIdx.x;
-    const bool empty = r.s == 0.0f;
-    const float m = empty ? 0.0f : r.m, log_s = logf(r.s);
-    if (tid < a.given) a.logprob[row * a.given + tid] = r.s != r.s ? r.s : given.there && !empty ? (given.z - m) / t - log_s : -INFINITY;
+    const bool empty = r.s == 0.0f, bad = r.s != r.s;
+    const float m = empty ? 0.0f : r.m;
+    // (only the first wavefront has something to write)
+    const double log_s = tid < 64 ? log_of_sum(r.s) : 0.0, inv_t = t == 1.0f ? 1.0 : 1.0 / (double)t;
+    auto logprob = [&](float z) { return (float)fma((double)z - (double)m, inv_t, -log_s); };
+    if (tid < a.given) a.logprob[row * a.given + tid] = bad ? r.s : given.there && !empty ? logprob(given.z) : -INFINITY;
     if (tid < a.top) {
         const uint64_t key = best[tid];
-        const bool some = key != 0ull && r.s == r.s;
+        const bool some = key != 0ull && !bad;
         const int32_t place = key_token(key);
         a.top_tok[row * a.top + tid] = !some ? -1 : a.idx ? a.idx[row * a.idx_row_stride + place] : place;
-        a.top_logprob[row * a.top + tid] = r.s != r.s ? r.s : some ? (key_value(key) - m) / t - log_s : -INFINITY;
+        a.top_logprob[row * a.top + tid] = bad ? r.s : some ? logprob(key_value(key)) : -INFINITY;
     }
     if (tid == 0) {
-        const float h = empty ? 0.0f : log_s - 0.6931471805599453f * (r.e / r.s);
+        const float h = empty ? 0.0f : (float)(log_s - 0.69314718055994530942 * (double)(r.e / r.s));
         if (a.entropy) a.entropy[row] = h;
         if (a.state) a.state[row] = make_float4(m, r.s, h, 0.0f);
     }
@@ -330,11 +333,8 @@ __global__ __launch_bounds__(NT) void token_rows_kernel(const TokenArgs a, const
     u32x4 only[U];
     const RowSums r = sum_part<true, DT, NT, U>(
         t, c, sums, [](int, float(&)[kN]) {},
-        [&](int chunk, const u32x4(&v)[U], const float(&z)[kN]) {
+        [&](int chunk, const u32x4(&v)[U], float most) {
             if constexpr (TOP) {
-                float most = z[0];
-#pragma unroll
-                for (int i = 1; i < kN; ++i) most = fmaxf(most, z[i]);
                 float* slot = chunk_most + (chunk >> 1) * NT + (int)threadIdx.x;
                 *slot = chunk & 1 ? fmaxf(*slot, most) : most;
                 thread_most = fmaxf(thread_most, most);
