@@ -30,7 +30,7 @@ struct DistillScratch {
     float2* sums;            // [rows x parts]: largest logit that is not listed, sum relative to it
     float4* state;           // [rows]
     int parts;
-    int64_t part;
+    int64_t part;            // elements of a part, a multiple of 32
 };
 
 struct ListWork {
@@ -202,7 +202,11 @@ __device__ __forceinline__ void enter_list(const Entry& e, int32_t* keys, ListWo
     clear_words<kThreads>(reinterpret_cast<uint32_t*>(keys), kSlots, (uint32_t)kEmptySlot);
     if (threadIdx.x == 0) w.again = 0u;
     __syncthreads();
-    if (e.there && enter_place<kSlots>(keys, e.id)) w.again = 1u;
+    if (e.there) {
+        bool again;
+        enter_key<kSlots>(keys, e.id, again);
+        if (again) w.again = 1u;
+    }
     w.id[threadIdx.x] = e.there ? e.id : -1;
     __syncthreads();
 }
@@ -297,7 +301,7 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(const DistillArg
     const Entry e = entry_of(a, row);
     if (skipped_row(a, row, weight)) return;
     const char* logits = a.logits + row * a.row_bytes;
-    const Part t = part_of<DT>(logits, a.n, 0, a.n);
+    const Part t = part_of<DT>(logits, a.n, 0, kWholeRow / kVec<DT>);
     const float c = 1.4426950408889634f / a.temperature;
     const float z = e.there ? logit_at<DT>(logits, e.id) : -INFINITY;
     if constexpr (REST) mark_list<DT>(t, e, bits, &w);
@@ -307,9 +311,9 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(const DistillArg
 }
 
 // One workgroup per row: loss and gradient, that is two passes over the row.  The fabric moves 7 TB/s whether the lines come from the last-level
-// cache or from memory, so the second pass reads as little as it can: a thread keeps its first KEPT vectors in registers -- 16, half of
-// 128256 bfloat16 logits, or 4 where the row has no more -- and walks the others backwards, of which the L2 then still holds most (4096 rows: 408 us, 422 with 8
-// kept, 441 with 4; 2.1 GB, a read and a write of each place).  Some of the others in LDS changed nothing.
+// cache or from memory, so the second pass reads as little as it can: a thread keeps its first KEPT vectors in registers -- 14, nearly half of
+// 128256 bfloat16 logits, or 4 where the row has no more -- and walks the others backwards, of which the L2 then still holds most (4096 rows: 413 us, 422 with 8
+// kept, 441 with 4, and 16 leave too few registers; 2.1 GB, a read and a write of each place).  Some of the others in LDS changed nothing.
 constexpr int kStep = 2;                                   // vectors of a chunk
 template <int DT, int GDT, bool REST, int KEPT>
 __global__ __launch_bounds__(kThreads, KEPT > 4 ? 4 : 6) void distill_step_kernel(const DistillArgs a, const int64_t first_row) {
@@ -322,7 +326,7 @@ __global__ __launch_bounds__(kThreads, KEPT > 4 ? 4 : 6) void distill_step_kerne
     const Entry e = entry_of(a, row);                      // (asked for before the row: loads come back in order)
     const char* logits = a.logits + row * a.row_bytes;
     char* out = a.grad + row * a.grad_row_bytes;
-    const Part t = part_of<DT>(logits, a.n, 0, a.n);
+    const Part t = part_of<DT>(logits, a.n, 0, kWholeRow / kVec<DT>);
     if (skipped_row(a, row, weight)) {
         write_zeros<DT, GDT>(t, out);
         return;
@@ -400,7 +404,7 @@ __global__ __launch_bounds__(kThreads, KEPT > 4 ? 4 : 6) void distill_step_kerne
     const Factors f = factors_of(a, weight, teacher, st, c);
     const double p = mass_of_token(e, teacher, a.known, w);
     auto write = [&](auto exact, int chunk, const u32x4 v0, const u32x4 v1) {
-        const bool whole = (chunk + 1) * (kStep * NT) <= t.full;
+        const bool whole = whole_chunk<NT, kStep>(t, chunk * (kStep * NT));
 #pragma unroll
         for (int u = 0; u < kStep; ++u) {
             float z[V], g[V];
@@ -440,7 +444,7 @@ __global__ __launch_bounds__(kThreads) void distill_parts_kernel(const DistillAr
     const int64_t row = first_row + blockIdx.x / (unsigned)x.parts;
     const int at = (int)(blockIdx.x % (unsigned)x.parts);
     if (weight_of_row(a, row) == 0.0f) return;
-    const Part t = part_of<DT>(a.logits + row * a.row_bytes, a.n, at * x.part, x.part);
+    const Part t = part_of<DT>(a.logits + row * a.row_bytes, a.n, at, x.part / kVec<DT>);
     const float c = 1.4426950408889634f / a.temperature;
     if constexpr (REST) mark_list<DT>(t, entry_of(a, row), bits, nullptr);
     const RowSums r = sums_of<DT, REST>(t, c, bits, scratch);
@@ -491,7 +495,7 @@ __global__ __launch_bounds__(kThreads, 8) void distill_grad_kernel(const Distill
     const float weight = weight_of_row(a, row);
     const Entry e = entry_of(a, row);
     const float4 st = a.state[row];
-    const Part t = part_of<DT>(a.logits + row * a.row_bytes, a.n, (int64_t)(blockIdx.x % (unsigned)parts) * kGradPart<DT>, kGradPart<DT>);
+    const Part t = part_of<DT>(a.logits + row * a.row_bytes, a.n, blockIdx.x % (unsigned)parts, kGradPart<DT> / V);
     char* out = a.grad + row * a.grad_row_bytes;
     if (weight == 0.0f) {
         write_zeros<DT, GDT>(t, out);
@@ -519,7 +523,7 @@ __global__ __launch_bounds__(kThreads, 8) void distill_grad_kernel(const Distill
             widen<DT>(v[u], z);
 #pragma unroll
             for (int i = 0; i < V; ++i) g[i] = f.of_rest * exp2_fast(octaves_at<decltype(exact)::value>(f.x, z[i]));
-            store_vector<GDT>(out, t, u * kThreads + tid, U * kThreads <= t.full, g);
+            store_vector<GDT>(out, t, u * kThreads + tid, whole_chunk<kThreads, U>(t, 0), g);
         }
     };
     if (f.x.exact) pass(std::true_type{});
@@ -542,14 +546,14 @@ __global__ __launch_bounds__(kThreads, 8) void distill_grad_kernel(const Distill
 constexpr int64_t kWantBlocks = 256, kLongRow = 65536, kFewRows = 128;
 DistillScratch scratch_of(int64_t rows, int64_t n, char* at) {
     DistillScratch x{};
-    int64_t parts = (n + kWholeRow - 1) / kWholeRow;
+    int64_t parts = (grid_of(n) + kWholeRow - 1) / kWholeRow;
     if (n > kLongRow && rows <= kFewRows) {
         int64_t wanted = kWantBlocks / rows;
         if (wanted > n / 4096) wanted = n / 4096;
         if (wanted > parts) parts = wanted;
     }
-    x.part = ((n + parts - 1) / parts + 31) / 32 * 32;
-    x.parts = (int)((n + x.part - 1) / x.part);
+    x.part = ((grid_of(n) + parts - 1) / parts + 31) / 32 * 32;
+    x.parts = (int)((grid_of(n) + x.part - 1) / x.part);
     x.state = reinterpret_cast<float4*>(at);
     x.sums = reinterpret_cast<float2*>(at + (size_t)rows * sizeof(float4));
     return x;
@@ -567,7 +571,7 @@ hipError_t launch_distill(int dt, int grad_dt, const DistillArgs& a, hipStream_t
     const bool rest = a.kind == kRest;
     const size_t marks = rest ? marks_bytes<DT_F32>(x.part) : 0;
     if (x.parts == 1) {
-        const bool small = a.n <= 4 * kThreads * (dt == DT_BF16 ? 8 : 4);
+        const bool small = grid_of(a.n) <= 4 * kThreads * (dt == DT_BF16 ? 8 : 4);
         const size_t lds = rest ? marks : kSlots * sizeof(int32_t);
         auto step = [&](auto kernel) {
             return over_rows(a.rows, kThreads, [&](int64_t first, int64_t rows) {
@@ -584,7 +588,7 @@ hipError_t launch_distill(int dt, int grad_dt, const DistillArgs& a, hipStream_t
             constexpr bool REST = decltype(with_rest)::value;
             if (!a.grad) return loss(&distill_rows_kernel<DT, REST>);
             if (small) return grad_dt == DT_BF16 ? step(&distill_step_kernel<DT, DT_BF16, REST, 4>) : step(&distill_step_kernel<DT, DT_F32, REST, 4>);
-            return grad_dt == DT_BF16 ? step(&distill_step_kernel<DT, DT_BF16, REST, 16>) : step(&distill_step_kernel<DT, DT_F32, REST, 16>);
+            return grad_dt == DT_BF16 ? step(&distill_step_kernel<DT, DT_BF16, REST, 14>) : step(&distill_step_kernel<DT, DT_F32, REST, 14>);
         };
         constexpr std::integral_constant<int, DT_BF16> bf16{};
         constexpr std::integral_constant<int, DT_F32> f32{};
@@ -612,7 +616,7 @@ hipError_t launch_distill(int dt, int grad_dt, const DistillArgs& a, hipStream_t
 
 hipError_t launch_distill_grad(int dt, int grad_dt, const DistillArgs& a, hipStream_t stream) {
     const int64_t part = dt == DT_BF16 ? kGradPart<DT_BF16> : kGradPart<DT_F32>;
-    const int parts = (int)((a.n + part - 1) / part);
+    const int parts = (int)((grid_of(a.n) + part - 1) / part);
     auto go = [&](auto kernel) {
         return over_rows(a.rows, (int64_t)parts * kThreads, [&](int64_t first, int64_t rows) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * parts)), dim3(kThreads), 0, stream, a, first, parts);

@@ -13,7 +13,7 @@ namespace sv {
 constexpr float kLowestF32 = -3.402823466e38f;
 constexpr float kNoMass = -1000.0f;                       // 2^-1000 is 0: an exponent that has to stay finite is cut off here
 
-// rows begin at any element: bfloat16 ones at any even address
+// gradients begin at any element: bfloat16 ones at any even address
 typedef unsigned int u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef unsigned int u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 
@@ -50,37 +50,50 @@ __device__ __forceinline__ float logit_at(const char* row, int64_t place) {
     else return reinterpret_cast<const float*>(row)[place];
 }
 
-// A row's places [first, first + n): a part begins at a multiple of 32 places (a word of the bitmaps) and has at most 2^18 of them.
+// A part of a row: the vectors [k * size, (k + 1) * size) of the 16-byte grid that its logits lie on.  A row begins at any element, so its first
+// vector may have up to 7 elements that are not the row's; they count as masked and are neither read nor written.  (By vectors from the row's own beginning
+// bfloat16 rows at odd elements take a fourth longer: 2048 x 128256, the gradient of log probabilities 203 us instead of 181, loss and gradient 255 instead
+// of 215.)
 struct Part {
-    const char* p;       // of its first logit
-    int64_t first;
-    int n;
+    const char* p;       // of its first vector
+    int64_t first;       // the place of that vector's first element: -skip in a row's first part
+    int n;               // elements from there; up to 2^18
+    int skip;            // of which these are not the row's
     int full;            // whole vectors
-    int vectors;         // with the one that the row ends in
+    int vectors;         // with the one that the row ends in; 0 in a part behind the row's end
 };
 
 template <int DT>
-__device__ __forceinline__ Part part_of(const char* row, int64_t n, int64_t first, int64_t most) {
+__device__ __forceinline__ Part part_of(const char* row, int64_t n, int64_t k, int64_t size) {
+    constexpr int V = kVec<DT>;
     Part t;
-    t.first = first;
-    t.n = (int)(n - first < most ? n - first : most);
-    t.p = row + first * kBytes<DT>;
-    t.full = t.n / kVec<DT>;
-    t.vectors = (t.n + kVec<DT> - 1) / kVec<DT>;
+    const int before = (int)((reinterpret_cast<uintptr_t>(row) & 15u) / kBytes<DT>);
+    const int64_t at = k * size * V;
+    int64_t left = n + before - at;
+    left = left < 0 ? 0 : left < size * V ? left : size * V;
+    t.p = row - before * kBytes<DT> + at * kBytes<DT>;
+    t.first = at - before;
+    t.n = (int)left;
+    t.skip = k == 0 ? before : 0;
+    t.full = t.n / V;
+    t.vectors = (t.n + V - 1) / V;
     return t;
 }
+// elements that rows of n places may take of the grid
+inline int64_t grid_of(int64_t n) { return n + 7; }
 
 // (of a vector behind the part's end: masked places)
 template <int DT>
 __device__ __forceinline__ u32x4 load_guarded(const Part& t, int iv) {
-    if (iv < t.full) return *reinterpret_cast<const u32x4_any*>(t.p + (uint32_t)iv * 16u);
+    const char* p = t.p + (uint32_t)iv * 16u;
+    const int from = iv == 0 ? t.skip : 0;
+    if (iv < t.full && from == 0) return *reinterpret_cast<const u32x4*>(p);
     u32x4 v = masked_vector<DT>();
     if (iv < t.vectors) {
         const int left = t.n - iv * kVec<DT>;
-        const char* p = t.p + (uint32_t)iv * 16u;
 #pragma unroll
         for (int i = 0; i < kVec<DT>; ++i) {
-            if (i >= left) continue;
+            if (i < from || i >= left) continue;
             if constexpr (DT == DT_BF16) {
                 const uint32_t x = reinterpret_cast<const uint16_t*>(p)[i];
                 v[i / 2] = (i & 1) ? (v[i / 2] & 0xFFFFu) | (x << 16) : (v[i / 2] & 0xFFFF0000u) | x;
@@ -92,16 +105,20 @@ __device__ __forceinline__ u32x4 load_guarded(const Part& t, int iv) {
     return v;
 }
 
+// true (the same for all) where the U x NT vectors from `first` on are whole ones of the row
+template <int NT, int U>
+__device__ __forceinline__ bool whole_chunk(const Part& t, int first) { return first + U * NT <= t.full && (first > 0 || t.skip == 0); }
+
 // vectors first + thread, first + NT + thread, ... of the part.  ONCE: nobody reads them again, their lines need not stay in the caches
 // (1024 x 128256 float32 logits summed: 82.7 us instead of 94.7; 512 x 151936 with 8 alternatives, of which a few lines are read again: 53.3 instead
 // of 59.6).
 template <int DT, int NT, int U, bool ONCE>
 __device__ __forceinline__ void load_chunk(const Part& t, int first, u32x4 (&v)[U]) {
     const int at = first + (int)threadIdx.x;
-    if (first + U * NT <= t.full) {
+    if (whole_chunk<NT, U>(t, first)) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const u32x4_any* p = reinterpret_cast<const u32x4_any*>(t.p + (uint32_t)(at + u * NT) * 16u);
+            const u32x4* p = reinterpret_cast<const u32x4*>(t.p + (uint32_t)(at + u * NT) * 16u);
             if constexpr (ONCE) v[u] = __builtin_nontemporal_load(p);
             else v[u] = *p;
         }
@@ -357,7 +374,7 @@ __device__ __forceinline__ RowSums sum_part(const Part& t, float a, float* scrat
     return r;
 }
 
-// ---- places that are marked: a bitmap of a part's places; a table of places that have been met
+// ---- places that are marked: a bitmap of a part's places; a table of ids that have been met
 template <int NT>
 __device__ __forceinline__ void clear_words(uint32_t* p, int words, uint32_t value = 0u) {
     for (int i = threadIdx.x; i < words; i += NT) p[i] = value;
@@ -372,15 +389,16 @@ __device__ __forceinline__ uint32_t marks_of(const uint32_t* bits, int iv) {
 
 constexpr int32_t kEmptySlot = -1;
 template <int SLOTS>
-__device__ __forceinline__ uint32_t slot_of(int32_t place) { return ((uint32_t)place * 2654435761u) >> (32 - __builtin_ctz(SLOTS)); }
+__device__ __forceinline__ uint32_t slot_of(int32_t key) { return ((uint32_t)key * 2654435761u) >> (32 - __builtin_ctz(SLOTS)); }
 
-// true if the place was in the table; there are at most SLOTS / 2 of them
+// the key's slot in a table of at most SLOTS / 2 keys; `again`: it was there
 template <int SLOTS>
-__device__ __forceinline__ bool enter_place(int32_t* keys, int32_t place) {
-    uint32_t s = slot_of<SLOTS>(place);
+__device__ __forceinline__ uint32_t enter_key(int32_t* keys, int32_t key, bool& again) {
+    uint32_t s = slot_of<SLOTS>(key);
     for (;;) {
-        const int32_t was = atomicCAS(&keys[s], kEmptySlot, place);
-        if (was == kEmptySlot || was == place) return was == place;
+        const int32_t was = atomicCAS(&keys[s], kEmptySlot, key);
+        again = was == key;
+        if (was == kEmptySlot || again) return s;
         s = (s + 1) & (SLOTS - 1);
     }
 }
@@ -420,13 +438,13 @@ __device__ __forceinline__ void store_one(char* row, int64_t place, float g) {
     else reinterpret_cast<float*>(row)[place] = g;
 }
 
-// The gradients of vector iv of a part, rounded to nearest even; nobody here reads them again.  whole: (the same for all) vectors up to it and its
-// neighbours' are whole ones.  One behind the part's end is not stored.
+// The gradients of vector iv of a part, rounded to nearest even; nobody here reads them again.  whole: (the same for all) it is a whole one of the
+// row; else its elements that are not the row's are not written.
 template <int GDT, int N>
 __device__ __forceinline__ void store_vector(char* row, const Part& t, int iv, bool whole, const float (&g)[N]) {
     row += t.first * (GDT == DT_BF16 ? 2 : 4);             // (a part's places are within 32 bits)
     const uint32_t place = (uint32_t)iv * N;
-    const int left = whole ? N : t.n - iv * N;
+    const int from = iv == 0 ? t.skip : 0, left = t.n - iv * N;
     if constexpr (GDT == DT_BF16) {
         typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
         uint32_t w[N / 2];
@@ -436,17 +454,17 @@ __device__ __forceinline__ void store_vector(char* row, const Part& t, int iv, b
             w[i] = __builtin_bit_cast(uint32_t, b);
         }
         char* p = row + place * 2u;
-        if (whole || left >= N) {
+        if (whole || (left >= N && from == 0)) {
             if constexpr (N == 8) __builtin_nontemporal_store(u32x4_any{w[0], w[1], w[2], w[3]}, reinterpret_cast<u32x4_any*>(p));
             else __builtin_nontemporal_store(u32x2_any{w[0], w[1]}, reinterpret_cast<u32x2_any*>(p));
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                if (i < left) reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+                if (i >= from && i < left) reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
         }
     } else {
         float* p = reinterpret_cast<float*>(row) + place;
-        if (whole || left >= N) {
+        if (whole || (left >= N && from == 0)) {
 #pragma unroll
             for (int q = 0; q < N / 4; ++q)
                 __builtin_nontemporal_store(u32x4_any{__float_as_uint(g[4 * q]), __float_as_uint(g[4 * q + 1]), __float_as_uint(g[4 * q + 2]),
@@ -455,7 +473,7 @@ __device__ __forceinline__ void store_vector(char* row, const Part& t, int iv, b
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                if (i < left) p[i] = g[i];
+                if (i >= from && i < left) p[i] = g[i];
         }
     }
 }

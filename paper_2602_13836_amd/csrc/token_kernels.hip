@@ -40,7 +40,7 @@ struct TokenScratch {
     PartSums* sums;          // [rows x parts]
     uint64_t* top;           // [rows x parts x top], largest first; 0: none
     int parts;
-    int64_t part;            // places of a part
+    int64_t part;            // elements of a part, a multiple of 32
 };
 
 // A bound that at least `want` of the keys reach and, unless equal keys prevent it, no more than `enough`.  Every wavefront finds it for itself.
@@ -229,10 +229,11 @@ __device__ __forceinline__ void select_top(const Part& t, int top, float thread_
 }
 
 // ---- a row's results, by one workgroup
+constexpr int kFindSlots = 2 * kMaxGiven;
 struct FindWork {
     uint32_t bits[256];
-    int32_t token[kMaxGiven];
-    int32_t place[kMaxGiven];
+    int32_t keys[kFindSlots];
+    int32_t place[kFindSlots];
 };
 
 // The logit of this thread's given token; `there`: it has a place.  Every thread calls.
@@ -246,12 +247,17 @@ __device__ __forceinline__ Given given_token(const TokenArgs& a, int64_t row, Fi
     Given g{false, -INFINITY};
     int32_t place = tid < a.given ? a.tokens[row * a.given + tid] : -1;
     if (a.idx && a.given > 0) {
-        // the first place whose id is the token's: the tokens' hashes in a bitmap tell which of the list's ids to look at
+        // the first place whose id is the token's: a bitmap of the tokens' hashes tells which of the list's ids to look up in their table
         clear_words<NT>(w.bits, 256);
-        __syncthreads();
-        if (tid < a.given) {
-            w.token[tid] = place;
+        if (tid < kFindSlots) {
+            w.keys[tid] = kEmptySlot;
             w.place[tid] = n;
+        }
+        __syncthreads();
+        uint32_t slot = 0;
+        if (place >= 0) {
+            bool again;
+            slot = enter_key<kFindSlots>(w.keys, place, again);
             const uint32_t h = slot_of<8192>(place);
             atomicOr(&w.bits[h >> 5], 1u << (h & 31));
         }
@@ -260,9 +266,12 @@ __device__ __forceinline__ Given given_token(const TokenArgs& a, int64_t row, Fi
         const int32_t* ids = a.idx + row * a.idx_row_stride;
         auto look = [&](int32_t id, int at) {
             const uint32_t h = slot_of<8192>(id);
-            if ((w.bits[h >> 5] >> (h & 31)) & 1u)
-                for (int j = 0; j < a.given; ++j)
-                    if (w.token[j] == id && id >= 0) atomicMin(&w.place[j], at);
+            if (id < 0 || !((w.bits[h >> 5] >> (h & 31)) & 1u)) return;
+            for (uint32_t s = slot_of<kFindSlots>(id);; s = (s + 1) & (kFindSlots - 1)) {
+                const int32_t key = w.keys[s];
+                if (key == id) atomicMin(&w.place[s], at);
+                if (key == id || key == kEmptySlot) return;
+            }
         };
         constexpr int kAtOnce = 4;
         int at = 4 * tid;
@@ -282,7 +291,7 @@ __device__ __forceinline__ Given given_token(const TokenArgs& a, int64_t row, Fi
         }
         if (tid < (n & 3)) look(ids[(n & ~3) + tid], (n & ~3) + tid);
         __syncthreads();
-        place = tid < a.given ? w.place[tid] : -1;
+        place = place >= 0 ? w.place[slot] : -1;
     }
     g.there = place >= 0 && place < a.n;
     if (g.there) g.z = logit_at<DT>(a.logits + row * a.row_bytes, place);
@@ -323,7 +332,7 @@ __global__ __launch_bounds__(NT) void token_rows_kernel(const TokenArgs a, const
     const int64_t row = first_row + (WHOLE ? blockIdx.x : blockIdx.x / (unsigned)x.parts);
     const int part_at = WHOLE ? 0 : (int)(blockIdx.x % (unsigned)x.parts);
     const char* logits = a.logits + row * a.row_bytes;
-    const Part t = part_of<DT>(logits, a.n, (int64_t)part_at * x.part, x.part);
+    const Part t = part_of<DT>(logits, a.n, part_at, x.part / kVec<DT>);
     const float temp = row_temperature(a.temperature, row);
     const float c = octaves_per_logit(temp);
     constexpr int U = kChunkVectors<DT>, kN = U * kVec<DT>;
@@ -432,7 +441,7 @@ __global__ __launch_bounds__(kGradThreads) void token_grad_kernel(const TokenGra
     __shared__ int32_t token[kMaxGiven];
     const int tid = threadIdx.x;
     const int64_t row = first_row + blockIdx.x / (unsigned)parts;
-    const Part t = part_of<DT>(a.logits + row * a.row_bytes, a.n, (int64_t)(blockIdx.x % (unsigned)parts) * kGradPart, kGradPart);
+    const Part t = part_of<DT>(a.logits + row * a.row_bytes, a.n, blockIdx.x % (unsigned)parts, U * NT);
     u32x4 v[U];
     load_chunk<DT, NT, U, true>(t, 0, v);
     const float4 st = a.state[row];
@@ -446,7 +455,7 @@ __global__ __launch_bounds__(kGradThreads) void token_grad_kernel(const TokenGra
         __syncthreads();
         for (int j = 0; j < a.given; ++j) g_sum += token[j] >= 0 && token[j] < a.n ? g_of[j] : 0.0f;
         if (tid < a.given) {
-            const int64_t at = token[tid] - t.first;
+            const int64_t at = token[tid] >= 0 && token[tid] < a.n ? token[tid] - t.first : -1;
             // (read before the part is written: the gradient may replace the logits)
             if (at >= 0 && at < t.n) {
                 z_mine = logit_at<DT>(t.p, at);
@@ -475,7 +484,7 @@ __global__ __launch_bounds__(kGradThreads) void token_grad_kernel(const TokenGra
             widen<DT>(v[u], z);
 #pragma unroll
             for (int i = 0; i < V; ++i) g[i] = gradient(exact, z[i]);
-            store_vector<GDT>(out, t, u * NT + tid, U * NT <= t.full, g);
+            store_vector<GDT>(out, t, u * NT + tid, whole_chunk<NT, U>(t, 0), g);
         }
     };
     if (x.exact) pass(std::true_type{});
@@ -496,15 +505,15 @@ constexpr int64_t kWantBlocks = 256, kLongRow = 98304, kFewRows = 64;
 constexpr int64_t kShortPart = 8192, kManyBlocks = 1024;
 TokenScratch scratch_of(int64_t rows, int64_t n, int top, char* at) {
     TokenScratch x{};
-    int64_t parts = (n + kMostPart - 1) / kMostPart;
+    int64_t parts = (grid_of(n) + kMostPart - 1) / kMostPart;
     if (n > kLongRow && rows <= kFewRows) {
         int64_t wanted = kWantBlocks / rows;
         if (wanted > kMaxTopParts) wanted = kMaxTopParts;
         if (wanted > n / 4096) wanted = n / 4096;
         if (wanted > parts) parts = wanted;
     }
-    x.part = ((n + parts - 1) / parts + 31) / 32 * 32;
-    x.parts = (int)((n + x.part - 1) / x.part);
+    x.part = ((grid_of(n) + parts - 1) / parts + 31) / 32 * 32;
+    x.parts = (int)((grid_of(n) + x.part - 1) / x.part);
     x.sums = reinterpret_cast<PartSums*>(at);
     x.top = reinterpret_cast<uint64_t*>(at + (size_t)rows * x.parts * sizeof(PartSums));
     return x;
@@ -544,7 +553,7 @@ hipError_t launch_token_logprobs(int dt, const TokenArgs& a, hipStream_t stream)
 }
 
 hipError_t launch_token_grad(int dt, int grad_dt, const TokenGradArgs& a, hipStream_t stream) {
-    const int parts = (int)((a.n + kGradPart - 1) / kGradPart);
+    const int parts = (int)((grid_of(a.n) + kGradPart - 1) / kGradPart);
     auto go = [&](auto kernel) {
         return over_rows(a.rows, (int64_t)parts * kGradThreads, [&](int64_t first, int64_t rows) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * parts)), dim3(kGradThreads), 0, stream, a, first, parts);
