@@ -280,16 +280,34 @@ __device__ __forceinline__ RowSums sums_by_reference(const Sums& run, float m, f
     r.s *= exp2_fast(-fmaf(m, a, -(m * a)));               // from the rounded reference to m
     return r;
 }
+// (one barrier; nobody has used scratch before)
 template <int NT>
 __device__ __forceinline__ RowSums sums_by_reference(const EntropySums& run, float a, float* scratch) {
-    RowSums r;
-    r.m = block_max_f32<NT>(run.m, scratch);
-    const float c = fminf(fmaxf(r.m * a, kLowestF32), -kLowestF32), d = fmaxf(run.c - c, kNoMass), rd = exp2_fast(d);
-    r.s = run.s * rd;
-    r.e = rd * fmaf(d, run.s, run.e);
-    block_sum_pair<NT>(r.s, r.e, scratch);
+    const int wave = threadIdx.x >> 6;
+    float m = wave_max_f32(run.m), c = wave_max_f32(run.c);
+    const float d = fmaxf(run.c - c, kNoMass), rd = exp2_fast(d);
+    const float s = wave_sum(run.s * rd), e = wave_sum(rd * fmaf(d, run.s, run.e));
+    if ((threadIdx.x & 63) == 0) {
+        scratch[4 * wave] = m;
+        scratch[4 * wave + 1] = c;
+        scratch[4 * wave + 2] = s;
+        scratch[4 * wave + 3] = e;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+        m = fmaxf(m, scratch[4 * w]);
+        c = fmaxf(c, scratch[4 * w + 1]);
+    }
+    RowSums r{m, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+        const float dw = fmaxf(scratch[4 * w + 1] - c, kNoMass), rw = exp2_fast(dw);
+        r.s = fmaf(scratch[4 * w + 2], rw, r.s);
+        r.e += rw * fmaf(dw, scratch[4 * w + 2], scratch[4 * w + 3]);
+    }
     if (r.s > 0.0f) {
-        const float shift = -fmaf(r.m, a, -c), rs = exp2_fast(shift);
+        const float shift = -fmaf(r.m, a, -c), rs = exp2_fast(shift);      // from the rounded reference to m
         r.e = rs * fmaf(shift, r.s, r.e);
         r.s *= rs;
     }
@@ -311,7 +329,7 @@ __device__ __forceinline__ RowSums sums_by_differences(const Running<ENTROPY>& r
 }
 
 // The sums of a part, the same for every thread and in the same order every time.  mask(chunk, z) may set places to -inf; seen(chunk, v, most)
-// gets a chunk and its largest logit (with entropies).  scratch: 2 * NT / 64 floats.
+// gets a chunk and its largest logit (with entropies).  scratch: 4 * NT / 64 floats.
 template <bool ENTROPY, int DT, int NT, int U, class Mask, class Seen>
 __device__ __forceinline__ RowSums sum_part(const Part& t, float a, float* scratch, Mask&& mask, Seen&& seen) {
     constexpr int N = U * kVec<DT>;

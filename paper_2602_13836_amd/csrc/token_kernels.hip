@@ -72,11 +72,9 @@ struct TopWork {
     uint32_t n_chunks, n_found, digit, above;
 };
 
-// best[0 .. top): the largest of found[0 .. n), largest first, 0 where there are no more.  The keys differ.
+// best[0 .. top): the largest of found[0 .. n), largest first; 0, as they were before, where there are no more.  The keys differ.
 template <int NT>
 __device__ __forceinline__ void rank_found(const uint64_t* found, int n, uint64_t* best, int top) {
-    for (int i = threadIdx.x; i < top; i += NT) best[i] = 0ull;
-    __syncthreads();
     for (int i = threadIdx.x; i < n; i += NT) {
         const uint64_t mine = found[i];
         int larger = 0;
@@ -172,6 +170,7 @@ __device__ __forceinline__ void select_top(const Part& t, int top, float thread_
     constexpr int kEach = NT / 64, V = kVec<DT>, U = kChunkVectors<DT>;
     const int tid = threadIdx.x;
     w.keys[tid] = f32_to_ord(thread_most);
+    if (tid < kMaxTop) w.best[tid] = 0ull;
     if (tid == 0) w.n_chunks = w.n_found = 0;
     __syncthreads();
     uint32_t k[kEach], most = 0, least = 0xFFFFFFFEu;
@@ -223,8 +222,10 @@ __device__ __forceinline__ void select_top(const Part& t, int top, float thread_
     __syncthreads();
     int n = (int)w.n_found;
     fits = fits && n <= kCandidates;
-    if (!fits) n = select_by_digits<DT, NT>(t, top, w);
-    __syncthreads();
+    if (!fits) {
+        n = select_by_digits<DT, NT>(t, top, w);
+        __syncthreads();
+    }
     rank_found<NT>(w.found, n, w.best, top);
 }
 
@@ -401,6 +402,7 @@ __global__ __launch_bounds__(kMergeThreads) void token_join_kernel(const TokenAr
 #pragma unroll
         for (int i = 0; i < kEach; ++i) mine = umax64(mine, keys[i]);
         most_of[tid] = mine;
+        if (tid < kMaxTop) best[tid] = 0ull;
         if (tid == 0) n_found = 0;
     }
     __syncthreads();
@@ -546,7 +548,7 @@ hipError_t launch_token_logprobs(int dt, const TokenArgs& a, hipStream_t stream)
         });
     };
     auto of_type = [&](auto type) {
-        if (x.part <= kShortPart || a.rows * x.parts >= kManyBlocks) return of_rows(type, std::integral_constant<int, 256>{});
+        if (x.part <= kShortPart + 32 || a.rows * x.parts >= kManyBlocks) return of_rows(type, std::integral_constant<int, 256>{});
         return of_rows(type, std::integral_constant<int, 512>{});
     };
     return dt == DT_BF16 ? of_type(std::integral_constant<int, DT_BF16>{}) : of_type(std::integral_constant<int, DT_F32>{});
