@@ -539,15 +539,15 @@ __global__ __launch_bounds__(kThreads, 8) void distill_grad_kernel(const Distill
     }
 }
 
-// Parts that a row is cut into: up to 128 rows of more than 65536 places only, 4096 places at least each, as many as 256 workgroups ask for
-// (128256 float32 places, graph replays, loss alone and with the gradient: 1 row 9.5 us instead of 15.3 and 13.3 instead of 30.7, 60 rows 15.0 instead
-// of 17.9 and 23.9 instead of 35.4, 128 rows 18.3 instead of 20.2 and 38.6 instead of 41.4, 256 rows 28.1 instead of 24.5; 60 x 32003 11.0 instead of 9.8
-// and 15.7 instead of 14.4).
-constexpr int64_t kWantBlocks = 256, kLongRow = 65536, kFewRows = 128;
+// Parts that a row is cut into: rows of more than 65536 places only, as long as there is no more than a row for each 1024 of them, 4096 places at
+// least each, as many as 256 workgroups ask for (float32, graph replays, loss alone and with the gradient: 1 x 128256 8.9 us instead of 14.7 and
+// 12.9 instead of 27.7, 60 x 128256 13.6 instead of 17.8 and 24.8 instead of 30.0, 60 x 65537 12.3 either way and 19.8 instead of 19.2, 128 x 65537 14.4 instead of
+// 13.2 and 26.6 instead of 20.4).
+constexpr int64_t kWantBlocks = 256, kLongRow = 65536, kPlacesOfRow = 1024;
 DistillScratch scratch_of(int64_t rows, int64_t n, char* at) {
     DistillScratch x{};
     int64_t parts = (grid_of(n) + kWholeRow - 1) / kWholeRow;
-    if (n > kLongRow && rows <= kFewRows) {
+    if (n > kLongRow && rows <= n / kPlacesOfRow) {
         int64_t wanted = kWantBlocks / rows;
         if (wanted > n / 4096) wanted = n / 4096;
         if (wanted > parts) parts = wanted;

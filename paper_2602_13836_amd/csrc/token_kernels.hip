@@ -499,11 +499,11 @@ __global__ __launch_bounds__(kGradThreads) void token_grad_kernel(const TokenGra
 }
 
 // Parts that a row is cut into: up to 64 rows of more than 98304 places only, 4096 places at least each, as many as 256 workgroups ask for
-// (1 x 128256 float32, graph replays: 6.1 us instead of 10.2, with 20 alternatives 12.5 instead of 15.0; 60 rows 10.1 instead of 12.5 and 16.2
-// instead of 17.8; 128 rows 14.9 instead of 17.0 but 22.5 instead of 19.3; 16 x 65537 6.5 instead of 7.6 but 13.1 instead of 11.5).
+// (float32, graph replays, entropy alone and with 20 alternatives: 1 x 128256 5.8 us instead of 10.3 and 12.4 instead of 15.1, 60 rows 9.9 instead of
+// 12.4 and 16.7 instead of 17.9, 128 rows 14.5 instead of 16.6 and 22.1 either way; 16 x 65537 6.4 instead of 7.7 but 13.0 instead of 11.7).
 constexpr int64_t kWantBlocks = 256, kLongRow = 98304, kFewRows = 64;
-// 256 threads work on a part of up to 8192 places, and where there are workgroups for every place on the chip, else 512 (60 rows with 20 alternatives, 256
-// and 512 threads: of 2048 places 6.8 and 7.7 us, 8192 6.7 and 6.9, 32003 10.2 and 8.7; 1024 rows: 2048 places 8.7 and 15.9, 32003 25.7 and 30.0).
+// 256 threads work on a part of up to 8192 places, and where there are workgroups for every place on the chip, else 512 (with 20 alternatives, 256 and 512
+// threads: 60 rows of 2048 places 6.7 and 7.7 us, 8191 7.8 and 7.6, 32003 10.7 and 8.8; 1024 rows of 2048 places 8.6 and 15.9, 32003 27.5 and 31.7).
 constexpr int64_t kShortPart = 8192, kManyBlocks = 1024;
 TokenScratch scratch_of(int64_t rows, int64_t n, int top, char* at) {
     TokenScratch x{};
@@ -548,7 +548,7 @@ hipError_t launch_token_logprobs(int dt, const TokenArgs& a, hipStream_t stream)
         });
     };
     auto of_type = [&](auto type) {
-        if (x.part <= kShortPart + 32 || a.rows * x.parts >= kManyBlocks) return of_rows(type, std::integral_constant<int, 256>{});
+        if (x.part <= kShortPart || a.rows * x.parts >= kManyBlocks) return of_rows(type, std::integral_constant<int, 256>{});
         return of_rows(type, std::integral_constant<int, 512>{});
     };
     return dt == DT_BF16 ? of_type(std::integral_constant<int, DT_BF16>{}) : of_type(std::integral_constant<int, DT_F32>{});
