@@ -456,43 +456,54 @@ __device__ __forceinline__ void store_one(char* row, int64_t place, float g) {
     else reinterpret_cast<float*>(row)[place] = g;
 }
 
+// two floats as bfloat16, rounded to nearest even, by one instruction (the empty one keeps the compiler from converting the halves one by
+// one where they are also stored so)
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    const bf16x2_t b = {(__bf16)lo, (__bf16)hi};
+    uint32_t w = __builtin_bit_cast(uint32_t, b);
+    asm("" : "+v"(w));
+    return w;
+}
+
 // The gradients of vector iv of a part, rounded to nearest even; nobody here reads them again.  whole: (the same for all) it is a whole one of the
 // row; else its elements that are not the row's are not written.
 template <int GDT, int N>
 __device__ __forceinline__ void store_vector(char* row, const Part& t, int iv, bool whole, const float (&g)[N]) {
     row += t.first * (GDT == DT_BF16 ? 2 : 4);             // (a part's places are within 32 bits)
     const uint32_t place = (uint32_t)iv * N;
-    const int from = iv == 0 ? t.skip : 0, left = t.n - iv * N;
+    uint32_t w[GDT == DT_BF16 ? N / 2 : N];
     if constexpr (GDT == DT_BF16) {
-        typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-        uint32_t w[N / 2];
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i) {
-            const bf16x2_t b = {(__bf16)g[2 * i], (__bf16)g[2 * i + 1]};
-            w[i] = __builtin_bit_cast(uint32_t, b);
-        }
-        char* p = row + place * 2u;
-        if (whole || (left >= N && from == 0)) {
-            if constexpr (N == 8) __builtin_nontemporal_store(u32x4_any{w[0], w[1], w[2], w[3]}, reinterpret_cast<u32x4_any*>(p));
-            else __builtin_nontemporal_store(u32x2_any{w[0], w[1]}, reinterpret_cast<u32x2_any*>(p));
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (i >= from && i < left) reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
-        }
+        for (int i = 0; i < N / 2; ++i) w[i] = bf16_pair(g[2 * i], g[2 * i + 1]);
     } else {
-        float* p = reinterpret_cast<float*>(row) + place;
-        if (whole || (left >= N && from == 0)) {
 #pragma unroll
-            for (int q = 0; q < N / 4; ++q)
-                __builtin_nontemporal_store(u32x4_any{__float_as_uint(g[4 * q]), __float_as_uint(g[4 * q + 1]), __float_as_uint(g[4 * q + 2]),
-                                                      __float_as_uint(g[4 * q + 3])},
-                                            reinterpret_cast<u32x4_any*>(p + 4 * q));
+        for (int i = 0; i < N; ++i) w[i] = __float_as_uint(g[i]);
+    }
+    auto store = [&] {
+        char* p = row + place * (GDT == DT_BF16 ? 2u : 4u);
+        if constexpr (GDT == DT_BF16 && N == 4) {
+            __builtin_nontemporal_store(u32x2_any{w[0], w[1]}, reinterpret_cast<u32x2_any*>(p));
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (i >= from && i < left) p[i] = g[i];
+            for (int q = 0; q < (int)(sizeof(w) / 16); ++q)
+                __builtin_nontemporal_store(u32x4_any{w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]}, reinterpret_cast<u32x4_any*>(p + 16 * q));
         }
+    };
+    if (whole) {
+        store();
+        return;
+    }
+    const int from = iv == 0 ? t.skip : 0, left = t.n - iv * N;
+    if (left >= N && from == 0) {
+        store();
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (i < from || i >= left) continue;
+        if constexpr (GDT == DT_BF16) reinterpret_cast<uint16_t*>(row)[place + i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+        else reinterpret_cast<uint32_t*>(row)[place + i] = w[i];
     }
 }
 
