@@ -385,7 +385,8 @@ int specvocab_quantized_sample_step(const void* h, const uint8_t* h_scales, int6
  * elements, aligned to an element.  -inf masks a place: it has probability 0 and no gradient.  Any other value is a logit, the type's
  * lowest too.  A row with a NaN or +inf has NaN throughout, and no alternatives (-1).  A row that is masked throughout has log probabilities of -inf, entropy
  * 0 and no gradient.  grad_out: device [rows x n] in `grad_dt` (SV_F32 or SV_BF16, rounded to nearest even), row stride ld_grad, every
- * place written; it may be the logits themselves (same base, stride and type) and must not overlap them otherwise.
+ * place written; it may be the logits themselves (same base, stride and type; another type is SV_ERR_DTYPE, another stride SV_ERR_SHAPE) and must not
+ * overlap them otherwise.
  * Results do not depend on the run.  Sums are float32, relative to a logit near the largest; probabilities below 2^-126 count as 0.
  * `state` is what a gradient needs of the forward call: device [rows x 4] float32, 16-byte aligned. */
 

@@ -510,9 +510,12 @@ int check_token_shape(int64_t rows, int64_t n, int64_t ld, int dt, int64_t given
     return top > 0 && n > sv::kTopVocab ? SV_ERR_UNSUPPORTED : SV_OK;
 }
 inline bool aligned_to(const void* p, int dt) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(esize_of(dt) - 1)) == 0; }
-int check_gradient(const void* grad, int64_t ld_grad, int grad_dt, int64_t n) {
+// a gradient may take the place of its logits, element by element
+int check_gradient(const void* grad, int64_t ld_grad, int grad_dt, const void* logits, int64_t ld, int dt, int64_t rows, int64_t n) {
     if (!dtype_ok(grad_dt)) return SV_ERR_DTYPE;
     if (ld_grad < n) return SV_ERR_SHAPE;
+    if (grad == logits && grad_dt != dt) return SV_ERR_DTYPE;
+    if (grad == logits && rows > 1 && ld_grad != ld) return SV_ERR_SHAPE;
     return aligned_to(grad, grad_dt) ? SV_OK : SV_ERR_ALIGN;
 }
 int check_scratch(size_t need, const void* ws, size_t ws_bytes) {
@@ -1147,7 +1150,7 @@ int specvocab_token_logprobs_grad(const void* logits, int64_t ld, int64_t rows, 
     int st = check_token_shape(rows, n, ld, dt, given, 0);
     if (st != SV_OK) return st;
     if (grad_logprob && given < 1) return SV_ERR_SHAPE;
-    st = check_gradient(grad_out, ld_grad, grad_dt, n);
+    st = check_gradient(grad_out, ld_grad, grad_dt, logits, ld, dt, rows, n);
     if (st != SV_OK) return st;
     if (!aligned_to(logits, dt) || !aligned16(state)) return SV_ERR_ALIGN;
     if (ensure_device() != SV_OK) return SV_ERR_HIP;
@@ -1178,7 +1181,7 @@ int specvocab_distill(const void* logits, int64_t ld, int64_t rows, int64_t n, i
     a.scratch = static_cast<char*>(ws);
     if (!loss_out) return SV_ERR_NULL;
     int st = check_distill(a, ld, dt, known);
-    if (st == SV_OK && grad_out) st = check_gradient(grad_out, ld_grad, grad_dt, n);
+    if (st == SV_OK && grad_out) st = check_gradient(grad_out, ld_grad, grad_dt, logits, ld, dt, rows, n);
     if (st == SV_OK) st = check_scratch(sv::distill_scratch_bytes(rows, n), ws, ws_bytes);
     if (st != SV_OK) return st;
     if (ensure_device() != SV_OK) return SV_ERR_HIP;
@@ -1195,7 +1198,7 @@ int specvocab_distill_grad(const void* logits, int64_t ld, int64_t rows, int64_t
         distill_args(logits, ld, rows, n, dt, tok, teacher, known, kind, temperature, weight, state, grad_out, ld_grad, grad_dt);
     if (!state || !grad_out) return SV_ERR_NULL;
     int st = check_distill(a, ld, dt, known);
-    if (st == SV_OK) st = check_gradient(grad_out, ld_grad, grad_dt, n);
+    if (st == SV_OK) st = check_gradient(grad_out, ld_grad, grad_dt, logits, ld, dt, rows, n);
     if (st != SV_OK) return st;
     if (ensure_device() != SV_OK) return SV_ERR_HIP;
     hipStream_t s = static_cast<hipStream_t>(stream);

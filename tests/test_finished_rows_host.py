@@ -41,7 +41,7 @@ def test_token_logprobs_refuses(lib, kw, status):
 
 
 def logprobs_grad(lib, **kw):
-    a = dict(z=P, ld=100, rows=2, n=100, dt=0, t=None, tokens=P, given=1, state=P, g=P, ge=P, out=P, ld_grad=100, gdt=0) | kw
+    a = dict(z=P, ld=100, rows=2, n=100, dt=0, t=None, tokens=P, given=1, state=P, g=P, ge=P, out=2 * P, ld_grad=100, gdt=0) | kw
     return lib.specvocab_token_logprobs_grad(*a.values(), None)
 
 
@@ -49,20 +49,20 @@ def logprobs_grad(lib, **kw):
     (dict(z=None), NULL), (dict(state=None), NULL), (dict(out=None), NULL), (dict(g=None, ge=None), NULL), (dict(tokens=None), NULL),
     (dict(rows=0), SHAPE), (dict(n=0), SHAPE), (dict(ld=99), SHAPE), (dict(ld_grad=99), SHAPE), (dict(given=0), SHAPE), (dict(given=65), SHAPE),
     (dict(dt=2), DTYPE), (dict(gdt=2), DTYPE), (dict(z=P + 2), ALIGN), (dict(out=P + 2), ALIGN), (dict(out=P + 1, gdt=1), ALIGN),
-    (dict(state=P + 4), ALIGN),
+    (dict(state=P + 4), ALIGN), (dict(out=P, gdt=1), DTYPE), (dict(out=P, ld_grad=101), SHAPE), (dict(out=P, dt=1), DTYPE),
 ])
 def test_token_logprobs_grad_refuses(lib, kw, status):
     assert logprobs_grad(lib, **kw) == status
 
 
 def distilled(lib, **kw):
-    a = dict(z=P, ld=100, rows=2, n=100, dt=0, tok=P, teacher=P, known=8, kind=0, t=1.0, w=None, loss=P, state=P, out=P, ld_grad=100, gdt=0, ws=None,
+    a = dict(z=P, ld=100, rows=2, n=100, dt=0, tok=P, teacher=P, known=8, kind=0, t=1.0, w=None, loss=P, state=P, out=2 * P, ld_grad=100, gdt=0, ws=None,
              ws_bytes=0) | kw
     return lib.specvocab_distill(*a.values(), None)
 
 
 def distilled_grad(lib, **kw):
-    a = dict(z=P, ld=100, rows=2, n=100, dt=0, tok=P, teacher=P, known=8, kind=0, t=1.0, w=None, state=P, out=P, ld_grad=100, gdt=0) | kw
+    a = dict(z=P, ld=100, rows=2, n=100, dt=0, tok=P, teacher=P, known=8, kind=0, t=1.0, w=None, state=P, out=2 * P, ld_grad=100, gdt=0) | kw
     return lib.specvocab_distill_grad(*a.values(), None)
 
 
@@ -73,6 +73,7 @@ def distilled_grad(lib, **kw):
     (dict(known=1 << 40), SHAPE), (dict(t=0.0), SHAPE), (dict(t=-1.0), SHAPE), (dict(t=math.nan), SHAPE), (dict(t=math.inf), SHAPE),
     (dict(t=1e-7), SHAPE), (dict(t=2e6), SHAPE), (dict(kind=3), DTYPE), (dict(kind=-1), DTYPE), (dict(dt=2), DTYPE), (dict(gdt=2), DTYPE),
     (dict(z=P + 2), ALIGN), (dict(out=P + 2), ALIGN), (dict(out=P + 1, gdt=1), ALIGN), (dict(state=P + 4), ALIGN),
+    (dict(out=P, gdt=1), DTYPE), (dict(out=P, ld_grad=101), SHAPE), (dict(out=P, dt=1), DTYPE),
 ])
 def test_distill_refuses(lib, call, kw, status):
     assert call(lib, **kw) == status
