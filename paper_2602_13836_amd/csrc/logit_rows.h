@@ -434,17 +434,19 @@ hipError_t over_rows(int64_t rows, int64_t threads_of_row, F&& f) {
 
 // ---- gradients
 //
-// 2^(a (z - m)) of a row's places as 2^(a z - c) times a factor near 1, c = a m rounded, so that a place takes one fused multiply-add; where
-// c leaves the range in which that is sound, by differences.
+// 2^(a (z - m)) of a row's places as 2^(a z - c) times a factor near 1, c = a m rounded, so that a place takes one fused multiply-add.  The factor puts
+// the rounding of c back: it is within an octave up to |c| = 2^25, and may leave float32's range from 2^31 on (a row of -1e10: 2^-440, while every
+// place has 2^440).  Where it is more than an octave, by differences; every thread of a row decides alike.
 struct Exponent {
     float a, m, c;
-    float shift;         // c - a m: 2^(a (z - m)) = 2^shift 2^(a z - c)
-    bool exact;
+    float shift;         // c - a m: 2^(a (z - m)) = 2^shift 2^(a z - c); at most 1 in size
+    bool exact;          // by differences; shift is 0
 };
 __device__ __forceinline__ Exponent exponent_of(float m, float a) {
     Exponent x{a, m, m * a, 0.0f, false};
-    x.exact = !(fabsf(x.c) < 0x1p100f);
-    if (!x.exact) x.shift = -fmaf(m, a, -x.c);
+    const float shift = -fmaf(m, a, -x.c);
+    x.exact = !(fabsf(shift) <= 1.0f);                     // (an infinite c, too)
+    if (!x.exact) x.shift = shift;
     return x;
 }
 template <bool EXACT>
