@@ -244,7 +244,8 @@ struct Given {
 };
 template <int DT, int NT>
 __device__ __forceinline__ Given given_token(const TokenArgs& a, int64_t row, FindWork& w) {
-    const int tid = threadIdx.x, n = (int)a.n;
+    const int tid = threadIdx.x;
+    const uint32_t n = (uint32_t)a.n;                      // (up to 2^31 - 1, and steps of up to 2^13 past it: within 32 bits without a sign only)
     Given g{false, -INFINITY};
     int32_t place = tid < a.given ? a.tokens[row * a.given + tid] : -1;
     if (a.idx && a.given > 0) {
@@ -252,7 +253,7 @@ __device__ __forceinline__ Given given_token(const TokenArgs& a, int64_t row, Fi
         clear_words<NT>(w.bits, 256);
         if (tid < kFindSlots) {
             w.keys[tid] = kEmptySlot;
-            w.place[tid] = n;
+            w.place[tid] = (int)n;
         }
         __syncthreads();
         uint32_t slot = 0;
@@ -265,32 +266,32 @@ __device__ __forceinline__ Given given_token(const TokenArgs& a, int64_t row, Fi
         __syncthreads();
         typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
         const int32_t* ids = a.idx + row * a.idx_row_stride;
-        auto look = [&](int32_t id, int at) {
+        auto look = [&](int32_t id, uint32_t at) {
             const uint32_t h = slot_of<8192>(id);
             if (id < 0 || !((w.bits[h >> 5] >> (h & 31)) & 1u)) return;
             for (uint32_t s = slot_of<kFindSlots>(id);; s = (s + 1) & (kFindSlots - 1)) {
                 const int32_t key = w.keys[s];
-                if (key == id) atomicMin(&w.place[s], at);
+                if (key == id) atomicMin(&w.place[s], (int)at);
                 if (key == id || key == kEmptySlot) return;
             }
         };
-        constexpr int kAtOnce = 4;
-        int at = 4 * tid;
+        constexpr uint32_t kAtOnce = 4;
+        uint32_t at = 4 * (uint32_t)tid;
         for (; at + 4 * NT * (kAtOnce - 1) + 3 < n; at += 4 * NT * kAtOnce) {
             i32x4_any id[kAtOnce];
 #pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) id[u] = *reinterpret_cast<const i32x4_any*>(ids + at + 4 * NT * u);
+            for (uint32_t u = 0; u < kAtOnce; ++u) id[u] = *reinterpret_cast<const i32x4_any*>(ids + at + 4 * NT * u);
 #pragma unroll
-            for (int u = 0; u < kAtOnce; ++u)
+            for (uint32_t u = 0; u < kAtOnce; ++u)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) look(id[u][e], at + 4 * NT * u + e);
+                for (uint32_t e = 0; e < 4; ++e) look(id[u][e], at + 4 * NT * u + e);
         }
         for (; at + 3 < n; at += 4 * NT) {
             const i32x4_any id = *reinterpret_cast<const i32x4_any*>(ids + at);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) look(id[e], at + e);
+            for (uint32_t e = 0; e < 4; ++e) look(id[e], at + e);
         }
-        if (tid < (n & 3)) look(ids[(n & ~3) + tid], (n & ~3) + tid);
+        if ((uint32_t)tid < (n & 3u)) look(ids[(n & ~3u) + tid], (n & ~3u) + tid);
         __syncthreads();
         place = place >= 0 ? w.place[slot] : -1;
     }
