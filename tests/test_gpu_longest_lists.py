@@ -1,4 +1,5 @@
 """Given tokens are looked up in lists of up to 2^31 - 1 ids; the walk over such a list steps past 2^31 before it ends."""
+import math
 
 import pytest
 import torch
