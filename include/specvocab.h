@@ -432,7 +432,8 @@ int specvocab_token_logprobs_grad(const void* logits, int64_t ld, int64_t rows, 
  * state_out[r] = (m, sum_v exp((z[v] - m) / T), the same two over the places that are not listed (SV_TEACHER_REST only, else 0)), m a logit near
  * the largest, or NULL.
  * grad_out may be NULL: the loss alone (or its gradient later, when the factors are known, by specvocab_distill_grad with the same arguments and
- * the state; weight[r] is then whatever factor the row's divergence has).  Both at once read the logits from memory once.
+ * the state; weight[r] is then whatever factor the row's divergence has -- but a row that had weight 0 in the forward call was not read, has a state
+ * of zeros and gets a gradient of 0 whatever its weight then is).  Both at once read the logits from memory once.
  * One launch; two, three with the gradient, and workspace where there are few rows for their length, or more than 2^18 places. */
 int specvocab_distill(const void* logits, int64_t ld, int64_t rows, int64_t n, int dt,
                       const int32_t* tok, const float* teacher, int64_t known, int kind, float temperature, const float* weight,

@@ -940,7 +940,7 @@ def distill_grad(logits: torch.Tensor, tok: torch.Tensor, teacher: torch.Tensor,
                  temperature: float = 1.0, weight: Optional[torch.Tensor] = None, grad_dtype: Optional[torch.dtype] = None,
                  grad_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """specvocab_distill_grad: the logits' gradient of distill's losses from the state that it left; weight: whatever factor each row's
-    divergence has by now."""
+    divergence has by now, but a row that distill was given with weight 0 has no gradient."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return distill_grad(logits, tok, teacher, state, kind, temperature, weight, grad_dtype, grad_out)

@@ -177,12 +177,13 @@ struct Factors {
     float m, of_listed;      // listed places: of_listed * 2^(c (z - m)) - scale * their sum of p
     Exponent x;
     float of_rest;           // others: of_rest * 2^(octaves_at(x, z))
-    float scale;             // w / T
+    float scale;             // w / T; 0 for a row without sums: masked throughout, or of weight 0 in the forward call
 };
 __device__ __forceinline__ Factors factors_of(const DistillArgs& a, float weight, const Teacher& t, const float4 st, float c) {
     Factors f;
-    f.scale = weight / a.temperature;
-    const bool some = st.y != 0.0f, rest = a.kind == kRest, other = rest && st.w != 0.0f;
+    const bool some = st.y != 0.0f;
+    f.scale = some ? weight / a.temperature : 0.0f;
+    const bool rest = a.kind == kRest, other = rest && st.w != 0.0f;
     const float left = other ? (float)t.left : 0.0f, of_row = some ? f.scale * (float)(t.mass + (double)left) / st.y : 0.0f;
     f.m = st.x;
     f.of_listed = of_row;
