@@ -429,8 +429,8 @@ int specvocab_token_logprobs_grad(const void* logits, int64_t ld, int64_t rows, 
  * token that is listed twice has both masses.  specvocab_token_logprobs writes such lists (top_tok_out, top_logprob_out).  A listed token with mass at a
  * masked place makes the loss +inf.  temperature: T, finite, within 2^-20 .. 2^20; weight: device [rows] float32, or NULL for 1; a row of weight 0
  * is not read: loss 0, gradient 0.  A mean over tokens or a factor T^2 goes into the weight.
- * state_out[r] = (m, sum_v exp((z[v] - m) / T), the same two over the places that are not listed (SV_TEACHER_REST only, else 0)), m a logit near
- * the largest, or NULL.
+ * state_out[r] = (m, sum_v exp((z[v] - m) / T), the same two over the places that are not listed (SV_TEACHER_REST only, else 0)), m a number
+ * near the largest of those logits, or NULL.
  * grad_out may be NULL: the loss alone (or its gradient later, when the factors are known, by specvocab_distill_grad with the same arguments and
  * the state; weight[r] is then whatever factor the row's divergence has -- but a row that had weight 0 in the forward call was not read, has a state
  * of zeros and gets a gradient of 0 whatever its weight then is).  Both at once read the logits from memory once.

@@ -119,6 +119,16 @@ __device__ __forceinline__ Teacher teacher_of(const DistillArgs& a, const Entry&
     return t;
 }
 
+// A sum that has outgrown its reference (by up to 2^90, see Sums) relative to one near the row's largest logit: 2^(c (m - m')) between the rest's and the
+// row's, or a small weight over such a sum, would leave float32's range while the places' probabilities are well within it.  Any number will do as a
+// reference as long as the sum is relative to that very number.
+__device__ __forceinline__ void move_reference(float& m, float& s, float c) {
+    if (!(s > 0x1p20f)) return;
+    const float to = m + __log2f(s) / c;
+    s = (float)((double)s * exp2(((double)m - (double)to) * (double)c));
+    m = to;
+}
+
 // The row's loss, and its state, which every thread gets.  sums: over the places that are not listed where the rest counts, else over all.  z: the logit
 // at this thread's entry.  One barrier.
 __device__ __forceinline__ float4 finish_row(const DistillArgs& a, int64_t row, float weight, const Entry& e, const Teacher& t, float z,
@@ -154,6 +164,8 @@ __device__ __forceinline__ float4 finish_row(const DistillArgs& a, int64_t row, 
         state.z = sums.m;
         state.w = sums.s;
     }
+    move_reference(state.x, state.y, c);
+    move_reference(state.z, state.w, c);
     if (threadIdx.x == 0) {
         double loss = 0.0;
         for (int i = 0; i < waves; ++i) loss += w.loss_sums[i];
