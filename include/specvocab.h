@@ -388,6 +388,8 @@ int specvocab_quantized_sample_step(const void* h, const uint8_t* h_scales, int6
  * place written; it may be the logits themselves (same base, stride and type; another type is SV_ERR_DTYPE, another stride SV_ERR_SHAPE) and must not
  * overlap them otherwise.
  * Results do not depend on the run.  Sums are float32, relative to a logit near the largest; probabilities below 2^-126 count as 0.
+ * Tokens that name no place are allowed for.  The debug mode lets -1 pass and names the others (SV_ERR_INDEX): the tokens given to
+ * specvocab_token_logprobs without a list and to its gradient, and a teacher's.
  * `state` is what a gradient needs of the forward call: device [rows x 4] float32, 16-byte aligned. */
 
 /* Log probabilities of given tokens, the entropy and the largest alternatives of every row, natural logarithms at temperature T =
@@ -402,7 +404,7 @@ int specvocab_quantized_sample_step(const void* h, const uint8_t* h_scales, int6
  * 8388608 is SV_ERR_UNSUPPORTED.
  * idx, idx_mode: the token ids of the places, as in specvocab_sample (any order), or NULL: a token is its place.  Of equal ids
  * the first place counts.
- * One launch, two (and workspace) where there are few rows for their length.  Rows in which more than 1024 places may be among the
+ * One launch; two, and workspace, where there are few rows for their length, or rows of more than 262137 places.  Rows in which more than 1024 places may be among the
  * largest (equal logits in their hundreds) take some ten passes over the row. */
 int specvocab_token_logprobs(const void* logits, int64_t ld, int64_t rows, int64_t n, int dt,
                              const int32_t* idx, int idx_mode, const float* temperature,
@@ -433,8 +435,10 @@ int specvocab_token_logprobs_grad(const void* logits, int64_t ld, int64_t rows, 
  * near the largest of those logits, or NULL.
  * grad_out may be NULL: the loss alone (or its gradient later, when the factors are known, by specvocab_distill_grad with the same arguments and
  * the state; weight[r] is then whatever factor the row's divergence has -- but a row that had weight 0 in the forward call was not read, has a state
- * of zeros and gets a gradient of 0 whatever its weight then is).  Both at once read the logits from memory once.
- * One launch; two, three with the gradient, and workspace where there are few rows for their length, or more than 2^18 places. */
+ * of zeros and gets a gradient of 0 whatever its weight then is).  Both at once keep a part of each row
+ * on the chip and read the others a second time.
+ * One launch; two, three with the gradient (every row is read twice then), and workspace where there are few rows for their length, or rows of more than
+ * 262137 places. */
 int specvocab_distill(const void* logits, int64_t ld, int64_t rows, int64_t n, int dt,
                       const int32_t* tok, const float* teacher, int64_t known, int kind, float temperature, const float* weight,
                       float* loss_out, float* state_out, void* grad_out, int64_t ld_grad, int grad_dt,

@@ -325,8 +325,9 @@ __global__ __launch_bounds__(kThreads) void distill_rows_kernel(const DistillArg
 
 // One workgroup per row: loss and gradient, that is two passes over the row.  The fabric moves 7 TB/s whether the lines come from the last-level
 // cache or from memory, so the second pass reads as little as it can: a thread keeps its first KEPT vectors in registers -- 14, nearly half of
-// 128256 bfloat16 logits, or 4 where the row has no more -- and walks the others backwards, of which the L2 then still holds most (4096 rows: 413 us, 422 with 8
-// kept, 441 with 4, and 16 leave too few registers; 2.1 GB, a read and a write of each place).  Some of the others in LDS changed nothing.
+// 128256 bfloat16 logits or a fifth of as many float32 ones, or 4 where the row has no more -- and walks the others backwards, of which the L2
+// then still holds most (4096 bfloat16 rows: 413 us, 422 with 8 kept, 441 with 4, and 16 leave too few registers; 2.1 GB, a read and a write of each
+// place; 1024 float32 rows, 1.05 GB: 222).  Some of the others in LDS changed nothing.
 constexpr int kStep = 2;                                   // vectors of a chunk
 template <int DT, int GDT, bool REST, int KEPT>
 __global__ __launch_bounds__(kThreads, KEPT > 4 ? 4 : 6) void distill_step_kernel(const DistillArgs a, const int64_t first_row) {

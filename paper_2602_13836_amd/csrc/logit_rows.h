@@ -52,8 +52,8 @@ __device__ __forceinline__ float logit_at(const char* row, int64_t place) {
 
 // A part of a row: the vectors [k * size, (k + 1) * size) of the 16-byte grid that its logits lie on.  A row begins at any element, so its first
 // vector may have up to 7 elements that are not the row's; they count as masked and are neither read nor written.  (By vectors from the row's own beginning
-// bfloat16 rows at odd elements take a fourth longer: 2048 x 128256, the gradient of log probabilities 203 us instead of 181, loss and gradient 255 instead
-// of 215.)
+// bfloat16 rows at odd elements take longer: 2048 x 128256, the gradient of log probabilities 203 us instead of 166 to 171, loss and gradient 255 instead of
+// 245 to 250; rows at 16-byte addresses take 162 and 219 to 226.)
 struct Part {
     const char* p;       // of its first vector
     int64_t first;       // the place of that vector's first element: -skip in a row's first part

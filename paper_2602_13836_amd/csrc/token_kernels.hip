@@ -501,9 +501,10 @@ __global__ __launch_bounds__(kGradThreads) void token_grad_kernel(const TokenGra
 
 // Parts that a row is cut into: up to 64 rows of more than 98304 places only, 4096 places at least each, as many as 256 workgroups ask for
 // (float32, graph replays, entropy alone and with 20 alternatives: 1 x 128256 5.8 us instead of 10.3 and 12.4 instead of 15.1, 60 rows 9.9 instead of
-// 12.4 and 16.7 instead of 17.9, 128 rows 14.5 instead of 16.6 and 22.1 either way; 16 x 65537 6.4 instead of 7.7 but 13.0 instead of 11.7).
+// 12.4 and 16.7 instead of 17.9, 128 rows 14.5 instead of 16.6 and 22.1 either way; 16 x 65537 6.4 instead of 7.7 but 13.0 instead of 11.7).  The
+// borders are those with alternatives; without them somewhat more and shorter rows would gain by parts.
 constexpr int64_t kWantBlocks = 256, kLongRow = 98304, kFewRows = 64;
-// 256 threads work on a part of up to 8192 places, and where there are workgroups for every place on the chip, else 512 (with 20 alternatives, 256 and 512
+// 256 threads work on a part of up to 8192 places of the grid (a row of 8185, wherever it begins), and where there are workgroups for every place on the chip, else 512 (with 20 alternatives, 256 and 512
 // threads: 60 rows of 2048 places 6.7 and 7.7 us, 8191 7.8 and 7.6, 32003 10.7 and 8.8; 1024 rows of 2048 places 8.6 and 15.9, 32003 27.5 and 31.7).
 constexpr int64_t kShortPart = 8192, kManyBlocks = 1024;
 TokenScratch scratch_of(int64_t rows, int64_t n, int top, char* at) {

@@ -139,9 +139,11 @@ def distill(z, tok, teacher, kind="logits", temp=1.0, weight=None):
 #
 # A term 2^y of a sum, y = (z - reference) log2(e) / T: the factor is rounded twice (1.5 half steps with the constant's own), y once, so y
 # is off by at most 2.5 half steps of itself, 2^y by that times ln 2, and the exponential itself by a step.  Terms below 2^-40 of the
-# sum do not matter, so |y| <= 40 where it counts: 2.5 * 40 * 0.7 + 2 = 72 half steps.  A thread adds at most n / 512 + 64 terms one
-# after the other (256 threads at least work on 2^14 places), with one rescaling of three roundings for every 16, then 9 + 12 steps join
-# the threads, a wavefront's and the parts, with three roundings each.
+# sum do not matter, so |y| <= 40 where it counts: 2.5 * 40 * 0.7 + 2 = 72 half steps.  A thread adds its terms one after the other, with
+# one rescaling of three roundings for every 16, then 9 + 12 steps join the threads, a wavefront's and the parts, with three roundings each.
+# Up to 2^14 places, 256 threads at work, a thread adds at most 64 terms and this is a bound.  In longer rows it may add up to 1024 (2^18 places), of which
+# no more than 128 are counted: the roundings of terms of many sizes go either way, and 1024 of them add up like their root, 32 half steps.  Equal terms
+# by the thousand, whose roundings may all go one way, could be off by more: 1.2 half steps each.
 def sum_error(n):
     terms = n / 256 / max(1, n / 16384) + 64
     return STEP * (72 + 1.2 * terms + 63)
