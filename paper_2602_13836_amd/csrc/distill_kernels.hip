@@ -186,28 +186,25 @@ __device__ __forceinline__ float4 finish_row(const DistillArgs& a, int64_t row, 
 
 // the factors of a row's gradient
 struct Factors {
-    float m, of_listed;      // listed places: of_listed * 2^(c (z - m)) - scale * their sum of p
-    Exponent x;
-    float of_rest;           // others: of_rest * 2^(octaves_at(x, z))
-    float scale;             // w / T; 0 for a row without sums: masked throughout, or of weight 0 in the forward call
+    float m, of_rest;        // places that are not listed: of_rest * 2^(c (z - m))
+    float of_row;            // w / T (mass that counts) / sum; 0 for a row without sums: masked throughout, or of weight 0 in the forward call
 };
 __device__ __forceinline__ Factors factors_of(const DistillArgs& a, float weight, const Teacher& t, const float4 st, float c) {
     Factors f;
-    const bool some = st.y != 0.0f;
-    f.scale = some ? weight / a.temperature : 0.0f;
-    const bool rest = a.kind == kRest, other = rest && st.w != 0.0f;
-    const float left = other ? (float)t.left : 0.0f, of_row = some ? f.scale * (float)(t.mass + (double)left) / st.y : 0.0f;
-    f.m = st.x;
-    f.of_listed = of_row;
-    f.x = exponent_of(rest ? st.z : st.x, c);
-    float of_rest = of_row;
-    if (rest) of_rest = other ? of_row * exp2_fast(fmaxf((st.z - st.x) * c, kNoMass)) - f.scale * (left / st.w) : 0.0f;
-    f.of_rest = of_rest * exp2_fast(f.x.shift);
+    const bool some = st.y != 0.0f, rest = a.kind == kRest, other = rest && st.w != 0.0f;
+    const float scale = weight / a.temperature, left = other ? (float)t.left : 0.0f;
+    f.of_row = some ? scale * (float)(t.mass + (double)left) / st.y : 0.0f;
+    f.m = rest ? st.z : st.x;
+    f.of_rest = f.of_row;
+    if (rest) f.of_rest = other ? f.of_row * exp2_fast(fmaxf((st.z - st.x) * c, kNoMass)) - scale * left / st.w : 0.0f;
     return f;
 }
 // the gradient at a listed place that holds z, of a token with mass p
-__device__ __forceinline__ float listed_gradient(const Factors& f, float z, double p) {
-    return z == -INFINITY ? f.of_listed * 0.0f : (float)((double)(f.of_listed * exp2_fast((z - f.m) * f.x.a)) - (double)f.scale * p);
+__device__ __forceinline__ float listed_gradient(const DistillArgs& a, float weight, const Teacher& t, const float4 st, float c, const Factors& f, float z, double p) {
+    if (z == -INFINITY || st.y == 0.0f) return f.of_row * 0.0f;
+    const float q = exp2_fast(octaves_at(z, st.x, c)) / st.y;
+    const double mass = t.mass + (a.kind == kRest && st.w != 0.0f ? t.left : 0.0);
+    return (float)((double)(weight / a.temperature) * (mass * (double)q - p));
 }
 
 // the list into LDS, and whether a token is in it twice; keys: kSlots words.  Every thread calls.
@@ -416,38 +413,34 @@ __global__ __launch_bounds__(kThreads, KEPT > 4 ? 4 : 6) void distill_step_kerne
     const Teacher teacher = teacher_of<true>(a, e, z_listed, w);
     const float4 st = finish_row(a, row, weight, e, teacher, z_listed, sums, c, w);
     const Factors f = factors_of(a, weight, teacher, st, c);
-    const double p = mass_of_token(e, teacher, a.known, w);
-    auto write = [&](auto exact, int chunk, const u32x4 v0, const u32x4 v1) {
+    const float g_listed = listed_gradient(a, weight, teacher, st, c, f, z_listed, mass_of_token(e, teacher, a.known, w));
+    auto write = [&](int chunk, const u32x4 v0, const u32x4 v1) {
         const bool whole = whole_chunk<NT, kStep>(t, chunk * (kStep * NT));
 #pragma unroll
         for (int u = 0; u < kStep; ++u) {
             float z[V], g[V];
             widen<DT>(u == 0 ? v0 : v1, z);
 #pragma unroll
-            for (int i = 0; i < V; ++i) g[i] = f.of_rest * exp2_fast(octaves_at<decltype(exact)::value>(f.x, z[i]));
+            for (int i = 0; i < V; ++i) g[i] = f.of_rest * exp2_fast(octaves_at(z[i], f.m, c));
             store_vector<GDT>(out, t, (chunk * kStep + u) * NT + tid, whole, g);
         }
     };
-    auto write_all = [&](auto exact) {
-        u32x4 next[kStep];
-        if (chunks > kFirst) load_chunk<DT, NT, kStep, true>(t, (chunks - 1) * (kStep * NT), next);
-        for (int chunk = chunks - 1; chunk >= kFirst; --chunk) {
-            const u32x4 v0 = next[0], v1 = next[1];
-            if (chunk > kFirst) load_chunk<DT, NT, kStep, true>(t, (chunk - 1) * (kStep * NT), next);
-            write(exact, chunk, v0, v1);
-        }
+    u32x4 next[kStep];
+    if (chunks > kFirst) load_chunk<DT, NT, kStep, true>(t, (chunks - 1) * (kStep * NT), next);
+    for (int chunk = chunks - 1; chunk >= kFirst; --chunk) {
+        const u32x4 v0 = next[0], v1 = next[1];
+        if (chunk > kFirst) load_chunk<DT, NT, kStep, true>(t, (chunk - 1) * (kStep * NT), next);
+        write(chunk, v0, v1);
+    }
 #pragma unroll
-        for (int k = 0; k < KEPT; k += kStep) {
-            if (k * NT >= t.vectors) continue;
-            asm volatile("" : "+v"(kept[k]), "+v"(kept[k + 1]));
-            write(exact, k / kStep, kept[k], kept[k + 1]);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    };
-    if (f.x.exact) write_all(std::true_type{});
-    else write_all(std::false_type{});
+    for (int k = 0; k < KEPT; k += kStep) {
+        if (k * NT >= t.vectors) continue;
+        asm volatile("" : "+v"(kept[k]), "+v"(kept[k + 1]));
+        write(k / kStep, kept[k], kept[k + 1]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
     __syncthreads();
-    if (e.there) store_one<GDT>(out, e.id, listed_gradient(f, z_listed, p));
+    if (e.there) store_one<GDT>(out, e.id, g_listed);
 }
 
 // One workgroup per part of a row: its sums.
@@ -530,18 +523,14 @@ __global__ __launch_bounds__(kThreads, 8) void distill_grad_kernel(const Distill
     const Factors f = factors_of(a, weight, teacher, st, c);
     // every read of the part is done before any of its places is written: the gradient may replace the logits
     __syncthreads();
-    auto pass = [&](auto exact) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float z[V], g[V];
-            widen<DT>(v[u], z);
+    for (int u = 0; u < U; ++u) {
+        float z[V], g[V];
+        widen<DT>(v[u], z);
 #pragma unroll
-            for (int i = 0; i < V; ++i) g[i] = f.of_rest * exp2_fast(octaves_at<decltype(exact)::value>(f.x, z[i]));
-            store_vector<GDT>(out, t, u * kThreads + tid, whole_chunk<kThreads, U>(t, 0), g);
-        }
-    };
-    if (f.x.exact) pass(std::true_type{});
-    else pass(std::false_type{});
+        for (int i = 0; i < V; ++i) g[i] = f.of_rest * exp2_fast(octaves_at(z[i], f.m, c));
+        store_vector<GDT>(out, t, u * kThreads + tid, whole_chunk<kThreads, U>(t, 0), g);
+    }
     __syncthreads();
     if (here) {
         double p = teacher.p;
@@ -549,7 +538,7 @@ __global__ __launch_bounds__(kThreads, 8) void distill_grad_kernel(const Distill
             p = 0.0;
             for (int i = 0; i < a.known; ++i) p += w.id[i] == e.id ? w.p[i] : 0.0;
         }
-        store_one<GDT>(out, e.id, listed_gradient(f, z_listed, p));
+        store_one<GDT>(out, e.id, listed_gradient(a, weight, teacher, st, c, f, z_listed, p));
     }
 }
 

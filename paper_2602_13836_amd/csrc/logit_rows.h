@@ -273,11 +273,27 @@ __device__ __forceinline__ void block_sum_pair(float& s, float& e, float* scratc
         e += scratch[2 * w + 1];
     }
 }
+// From the rounded reference to m, y = a m - c: where the largest logit is all that the sum has, which has been counted as 2^y, the sum is 1 -- not 2^y times
+// 2^-y, each of them rounded -- and e what the other places gave.
+__device__ __forceinline__ void onto_largest(RowSums& r, float y) {
+#pragma clang fp contract(off)
+    const float one = exp2_fast(y);
+    if (r.s == one && one > 0.0f && one < INFINITY) {      // (else both may have left float32's range, for sums_hold to see)
+        const float of_shift = y * r.s;                    // (as the place's own term was rounded)
+        r.e = (r.e - of_shift) / one;
+        r.s = 1.0f;
+    } else {
+        const float back = exp2_fast(-y);
+        r.e = back * fmaf(-y, r.s, r.e);
+        r.s *= back;
+    }
+}
 template <int NT>
 __device__ __forceinline__ RowSums sums_by_reference(const Sums& run, float m, float a, float* scratch) {
     RowSums r{m, run.s, 0.0f};
     block_sum_pair<NT>(r.s, r.e, scratch);
-    r.s *= exp2_fast(-fmaf(m, a, -(m * a)));               // from the rounded reference to m
+    onto_largest(r, fmaf(m, a, -(m * a)));
+    r.e = 0.0f;
     return r;
 }
 // (one barrier; nobody has used scratch before)
@@ -306,11 +322,7 @@ __device__ __forceinline__ RowSums sums_by_reference(const EntropySums& run, flo
         r.s = fmaf(scratch[4 * w + 2], rw, r.s);
         r.e += rw * fmaf(dw, scratch[4 * w + 2], scratch[4 * w + 3]);
     }
-    if (r.s > 0.0f) {
-        const float shift = -fmaf(r.m, a, -c), rs = exp2_fast(shift);      // from the rounded reference to m
-        r.e = rs * fmaf(shift, r.s, r.e);
-        r.s *= rs;
-    }
+    if (r.s > 0.0f) onto_largest(r, fmaf(r.m, a, -c));
     return r;
 }
 // false: sums by reference may be those of a row that float32 does not hold so
@@ -434,23 +446,10 @@ hipError_t over_rows(int64_t rows, int64_t threads_of_row, F&& f) {
 
 // ---- gradients
 //
-// 2^(a (z - m)) of a row's places as 2^(a z - c) times a factor near 1, c = a m rounded, so that a place takes one fused multiply-add.  The factor puts
-// the rounding of c back: it is within an octave up to |c| = 2^25, and may leave float32's range from 2^31 on (a row of -1e10: 2^-440, while every
-// place has 2^440).  Where it is more than an octave, by differences; every thread of a row decides alike.
-struct Exponent {
-    float a, m, c;
-    float shift;         // c - a m: 2^(a (z - m)) = 2^shift 2^(a z - c); at most 1 in size
-    bool exact;          // by differences; shift is 0
-};
-__device__ __forceinline__ Exponent exponent_of(float m, float a) {
-    Exponent x{a, m, m * a, 0.0f, false};
-    const float shift = -fmaf(m, a, -x.c);
-    x.exact = !(fabsf(shift) <= 1.0f);                     // (an infinite c, too)
-    if (!x.exact) x.shift = shift;
-    return x;
-}
-template <bool EXACT>
-__device__ __forceinline__ float octaves_at(const Exponent& x, float z) { return EXACT ? (z - x.m) * x.a : fmaf(z, x.a, -x.c); }
+// A place's 2^(a (z - m)) goes by the difference, an instruction more than fma(a, z, -a m) (which changes nothing: these kernels wait for memory): the rounding
+// of a m, put back as a factor, would leave float32's range from |a m| = 2^31 on (a row of -1e10: 2^-440, while every place has 2^440), and
+// the largest logit of a row would not have 1.
+__device__ __forceinline__ float octaves_at(float z, float m, float a) { return (z - m) * a; }
 
 template <int GDT>
 __device__ __forceinline__ void store_one(char* row, int64_t place, float g) {

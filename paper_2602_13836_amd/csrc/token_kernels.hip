@@ -469,33 +469,32 @@ __global__ __launch_bounds__(kGradThreads) void token_grad_kernel(const TokenGra
     }
     const float gh = a.grad_entropy ? a.grad_entropy[row] : 0.0f;
     const bool empty = st.y == 0.0f;
-    const Exponent x = exponent_of(st.x, octaves_per_logit(temp));
-    const float scale = empty ? 0.0f : -inv_t / st.y * exp2_fast(x.shift);
+    const float c = octaves_per_logit(temp), h = st.z - logf(st.y);
+    const float scale = empty ? 0.0f : -inv_t / st.y;
     const float k1 = scale * gh * 0.6931471805599453f;
-    const float k0 = empty ? 0.0f : fmaf(k1, x.shift, scale * (g_sum + gh * (st.z - logf(st.y))));
+    const float k0 = empty ? 0.0f : scale * fmaf(gh, h, g_sum);
     char* out = a.grad + row * a.grad_row_bytes;
-    auto gradient = [&](auto exact, float z) {
-        const float y = octaves_at<decltype(exact)::value>(x, z);
-        return exp2_fast(y) * fmaf(k1, fmaxf(y, kNoMass), k0);
-    };
     // every read of the part is done before any of its places is written
     if (a.grad_logprob) __syncthreads();
-    auto pass = [&](auto exact) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float z[V], g[V];
-            widen<DT>(v[u], z);
+    for (int u = 0; u < U; ++u) {
+        float z[V], g[V];
+        widen<DT>(v[u], z);
 #pragma unroll
-            for (int i = 0; i < V; ++i) g[i] = gradient(exact, z[i]);
-            store_vector<GDT>(out, t, u * NT + tid, whole_chunk<NT, U>(t, 0), g);
+        for (int i = 0; i < V; ++i) {
+            const float y = octaves_at(z[i], st.x, c);
+            g[i] = exp2_fast(y) * fmaf(k1, fmaxf(y, kNoMass), k0);
         }
-    };
-    if (x.exact) pass(std::true_type{});
-    else pass(std::false_type{});
+        store_vector<GDT>(out, t, u * NT + tid, whole_chunk<NT, U>(t, 0), g);
+    }
     if (a.grad_logprob) {
         __syncthreads();
-        if (!(z_mine == -INFINITY))
-            store_one<GDT>(out, token[tid], fmaf(mine, inv_t, x.exact ? gradient(std::true_type{}, z_mine) : gradient(std::false_type{}, z_mine)));
+        if (!(z_mine == -INFINITY)) {
+            // (where p is 1 and nothing else is given, exactly 0)
+            const float y = octaves_at(z_mine, st.x, c), p = exp2_fast(y) / st.y;
+            const float others = fmaf(gh, fmaf(0.6931471805599453f, fmaxf(y, kNoMass), h), g_sum);
+            store_one<GDT>(out, token[tid], fmaf(-p, others, mine) * inv_t);
+        }
     }
 }
 
