@@ -8,7 +8,7 @@
 //
 // One pass sums exp((z - M) / T).  With the rest as one more token it sums over the places that are NOT listed (a bitmap of the row in LDS
 // tells; a vector of 4 or 8 places costs one LDS byte), so q' is a sum of its own and not the small difference of two large ones, and the
-// listed places are gathered and added.  The gradient of every place that is not listed is then one factor times 2^(a z - c).  Listed places are
+// listed places are gathered and added.  The gradient of every place that is not listed is then one factor times 2^(a (z - m)).  Listed places are
 // written once more when the workgroup has written its part; a token that is listed twice has both its masses, whatever the order.
 //
 // Loss and gradient at once: the workgroup that has summed a row walks it again, backwards.  Few rows are cut into parts.
@@ -200,7 +200,8 @@ __device__ __forceinline__ Factors factors_of(const DistillArgs& a, float weight
     return f;
 }
 // the gradient at a listed place that holds z, of a token with mass p
-__device__ __forceinline__ float listed_gradient(const DistillArgs& a, float weight, const Teacher& t, const float4 st, float c, const Factors& f, float z, double p) {
+__device__ __forceinline__ float listed_gradient(const DistillArgs& a, float weight, const Teacher& t, const float4 st, float c, const Factors& f,
+                                                 float z, double p) {
     if (z == -INFINITY || st.y == 0.0f) return f.of_row * 0.0f;
     const float q = exp2_fast(octaves_at(z, st.x, c)) / st.y;
     const double mass = t.mass + (a.kind == kRest && st.w != 0.0f ? t.left : 0.0);

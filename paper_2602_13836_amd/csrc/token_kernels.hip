@@ -428,8 +428,8 @@ __global__ __launch_bounds__(kMergeThreads) void token_join_kernel(const TokenAr
     write_row<NT>(a, row, temp, r, best, given);
 }
 
-// ---- gradient: grad_v = e (k0 + k1 x) with x = (z_v - M) / T in octaves and e = 2^x; then g_j / T more at the given tokens, whose places are
-// written once more when the workgroup has written its part.
+// ---- gradient: grad_v = e (k0 + k1 x) with x = (z_v - M) / T in octaves and e = 2^x.  The given tokens' places are written once more, with their g_j, when
+// the workgroup has written its part.
 //
 // A workgroup has one small part, which it asks for before it looks at anything else: reads and writes of all that run stay within a few
 // tens of megabytes (2048 x 151936 bfloat16, 1.24 GB: 198.5 us, 6.3 TB/s, with 8192 places; 225 with 16384, 245 with 65536; a copy as torch
@@ -503,8 +503,9 @@ __global__ __launch_bounds__(kGradThreads) void token_grad_kernel(const TokenGra
 // 12.4 and 16.7 instead of 17.9, 128 rows 14.5 instead of 16.6 and 22.1 either way; 16 x 65537 6.4 instead of 7.7 but 13.0 instead of 11.7).  The
 // borders are those with alternatives; without them somewhat more and shorter rows would gain by parts.
 constexpr int64_t kWantBlocks = 256, kLongRow = 98304, kFewRows = 64;
-// 256 threads work on a part of up to 8192 places of the grid (a row of 8185, wherever it begins), and where there are workgroups for every place on the chip, else 512 (with 20 alternatives, 256 and 512
-// threads: 60 rows of 2048 places 6.7 and 7.7 us, 8191 7.8 and 7.6, 32003 10.7 and 8.8; 1024 rows of 2048 places 8.6 and 15.9, 32003 27.5 and 31.7).
+// 256 threads work on a part of up to 8192 places of the grid (a row of 8185, wherever it begins), and where there are workgroups for every place on
+// the chip, else 512 (with 20 alternatives, 256 and 512 threads: 60 rows of 2048 places 6.7 and 7.7 us, 8191 7.8 and 7.6, 32003 10.7 and 8.8; 1024 rows
+// of 2048 places 8.6 and 15.9, 32003 27.5 and 31.7).
 constexpr int64_t kShortPart = 8192, kManyBlocks = 1024;
 TokenScratch scratch_of(int64_t rows, int64_t n, int top, char* at) {
     TokenScratch x{};

@@ -16,8 +16,7 @@ DEV = "cuda:0"
 F32, BF16, I32 = torch.float32, torch.bfloat16, torch.int32
 TEMPERATURES = [1.0, 0.300000011920929, 3.0, 2.0 ** -20]          # (numbers of float32: the plain forms take them as they are)
 TYPES = [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)]
-# fma(a, z, -c) with c the rounding of a z: up to 2^25 the rounding of c is within an octave, from 2^31 on it may leave the range of an
-# exponential; past 2^128 c itself is infinite
+# A reference a m is rounded: up to 2^25 within an octave; from 2^31 on the rounding may leave the range of an exponential; past 2^128 a m itself is infinite.
 SIZES = [1e5, 1e7, 12345678.0, 1e8, 1e9, 1e10, 1e12, 1e15, 1e20, 1e29]
 
 
